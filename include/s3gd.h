@@ -338,6 +338,95 @@ S3GD_API s3gd_status s3gd_majority_vote_noalloc(const uint32_t* idx, const uint3
                                                 void* stream);
 
 /*
+ * Operators for the parameters of a language model that is trained with the calls above: its matrices
+ * (orthogonalised updates, which take the workers' vote or any other gradient) and its embedding table
+ * (lookup, and the gradient that a worker's row of `grads` holds for it).
+ *
+ * Element types.  Every tensor argument names its own; which are accepted stands at each call.
+ */
+typedef enum s3gd_dtype { S3GD_F32 = 0, S3GD_BF16 = 1, S3GD_I8 = 2, S3GD_I32 = 3, S3GD_I64 = 4 } s3gd_dtype;
+
+/* A batch of matrices in device memory.  Entry (r, c) of matrix k lies batch_stride * k + row_stride * r + c elements
+ * after `data`; strides in elements, row_stride >= cols, batch_stride >= 0 (only read for batch > 1, where matrices that
+ * are written must not overlap).  `data` is aligned to its element type. */
+typedef struct s3gd_matrix {
+  void* data;
+  int dtype; /* s3gd_dtype */
+  int64_t row_stride, batch_stride;
+} s3gd_matrix;
+
+/*
+ * Orthogonalised matrices by Newton-Schulz products.  For each [rows x cols] matrix G of the batch, with the quintic
+ * p(Y) = a Y + b (Y Y^T) Y + c (Y Y^T)^2 Y:
+ *     Y_0 = G / (|G|_F + eps),   Y_(i+1) = p(Y_i),   out = Y_steps
+ * which moves every singular value by s <- a s + b s^3 + c s^5 and leaves the singular vectors alone; with
+ * (a, b, c) = (3.4445, -4.7750, 2.0315) five steps bring all but the smallest into about [0.7, 1.2].  The transposed
+ * matrix is worked on where rows > cols (the result is the same).  A matrix of zeros gives zeros (eps > 0); one that
+ * holds an Inf or NaN gives NaN throughout and does not touch its neighbours in the batch.
+ *
+ *  g      F32, BF16 or I8 (a vote), const        out    F32 or BF16; may be g itself (same type and strides)
+ *  steps  1..32       a, b, c, eps  finite, eps >= 0; refused where some s in [0, 1] would leave [-2, 2] on its way, or
+ *                     |b s^2 + c s^4| pass 24, which the internal 16-bit forms are not made for
+ *  split_steps  how many of the first steps hold their matrices in two 16-bit pieces (22 bits) instead of one (11 bits):
+ *                     0..steps, or -1: all for an F32 result, the first two for a BF16 result
+ *  ws           >= s3gd_orthogonalise_workspace_bytes(batch, rows, cols), 256-byte aligned, not preserved
+ * Sums are held in 32 bits, norms in 64.  s3gd_device_status(ws) reports a kernel that gave up (S3GD_ERR_INTERNAL).
+ * Limits: 1 <= batch <= 65535, rows and cols < 2^24.
+ */
+S3GD_API size_t s3gd_orthogonalise_workspace_bytes(int batch, uint64_t rows, uint64_t cols);
+S3GD_API s3gd_status s3gd_orthogonalise(const s3gd_matrix* g, const s3gd_matrix* out, int batch, uint64_t rows,
+                                        uint64_t cols, int steps, float a, float b, float c, float eps, int split_steps,
+                                        void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One step of a (batch of) matrix parameters by their orthogonalised momentum, in place:
+ *     v <- mu v + g,   u = v  or  g + mu v (nesterov),   x <- (1 - lr weight_decay) x - (lr scale) orthogonalise(u)
+ * with every operation in 32 bits and x rounded once.
+ *
+ *  x      F32 or BF16, updated       opt_v  F32, updated, or NULL: u = g (mu and nesterov are not used)
+ *  g      F32, BF16 or I8 (the vote of s3gd_majority_vote / s3gd_step as the gradient), const
+ *  the rest as for s3gd_orthogonalise; split_steps = -1 goes by the type of x
+ */
+S3GD_API s3gd_status s3gd_step_ortho(const s3gd_matrix* x, const s3gd_matrix* opt_v, const s3gd_matrix* g, int batch,
+                                     uint64_t rows, uint64_t cols, float mu, int nesterov, float lr, float weight_decay,
+                                     float scale, int steps, float a, float b, float c, float eps, int split_steps,
+                                     void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Rows of an embedding table by token: out[t] = scale * table[ids[t]], rounded once.
+ * A negative id marks an empty place (padding, a masked token): its row is zero.  An id >= vocab gives a zero row too and
+ * is counted in opt_bad_count.
+ *
+ *  table  [vocab x dim] F32 or BF16, rows table_stride elements apart      ids   [n] I32 or I64
+ *  out    [n x dim] F32 or BF16, rows out_stride elements apart            opt_bad_count  dev or NULL, one uint32
+ * n may be 0.  Limits: vocab < 2^31, dim < 2^31, n < 2^40.
+ */
+S3GD_API s3gd_status s3gd_embed(const void* table, int table_dtype, int64_t table_stride, uint64_t vocab, uint64_t dim,
+                                const void* ids, int ids_dtype, uint64_t n, float scale, void* out, int out_dtype,
+                                int64_t out_stride, uint32_t* opt_bad_count, void* stream);
+
+/*
+ * The embedding table's gradient of M workers, each into its own row of the gradient buffer:
+ *     grads[m][v * dim + j]  =  scale * sum over t with ids[m][t] == v of dout[m][t][j]
+ * Tokens are summed in ascending groups, each group in ascending order: the result does not depend on the run.
+ * Every entry of the vocab * dim is written, with zeros for tokens that no worker's id names; with accumulate != 0 the
+ * sum is added to what is there (one rounding) and rows without a token are left alone.  Negative ids and ids >= vocab
+ * are skipped (whatever dout holds there), the latter counted in opt_bad_count.
+ *
+ *  dout   [M x T x dim] F32 or BF16, dout_stride elements from token to token, dout_worker_stride from worker to worker
+ *  ids    [M x T] I32 or I64
+ *  grads  F32 or BF16, grads_stride elements from worker to worker (>= vocab * dim; the row of s3gd_step's grads that the
+ *         table is a part of), already pointing at the table's first coordinate
+ *  ws     >= s3gd_embed_grad_workspace_bytes(M, T, vocab, dim), 256-byte aligned
+ * T may be 0.  M = 1 is the ordinary gradient.  Limits: M <= 65535, T < 2^31, vocab < 2^31, dim < 2^31.
+ */
+S3GD_API size_t s3gd_embed_grad_workspace_bytes(int M, uint64_t T, uint64_t vocab, uint64_t dim);
+S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t dout_stride, int64_t dout_worker_stride,
+                                     const void* ids, int ids_dtype, int M, uint64_t T, uint64_t vocab, uint64_t dim,
+                                     float scale, void* grads, int grads_dtype, int64_t grads_stride, int accumulate,
+                                     uint32_t* opt_bad_count, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Measurement aid (the paper reports no timings; this has no counterpart there).
  * Between s3gd_profile_begin(max_steps) and s3gd_profile_end(), every s3gd_step call of
  * this process records CUDA events on its stream at its phase boundaries, for at most

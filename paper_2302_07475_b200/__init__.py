@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     s3gd_randk_sign, s3gd_step_randk, s3gd_last_device_status, s3gd_debug_topk_sign, s3gd_debug_step,
     s3gd_vote_apply, s3gd_vote_counts, s3gd_encode_vote2, s3gd_apply_vote2,
     s3gd_sparse_workspace_bytes, s3gd_encode_vote_sparse, s3gd_apply_vote_sparse,
+    alloc_embed_workspace, alloc_ortho_workspace, s3gd_embed, s3gd_embed_grad, s3gd_embed_grad_workspace_bytes,
+    s3gd_orthogonalise, s3gd_orthogonalise_workspace_bytes, s3gd_step_ortho,
 )

@@ -29,13 +29,20 @@ EXPORTS = ("s3gd_status_string", "s3gd_workspace_bytes", "s3gd_topk_sign", "s3gd
            "s3gd_randk_sign", "s3gd_step_randk", "s3gd_profile_begin_filter", "s3gd_last_device_status",
            "s3gd_debug_topk_sign", "s3gd_debug_step", "s3gd_vote_apply", "s3gd_vote_counts", "s3gd_encode_vote2",
            "s3gd_apply_vote2", "s3gd_sparse_workspace_bytes", "s3gd_encode_vote_sparse", "s3gd_apply_vote_sparse",
-           "s3gd_profile_begin_filter_every")
+           "s3gd_profile_begin_filter_every", "s3gd_orthogonalise_workspace_bytes", "s3gd_orthogonalise", "s3gd_step_ortho",
+           "s3gd_embed", "s3gd_embed_grad_workspace_bytes", "s3gd_embed_grad")
 
 
 class S3gdError(RuntimeError):
     def __init__(self, call: str, code: int):
         super().__init__(f"{call} returned {STATUS_NAMES.get(code, code)}")
         self.code = code
+
+
+class Matrix(ctypes.Structure):
+    """s3gd_matrix of the C ABI."""
+
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int), ("row_stride", ctypes.c_int64), ("batch_stride", ctypes.c_int64)]
 
 
 _lib = None
@@ -109,6 +116,19 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.s3gd_encode_vote_sparse.argtypes = [vp, ctypes.c_int, u32, u64, u32, u32, u32p, vp, sz, vp]
     lib.s3gd_apply_vote_sparse.restype = ctypes.c_int
     lib.s3gd_apply_vote_sparse.argtypes = [vp, u32p, ctypes.c_int, u64, u32, u64, ctypes.c_float, vp, vp]
+    f32, i32, i64, mat = ctypes.c_float, ctypes.c_int, ctypes.c_int64, ctypes.POINTER(Matrix)
+    lib.s3gd_orthogonalise_workspace_bytes.restype = sz
+    lib.s3gd_orthogonalise_workspace_bytes.argtypes = [i32, u64, u64]
+    lib.s3gd_orthogonalise.restype = i32
+    lib.s3gd_orthogonalise.argtypes = [mat, mat, i32, u64, u64, i32, f32, f32, f32, f32, i32, vp, sz, vp]
+    lib.s3gd_step_ortho.restype = i32
+    lib.s3gd_step_ortho.argtypes = [mat, mat, mat, i32, u64, u64, f32, i32, f32, f32, f32, i32, f32, f32, f32, f32, i32, vp, sz, vp]
+    lib.s3gd_embed.restype = i32
+    lib.s3gd_embed.argtypes = [vp, i32, i64, u64, u64, vp, i32, u64, f32, vp, i32, i64, vp, vp]
+    lib.s3gd_embed_grad_workspace_bytes.restype = sz
+    lib.s3gd_embed_grad_workspace_bytes.argtypes = [i32, u64, u64, u64]
+    lib.s3gd_embed_grad.restype = i32
+    lib.s3gd_embed_grad.argtypes = [vp, i32, i64, i64, vp, i32, i32, u64, u64, u64, f32, vp, i32, i64, i32, vp, vp, sz, vp]
     if path is None:
         _lib = lib
     return lib
@@ -430,3 +450,172 @@ def s3gd_step_randk(x: torch.Tensor, grads: torch.Tensor, K: int, lr: float, see
     with torch.cuda.device(x.device):
         code = load().s3gd_step_randk(*args, _stream(x))
     _check("s3gd_step_randk", code)
+
+
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.int8: 2, torch.int32: 3, torch.int64: 4}
+_REAL = (torch.float32, torch.bfloat16)
+#: Coefficients of the quintic that five steps of are usually taken.
+ORTHO_COEFFS = (3.4445, -4.7750, 2.0315)
+
+
+def s3gd_orthogonalise_workspace_bytes(batch: int, rows: int, cols: int) -> int:
+    return int(load().s3gd_orthogonalise_workspace_bytes(int(batch), int(rows), int(cols)))
+
+
+def alloc_ortho_workspace(batch: int, rows: int, cols: int, device="cuda") -> torch.Tensor:
+    """A uint8 CUDA tensor for s3gd_orthogonalise / s3gd_step_ortho on [batch, rows, cols] (batch 1: one matrix)."""
+    n = s3gd_orthogonalise_workspace_bytes(batch, rows, cols)
+    if n == 0:
+        raise ValueError("invalid (batch, rows, cols)")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _matrices(**tensors):
+    """The named tensors ([rows, cols] or [batch, rows, cols], all of one shape) as s3gd_matrix, and (batch, rows, cols).
+
+    Rows lie contiguous in all of them, or columns in all of them: the transposed problem is then passed on."""
+    given = {k: t for k, t in tensors.items() if t is not None}
+    first = next(iter(given.values()))
+    for k, t in given.items():
+        if not (isinstance(t, torch.Tensor) and t.is_cuda and t.device == first.device):
+            raise TypeError(f"{k} must be a CUDA tensor on the device of the others")
+        if t.dim() not in (2, 3) or t.shape != first.shape:
+            raise ValueError(f"{k} has shape {tuple(t.shape)}, needs [rows, cols] or [batch, rows, cols] like the others")
+    rows, cols = first.shape[-2:]
+
+    def whole(t, inner, outer, n_inner, n_outer):       # unit stride inside, rows that do not run into each other
+        return (t.stride(inner) == 1 or n_inner == 1) and (t.stride(outer) >= n_inner or n_outer == 1)
+
+    if all(whole(t, -1, -2, cols, rows) for t in given.values()):
+        outer = -2
+    elif all(whole(t, -2, -1, rows, cols) for t in given.values()):
+        outer, rows, cols = -1, cols, rows
+    else:
+        raise ValueError(" and ".join(given) + " must all have contiguous rows, or all contiguous columns")
+    mats = {}
+    for k, t in tensors.items():
+        if t is None:
+            mats[k] = None
+            continue
+        mats[k] = ctypes.byref(Matrix(t.data_ptr(), _DTYPES.get(t.dtype, -1), t.stride(outer) if rows > 1 else cols,
+                                      t.stride(0) if t.dim() == 3 else 0))
+    return mats, first.shape[0] if first.dim() == 3 else 1, rows, cols
+
+
+def _of(t: Optional[torch.Tensor], dtypes, name: str) -> None:
+    if t is not None and t.dtype not in dtypes:
+        raise TypeError(f"{name} has dtype {t.dtype}, needs one of {', '.join(str(d) for d in dtypes)}")
+
+
+def s3gd_orthogonalise(g: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, steps: int = 5, coeffs=ORTHO_COEFFS,
+                       eps: float = 1e-7, split_steps: int = -1) -> None:
+    """out <- g with its singular values moved towards 1 by `steps` Newton-Schulz products, per matrix of the batch.
+
+    g fp32, bf16 or an int8 vote; out fp32 or bf16, g itself allowed.  split_steps: see include/s3gd.h (-1: by out's type)."""
+    m, batch, rows, cols = _matrices(g=g, out=out)
+    _of(g, _REAL + (torch.int8,), "g")
+    _of(out, _REAL, "out")
+    a, b, c = coeffs
+    w = _ptr(ws, torch.uint8, name="ws")
+    with torch.cuda.device(out.device):
+        code = load().s3gd_orthogonalise(m["g"], m["out"], batch, rows, cols, steps, a, b, c, eps, split_steps, w, ws.numel(), _stream(out))
+    _check("s3gd_orthogonalise", code)
+
+
+def s3gd_step_ortho(x: torch.Tensor, g: torch.Tensor, lr: float, ws: torch.Tensor, v: Optional[torch.Tensor] = None,
+                    mu: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, scale: float = 1.0, steps: int = 5,
+                    coeffs=ORTHO_COEFFS, eps: float = 1e-7, split_steps: int = -1) -> None:
+    """x <- (1 - lr weight_decay) x - lr scale orthogonalise(u), u from the momentum v <- mu v + g (v None: u = g); in place.
+
+    x fp32 or bf16; v fp32; g fp32, bf16 or the int8 vote."""
+    m, batch, rows, cols = _matrices(x=x, v=v, g=g)
+    _of(x, _REAL, "x")
+    _of(v, (torch.float32,), "v")
+    _of(g, _REAL + (torch.int8,), "g")
+    a, b, c = coeffs
+    w = _ptr(ws, torch.uint8, name="ws")
+    with torch.cuda.device(x.device):
+        code = load().s3gd_step_ortho(m["x"], m["v"], m["g"], batch, rows, cols, mu, int(nesterov), lr, weight_decay, scale, steps, a, b, c,
+                                      eps, split_steps, w, ws.numel(), _stream(x))
+    _check("s3gd_step_ortho", code)
+
+
+def _rows(t: torch.Tensor, dtypes, name: str, dim: Optional[int] = None):
+    """Checks a CUDA tensor whose last axis is contiguous."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() >= 1):
+        raise TypeError(f"{name} must be a CUDA tensor")
+    _of(t, dtypes, name)
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous along its last axis")
+    if dim is not None and t.shape[-1] != dim:
+        raise ValueError(f"{name} has rows of {t.shape[-1]}, needs {dim}")
+
+
+def _ids(ids: torch.Tensor):
+    if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.is_contiguous() and ids.dtype in (torch.int32, torch.int64)):
+        raise TypeError("ids must be a contiguous CUDA tensor of dtype int32 or int64")
+
+
+def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
+               opt_bad_count: Optional[torch.Tensor] = None) -> None:
+    """out[..., :] <- scale * table[ids[...], :]; a negative id gives a zero row.  table [vocab, dim], out ids.shape + [dim]."""
+    _rows(table, _REAL, "table")
+    _ids(ids)
+    if table.dim() != 2 or out.shape[:-1] != ids.shape:
+        raise ValueError(f"table must be [vocab, dim] and out {tuple(ids.shape)} + [dim]")
+    vocab, dim = table.shape
+    _rows(out, _REAL, "out", dim)
+    n = ids.numel()
+    if out.dim() == 2:
+        out_stride = out.stride(0) if n > 1 else dim
+    elif out.is_contiguous():
+        out_stride = dim
+    else:
+        raise ValueError("out must be contiguous, or [n, dim] with contiguous rows")
+    args = (table.data_ptr(), _DTYPES[table.dtype], table.stride(0) if vocab > 1 else dim, vocab, dim, ids.data_ptr(), _DTYPES[ids.dtype], n,
+            scale, out.data_ptr(), _DTYPES[out.dtype], out_stride, _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
+    with torch.cuda.device(out.device):
+        code = load().s3gd_embed(*args, _stream(out))
+    _check("s3gd_embed", code)
+
+
+def s3gd_embed_grad_workspace_bytes(M: int, T: int, vocab: int, dim: int) -> int:
+    return int(load().s3gd_embed_grad_workspace_bytes(int(M), int(T), int(vocab), int(dim)))
+
+
+def alloc_embed_workspace(M: int, T: int, vocab: int, dim: int, device="cuda") -> torch.Tensor:
+    """A uint8 CUDA tensor for s3gd_embed_grad of M workers with T tokens each."""
+    n = s3gd_embed_grad_workspace_bytes(M, T, vocab, dim)
+    if n == 0:
+        raise ValueError("invalid (M, T, vocab, dim)")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, vocab: int, ws: torch.Tensor, scale: float = 1.0,
+                    accumulate: bool = False, opt_bad_count: Optional[torch.Tensor] = None) -> None:
+    """Each worker's gradient of the table: dout [M, T, dim], ids [M, T] -> the first vocab * dim entries of each row of grads.
+
+    grads is [M, >= vocab * dim] (a column slice of the step's gradient buffer), [M, vocab, dim], or [vocab, dim] where dout is
+    [T, dim] and ids [T] (one worker).  Negative ids are skipped; accumulate adds to what grads holds."""
+    _rows(dout, _REAL, "dout")
+    _ids(ids)
+    if dout.dim() != ids.dim() + 1 or dout.shape[:-1] != ids.shape or ids.dim() not in (1, 2):
+        raise ValueError("dout must be [M, T, dim] with ids [M, T], or [T, dim] with ids [T]")
+    M, T, dim = (ids.shape[0] if ids.dim() == 2 else 1), ids.shape[-1], dout.shape[-1]
+    _of(grads, _REAL, "grads")
+    if not (grads.is_cuda and grads.dim() >= 2):
+        raise TypeError("grads must be a CUDA tensor of two or three axes")
+    if grads.shape[-2:] == (vocab, dim) and grads.dim() == ids.dim() + 1:
+        per, rows_of = vocab * dim, grads if grads.dim() == 3 else grads.unsqueeze(0)
+        whole = (dim == 1 or grads.stride(-1) == 1) and (vocab == 1 or grads.stride(-2) == dim)
+    else:
+        per, rows_of = grads.shape[-1], grads
+        whole = grads.dim() == 2 and (per == 1 or grads.stride(-1) == 1)
+    if not whole or rows_of.shape[0] != M or per < vocab * dim:
+        raise ValueError(f"grads must be [{M}, >= {vocab * dim}] or [{M}, {vocab}, {dim}], contiguous within a worker")
+    args = (dout.data_ptr(), _DTYPES[dout.dtype], dout.stride(-2), dout.stride(0) if ids.dim() == 2 else 0, ids.data_ptr(), _DTYPES[ids.dtype],
+            M, T, vocab, dim, scale, grads.data_ptr(), _DTYPES[grads.dtype], rows_of.stride(0) if M > 1 else vocab * dim, int(accumulate),
+            _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
+    with torch.cuda.device(grads.device):
+        code = load().s3gd_embed_grad(*args, _stream(grads))
+    _check("s3gd_embed_grad", code)

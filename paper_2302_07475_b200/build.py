@@ -13,8 +13,9 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libs3gd.so")
-SOURCES = ["s3gd_api.cu", "s3gd_vote.cu", "s3gd_signplane.cu", "s3gd_filter.cu", "s3gd_select.cu", "s3gd_select_small.cu", "s3gd_noalloc.cu", "s3gd_randk.cu", "s3gd_exchange.cu"]
-HEADERS = ["s3gd_common.cuh", "s3gd_tile.cuh", "s3gd_select_emit.inl"]
+SOURCES = ["s3gd_api.cu", "s3gd_vote.cu", "s3gd_signplane.cu", "s3gd_filter.cu", "s3gd_select.cu", "s3gd_select_small.cu", "s3gd_noalloc.cu", "s3gd_randk.cu", "s3gd_exchange.cu",
+           "s3gd_ortho.cu", "s3gd_embed.cu"]
+HEADERS = ["s3gd_common.cuh", "s3gd_tile.cuh", "s3gd_select_emit.inl", "s3gd_ops.cuh"]
 
 
 def _nvcc() -> str:
@@ -40,7 +41,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return LIB
     cmd = [
         _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-        "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-shared",
+        "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "-shared", "--threads", "0",
         "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-DS3GD_NOALLOC_MAX_D=4194304ull",
     ]
     if verbose:
