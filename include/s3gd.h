@@ -367,11 +367,11 @@ typedef struct s3gd_matrix {
  *  g      F32, BF16 or I8 (a vote), const        out    F32 or BF16; may be g itself (same type and strides)
  *  steps  1..32       a, b, c, eps  finite, eps >= 0; refused where some s in [0, 1] would leave [-2, 2] on its way, or
  *                     |b s^2 + c s^4| pass 24, which the internal 16-bit forms are not made for
- *  split_steps  how many of the first steps hold their matrices in two 16-bit pieces (22 bits) instead of one (11 bits):
- *                     0..steps, or -1: all for an F32 result, the first two for a BF16 result
+ *  split_steps  how many of the first steps take their products from two 16-bit pieces of each operand (22 bits) instead
+ *                     of one (11 bits): 0..steps, or -1: all for an F32 result, none for a BF16 result
  *  ws           >= s3gd_orthogonalise_workspace_bytes(batch, rows, cols), 256-byte aligned, not preserved
  * Sums are held in 32 bits, norms in 64.  s3gd_device_status(ws) reports a kernel that gave up (S3GD_ERR_INTERNAL).
- * Limits: 1 <= batch <= 65535, rows and cols < 2^24.
+ * Limits: 1 <= batch <= 65535, rows and cols < 2^24, batch * rows * cols <= 10^12.
  */
 S3GD_API size_t s3gd_orthogonalise_workspace_bytes(int batch, uint64_t rows, uint64_t cols);
 S3GD_API s3gd_status s3gd_orthogonalise(const s3gd_matrix* g, const s3gd_matrix* out, int batch, uint64_t rows,

@@ -1,42 +1,32 @@
 // Orthogonalised updates: momentum, Newton-Schulz products, update of the matrices (see include/s3gd.h).
 #include <math.h>
 
-#include "s3gd_ops.cuh"
+#include "s3gd_ortho.cuh"
 
 namespace s3gd {
 namespace {
 
 constexpr int kPrepThreads = 256;
 constexpr int kMaxNormBlocks = 512;       // partial sums of squares per matrix
-constexpr float kMaxSingular = 2.f, kMaxPoly = 24.f;
-
-// one matrix batch as the kernels see it
-struct Mat {
-  char* p;
-  long long row, batch;                   // strides in elements
-};
-
-struct OrthoPlan {
-  int batch;
-  uint64_t rows, cols, m, n;              // m = shorter side, n = longer: X is [m x n]
-  int norm_blocks;
-  size_t off_hdr, off_norm, off_x, off_y, off_s, off_b, total;
-};
 
 bool make_plan(int batch, uint64_t rows, uint64_t cols, OrthoPlan* P) {
   if (batch < 1 || batch > 65535 || rows == 0 || cols == 0 || rows >= (1u << 24) || cols >= (1u << 24)) return false;
+  if ((double)batch * (double)rows * (double)cols > 1e12 || (double)batch * (double)(rows < cols ? rows : cols) > 1e9) return false;
   P->batch = batch; P->rows = rows; P->cols = cols;
-  P->m = rows < cols ? rows : cols;
-  P->n = rows < cols ? cols : rows;
+  P->m = (int)(rows < cols ? rows : cols);
+  P->n = (int)(rows < cols ? cols : rows);
+  P->ldx = (P->n + 7) / 8 * 8;            // TMA wants rows that start on 16 bytes
+  P->lds = (P->m + 7) / 8 * 8;
   const uint64_t want = (rows * cols + 4095) / 4096, share = (uint64_t)(kMaxNormBlocks + batch - 1) / batch;
   P->norm_blocks = (int)(want < share ? want : share);
+  const size_t x_bytes = (size_t)batch * 2 * P->m * P->ldx * 2, s_bytes = (size_t)batch * 2 * P->m * P->lds * 2;
   size_t off = 0;
   P->off_hdr = off;   off = align_up(off + kHdrWords * sizeof(uint32_t), 256);
   P->off_norm = off;  off = align_up(off + (size_t)batch * P->norm_blocks * sizeof(double), 256);
-  P->off_x = off;     off = align_up(off + (size_t)batch * P->m * P->n * 4, 256);
-  P->off_y = off;     off = align_up(off + (size_t)batch * P->m * P->n * 4, 256);
-  P->off_s = off;     off = align_up(off + (size_t)batch * P->m * P->m * 4, 256);
-  P->off_b = off;     off = align_up(off + (size_t)batch * P->m * P->m * 4, 256);
+  P->off_x = off;     off = align_up(off + x_bytes, 256);
+  P->off_y = off;     off = align_up(off + x_bytes, 256);
+  P->off_s = off;     off = align_up(off + s_bytes, 256);
+  P->off_b = off;     off = align_up(off + s_bytes, 256);
   P->total = off;
   return true;
 }
@@ -76,80 +66,46 @@ __global__ void momentum_norm_kernel(Mat g, Mat v, bool has_v, uint64_t rows, ui
   if (threadIdx.x == 0) partial[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = sum;
 }
 
-// X_0 = u / (|u| + eps), transposed where the matrix is tall
+// X_0 = u / (|u| + eps) in two fp16 pieces, transposed where the matrix is tall: 64 x 64 tiles through shared memory
 template <typename G>
-__global__ void normalise_kernel(Mat g, Mat v, bool has_v, uint64_t rows, uint64_t cols, float mu, int nesterov, float eps,
-                                 const double* partial, int norm_blocks, float* x) {
+__global__ void __launch_bounds__(kPrepThreads) normalise_kernel(Mat g, Mat v, bool has_v, uint64_t rows, uint64_t cols, float mu, int nesterov,
+                                                                 float eps, const double* partial, int norm_blocks, __half* x, int m, int n,
+                                                                 int ldx) {
   __shared__ double warp_sums[kPrepThreads / 32];
-  const G* gp = reinterpret_cast<const G*>(g.p) + (size_t)blockIdx.y * g.batch;
-  const float* vp = reinterpret_cast<const float*>(v.p) + (has_v ? (size_t)blockIdx.y * v.batch : 0);
-  double s = 0.0;
-  for (int i = threadIdx.x; i < norm_blocks; i += kPrepThreads) s += partial[(size_t)blockIdx.y * norm_blocks + i];
-  const float inv = (float)(1.0 / (sqrt(block_sum(s, warp_sums)) + (double)eps));
-  x += (size_t)blockIdx.y * rows * cols;
-  for (uint64_t e = (uint64_t)blockIdx.x * kPrepThreads + threadIdx.x; e < rows * cols; e += (uint64_t)gridDim.x * kPrepThreads) {
-    const uint64_t r = e / cols, c = e % cols;
-    float u = to_f32(gp[r * g.row + c]);
-    if (has_v) {
-      const float nv = vp[r * v.row + c];
-      u = nesterov ? __fadd_rn(u, __fmul_rn(mu, nv)) : nv;
-    }
-    x[rows > cols ? c * rows + r : e] = u * inv;
-  }
-}
-
-// C = ca * Add + cb * P Q (Q transposed where kNT): 64 x 64 tiles, 4 x 4 entries per thread.
-struct Store {
-  char* p;                 // user matrix of the last product; NULL: C
-  int dtype;
-  long long row, batch;
-  bool transpose, update;  // update: p <- keep * p - rate * value
-  float keep, rate;
-};
-template <bool kNT>
-__global__ void __launch_bounds__(256) simple_product_kernel(const float* P, const float* Q, const float* Add, float* C, int m, int n, int k,
-                                                             float ca, float cb, Store st) {
-  __shared__ float ps[16][65], qs[16][65];
+  __shared__ float tile[64][65];
   const size_t b = blockIdx.z;
-  P += b * m * k; Q += b * (size_t)k * n;
-  const int i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, ti = threadIdx.x / 16, tj = threadIdx.x % 16;
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < k; k0 += 16) {
-    for (int e = threadIdx.x; e < 64 * 16; e += 256) {
-      const int r = e / 16, kk = e % 16;
-      ps[kk][r] = i0 + r < m && k0 + kk < k ? P[(size_t)(i0 + r) * k + k0 + kk] : 0.f;
-      if (kNT) {
-        qs[kk][r] = j0 + r < n && k0 + kk < k ? Q[(size_t)(j0 + r) * k + k0 + kk] : 0.f;
-      } else {
-        const int kr = e / 64, c = e % 64;
-        qs[kr][c] = j0 + c < n && k0 + kr < k ? Q[(size_t)(k0 + kr) * n + j0 + c] : 0.f;
+  const G* gp = reinterpret_cast<const G*>(g.p) + b * g.batch;
+  const float* vp = reinterpret_cast<const float*>(v.p) + (has_v ? b * v.batch : 0);
+  double s = 0.0;
+  for (int i = threadIdx.x; i < norm_blocks; i += kPrepThreads) s += partial[b * norm_blocks + i];
+  const float inv = (float)((double)kScaleX / (sqrt(block_sum(s, warp_sums)) + (double)eps));
+  const bool tall = rows > cols;
+  const uint64_t i0 = (uint64_t)blockIdx.y * 64, j0 = (uint64_t)blockIdx.x * 64;    // of X
+  const uint64_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                          // of the matrix
+  for (int e = threadIdx.x; e < 64 * 64; e += kPrepThreads) {
+    const int dr = e / 64, dc = e % 64;
+    float u = 0.f;
+    if (r0 + dr < rows && c0 + dc < cols) {
+      u = to_f32(gp[(r0 + dr) * g.row + c0 + dc]);
+      if (has_v) {
+        const float nv = vp[(r0 + dr) * v.row + c0 + dc];
+        u = nesterov ? __fadd_rn(u, __fmul_rn(mu, nv)) : nv;
       }
     }
-    __syncthreads();
-    float part[4][4] = {};                 // sums in two levels: a long row's squares lose less than in one chain
-    for (int kk = 0; kk < 16; ++kk)
-      for (int a = 0; a < 4; ++a)
-        for (int c = 0; c < 4; ++c) part[a][c] += ps[kk][ti * 4 + a] * qs[kk][tj * 4 + c];
-    for (int a = 0; a < 4; ++a)
-      for (int c = 0; c < 4; ++c) acc[a][c] += part[a][c];
-    __syncthreads();
+    tile[tall ? dc : dr][tall ? dr : dc] = u * inv;
   }
-  for (int a = 0; a < 4; ++a)
-    for (int c = 0; c < 4; ++c) {
-      const int i = i0 + ti * 4 + a, j = j0 + tj * 4 + c;
-      if (i >= m || j >= n) continue;
-      const size_t at = b * m * n + (size_t)i * n + j;
-      const float val = __fmaf_rn(ca, Add ? Add[at] : 0.f, __fmul_rn(cb, acc[a][c]));
-      if (st.p == nullptr) { C[at] = val; continue; }
-      const size_t to = b * st.batch + (st.transpose ? (size_t)j * st.row + i : (size_t)i * st.row + j);
-      if (st.dtype == S3GD_F32) {
-        float* o = reinterpret_cast<float*>(st.p) + to;
-        *o = st.update ? __fmaf_rn(-st.rate, val, __fmul_rn(st.keep, *o)) : val;
-      } else {
-        __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(st.p) + to;
-        *o = __float2bfloat16_rn(st.update ? __fmaf_rn(-st.rate, val, __fmul_rn(st.keep, __bfloat162float(*o))) : val);
-      }
-    }
+  __syncthreads();
+  __half* hi_row = x + b * 2 * m * (size_t)ldx;
+  for (int e = threadIdx.x; e < 64 * 32; e += kPrepThreads) {
+    const int di = e / 32, dj = (e % 32) * 2;
+    if (i0 + di >= (uint64_t)m || j0 + dj >= (uint64_t)ldx) continue;               // ldx is even: both or neither
+    __half h0, l0, h1, l1;
+    split_half(tile[di][dj], &h0, &l0);
+    split_half(tile[di][dj + 1], &h1, &l1);
+    const size_t at = (i0 + di) * ldx + j0 + dj;
+    *reinterpret_cast<__half2*>(hi_row + at) = __halves2half2(h0, h1);
+    *reinterpret_cast<__half2*>(hi_row + (size_t)m * ldx + at) = __halves2half2(l0, l1);
+  }
 }
 
 bool mat_ok(const s3gd_matrix* a, int batch, uint64_t cols, bool written) {
@@ -172,47 +128,28 @@ bool poly_ok(int steps, float a, float b, float c, float eps) {
   return true;
 }
 
-struct Request {
-  Mat g, v;
-  int g_dtype;
-  bool has_v;
-  float mu; int nesterov;
-  Store out;
-  int steps, split;
-  float a, b, c, eps;
-};
-
 template <typename G>
-cudaError_t prepare(const OrthoPlan& P, const Request& R, char* ws, cudaStream_t st) {
+cudaError_t prepare(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st) {
   double* partial = reinterpret_cast<double*>(ws + P.off_norm);
   count_launch(2);
   momentum_norm_kernel<G><<<dim3(P.norm_blocks, P.batch), kPrepThreads, 0, st>>>(R.g, R.v, R.has_v, P.rows, P.cols, R.mu, R.nesterov, partial);
-  const uint64_t blocks = (P.rows * P.cols + 1023) / 1024;
-  normalise_kernel<G><<<dim3((unsigned)(blocks < 4096 ? blocks : 4096), P.batch), kPrepThreads, 0, st>>>(
-      R.g, R.v, R.has_v, P.rows, P.cols, R.mu, R.nesterov, R.eps, partial, P.norm_blocks, reinterpret_cast<float*>(ws + P.off_x));
+  normalise_kernel<G><<<dim3((P.n + 63) / 64, (P.m + 63) / 64, P.batch), kPrepThreads, 0, st>>>(
+      R.g, R.v, R.has_v, P.rows, P.cols, R.mu, R.nesterov, R.eps, partial, P.norm_blocks, reinterpret_cast<__half*>(ws + P.off_x), P.m, P.n,
+      P.ldx);
   return cudaGetLastError();
 }
 
-cudaError_t run(const OrthoPlan& P, const Request& R, char* ws, cudaStream_t st) {
+cudaError_t run(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st) {
   cudaError_t e = cudaMemsetAsync(ws + P.off_hdr, 0, kHdrWords * sizeof(uint32_t), st);
   if (e != cudaSuccess) return e;
   e = R.g_dtype == S3GD_F32 ? prepare<float>(P, R, ws, st) : R.g_dtype == S3GD_BF16 ? prepare<__nv_bfloat16>(P, R, ws, st) : prepare<int8_t>(P, R, ws, st);
-  if (e != cudaSuccess) return e;
-  float* x = reinterpret_cast<float*>(ws + P.off_x);
-  float* y = reinterpret_cast<float*>(ws + P.off_y);
-  float* s = reinterpret_cast<float*>(ws + P.off_s);
-  float* q = reinterpret_cast<float*>(ws + P.off_b);
-  const int m = (int)P.m, n = (int)P.n;
-  const dim3 sq((m + 63) / 64, (m + 63) / 64, P.batch), wide((n + 63) / 64, (m + 63) / 64, P.batch);
-  Store none = {};
-  count_launch(3 * R.steps);
-  for (int k = 0; k < R.steps; ++k) {
-    simple_product_kernel<true><<<sq, 256, 0, st>>>(x, x, nullptr, s, m, m, n, 0.f, 1.f, none);
-    simple_product_kernel<true><<<sq, 256, 0, st>>>(s, s, s, q, m, m, m, R.b, R.c, none);
-    simple_product_kernel<false><<<wide, 256, 0, st>>>(q, x, x, y, m, n, m, R.a, 1.f, k + 1 == R.steps ? R.out : none);
-    float* t = x; x = y; y = t;
-  }
-  return cudaGetLastError();
+  return e == cudaSuccess ? launch_products(P, R, ws, st) : e;
+}
+
+Store as_store(const s3gd_matrix* a, int batch, bool transpose, bool update, float keep, float rate) {
+  const size_t four = 4 * dtype_bytes(a->dtype);
+  const bool wide = is_aligned(a->data, four) && a->row_stride % 4 == 0 && (batch == 1 || a->batch_stride % 4 == 0);
+  return {{static_cast<char*>(a->data), (long long)a->row_stride, (long long)a->batch_stride}, a->dtype, transpose, update, wide, keep, rate};
 }
 
 s3gd_status common_checks(const s3gd_matrix* g, int batch, uint64_t rows, uint64_t cols, int steps, float a, float b, float c, float eps,
@@ -227,7 +164,7 @@ Mat as_mat(const s3gd_matrix* a) { return {static_cast<char*>(a->data), (long lo
 
 int split_rule(int split_steps, int steps, int dtype) {
   if (split_steps >= 0) return split_steps;
-  return dtype == S3GD_F32 ? steps : (steps < 2 ? steps : 2);
+  return dtype == S3GD_F32 ? steps : 0;
 }
 
 }  // namespace
@@ -248,9 +185,9 @@ extern "C" s3gd_status s3gd_orthogonalise(const s3gd_matrix* g, const s3gd_matri
   if (s != S3GD_OK) return s;
   if (!mat_ok(out, batch, cols, true) || (out->dtype != S3GD_F32 && out->dtype != S3GD_BF16)) return S3GD_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < P.total || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
-  Request R = {};
+  OrthoRequest R = {};
   R.g = as_mat(g); R.g_dtype = g->dtype;
-  R.out = {static_cast<char*>(out->data), out->dtype, (long long)out->row_stride, (long long)out->batch_stride, rows > cols, false, 0.f, 0.f};
+  R.out = as_store(out, batch, rows > cols, false, 0.f, 0.f);
   R.steps = steps; R.split = split_rule(split_steps, steps, out->dtype);
   R.a = a; R.b = b; R.c = c; R.eps = eps;
   return run(P, R, static_cast<char*>(ws), static_cast<cudaStream_t>(stream)) == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
@@ -265,13 +202,12 @@ extern "C" s3gd_status s3gd_step_ortho(const s3gd_matrix* x, const s3gd_matrix* 
   if (!mat_ok(x, batch, cols, true) || (x->dtype != S3GD_F32 && x->dtype != S3GD_BF16)) return S3GD_ERR_INVALID_ARG;
   if (opt_v != nullptr && (!mat_ok(opt_v, batch, cols, true) || opt_v->dtype != S3GD_F32)) return S3GD_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < P.total || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
-  Request R = {};
+  OrthoRequest R = {};
   R.g = as_mat(g); R.g_dtype = g->dtype;
   R.has_v = opt_v != nullptr;
   if (R.has_v) R.v = as_mat(opt_v);
   R.mu = mu; R.nesterov = nesterov;
-  R.out = {static_cast<char*>(x->data), x->dtype, (long long)x->row_stride, (long long)x->batch_stride, rows > cols, true,
-           1.f - lr * weight_decay, lr * scale};
+  R.out = as_store(x, batch, rows > cols, true, 1.f - lr * weight_decay, lr * scale);
   R.steps = steps; R.split = split_rule(split_steps, steps, x->dtype);
   R.a = a; R.b = b; R.c = c; R.eps = eps;
   return run(P, R, static_cast<char*>(ws), static_cast<cudaStream_t>(stream)) == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;

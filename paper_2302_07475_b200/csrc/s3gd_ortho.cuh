@@ -1,0 +1,70 @@
+// What the kernels of the orthogonalised updates share.  Internal.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "s3gd_ops.cuh"
+
+namespace s3gd {
+
+// X is held times 2^10, S = X X^T times 2^12, B = b S + c S^2 times 2^10: with singular values up to 2 and |B| up to 24 the
+// largest entries stay under fp16's 65504, and the entries of an 8192-wide X_0 (about 1e-4) lie far above its subnormals.
+constexpr float kScaleX = 1024.f, kScaleS = 4096.f, kScaleB = 1024.f;
+constexpr float kMaxSingular = 2.f, kMaxPoly = 24.f;
+
+// one matrix batch of the caller's as the kernels see it
+struct Mat {
+  char* p;
+  long long row, batch;                   // strides in elements
+};
+
+// where the last product goes: p <- value, or (update) p <- keep * p - rate * value
+struct Store {
+  Mat to;
+  int dtype;
+  bool transpose, update, wide;           // wide: rows and base allow four entries in one access
+  float keep, rate;
+};
+
+struct OrthoPlan {
+  int batch;
+  uint64_t rows, cols;
+  int m, n;                               // shorter and longer side: X is [m x n]
+  int ldx, lds;                           // row lengths of the 16-bit matrices
+  int norm_blocks;
+  size_t off_hdr, off_norm, off_x, off_y, off_s, off_b, total;   // each matrix: [batch][two pieces][m][ld]
+};
+
+struct OrthoRequest {
+  Mat g, v;
+  int g_dtype;
+  bool has_v;
+  float mu;
+  int nesterov;
+  Store out;
+  int steps, split;
+  float a, b, c, eps;
+};
+
+// For how many of the first steps X is held in two pieces: where the products take two, and otherwise for the a X term
+// alone in all but the last two steps.  The products of one-piece operands lose little where singular values are small
+// (B is of second order in them), while X itself must keep them through the steps that raise them: with a part of rank 16
+// ten times above the rest the result is off by 5e-4 this way, 3.6e-3 with X in one piece, and 1e-3 with two full steps of
+// three products.  In the last steps the rounding of X in both terms cancels in part, so one piece is as good there.
+inline int carried_steps(int steps, int split) {
+  const int c = steps > 3 ? steps - 2 : 1;
+  return c > split ? c : split;
+}
+
+#ifdef __CUDACC__
+// a value as two fp16 pieces, 22 bits together
+__device__ __forceinline__ void split_half(float v, __half* hi, __half* lo) {
+  *hi = __float2half_rn(v);
+  *lo = __float2half_rn(v - __half2float(*hi));
+}
+#endif
+
+// X_0 lies in off_x; enqueues all products, the last of which writes R.out
+cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st);
+
+}  // namespace s3gd
