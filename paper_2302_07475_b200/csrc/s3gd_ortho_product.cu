@@ -4,13 +4,16 @@
 //   B = b S + c S S    symmetric too (S S^T, both operands rows of S)
 //   Y = a X + B X      B is its own transpose; X is read along its rows as the second operand (MN-major)
 //
-// One persistent kernel per product.  Operands are fp16 tiles brought by TMA into a ring of slots; one thread issues
-// tcgen05.mma with fp32 sums in tensor memory, two sums in turn so that the epilogue of one tile runs under the products of
-// the next.  kCta = 2: two CTAs of a cluster share a 256 x 256 tile and each holds half of either operand.
+// One kernel per product.  Operands are fp16 tiles brought by TMA into slots; one thread issues tcgen05.mma with fp32 sums in
+// tensor memory, two sums in turn, and eight warps take the sums out and finish the tile.  wide_kernel: two CTAs share a
+// 256 x 256 tile (cta_group::2), each with half of either operand, and go from tile to tile, so that the epilogue of one runs
+// under the products of the next.  narrow_kernel, where there are fewer tiles than SMs: 128 x 128 tiles, each by a cluster of
+// up to eight CTAs that share out k and join their sums through distributed shared memory.
 //
 // Precision.  One fp16 piece per entry (11 bits), or two (kSplit, 22 bits): then hi hi + hi lo + lo hi, three products.
-// The tensor cores add to the running fp32 sum without rounding to nearest, which biases a long sum of squares (the diagonal
-// of S); with two pieces the sum is therefore taken out of tensor memory every kChunk slots of k and added in registers.
+// The tensor cores cut off, rather than round, what falls below the running fp32 sum, which biases a long sum of squares (the
+// diagonal of S); with two pieces the sum is therefore taken out of tensor memory every kChunk slots of k and added in
+// registers, and the small products go first.
 #include <atomic>
 
 #include "s3gd_ortho.cuh"
@@ -72,15 +75,15 @@ __device__ __forceinline__ T stored(const Store& s, T old, float v) {
   return from_f32<T>(s.update ? __fmaf_rn(-s.rate, v, __fmul_rn(s.keep, to_f32(old))) : v);
 }
 
-// 32 rows x 64 columns of the caller's matrix from the warp's buffer (row r: 256 bytes, 16-byte pieces exchanged by r & 7)
-template <typename T>
-__device__ __forceinline__ void store_rows(const Store& s, const float* buf, int b, int i0, int j0, int m, int n) {
+// Rows r0 .. r0 + kRows of 32, 64 columns, of the caller's matrix from a buffer (row r: 256 bytes, 16-byte pieces exchanged by r & 7)
+template <typename T, int kRows>
+__device__ __forceinline__ void store_rows(const Store& s, const float* buf, int b, int i0, int j0, int r0, int m, int n) {
   T* base = reinterpret_cast<T*>(s.to.p) + (size_t)b * s.to.batch;
   const int lane = lane_id();
   if (s.wide) {
-#pragma unroll 4
-    for (int it = 0; it < 16; ++it) {
-      const int r = it * 2 + lane / 16, q = lane % 16, j = j0 + q * 4;
+#pragma unroll
+    for (int it = 0; it < kRows / 2; ++it) {
+      const int r = r0 + it * 2 + lane / 16, q = lane % 16, j = j0 + q * 4;
       if (i0 + r >= m || j >= n) continue;
       const float4 v = *reinterpret_cast<const float4*>(buf + r * 64 + ((q ^ (r & 7)) << 2));
       T* p = base + (size_t)(i0 + r) * s.to.row + j;
@@ -96,7 +99,7 @@ __device__ __forceinline__ void store_rows(const Store& s, const float* buf, int
       }
     }
   } else {
-    for (int r = 0; r < 32 && i0 + r < m; ++r)
+    for (int r = r0; r < r0 + kRows && i0 + r < m; ++r)
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const int c = h * 32 + lane;
@@ -119,24 +122,237 @@ __device__ __forceinline__ void store_columns(const Store& s, const float* v, in
     }
 }
 
-template <int kCta, bool kSplit, bool kMn>
-__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ ProductArgs P) {
-  extern __shared__ char smem_raw[];
-  constexpr int kTile = 128 * kCta;               // rows and columns of a tile
-  constexpr int kCols = kTile / 2;                // columns of one epilogue warp
-  constexpr int kTmemCols = 2 * kTile;
-  constexpr int kPieces = kSplit ? 2 : 1;
-  const uint32_t raw = smem_addr(smem_raw);
-  const uint32_t base = (raw + 1023) & ~1023u;
-  char* base_ptr = smem_raw + (base - raw);
-  Shared* sh = reinterpret_cast<Shared*>(base_ptr + kSlots * kSlotBytes + kEpiWarps * kEpiBytes);
-  const int warp = threadIdx.x >> 5;
-  const uint32_t rank = kCta == 2 ? cluster_rank() : 0;
-  const bool symmetric = P.kind <= kPoly;
-  const int tiles = P.batch * (symmetric ? P.tiles_m * (P.tiles_m + 1) / 2 : P.tiles_m * P.tiles_n);
-  const int first = blockIdx.x / kCta, stride = gridDim.x / kCta;
-  const int blocks_k = (P.k + kBlockK - 1) / kBlockK;
+// ------------------------------------------------------------------ the three roles
+// The slots of a CTA.  One piece: a ring of kSlots.  Two pieces: a ring of kHiSlots for the leading pieces of both operands and
+// one of the rest for the trailing pieces.
+constexpr int kHiSlots = 3;
+struct Ring {
+  int first, count, slot;
+  uint32_t phase;
+  __device__ __forceinline__ Ring(int f, int c) : first(f), count(c), slot(f), phase(0) {}
+  __device__ __forceinline__ void next() {
+    if (++slot == first + count) { slot = first; phase ^= 1; }
+  }
+};
 
+// Loads slots k of [from, to): rows row_a.. of the first operand and row_b.. of the second, 128 each.
+template <int kCta, bool kSplit, bool kMn>
+__device__ __forceinline__ bool load_slots(const ProductArgs& P, Shared* sh, uint32_t base, uint32_t rank, int b, int row_a, int row_b, int from,
+                                           int to, Ring* ring) {
+  for (int kb = from; kb < to; ++kb)
+    for (int piece = 0; piece < (kSplit ? 2 : 1); ++piece) {
+      Ring& r = ring[piece];
+      if (!mbar_wait(smem_addr(&sh->empty[r.slot]), r.phase ^ 1)) return false;
+      uint32_t bar = smem_addr(&sh->full[r.slot]);
+      if (rank == 0) mbar_expect_tx(bar, kCta * kSlotBytes);
+      if (kCta == 2) bar = cluster_addr(bar, 0);
+      const uint32_t dst = base + r.slot * kSlotBytes;
+      const int k0 = kb * kBlockK, z = 2 * b + piece;
+      for (int h = 0; h < 2; ++h) tma_load<kCta>(dst + h * 8192, &P.a, k0, row_a + h * 64, z, bar);
+      for (int h = 0; h < 2; ++h)
+        if (kMn) tma_load<kCta>(dst + 16384 + h * 8192, &P.b, row_b + h * 64, k0, z, bar);
+        else tma_load<kCta>(dst + 16384 + h * 8192, &P.b, k0, row_b + h * 64, z, bar);
+      r.next();
+    }
+  return true;
+}
+
+// The two sums in tensor memory that take turns.
+struct Turn {
+  uint32_t sum = 0, phase = 0;
+  __device__ __forceinline__ void next() {
+    sum ^= 1;
+    if (sum == 0) phase ^= 1;
+  }
+};
+
+// Products of `blocks` slots of k.  Two pieces: per kChunk slots first hi lo + lo hi, then hi hi, so that few additions
+// are cut off at the size of the full sum.
+template <int kCta, bool kSplit, bool kMn>
+__device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32_t tmem, int blocks, Ring* ring, Turn* turn) {
+  constexpr int kTile = 128 * kCta;
+  constexpr uint32_t idesc = product_desc(kTile, kTile, kMn);
+  auto product = [&](uint32_t d, int sa, int sb, bool add) {
+    const uint32_t a = base + sa * kSlotBytes, bb = base + sb * kSlotBytes + 16384;
+#pragma unroll
+    for (int k = 0; k < kBlockK / 16; ++k)
+      mma_f16<kCta>(d, operand_desc(a + k * 32), kMn ? operand_desc(bb + k * 2048, 8192) : operand_desc(bb + k * 32), idesc, add || k > 0);
+  };
+  for (int kb = 0; kb < blocks;) {
+    if (!mbar_wait(smem_addr(&sh->sum_empty[turn->sum]), turn->phase ^ 1)) return false;
+    tcgen05_fence_after();
+    const uint32_t d = tmem + turn->sum * kTile;
+    if (kSplit) {
+      int hi[kChunk];
+      const int n = min(kChunk, blocks - kb);
+#pragma unroll
+      for (int c = 0; c < kChunk; ++c) {
+        if (c >= n) break;
+        hi[c] = ring[0].slot;
+        const int lo = ring[1].slot;
+        if (!mbar_wait(smem_addr(&sh->full[hi[c]]), ring[0].phase)) return false;
+        if (!mbar_wait(smem_addr(&sh->full[lo]), ring[1].phase)) return false;
+        tcgen05_fence_after();
+        product(d, hi[c], lo, c > 0);
+        product(d, lo, hi[c], true);
+        mma_commit<kCta>(smem_addr(&sh->empty[lo]));
+        ring[0].next();
+        ring[1].next();
+      }
+#pragma unroll
+      for (int c = 0; c < kChunk; ++c) {
+        if (c >= n) break;
+        product(d, hi[c], hi[c], true);
+        mma_commit<kCta>(smem_addr(&sh->empty[hi[c]]));
+      }
+      kb += n;
+    } else {
+      for (int k = 0; k < blocks; ++k) {
+        if (!mbar_wait(smem_addr(&sh->full[ring[0].slot]), ring[0].phase)) return false;
+        tcgen05_fence_after();
+        product(d, ring[0].slot, ring[0].slot, k > 0);
+        mma_commit<kCta>(smem_addr(&sh->empty[ring[0].slot]));
+        ring[0].next();
+      }
+      kb = blocks;
+    }
+    mma_commit<kCta>(smem_addr(&sh->sum_full[turn->sum]));
+    turn->next();
+  }
+  return true;
+}
+__host__ __device__ constexpr int sums_of(bool split, int blocks) { return split ? (blocks + kChunk - 1) / kChunk : 1; }
+
+// One epilogue warp's part of `sums` consecutive sums, added up: 32 rows (lanes), kCols columns from `column`.
+template <int kTile, int kCols>
+__device__ __forceinline__ bool take_sums(Shared* sh, uint32_t tmem, int quad, int column, int sums, const uint32_t* empty_bar, Turn* turn,
+                                          float* acc) {
+  for (int c = 0; c < sums; ++c) {
+    if (!__all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sum_full[turn->sum]), turn->phase))) return false;
+    tcgen05_fence_after();
+    const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + turn->sum * kTile + column;
+    if (c == 0) {
+#pragma unroll
+      for (int x = 0; x < kCols; x += 32) tmem_load32(at + x, acc + x);
+      tmem_load_wait();
+    } else {
+#pragma unroll
+      for (int x = 0; x < kCols; x += 32) {
+        float part[32];
+        tmem_load32(at + x, part);
+        tmem_load_wait();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) acc[x + e] += part[e];
+      }
+    }
+    tcgen05_fence_before();
+    __syncwarp();
+    if (lane_id() == 0) mbar_arrive_cluster(empty_bar[turn->sum]);
+    turn->next();
+  }
+  return true;
+}
+
+// Brings the 32 x 64 entries at (i0, j0) of the matrix that is added into the warp's buffer (one lane).
+__device__ __forceinline__ void load_add(const ProductArgs& P, uint32_t buf_addr, uint32_t bar, int b, int i0, int j0) {
+  tma_store_wait_read();
+  mbar_expect_tx(bar, P.add_pieces * 4096);
+  for (int piece = 0; piece < P.add_pieces; ++piece) tma_load<1>(buf_addr + piece * 4096, &P.add, j0, i0, 2 * b + piece, bar);
+}
+
+// Eight entries of a row from their sums in x, in place, and (unless they are the caller's) in the buffer at `off` as they are
+// stored; what is added lies there before.
+__device__ __forceinline__ void finish_piece(const ProductArgs& P, char* buf, int off, bool has_add, float* x) {
+  float add[8] = {};
+  if (has_add) {
+    const uint4 h4 = *reinterpret_cast<const uint4*>(buf + off);
+    const __half2* h = reinterpret_cast<const __half2*>(&h4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 f = __half22float2(h[e]);
+      add[2 * e] = f.x; add[2 * e + 1] = f.y;
+    }
+    if (P.add_pieces == 2) {
+      const uint4 l4 = *reinterpret_cast<const uint4*>(buf + 4096 + off);
+      const __half2* l = reinterpret_cast<const __half2*>(&l4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float2 f = __half22float2(l[e]);
+        add[2 * e] += f.x; add[2 * e + 1] += f.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = __fmaf_rn(P.c_add, add[e], __fmul_rn(P.c_acc, x[e]));
+  if (P.kind != kFinal) {
+    __align__(16) __half hi[8], lo[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) split_half(x[e], &hi[e], &lo[e]);
+    *reinterpret_cast<uint4*>(buf + off) = *reinterpret_cast<uint4*>(hi);
+    if (P.out_pieces == 2) *reinterpret_cast<uint4*>(buf + 4096 + off) = *reinterpret_cast<uint4*>(lo);
+  }
+}
+
+// 32 x 64 entries of the result from the sums in v: rows i0 + lane, columns j0 ..  The matrix that is added lies in the buffer.
+__device__ __forceinline__ void finish(const ProductArgs& P, char* buf, uint32_t buf_addr, int b, int i0, int j0, bool mirror, float* v) {
+  const int lane = lane_id();
+  const bool has_add = P.kind != kGram;
+  if (!has_add) {
+    if (lane == 0) tma_store_wait_read();
+    __syncwarp();
+  }
+  // row `lane` of the buffer: 16-byte pieces exchanged by lane & 7, as TMA lays them
+#pragma unroll
+  for (int q = 0; q < 8; ++q) finish_piece(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), has_add, v + q * 8);
+  if (P.kind != kFinal) {
+    fence_async_smem();
+    __syncwarp();
+    if (lane == 0) {
+      tma_store(&P.out, j0, i0, 2 * b, buf_addr);
+      if (P.out_pieces == 2) tma_store(&P.out, j0, i0, 2 * b + 1, buf_addr + 4096);
+      tma_store_commit();
+    }
+    if (mirror) {                                         // rows j0 + e, columns i0 ..
+      if (lane == 0) tma_store_wait_read();
+      __syncwarp();
+#pragma unroll
+      for (int e = 0; e < 64; ++e) {
+        __half hi, lo;
+        split_half(v[e], &hi, &lo);
+        *reinterpret_cast<__half*>(buf + e * 64 + lane * 2) = hi;
+        if (P.out_pieces == 2) *reinterpret_cast<__half*>(buf + 4096 + e * 64 + lane * 2) = lo;
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        tma_store(&P.mirror, i0, j0, 2 * b, buf_addr);
+        if (P.out_pieces == 2) tma_store(&P.mirror, i0, j0, 2 * b + 1, buf_addr + 4096);
+        tma_store_commit();
+      }
+    }
+    return;
+  }
+  if (P.store.transpose) {
+    if (P.store.dtype == S3GD_F32) store_columns<float, 64>(P.store, v, b, i0 + lane, j0, P.m, P.n);
+    else store_columns<__nv_bfloat16, 64>(P.store, v, b, i0 + lane, j0, P.m, P.n);
+  } else {
+    __syncwarp();
+    float* f = reinterpret_cast<float*>(buf);
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+      *reinterpret_cast<float4*>(f + lane * 64 + ((q ^ (lane & 7)) << 2)) = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+    __syncwarp();
+    if (P.store.dtype == S3GD_F32) store_rows<float, 32>(P.store, f, b, i0, j0, 0, P.m, P.n);
+    else store_rows<__nv_bfloat16, 32>(P.store, f, b, i0, j0, 0, P.m, P.n);
+  }
+  fence_async_smem();
+  __syncwarp();
+}
+
+// Barriers, tensor memory, the wait for the kernel before: the same for both kernels.  Returns the tensor memory's address.
+template <int kCta>
+__device__ __forceinline__ uint32_t set_up(const ProductArgs& P, Shared* sh, int columns) {
+  const int warp = threadIdx.x >> 5;
   if (warp == 0) {
     if (lane_id() == 0) {
       for (int s = 0; s < kSlots; ++s) {
@@ -151,222 +367,20 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
       asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncwarp();
-    tmem_alloc<kCta>(smem_addr(&sh->tmem), kTmemCols);
+    tmem_alloc<kCta>(smem_addr(&sh->tmem), columns);
     tcgen05_fence_before();
+  } else if (warp == 1 && lane_id() == 0) {
+    tma_prefetch(&P.a); tma_prefetch(&P.b); tma_prefetch(&P.add); tma_prefetch(&P.out); tma_prefetch(&P.mirror);
   }
   __syncthreads();
   if (kCta == 2) cluster_sync();
   tcgen05_fence_after();
-  const uint32_t tmem = sh->tmem;
   grid_dependency_wait();
   launch_dependents();
-
-  bool ok = true;
-  if (warp == 0) {
-    if (lane_id() == 0) {                                   // ---- loads
-      int slot = 0;
-      uint32_t phase = 0;
-      for (int t = first; t < tiles && ok; t += stride) {
-        int b, tm, tn;
-        tile_at(P, t, symmetric, &b, &tm, &tn);
-        const int row_a = tm * kTile + (int)rank * 128, row_b = tn * kTile + (int)rank * 128;
-        for (int kb = 0; kb < blocks_k && ok; ++kb)
-          for (int piece = 0; piece < kPieces; ++piece) {
-            if (!mbar_wait(smem_addr(&sh->empty[slot]), phase ^ 1)) { ok = false; break; }
-            uint32_t bar = smem_addr(&sh->full[slot]);
-            if (rank == 0) mbar_expect_tx(bar, kCta * kSlotBytes);
-            if (kCta == 2) bar = cluster_addr(bar, 0);
-            const uint32_t dst = base + slot * kSlotBytes;
-            const int k0 = kb * kBlockK, z = 2 * b + piece;
-            for (int h = 0; h < 2; ++h) tma_load<kCta>(dst + h * 8192, &P.a, k0, row_a + h * 64, z, bar);
-            for (int h = 0; h < 2; ++h)
-              if (kMn) tma_load<kCta>(dst + 16384 + h * 8192, &P.b, row_b + h * 64, k0, z, bar);
-              else tma_load<kCta>(dst + 16384 + h * 8192, &P.b, k0, row_b + h * 64, z, bar);
-            if (++slot == kSlots) { slot = 0; phase ^= 1; }
-          }
-      }
-    }
-  } else if (warp == 1) {
-    if (lane_id() == 0 && rank == 0) {                      // ---- products
-      constexpr uint32_t idesc = product_desc(kTile, kTile, kMn);
-      int slot = 0;
-      uint32_t phase = 0, sum = 0, sum_phase = 0;
-      auto step = [&](uint32_t d, int sa, int sb, bool add) {
-        const uint32_t a = base + sa * kSlotBytes, bb = base + sb * kSlotBytes + 16384;
-        for (int k = 0; k < kBlockK / 16; ++k)
-          mma_f16<kCta>(d, operand_desc(a + k * 32), kMn ? operand_desc(bb + k * 2048, 8192) : operand_desc(bb + k * 32), idesc, add || k > 0);
-      };
-      for (int t = first; t < tiles && ok; t += stride) {
-        for (int kb = 0; kb < blocks_k && ok; ++kb) {
-          const bool fresh = kSplit ? kb % kChunk == 0 : kb == 0;
-          const bool last = kb + 1 == blocks_k || (kSplit && (kb + 1) % kChunk == 0);
-          if (fresh && !mbar_wait(smem_addr(&sh->sum_empty[sum]), sum_phase ^ 1)) { ok = false; break; }
-          const uint32_t d = tmem + sum * kTile;
-          const int s0 = slot;
-          const uint32_t p0 = phase;
-          if (!mbar_wait(smem_addr(&sh->full[s0]), p0)) { ok = false; break; }
-          tcgen05_fence_after();
-          step(d, s0, s0, !fresh);
-          if (++slot == kSlots) { slot = 0; phase ^= 1; }
-          if (kSplit) {
-            const int s1 = slot;
-            if (!mbar_wait(smem_addr(&sh->full[s1]), phase)) { ok = false; break; }
-            tcgen05_fence_after();
-            step(d, s0, s1, true);
-            step(d, s1, s0, true);
-            mma_commit<kCta>(smem_addr(&sh->empty[s0]));
-            mma_commit<kCta>(smem_addr(&sh->empty[s1]));
-            if (++slot == kSlots) { slot = 0; phase ^= 1; }
-          } else {
-            mma_commit<kCta>(smem_addr(&sh->empty[s0]));
-          }
-          if (last) {
-            mma_commit<kCta>(smem_addr(&sh->sum_full[sum]));
-            sum ^= 1;
-            if (sum == 0) sum_phase ^= 1;
-          }
-        }
-      }
-    }
-  } else {                                                  // ---- epilogue
-    const int w = warp - 2, quad = warp & 3, half = w >> 2, lane = lane_id();
-    char* buf = base_ptr + kSlots * kSlotBytes + w * kEpiBytes;
-    const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[w]);
-    const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), 0), cluster_addr(smem_addr(&sh->sum_empty[1]), 0)};
-    const bool has_add = P.kind != kGram;
-    uint32_t sum = 0, sum_phase = 0, add_phase = 0;
-    const int chunks = kSplit ? (blocks_k + kChunk - 1) / kChunk : 1;
-    auto load_add = [&](int b, int i0, int j0) {            // one lane, once the buffer is free
-      tma_store_wait_read();
-      mbar_expect_tx(add_bar, P.add_pieces * 4096);
-      for (int piece = 0; piece < P.add_pieces; ++piece) tma_load<1>(buf_addr + piece * 4096, &P.add, j0, i0, 2 * b + piece, add_bar);
-    };
-    for (int t = first; t < tiles && ok; t += stride) {
-      int b, tm, tn;
-      tile_at(P, t, symmetric, &b, &tm, &tn);
-      const int i0 = tm * kTile + (int)rank * 128 + quad * 32, jt = tn * kTile + half * kCols;
-      const bool here = i0 < P.m && jt < P.n;
-      if (has_add && here && lane == 0) load_add(b, i0, jt);
-      float acc[kCols];
-      for (int c = 0; c < chunks; ++c) {
-        if (!__all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sum_full[sum]), sum_phase))) { ok = false; break; }
-        tcgen05_fence_after();
-        const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + sum * kTile + half * kCols;
-        if (c == 0) {
-#pragma unroll
-          for (int x = 0; x < kCols; x += 32) tmem_load32(at + x, acc + x);
-          tmem_load_wait();
-        } else {
-#pragma unroll
-          for (int x = 0; x < kCols; x += 32) {
-            float part[32];
-            tmem_load32(at + x, part);
-            tmem_load_wait();
-#pragma unroll
-            for (int e = 0; e < 32; ++e) acc[x + e] += part[e];
-          }
-        }
-        tcgen05_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(empty_bar[sum]);
-        sum ^= 1;
-        if (sum == 0) sum_phase ^= 1;
-      }
-      if (!ok) break;
-      if (!here) continue;
-#pragma unroll
-      for (int c = 0; c < kCols / 64; ++c) {
-        const int j0 = jt + c * 64;
-        if (j0 >= P.n) break;
-        float* v = acc + c * 64;
-        if (has_add) {
-          if (c > 0 && lane == 0) load_add(b, i0, j0);
-          if (!__all_sync(0xffffffffu, mbar_wait(add_bar, add_phase))) { ok = false; break; }
-          add_phase ^= 1;
-        } else {
-          if (lane == 0) tma_store_wait_read();
-          __syncwarp();
-        }
-        // row `lane` of the buffer: 16-byte pieces exchanged by lane & 7, as TMA lays them
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          const int off = lane * 128 + ((q ^ (lane & 7)) << 4);
-          float add[8] = {};
-          if (has_add) {
-            const uint4 h4 = *reinterpret_cast<const uint4*>(buf + off);
-            const __half2* h = reinterpret_cast<const __half2*>(&h4);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 f = __half22float2(h[e]);
-              add[2 * e] = f.x; add[2 * e + 1] = f.y;
-            }
-            if (P.add_pieces == 2) {
-              const uint4 l4 = *reinterpret_cast<const uint4*>(buf + 4096 + off);
-              const __half2* l = reinterpret_cast<const __half2*>(&l4);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float2 f = __half22float2(l[e]);
-                add[2 * e] += f.x; add[2 * e + 1] += f.y;
-              }
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[q * 8 + e] = __fmaf_rn(P.c_add, add[e], __fmul_rn(P.c_acc, v[q * 8 + e]));
-          if (P.kind != kFinal) {
-            __align__(16) __half hi[8], lo[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) split_half(v[q * 8 + e], &hi[e], &lo[e]);
-            *reinterpret_cast<uint4*>(buf + off) = *reinterpret_cast<uint4*>(hi);
-            if (P.out_pieces == 2) *reinterpret_cast<uint4*>(buf + 4096 + off) = *reinterpret_cast<uint4*>(lo);
-          }
-        }
-        if (P.kind != kFinal) {
-          fence_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            tma_store(&P.out, j0, i0, 2 * b, buf_addr);
-            if (P.out_pieces == 2) tma_store(&P.out, j0, i0, 2 * b + 1, buf_addr + 4096);
-            tma_store_commit();
-          }
-          if (symmetric && tm != tn) {                      // the mirror image: row j0 + e, columns i0 ..
-            if (lane == 0) tma_store_wait_read();
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < 64; ++e) {
-              __half hi, lo;
-              split_half(v[e], &hi, &lo);
-              *reinterpret_cast<__half*>(buf + e * 64 + lane * 2) = hi;
-              if (P.out_pieces == 2) *reinterpret_cast<__half*>(buf + 4096 + e * 64 + lane * 2) = lo;
-            }
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) {
-              tma_store(&P.mirror, i0, j0, 2 * b, buf_addr);
-              if (P.out_pieces == 2) tma_store(&P.mirror, i0, j0, 2 * b + 1, buf_addr + 4096);
-              tma_store_commit();
-            }
-          }
-        } else if (P.store.transpose) {
-          if (P.store.dtype == S3GD_F32) store_columns<float, 64>(P.store, v, b, i0 + lane, j0, P.m, P.n);
-          else store_columns<__nv_bfloat16, 64>(P.store, v, b, i0 + lane, j0, P.m, P.n);
-          fence_async_smem();
-          __syncwarp();
-        } else {
-          __syncwarp();
-          float* f = reinterpret_cast<float*>(buf);
-#pragma unroll
-          for (int q = 0; q < 16; ++q)
-            *reinterpret_cast<float4*>(f + lane * 64 + ((q ^ (lane & 7)) << 2)) = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-          __syncwarp();
-          if (P.store.dtype == S3GD_F32) store_rows<float>(P.store, f, b, i0, j0, P.m, P.n);
-          else store_rows<__nv_bfloat16>(P.store, f, b, i0, j0, P.m, P.n);
-          fence_async_smem();
-          __syncwarp();
-        }
-      }
-    }
-    if (lane == 0) tma_store_wait();
-  }
+  return sh->tmem;
+}
+template <int kCta>
+__device__ __forceinline__ void tear_down(const ProductArgs& P, bool ok, uint32_t tmem, int columns, bool cluster) {
   if (!ok) {                                                // a wait gave up: say so, let copies in flight land
     atomicOr(&P.hdr[kHdrStatus], (uint32_t)kFlagInternal);
     for (int i = 0; i < 1000; ++i) __nanosleep(1000);
@@ -374,9 +388,206 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
   __syncwarp();
   tcgen05_fence_before();
   __syncthreads();
-  if (kCta == 2) cluster_sync();
+  if (cluster) cluster_sync();
   tcgen05_fence_after();
-  if (warp == 0) tmem_free<kCta>(tmem, kTmemCols);
+  if (threadIdx.x < 32) tmem_free<kCta>(tmem, columns);
+}
+
+// Many tiles: persistent, two CTAs to a 256 x 256 tile.
+template <bool kSplit, bool kMn>
+__global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant__ ProductArgs P) {
+  extern __shared__ char smem_raw[];
+  constexpr int kTile = 256, kCols = 128;
+  const uint32_t raw = smem_addr(smem_raw);
+  const uint32_t base = (raw + 1023) & ~1023u;
+  char* epi = smem_raw + (base - raw) + kSlots * kSlotBytes;
+  Shared* sh = reinterpret_cast<Shared*>(epi + kEpiWarps * kEpiBytes);
+  const int warp = threadIdx.x >> 5;
+  const uint32_t rank = cluster_rank();
+  const bool symmetric = P.kind <= kPoly;
+  const int tiles = P.batch * (symmetric ? P.tiles_m * (P.tiles_m + 1) / 2 : P.tiles_m * P.tiles_n);
+  const int first = blockIdx.x / 2, stride = gridDim.x / 2;
+  const int blocks = (P.k + kBlockK - 1) / kBlockK;
+  const uint32_t tmem = set_up<2>(P, sh, 512);
+  Ring ring[2] = {Ring(0, kSplit ? kHiSlots : kSlots), Ring(kHiSlots, kSlots - kHiSlots)};
+  Turn turn;
+  bool ok = true;
+  if (warp == 0) {
+    if (lane_id() == 0)
+      for (int t = first; t < tiles && ok; t += stride) {
+        int b, tm, tn;
+        tile_at(P, t, symmetric, &b, &tm, &tn);
+        ok = load_slots<2, kSplit, kMn>(P, sh, base, rank, b, tm * kTile + (int)rank * 128, tn * kTile + (int)rank * 128, 0, blocks, ring);
+      }
+  } else if (warp == 1) {
+    if (lane_id() == 0 && rank == 0)
+      for (int t = first; t < tiles && ok; t += stride) ok = issue_products<2, kSplit, kMn>(sh, base, tmem, blocks, ring, &turn);
+  } else {
+    const int w = warp - 2, quad = warp & 3, half = w >> 2, lane = lane_id();
+    char* buf = epi + w * kEpiBytes;
+    const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[w]);
+    const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), 0), cluster_addr(smem_addr(&sh->sum_empty[1]), 0)};
+    const bool has_add = P.kind != kGram;
+    uint32_t add_phase = 0;
+    for (int t = first; t < tiles && ok; t += stride) {
+      int b, tm, tn;
+      tile_at(P, t, symmetric, &b, &tm, &tn);
+      const int i0 = tm * kTile + (int)rank * 128 + quad * 32, jt = tn * kTile + half * kCols;
+      const bool here = i0 < P.m && jt < P.n;
+      if (has_add && here && lane == 0) load_add(P, buf_addr, add_bar, b, i0, jt);
+      float acc[kCols];
+      ok = take_sums<kTile, kCols>(sh, tmem, quad, half * kCols, sums_of(kSplit, blocks), empty_bar, &turn, acc);
+      if (!ok || !here) continue;
+#pragma unroll
+      for (int c = 0; c < kCols / 64; ++c) {
+        const int j0 = jt + c * 64;
+        if (j0 >= P.n) break;
+        if (has_add) {
+          if (c > 0 && lane == 0) load_add(P, buf_addr, add_bar, b, i0, j0);
+          ok = __all_sync(0xffffffffu, mbar_wait(add_bar, add_phase));
+          if (!ok) break;
+          add_phase ^= 1;
+        }
+        finish(P, buf, buf_addr, b, i0, j0, symmetric && tm != tn, acc + c * 64);
+      }
+    }
+    if (lane == 0) tma_store_wait_read();
+  }
+  tear_down<2>(P, ok, tmem, 512, true);
+}
+
+// Few tiles: a cluster of kWays CTAs takes one 128 x 128 tile, each a part of k.  The eight 32 x 64 parts of the tile are dealt
+// over the CTAs.  Every CTA lays its sums into its own shared memory (the slots are free by then) and reads those of its parts
+// from all of them, in the order of the parts of k; all eight warps of a CTA finish its parts, kMine * 8 columns each.
+template <bool kSplit, bool kMn, int kWays>
+__global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_constant__ ProductArgs P) {
+  extern __shared__ char smem_raw[];
+  constexpr int kTile = 128, kCols = 64;
+  constexpr int kMine = 8 / kWays;                            // parts per CTA, and 8-column pieces per warp
+  const uint32_t raw = smem_addr(smem_raw);
+  const uint32_t base = (raw + 1023) & ~1023u;
+  char* base_ptr = smem_raw + (base - raw);
+  char* epi = base_ptr + kSlots * kSlotBytes;
+  Shared* sh = reinterpret_cast<Shared*>(epi + kEpiWarps * kEpiBytes);
+  const int warp = threadIdx.x >> 5;
+  const uint32_t rank = kWays > 1 ? cluster_rank() : 0;
+  const bool symmetric = P.kind <= kPoly, has_add = P.kind != kGram;
+  const int blocks = (P.k + kBlockK - 1) / kBlockK;
+  const int from = (int)rank * blocks / kWays, to = ((int)rank + 1) * blocks / kWays;
+  int b, tm, tn;
+  tile_at(P, blockIdx.x / kWays, symmetric, &b, &tm, &tn);
+  const uint32_t tmem = set_up<1>(P, sh, 256);
+  const int w = warp - 2, quad = warp & 3, lane = lane_id();
+  // what this warp finishes: pieces q0 .. q0 + kMine of part `part`
+  const int pl = kWays == 1 ? quad * 2 + (w >> 2) : w * kMine / 8, part = (int)rank * kMine + pl, q0 = w * kMine % 8;
+  const int i0 = tm * kTile + (part >> 1) * 32, j0 = tn * kTile + (part & 1) * kCols;
+  const bool here = warp >= 2 && i0 < P.m && j0 < P.n, leads = q0 == 0 && lane == 0;
+  char* buf = epi + (warp >= 2 ? pl : 0) * kEpiBytes;         // what is added, then the result
+  char* side = base_ptr + 8 * 8192 + (warp >= 2 ? pl : 0) * 8192;   // its mirror image, or the caller's rows
+  const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[warp >= 2 ? pl : 0]);
+  Ring ring[2] = {Ring(0, kSplit ? kHiSlots : kSlots), Ring(kHiSlots, kSlots - kHiSlots)};
+  Turn turn;
+  bool ok = true;
+  float v[8 * kMine];
+  if (warp == 0) {
+    if (lane == 0) ok = load_slots<1, kSplit, kMn>(P, sh, base, 0, b, tm * kTile, tn * kTile, from, to, ring);
+  } else if (warp == 1) {
+    if (lane == 0) ok = issue_products<1, kSplit, kMn>(sh, base, tmem, to - from, ring, &turn);
+  } else {
+    if (has_add && here && leads) load_add(P, buf_addr, add_bar, b, i0, j0);
+    const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), rank), cluster_addr(smem_addr(&sh->sum_empty[1]), rank)};
+    float acc[kCols];
+    ok = take_sums<kTile, kCols>(sh, tmem, quad, (w >> 2) * kCols, sums_of(kSplit, to - from), empty_bar, &turn, acc);
+    if (kWays == 1) {                                         // the part whose sums this warp holds
+#pragma unroll
+      for (int e = 0; e < 8 * kMine; ++e) v[e] = acc[e];
+    } else {
+      char* mine = base_ptr + (quad * 2 + (w >> 2)) * 8192 + lane * 16;
+#pragma unroll
+      for (int q = 0; q < 16; ++q) *reinterpret_cast<float4*>(mine + q * 512) = make_float4(acc[q * 4], acc[q * 4 + 1], acc[q * 4 + 2], acc[q * 4 + 3]);
+    }
+  }
+  if (kWays > 1) {
+    __syncwarp();
+    cluster_sync();
+    if (here) {
+      float4 got[2 * kMine][kWays];
+#pragma unroll
+      for (int r = 0; r < kWays; ++r) {
+        const uint32_t at = cluster_addr(base + (uint32_t)part * 8192u + (uint32_t)(q0 * 2) * 512u + lane * 16, r);
+#pragma unroll
+        for (int l = 0; l < 2 * kMine; ++l)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(got[l][r].x), "=f"(got[l][r].y), "=f"(got[l][r].z), "=f"(got[l][r].w) : "r"(at + l * 512));
+      }
+#pragma unroll
+      for (int l = 0; l < 2 * kMine; ++l) {
+        float4 sum = got[l][0];
+#pragma unroll
+        for (int r = 1; r < kWays; ++r) { sum.x += got[l][r].x; sum.y += got[l][r].y; sum.z += got[l][r].z; sum.w += got[l][r].w; }
+        v[l * 4] = sum.x; v[l * 4 + 1] = sum.y; v[l * 4 + 2] = sum.z; v[l * 4 + 3] = sum.w;
+      }
+    }
+    __syncwarp();
+    cluster_arrive();                                         // the others may go once this CTA has read their sums
+  }
+  if (here) {
+    if (has_add) ok = __all_sync(0xffffffffu, mbar_wait(add_bar, 0)) && ok;
+    const bool mirror = symmetric && tm != tn;
+    // the part that warps finish together: one warp (kWays 1), or 8 / kMine of them
+    auto together = [&] {
+      if (kWays == 1) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"(1 + pl), "r"(32 * kWays) : "memory");
+    };
+#pragma unroll
+    for (int p = 0; p < kMine; ++p) {
+      const int q = q0 + p, off = lane * 128 + ((q ^ (lane & 7)) << 4);
+      float* x = v + p * 8;
+      finish_piece(P, buf, off, has_add, x);
+      if (mirror) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          __half hi, lo;
+          split_half(x[e], &hi, &lo);
+          *reinterpret_cast<__half*>(side + (q * 8 + e) * 64 + lane * 2) = hi;
+          if (P.out_pieces == 2) *reinterpret_cast<__half*>(side + 4096 + (q * 8 + e) * 64 + lane * 2) = lo;
+        }
+      }
+      if (P.kind == kFinal) {
+        if (P.store.transpose) {
+          if (P.store.dtype == S3GD_F32) store_columns<float, 8>(P.store, x, b, i0 + lane, j0 + q * 8, P.m, P.n);
+          else store_columns<__nv_bfloat16, 8>(P.store, x, b, i0 + lane, j0 + q * 8, P.m, P.n);
+        } else {
+          float* f = reinterpret_cast<float*>(side) + lane * 64;
+          *reinterpret_cast<float4*>(f + (((2 * q) ^ (lane & 7)) << 2)) = make_float4(x[0], x[1], x[2], x[3]);
+          *reinterpret_cast<float4*>(f + (((2 * q + 1) ^ (lane & 7)) << 2)) = make_float4(x[4], x[5], x[6], x[7]);
+        }
+      }
+    }
+    if (P.kind != kFinal) {
+      fence_async_smem();
+      together();
+      if (leads && ok) {
+        for (int piece = 0; piece < P.out_pieces; ++piece) {
+          tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
+          if (mirror) tma_store(&P.mirror, i0, j0, 2 * b + piece, smem_addr(side) + piece * 4096);
+        }
+        tma_store_commit();
+        tma_store_wait_read();
+      }
+    } else if (!P.store.transpose) {
+      together();
+      const float* f = reinterpret_cast<const float*>(side);
+      constexpr int kRows = 32 / kWays;                       // of the part's 32 rows, per warp
+      if (P.store.dtype == S3GD_F32) store_rows<float, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
+      else store_rows<__nv_bfloat16, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
+    }
+  }
+  tear_down<1>(P, ok, tmem, 256, false);
+  if (kWays > 1) {
+    __syncwarp();
+    cluster_wait();
+  }
 }
 
 // ------------------------------------------------------------------ host
@@ -409,19 +620,11 @@ bool make_map(CUtensorMap* map, void* p, int rows, int cols, int ld, int planes,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kCta, bool kSplit, bool kMn>
-cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
-  static int done[kMaxDevices];
-  auto kernel = product_kernel<kCta, kSplit, kMn>;
+cudaError_t launch_cluster(void (*kernel)(ProductArgs), const ProductArgs& A, unsigned grid, int cluster, int* done, cudaStream_t st) {
   cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmemBytes, done);
   if (e != cudaSuccess) return e;
-  const int tile = 128 * kCta;
-  A.tiles_m = (A.m + tile - 1) / tile;
-  A.tiles_n = (A.n + tile - 1) / tile;
-  const int64_t tiles = (int64_t)A.batch * (A.kind <= kPoly ? (int64_t)A.tiles_m * (A.tiles_m + 1) / 2 : (int64_t)A.tiles_m * A.tiles_n);
-  const int64_t groups = sm_count() / kCta;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((tiles < groups ? tiles : groups) * kCta));
+  cfg.gridDim = dim3(grid);
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = kSmemBytes;
   cfg.stream = st;
@@ -429,17 +632,82 @@ cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = kCta; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
-  cfg.attrs = attr; cfg.numAttrs = kCta == 2 ? 2 : 1;
+  attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = cluster > 1 ? 2 : 1;
   count_launch();
   return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
-template <bool kMn>
-cudaError_t launch_by(ProductArgs& A, bool pair, bool split, cudaStream_t st) {
-  if (pair) return split ? launch_product<2, true, kMn>(A, st) : launch_product<2, false, kMn>(A, st);
-  return split ? launch_product<1, true, kMn>(A, st) : launch_product<1, false, kMn>(A, st);
+int64_t tiles_of(const ProductArgs& A, int tile) {
+  const int64_t tm = (A.m + tile - 1) / tile, tn = (A.n + tile - 1) / tile;
+  return A.batch * (A.kind <= kPoly ? tm * (tm + 1) / 2 : tm * tn);
 }
+
+// Clusters of `ways` CTAs of this kernel that run at a time (the SMs of a GPC are not always a multiple of it); asked once.
+int clusters_at_a_time(void (*kernel)(ProductArgs), int ways, int* cached) {
+  int dev = 0;
+  const bool keep = cudaGetDevice(&dev) == cudaSuccess && dev >= 0 && dev < kMaxDevices;
+  int n = keep ? __atomic_load_n(&cached[dev], __ATOMIC_RELAXED) : 0;
+  if (n > 0) return n;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ways);
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = kSmemBytes;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = ways; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) n = sm_count() / ways;
+  if (keep) __atomic_store_n(&cached[dev], n, __ATOMIC_RELAXED);
+  return n;
+}
+
+struct Choice { int64_t cost; int ways; };                  // ways 0: the wide kernel
+
+// What counts is the slots of k that follow one another on an SM (both kernels take about as long for one), with kStart
+// slots' worth of time for each start of a narrow tile and kJoin for joining its parts.
+constexpr int kStart = 16, kJoin = 7;
+
+template <bool kSplit, bool kMn, int kWays>
+cudaError_t try_narrow(ProductArgs& A, Choice* best, bool launch, cudaStream_t st) {
+  static int done[kMaxDevices], at_a_time[kMaxDevices];
+  auto kernel = narrow_kernel<kSplit, kMn, kWays>;
+  const int64_t tiles = tiles_of(A, 128), blocks = (A.k + kBlockK - 1) / kBlockK;
+  if (launch) return best->ways == kWays ? launch_cluster(kernel, A, (unsigned)(tiles * kWays), kWays, done, st) : cudaSuccess;
+  if (blocks < kWays || tiles * kWays >= (1ll << 31)) return cudaSuccess;
+  cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmemBytes, done);
+  if (e != cudaSuccess) return e;
+  const int room = kWays > 1 ? clusters_at_a_time(kernel, kWays, at_a_time) : sm_count();
+  const int64_t waves = (tiles + room - 1) / room;
+  const int64_t cost = waves * (kStart + (blocks + kWays - 1) / kWays * (kSplit ? 3 : 1) + (kWays > 1 ? kJoin : 0));
+  if (cost < best->cost) *best = {cost, kWays};
+  return cudaSuccess;
+}
+
+template <bool kSplit, bool kMn>
+cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
+  static int done[kMaxDevices];
+  const int pairs = sm_count() / 2;
+  const int64_t wide = tiles_of(A, 256), blocks = (A.k + kBlockK - 1) / kBlockK;
+  Choice best = {(wide + pairs - 1) / pairs * blocks * (kSplit ? 3 : 1) + kStart, 0};
+  for (int launch = 0; launch < 2; ++launch) {
+    if (launch) {
+      const int tile = best.ways == 0 ? 256 : 128;
+      A.tiles_m = (A.m + tile - 1) / tile;
+      A.tiles_n = (A.n + tile - 1) / tile;
+      if (best.ways == 0) return launch_cluster(wide_kernel<kSplit, kMn>, A, (unsigned)(wide < pairs ? wide : pairs) * 2, 2, done, st);
+    }
+    cudaError_t e = try_narrow<kSplit, kMn, 1>(A, &best, launch, st);
+    if (e == cudaSuccess) e = try_narrow<kSplit, kMn, 2>(A, &best, launch, st);
+    if (e == cudaSuccess) e = try_narrow<kSplit, kMn, 4>(A, &best, launch, st);
+    if (e == cudaSuccess) e = try_narrow<kSplit, kMn, 8>(A, &best, launch, st);
+    if (e != cudaSuccess) return e;
+  }
+  return cudaSuccess;
+}
+
+template <bool kMn>
+cudaError_t launch_by(ProductArgs& A, bool split, cudaStream_t st) { return split ? launch_product<true, kMn>(A, st) : launch_product<false, kMn>(A, st); }
 
 }  // namespace
 
@@ -454,7 +722,6 @@ cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws,
        make_map(&s_mirror, ws + P.off_s, m, m, P.lds, planes, 32, 64) && make_map(&b_load, ws + P.off_b, m, m, P.lds, planes, 64, 64) &&
        make_map(&b_epi, ws + P.off_b, m, m, P.lds, planes, 64, 32) && make_map(&b_mirror, ws + P.off_b, m, m, P.lds, planes, 32, 64);
   if (!ok) return cudaErrorInvalidValue;
-  const bool pair = (int64_t)P.batch * ((m + 255) / 256) * ((n + 255) / 256) >= sm_count() / 2;
   const int carried = carried_steps(R.steps, R.split);
   for (int k = 0; k < R.steps; ++k) {
     const bool split = k < R.split;
@@ -467,12 +734,12 @@ cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws,
     A.kind = kGram; A.m = m; A.n = m; A.k = n;
     A.a = A.b = x_load[from]; A.add = s_epi; A.out = s_epi; A.mirror = s_mirror;
     A.c_add = 0.f; A.c_acc = kScaleS / (kScaleX * kScaleX);
-    cudaError_t e = launch_by<false>(A, pair, split, st);
+    cudaError_t e = launch_by<false>(A, split, st);
     if (e != cudaSuccess) return e;
     A.kind = kPoly; A.k = m;
     A.a = A.b = s_load; A.add = s_epi; A.out = b_epi; A.mirror = b_mirror;
     A.c_add = R.b * (kScaleB / kScaleS); A.c_acc = R.c * (kScaleB / (kScaleS * kScaleS));
-    e = launch_by<false>(A, pair, split, st);
+    e = launch_by<false>(A, split, st);
     if (e != cudaSuccess) return e;
     const bool last = k + 1 == R.steps;
     const float unit = last ? 1.f / kScaleX : 1.f;
@@ -481,7 +748,7 @@ cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws,
     A.add_pieces = k < carried ? 2 : 1;
     A.out_pieces = k + 1 < carried ? 2 : 1;
     A.c_add = R.a * unit; A.c_acc = unit / kScaleB;
-    e = launch_by<true>(A, pair, split, st);
+    e = launch_by<true>(A, split, st);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
