@@ -142,6 +142,7 @@ cudaError_t prepare(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStr
 cudaError_t run(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st) {
   cudaError_t e = cudaMemsetAsync(ws + P.off_hdr, 0, kHdrWords * sizeof(uint32_t), st);
   if (e != cudaSuccess) return e;
+  if (is_small(P)) return launch_small(P, R, ws, st);
   e = R.g_dtype == S3GD_F32 ? prepare<float>(P, R, ws, st) : R.g_dtype == S3GD_BF16 ? prepare<__nv_bfloat16>(P, R, ws, st) : prepare<int8_t>(P, R, ws, st);
   return e == cudaSuccess ? launch_products(P, R, ws, st) : e;
 }

@@ -66,5 +66,8 @@ __device__ __forceinline__ void split_half(float v, __half* hi, __half* lo) {
 
 // X_0 lies in off_x; enqueues all products, the last of which writes R.out
 cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st);
+// Matrices that one CTA holds: everything in one launch
+bool is_small(const OrthoPlan& P);
+cudaError_t launch_small(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st);
 
 }  // namespace s3gd
