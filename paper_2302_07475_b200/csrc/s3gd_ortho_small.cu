@@ -1,7 +1,7 @@
 // Whole orthogonalised updates of small matrices: one CTA per matrix, one launch for momentum, norm, all products and the
 // update.  X (up to 128 x 256) and S stay in shared memory, as two fp16 pieces each, in the layout that the tensor cores read
 // both ways: rows of 64 entries in 128 swizzled bytes serve as K-major operand for X X^T and S S^T and as MN-major operand for
-// B X.  A step is three products, each followed by all eight warps taking the sums out of tensor memory and writing the next
+// B X.  A step is three products, each followed by all sixteen warps taking the sums out of tensor memory and writing the next
 // operand in place; the chain of these (about 3 us a step for 64 x 128), not bytes or operations, is what the time is made of.
 #include "s3gd_ortho.cuh"
 #include "s3gd_tcgen05.cuh"
@@ -9,7 +9,7 @@
 namespace s3gd {
 namespace {
 
-constexpr int kSmallThreads = 256;
+constexpr int kGroups = 16;                        // of four entries per thread: 512 threads hold 128 x 256
 constexpr int kPanel = 128 * 128;                  // bytes of 128 rows x 64 entries
 
 struct SmallArgs {
@@ -20,12 +20,13 @@ struct SmallArgs {
   int nesterov, has_v, steps, split, carried;
   int rows, cols, m, n;
   int panels_x, panels_s, tmem_cols;
+  int g_wide, v_wide;                              // rows and base allow four entries in one access
 };
 
 struct SmallShared {
   uint64_t done;
   uint32_t tmem;
-  double warp_sums[kSmallThreads / 32];
+  double warp_sums[16];
 };
 
 __device__ __forceinline__ int entry_offset(int i, int j) {       // bytes, of entry (i, j) in its piece
@@ -63,9 +64,25 @@ __device__ __forceinline__ void write8(char* hi, char* lo, int off, const float*
 }
 
 template <typename T>
+__device__ __forceinline__ T stored(const Store& s, T old, float v) {
+  return from_f32<T>(s.update ? __fmaf_rn(-s.rate, v, __fmul_rn(s.keep, to_f32(old))) : v);
+}
+template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
+
+// eight neighbouring entries of row i to the caller's matrix
+template <typename T>
 __device__ __forceinline__ void put8(const Store& s, int mat, int i, int j0, int m, int n, const float* x) {
   if (i >= m) return;
   T* base = reinterpret_cast<T*>(s.to.p) + (size_t)mat * s.to.batch;
+  if (s.wide && !s.transpose && j0 + 8 <= n) {
+    Four<T>* p = reinterpret_cast<Four<T>*>(base + (size_t)i * s.to.row + j0);
+    Four<T> o[2] = {};
+    if (s.update) { o[0] = p[0]; o[1] = p[1]; }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e / 4].v[e % 4] = stored(s, o[e / 4].v[e % 4], x[e]);
+    p[0] = o[0]; p[1] = o[1];
+    return;
+  }
   const size_t step = s.transpose ? s.to.row : 1;
   base += s.transpose ? (size_t)j0 * s.to.row + i : (size_t)i * s.to.row + j0;
   T old[8] = {};
@@ -75,11 +92,24 @@ __device__ __forceinline__ void put8(const Store& s, int mat, int i, int j0, int
       if (j0 + e < n) old[e] = base[e * step];
 #pragma unroll
   for (int e = 0; e < 8; ++e)
-    if (j0 + e < n) base[e * step] = from_f32<T>(s.update ? __fmaf_rn(-s.rate, x[e], __fmul_rn(s.keep, to_f32(old[e]))) : x[e]);
+    if (j0 + e < n) base[e * step] = stored(s, old[e], x[e]);
 }
 
-template <typename G>
-__global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P) {
+// up to four neighbouring entries of a row as floats
+template <typename T>
+__device__ __forceinline__ void get4(const T* p, bool wide, int left, float* x) {
+  if (wide && left >= 4) {
+    const Four<T> f = *reinterpret_cast<const Four<T>*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = to_f32(f.v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = e < left ? to_f32(p[e]) : 0.f;
+  }
+}
+
+template <typename G, int kSmallThreads>
+__global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kernel(const SmallArgs P) {
   extern __shared__ char smem_raw[];
   const uint32_t raw = smem_addr(smem_raw), base = (raw + 1023) & ~1023u;
   char* x_hi = smem_raw + (base - raw);
@@ -101,31 +131,49 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P)
   for (int o = threadIdx.x * 16; o < 2 * (P.panels_x + P.panels_s) * kPanel; o += kSmallThreads * 16)
     *reinterpret_cast<uint4*>(x_hi + o) = make_uint4(0, 0, 0, 0);            // what lies beside m and n counts as zero
   grid_dependency_wait();
-  // ---- momentum and norm (sum of squares in 64 bits), then X_0; the matrix is read twice, the second time from cache
+  // ---- momentum, norm (sum of squares in 64 bits) and X_0; u stays in registers in between
   const G* g = reinterpret_cast<const G*>(P.g.p) + (size_t)mat * P.g.batch;
   float* v = reinterpret_cast<float*>(P.v.p) + (P.has_v ? (size_t)mat * P.v.batch : 0);
-  const int count = P.rows * P.cols;
-  constexpr int kAhead = 8;
+  const int per_row = (P.cols + 3) / 4, groups = P.rows * per_row;
+  float u[kGroups][4];
   double sum = 0.0;
-  for (int e0 = threadIdx.x; e0 < count; e0 += kAhead * kSmallThreads) {
-    float u[kAhead], old[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int e = e0 + k * kSmallThreads, r = e / P.cols, c = e - r * P.cols;
-      u[k] = e < count ? to_f32(g[(size_t)r * P.g.row + c]) : 0.f;
-      old[k] = e < count && P.has_v ? v[(size_t)r * P.v.row + c] : 0.f;
-    }
+  for (int k = 0; k < kGroups; ++k) {
+    const int e = k * kSmallThreads + threadIdx.x, r = e / per_row, c = (e - r * per_row) * 4;
+    if (e < groups) get4(g + (size_t)r * P.g.row + c, P.g_wide, P.cols - c, u[k]);
+    else u[k][0] = u[k][1] = u[k][2] = u[k][3] = 0.f;
+  }
+  if (P.has_v) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int e = e0 + k * kSmallThreads, r = e / P.cols, c = e - r * P.cols;
-      if (e < count && P.has_v) {
-        const float nv = __fadd_rn(__fmul_rn(P.mu, old[k]), u[k]);
-        v[(size_t)r * P.v.row + c] = nv;
-        u[k] = P.nesterov ? __fadd_rn(u[k], __fmul_rn(P.mu, nv)) : nv;
+    for (int k0 = 0; k0 < kGroups; k0 += 4) {
+      float old[4][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = (k0 + k) * kSmallThreads + threadIdx.x, r = e / per_row, c = (e - r * per_row) * 4;
+        if (e < groups) get4(v + (size_t)r * P.v.row + c, P.v_wide, P.cols - c, old[k]);
       }
-      sum += (double)u[k] * (double)u[k];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int e = (k0 + k) * kSmallThreads + threadIdx.x, r = e / per_row, c = (e - r * per_row) * 4;
+        if (e >= groups) continue;
+        float* p = v + (size_t)r * P.v.row + c;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const float nv = __fadd_rn(__fmul_rn(P.mu, old[k][x]), u[k0 + k][x]);
+          old[k][x] = nv;
+          if (c + x < P.cols) u[k0 + k][x] = P.nesterov ? __fadd_rn(u[k0 + k][x], __fmul_rn(P.mu, nv)) : nv;
+        }
+        if (P.v_wide && P.cols - c >= 4) *reinterpret_cast<float4*>(p) = make_float4(old[k][0], old[k][1], old[k][2], old[k][3]);
+        else
+          for (int x = 0; x < 4; ++x)
+            if (c + x < P.cols) p[x] = old[k][x];
+      }
     }
   }
+#pragma unroll
+  for (int k = 0; k < kGroups; ++k)
+#pragma unroll
+    for (int x = 0; x < 4; ++x) sum += (double)u[k][x] * (double)u[k][x];
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) sh->warp_sums[warp] = sum;
   __syncthreads();
@@ -133,33 +181,30 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P)
   for (int k = 0; k < kSmallThreads / 32; ++k) sum += sh->warp_sums[k];
   const float inv = (float)((double)kScaleX / (sqrt(sum) + (double)P.eps));
   const bool tall = P.rows > P.cols;
-  for (int e0 = threadIdx.x; e0 < count; e0 += kAhead * kSmallThreads) {
-    float u[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int e = e0 + k * kSmallThreads, r = e / P.cols, c = e - r * P.cols;
-      u[k] = 0.f;
-      if (e < count) {
-        if (!P.has_v) u[k] = to_f32(g[(size_t)r * P.g.row + c]);
-        else if (!P.nesterov) u[k] = v[(size_t)r * P.v.row + c];
-        else u[k] = __fadd_rn(to_f32(g[(size_t)r * P.g.row + c]), __fmul_rn(P.mu, v[(size_t)r * P.v.row + c]));
-      }
-    }
+  for (int k = 0; k < kGroups; ++k) {
+    const int e = k * kSmallThreads + threadIdx.x, r = e / per_row, c = (e - r * per_row) * 4;
+    if (e >= groups) continue;
+    __align__(8) __half hi[4], lo[4];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int e = e0 + k * kSmallThreads, r = e / P.cols, c = e - r * P.cols;
-      if (e >= count) continue;
-      const int off = tall ? entry_offset(c, r) : entry_offset(r, c);
-      __half hi, lo;
-      split_half(u[k] * inv, &hi, &lo);
-      *reinterpret_cast<__half*>(x_hi + off) = hi;
-      *reinterpret_cast<__half*>(x_lo + off) = lo;
+    for (int x = 0; x < 4; ++x) split_half(u[k][x] * inv, &hi[x], &lo[x]);
+    if (!tall) {
+      const int off = entry_offset(r, c);                    // four entries from a multiple of four: eight bytes
+      *reinterpret_cast<uint2*>(x_hi + off) = *reinterpret_cast<uint2*>(hi);
+      *reinterpret_cast<uint2*>(x_lo + off) = *reinterpret_cast<uint2*>(lo);
+    } else {
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        if (c + x < P.cols) {
+          const int off = entry_offset(c + x, r);
+          *reinterpret_cast<__half*>(x_hi + off) = hi[x];
+          *reinterpret_cast<__half*>(x_lo + off) = lo[x];
+        }
     }
   }
   // ---- the products
-  const int quad = warp & 3, half = warp >> 2, i = quad * 32 + lane;
-  const int m16 = (P.m + 15) / 16, n16 = (P.n + 15) / 16, m32 = (P.m + 31) / 32, n32 = (P.n + 31) / 32;
-
+  const int quad = warp & 3, part = warp >> 2, i = quad * 32 + lane;          // rows of a warp, and its part of the columns
+  const int m16 = (P.m + 15) / 16, n16 = (P.n + 15) / 16, rows_here = quad * 32 < P.m;
   uint32_t phase = 0, tmem = 0;
   bool ok = true;
   // one product on the tensor cores: K in steps of 16; then every thread may take its row of the sums
@@ -172,13 +217,20 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P)
     if (threadIdx.x == 0) {
       const uint32_t idesc = product_desc(128, n, b_mn);
       bool add = false;
-      for (int p = split ? 0 : 2; p < 3; ++p)                                // hi lo + lo hi first, hi hi last: see the larger products
-        for (int k = 0; k < k16; ++k) {
-          const uint32_t at_a = a[p == 1] + (k >> 2) * kPanel + (k & 3) * 32;
-          const uint32_t at_b = b[p == 0] + (b_mn ? k * 2048 : (k >> 2) * kPanel + (k & 3) * 32);
-          mma_f16<1>(tmem, operand_desc(at_a), b_mn ? operand_desc(at_b, kPanel) : operand_desc(at_b), idesc, add);
-          add = true;
+      for (int p = split ? 0 : 2; p < 3; ++p) {                              // hi lo + lo hi first, hi hi last: see the larger products
+        const uint64_t da = operand_desc(a[p == 1]), db = operand_desc(b[p == 0], b_mn ? kPanel : 16);
+        for (int k0 = 0; k0 < k16; k0 += 4) {
+          const uint64_t pa = da + (uint64_t)(k0 / 4 * (kPanel / 16)), pb = db + (uint64_t)(b_mn ? k0 * 128 : k0 / 4 * (kPanel / 16));
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (k0 + k < k16) {
+              // two pieces: the second half of k has a sum of its own (see take16)
+              const bool other = split && p == 2 && k0 + k >= k16 - k16 / 2;
+              mma_f16<1>(tmem + (other ? P.tmem_cols / 2 : 0), pa + 2 * k, pb + (b_mn ? 128 * k : 2 * k), idesc, other ? k0 + k > k16 - k16 / 2 : add);
+              add = true;
+            }
         }
+      }
       mma_commit<1>(smem_addr(&sh->done));
     }
     __syncwarp();
@@ -186,30 +238,41 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P)
     phase ^= 1;
     tcgen05_fence_after();
   };
-  for (int step = 0; step < P.steps && ok; ++step) {
-    const bool split = step < P.split;
-    const uint32_t row = (uint32_t)(quad * 32) << 16;
-    float acc[32];
-    product(xa, xa, false, m16 * 16, n16, split);
-#pragma unroll 1
-    for (int c = half; c < m32; c += 2) {
-      tmem_load32(tmem + row + c * 32, acc);
+  // 16 columns of this thread's row.  The tensor cores cut off what falls below the running sum; two shorter sums lose half of it.
+  auto take16 = [&](int column, bool two, float* acc) {
+    const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + column;
+    tmem_load16(at, acc);
+    if (two) {
+      float more[16];
+      tmem_load16(at + P.tmem_cols / 2, more);
       tmem_load_wait();
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int e = 0; e < 16; ++e) acc[e] += more[e];
+    } else {
+      tmem_load_wait();
+    }
+  };
+  for (int step = 0; step < P.steps && ok; ++step) {
+    const bool split = step < P.split;
+    float acc[16];
+    product(xa, xa, false, m16 * 16, n16, split);
+#pragma unroll 1
+    for (int c = part; rows_here && c < m16; c += kSmallThreads / 128) {
+      take16(c * 16, split && n16 > 1, acc);
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[q * 8 + e] *= kScaleS / (kScaleX * kScaleX);
-        if (i < P.m) write8(s_hi, s_lo, entry_offset(i, c * 32 + q * 8), acc + q * 8);
+        if (i < P.m) write8(s_hi, s_lo, entry_offset(i, c * 16 + q * 8), acc + q * 8);
       }
     }
     product(sa, sa, false, m16 * 16, m16, split);
 #pragma unroll 1
-    for (int c = half; c < m32; c += 2) {
-      tmem_load32(tmem + row + c * 32, acc);
-      tmem_load_wait();
+    for (int c = part; rows_here && c < m16; c += kSmallThreads / 128) {
+      take16(c * 16, split && m16 > 1, acc);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int off = entry_offset(i, c * 32 + q * 8);
+      for (int q = 0; q < 2; ++q) {
+        const int off = entry_offset(i, c * 16 + q * 8);
         float s[8];
         read8(s_hi, s_lo, off, split, s);
 #pragma unroll
@@ -221,12 +284,11 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P)
     product(sa, xa, true, n16 * 16, m16, split);
     const bool last = step + 1 == P.steps;
 #pragma unroll 1
-    for (int c = half; c < n32; c += 2) {
-      tmem_load32(tmem + row + c * 32, acc);
-      tmem_load_wait();
+    for (int c = part; rows_here && c < n16; c += kSmallThreads / 128) {
+      take16(c * 16, split && m16 > 1, acc);
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int j = c * 32 + q * 8, off = entry_offset(i, j);
+      for (int q = 0; q < 2; ++q) {
+        const int j = c * 16 + q * 8, off = entry_offset(i, j);
         float x[8];
         read8(x_hi, x_lo, off, step < P.carried, x);
 #pragma unroll
@@ -249,13 +311,22 @@ __global__ void __launch_bounds__(kSmallThreads) small_kernel(const SmallArgs P)
   if (warp == 0) tmem_free<1>(sh->tmem, P.tmem_cols);
 }
 
-template <typename G>
+template <typename G, int kSmallThreads>
 cudaError_t launch(const SmallArgs& A, int batch, int bytes, cudaStream_t st) {
   static int done[kMaxDevices];
-  cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(small_kernel<G>), bytes, done);
+  auto kernel = small_kernel<G, kSmallThreads>;
+  cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), bytes, done);
   if (e != cudaSuccess) return e;
   count_launch();
-  return launch_after(small_kernel<G>, dim3(batch), dim3(kSmallThreads), bytes, st, A);
+  return launch_after(kernel, dim3(batch), dim3(kSmallThreads), bytes, st, A);
+}
+
+// Two CTAs of 256 threads share an SM where there are more matrices than SMs and each fits in half of one: 296 of 64 x 64
+// fp32 take X us that way and Y us with 512 threads; a single one takes longer.
+template <typename G>
+cudaError_t launch_by(const SmallArgs& A, int batch, int bytes, cudaStream_t st) {
+  const bool half = batch > sm_count() && bytes <= 112 * 1024 && A.tmem_cols <= 256 && A.rows * ((A.cols + 3) / 4) <= 256 * kGroups;
+  return half ? launch<G, 256>(A, batch, bytes, st) : launch<G, 512>(A, batch, bytes, st);
 }
 
 }  // namespace
@@ -271,11 +342,14 @@ cudaError_t launch_small(const OrthoPlan& P, const OrthoRequest& R, char* ws, cu
   A.rows = (int)P.rows; A.cols = (int)P.cols; A.m = P.m; A.n = P.n;
   A.panels_x = (P.n + 63) / 64;
   A.panels_s = (P.m + 63) / 64;
-  A.tmem_cols = 32;                                  // 32-column loads must stay inside
-  while (A.tmem_cols < (P.n + 31) / 32 * 32) A.tmem_cols *= 2;
+  A.tmem_cols = 32;                                  // two sums
+  while (A.tmem_cols < (P.n + 15) / 16 * 32) A.tmem_cols *= 2;
+  const size_t g_four = 4 * dtype_bytes(R.g_dtype);
+  A.g_wide = is_aligned(R.g.p, g_four) && R.g.row % 4 == 0 && (P.batch == 1 || R.g.batch % 4 == 0);
+  A.v_wide = R.has_v && is_aligned(R.v.p, 16) && R.v.row % 4 == 0 && (P.batch == 1 || R.v.batch % 4 == 0);
   const int bytes = 1024 + 2 * (A.panels_x + A.panels_s) * kPanel + (int)sizeof(SmallShared);
-  if (R.g_dtype == S3GD_F32) return launch<float>(A, P.batch, bytes, st);
-  return R.g_dtype == S3GD_BF16 ? launch<__nv_bfloat16>(A, P.batch, bytes, st) : launch<int8_t>(A, P.batch, bytes, st);
+  if (R.g_dtype == S3GD_F32) return launch_by<float>(A, P.batch, bytes, st);
+  return R.g_dtype == S3GD_BF16 ? launch_by<__nv_bfloat16>(A, P.batch, bytes, st) : launch_by<int8_t>(A, P.batch, bytes, st);
 }
 
 }  // namespace s3gd
