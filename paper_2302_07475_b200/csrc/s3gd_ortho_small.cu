@@ -214,24 +214,26 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
     __syncthreads();
     tcgen05_fence_after();
     tmem = sh->tmem;
-    if (threadIdx.x == 0) {
+    if (warp == 0) {                                         // the whole warp counts along, one lane issues
       const uint32_t idesc = product_desc(128, n, b_mn);
-      bool add = false;
-      for (int p = split ? 0 : 2; p < 3; ++p) {                              // hi lo + lo hi first, hi hi last: see the larger products
-        const uint64_t da = operand_desc(a[p == 1]), db = operand_desc(b[p == 0], b_mn ? kPanel : 16);
-        for (int k0 = 0; k0 < k16; k0 += 4) {
-          const uint64_t pa = da + (uint64_t)(k0 / 4 * (kPanel / 16)), pb = db + (uint64_t)(b_mn ? k0 * 128 : k0 / 4 * (kPanel / 16));
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (k0 + k < k16) {
-              // two pieces: the second half of k has a sum of its own (see take16)
-              const bool other = split && p == 2 && k0 + k >= k16 - k16 / 2;
-              mma_f16<1>(tmem + (other ? P.tmem_cols / 2 : 0), pa + 2 * k, pb + (b_mn ? 128 * k : 2 * k), idesc, other ? k0 + k > k16 - k16 / 2 : add);
-              add = true;
-            }
+      auto pass = [&](uint32_t d, uint32_t at_a, uint32_t at_b, int from, int to, bool add) {
+        const uint64_t da = operand_desc(at_a), db = operand_desc(at_b, b_mn ? kPanel : 16);
+        for (int k = from; k < to; ++k) {
+          const uint32_t step = (uint32_t)(k >> 2) * (kPanel / 16) + (uint32_t)(k & 3) * 2;
+          mma_f16_elect(d, da + step, db + (b_mn ? (uint32_t)k * 128 : step), idesc, add);
+          add = true;
         }
+      };
+      // two pieces: hi lo + lo hi before hi hi, as in the larger products, and the second half of hi hi into a sum of its own
+      if (split) {
+        pass(tmem, a[0], b[1], 0, k16, false);
+        pass(tmem, a[1], b[0], 0, k16, true);
+        pass(tmem, a[0], b[0], 0, k16 - k16 / 2, true);
+        pass(tmem + P.tmem_cols / 2, a[0], b[0], k16 - k16 / 2, k16, false);
+      } else {
+        pass(tmem, a[0], b[0], 0, k16, false);
       }
-      mma_commit<1>(smem_addr(&sh->done));
+      mma_commit_elect(smem_addr(&sh->done));
     }
     __syncwarp();
     ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->done), phase)) && ok;
