@@ -41,25 +41,43 @@ __device__ __forceinline__ double block_sum(double v, double* warp_sums) {
   return v;
 }
 
-// v <- mu v + g, and the sum of squares of u, in 64 bits (no overflow for any finite fp32 input).
+// v <- mu v + g, and the sum of squares of u, in 64 bits (no overflow for any finite fp32 input).  The matrix counts as one row
+// where its rows follow one another.  Four times four entries per lane are under way.
 template <typename G>
-__global__ void momentum_norm_kernel(Mat g, Mat v, bool has_v, uint64_t rows, uint64_t cols, float mu, int nesterov,
-                                     double* partial) {
+__global__ void __launch_bounds__(kPrepThreads) momentum_norm_kernel(Mat g, Mat v, bool has_v, bool g_wide, bool v_wide, uint64_t rows,
+                                                                     uint64_t cols, float mu, int nesterov, double* partial, uint32_t* hdr) {
   __shared__ double warp_sums[kPrepThreads / 32];
+  constexpr int kSeg = 512;
+  grid_dependency_wait();
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < kHdrWords) hdr[threadIdx.x] = 0;
   const G* gp = reinterpret_cast<const G*>(g.p) + (size_t)blockIdx.y * g.batch;
   float* vp = reinterpret_cast<float*>(v.p) + (has_v ? (size_t)blockIdx.y * v.batch : 0);
-  const uint64_t segs = (cols + 127) / 128, warps = (uint64_t)gridDim.x * (kPrepThreads / 32);
+  const uint64_t segs = (cols + kSeg - 1) / kSeg, warps = (uint64_t)gridDim.x * (kPrepThreads / 32);
   double sum = 0.0;
   for (uint64_t s = (uint64_t)blockIdx.x * (kPrepThreads / 32) + (threadIdx.x >> 5); s < segs * rows; s += warps) {
-    const uint64_t r = s / segs, c0 = (s % segs) * 128;
-    for (uint64_t c = c0 + lane_id(); c < cols && c < c0 + 128; c += 32) {
-      float u = to_f32(gp[r * g.row + c]);
+    const uint64_t r = s / segs, c0 = (s % segs) * kSeg + lane_id() * 4;
+    const G* gr = gp + r * g.row;
+    float* vr = vp + (has_v ? r * v.row : 0);
+    float u[4][4], old[4][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint64_t c = c0 + k * 128;
+      get4(gr + c, g_wide, (int64_t)cols - (int64_t)c, u[k]);
+      if (has_v) get4(vr + c, v_wide, (int64_t)cols - (int64_t)c, old[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint64_t c = c0 + k * 128;
       if (has_v) {
-        const float nv = __fadd_rn(__fmul_rn(mu, vp[r * v.row + c]), u);
-        vp[r * v.row + c] = nv;
-        u = nesterov ? __fadd_rn(u, __fmul_rn(mu, nv)) : nv;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          old[k][x] = __fadd_rn(__fmul_rn(mu, old[k][x]), u[k][x]);
+          u[k][x] = nesterov ? __fadd_rn(u[k][x], __fmul_rn(mu, old[k][x])) : old[k][x];   // beside the matrix: zero
+        }
+        put4(vr + c, v_wide, (int64_t)cols - (int64_t)c, old[k]);
       }
-      sum += (double)u * (double)u;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum += (double)u[k][x] * (double)u[k][x];
     }
   }
   sum = block_sum(sum, warp_sums);
@@ -68,43 +86,53 @@ __global__ void momentum_norm_kernel(Mat g, Mat v, bool has_v, uint64_t rows, ui
 
 // X_0 = u / (|u| + eps) in two fp16 pieces, transposed where the matrix is tall: 64 x 64 tiles through shared memory
 template <typename G>
-__global__ void __launch_bounds__(kPrepThreads) normalise_kernel(Mat g, Mat v, bool has_v, uint64_t rows, uint64_t cols, float mu, int nesterov,
-                                                                 float eps, const double* partial, int norm_blocks, __half* x, int m, int n,
-                                                                 int ldx) {
+__global__ void __launch_bounds__(kPrepThreads) normalise_kernel(Mat g, Mat v, bool has_v, bool g_wide, bool v_wide, uint64_t rows, uint64_t cols,
+                                                                 float mu, int nesterov, float eps, const double* partial, int norm_blocks,
+                                                                 __half* x, int m, int n, int ldx) {
   __shared__ double warp_sums[kPrepThreads / 32];
   __shared__ float tile[64][65];
   const size_t b = blockIdx.z;
   const G* gp = reinterpret_cast<const G*>(g.p) + b * g.batch;
   const float* vp = reinterpret_cast<const float*>(v.p) + (has_v ? b * v.batch : 0);
+  const bool tall = rows > cols;
+  const uint64_t i0 = (uint64_t)blockIdx.y * 64, j0 = (uint64_t)blockIdx.x * 64;    // of X
+  const uint64_t r0 = tall ? j0 : i0, c0 = (tall ? i0 : j0) + (threadIdx.x & 15) * 4;   // of the matrix
+  grid_dependency_wait();
+  float u[4][4], old[4][4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint64_t r = r0 + k * 16 + (threadIdx.x >> 4);
+    const int64_t left = r < rows ? (int64_t)cols - (int64_t)c0 : 0;
+    const bool from_v = has_v && !nesterov;
+    if (!from_v) get4(gp + r * g.row + c0, g_wide, left, u[k]);
+    if (has_v) get4(vp + r * v.row + c0, v_wide, left, from_v ? u[k] : old[k]);
+  }
   double s = 0.0;
   for (int i = threadIdx.x; i < norm_blocks; i += kPrepThreads) s += partial[b * norm_blocks + i];
   const float inv = (float)((double)kScaleX / (sqrt(block_sum(s, warp_sums)) + (double)eps));
-  const bool tall = rows > cols;
-  const uint64_t i0 = (uint64_t)blockIdx.y * 64, j0 = (uint64_t)blockIdx.x * 64;    // of X
-  const uint64_t r0 = tall ? j0 : i0, c0 = tall ? i0 : j0;                          // of the matrix
-  for (int e = threadIdx.x; e < 64 * 64; e += kPrepThreads) {
-    const int dr = e / 64, dc = e % 64;
-    float u = 0.f;
-    if (r0 + dr < rows && c0 + dc < cols) {
-      u = to_f32(gp[(r0 + dr) * g.row + c0 + dc]);
-      if (has_v) {
-        const float nv = vp[(r0 + dr) * v.row + c0 + dc];
-        u = nesterov ? __fadd_rn(u, __fmul_rn(mu, nv)) : nv;
-      }
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const int dr = k * 16 + (threadIdx.x >> 4), dc = (threadIdx.x & 15) * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float w = has_v && nesterov ? __fadd_rn(u[k][e], __fmul_rn(mu, old[k][e])) : u[k][e];
+      tile[tall ? dc + e : dr][tall ? dr : dc + e] = w * inv;
     }
-    tile[tall ? dc : dr][tall ? dr : dc] = u * inv;
   }
   __syncthreads();
   __half* hi_row = x + b * 2 * m * (size_t)ldx;
-  for (int e = threadIdx.x; e < 64 * 32; e += kPrepThreads) {
-    const int di = e / 32, dj = (e % 32) * 2;
-    if (i0 + di >= (uint64_t)m || j0 + dj >= (uint64_t)ldx) continue;               // ldx is even: both or neither
-    __half h0, l0, h1, l1;
-    split_half(tile[di][dj], &h0, &l0);
-    split_half(tile[di][dj + 1], &h1, &l1);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int di = k * 32 + (threadIdx.x >> 3), dj = (threadIdx.x & 7) * 8;
+    if (i0 + di >= (uint64_t)m || j0 + dj >= (uint64_t)ldx) continue;               // ldx is a multiple of eight
+    float w[8];
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[e] = tile[di][dj + e];
+    split8(w, true, hi, lo);
     const size_t at = (i0 + di) * ldx + j0 + dj;
-    *reinterpret_cast<__half2*>(hi_row + at) = __halves2half2(h0, h1);
-    *reinterpret_cast<__half2*>(hi_row + (size_t)m * ldx + at) = __halves2half2(l0, l1);
+    *reinterpret_cast<uint4*>(hi_row + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(hi_row + (size_t)m * ldx + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
 }
 
@@ -128,22 +156,29 @@ bool poly_ok(int steps, float a, float b, float c, float eps) {
   return true;
 }
 
+bool wide_rows(const Mat& a, int dtype, int batch) {
+  return is_aligned(a.p, 4 * dtype_bytes(dtype)) && a.row % 4 == 0 && (batch == 1 || a.batch % 4 == 0);
+}
+
 template <typename G>
 cudaError_t prepare(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st) {
   double* partial = reinterpret_cast<double*>(ws + P.off_norm);
+  const bool g_wide = wide_rows(R.g, R.g_dtype, P.batch), v_wide = R.has_v && wide_rows(R.v, S3GD_F32, P.batch);
+  const bool one_row = R.g.row == (long long)P.cols && (!R.has_v || R.v.row == (long long)P.cols);
   count_launch(2);
-  momentum_norm_kernel<G><<<dim3(P.norm_blocks, P.batch), kPrepThreads, 0, st>>>(R.g, R.v, R.has_v, P.rows, P.cols, R.mu, R.nesterov, partial);
-  normalise_kernel<G><<<dim3((P.n + 63) / 64, (P.m + 63) / 64, P.batch), kPrepThreads, 0, st>>>(
-      R.g, R.v, R.has_v, P.rows, P.cols, R.mu, R.nesterov, R.eps, partial, P.norm_blocks, reinterpret_cast<__half*>(ws + P.off_x), P.m, P.n,
-      P.ldx);
-  return cudaGetLastError();
+  cudaError_t e = launch_after(momentum_norm_kernel<G>, dim3(P.norm_blocks, P.batch), dim3(kPrepThreads), 0, st, R.g, R.v, R.has_v, g_wide, v_wide,
+                               one_row ? (uint64_t)1 : P.rows, one_row ? P.rows * P.cols : P.cols, R.mu, R.nesterov, partial,
+                               reinterpret_cast<uint32_t*>(ws + P.off_hdr));
+  if (e != cudaSuccess) return e;
+  return launch_after(normalise_kernel<G>, dim3((P.n + 63) / 64, (P.m + 63) / 64, P.batch), dim3(kPrepThreads), 0, st, R.g, R.v, R.has_v, g_wide,
+                      v_wide, P.rows, P.cols, R.mu, R.nesterov, R.eps, partial, P.norm_blocks, reinterpret_cast<__half*>(ws + P.off_x), P.m, P.n,
+                      P.ldx);
 }
 
 cudaError_t run(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st) {
-  cudaError_t e = cudaMemsetAsync(ws + P.off_hdr, 0, kHdrWords * sizeof(uint32_t), st);
-  if (e != cudaSuccess) return e;
   if (is_small(P)) return launch_small(P, R, ws, st);
-  e = R.g_dtype == S3GD_F32 ? prepare<float>(P, R, ws, st) : R.g_dtype == S3GD_BF16 ? prepare<__nv_bfloat16>(P, R, ws, st) : prepare<int8_t>(P, R, ws, st);
+  cudaError_t e = R.g_dtype == S3GD_F32 ? prepare<float>(P, R, ws, st) : R.g_dtype == S3GD_BF16 ? prepare<__nv_bfloat16>(P, R, ws, st)
+                                                                                             : prepare<int8_t>(P, R, ws, st);
   return e == cudaSuccess ? launch_products(P, R, ws, st) : e;
 }
 

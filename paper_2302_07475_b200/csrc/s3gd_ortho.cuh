@@ -62,6 +62,64 @@ __device__ __forceinline__ void split_half(float v, __half* hi, __half* lo) {
   *hi = __float2half_rn(v);
   *lo = __float2half_rn(v - __half2float(*hi));
 }
+
+// eight neighbouring entries of a swizzled row as floats, from one or two pieces
+__device__ __forceinline__ void read8(const char* hi, const char* lo, int off, bool two, float* x) {
+  const uint4 h4 = *reinterpret_cast<const uint4*>(hi + off);
+  const __half2* h = reinterpret_cast<const __half2*>(&h4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = __half22float2(h[e]);
+    x[2 * e] = f.x; x[2 * e + 1] = f.y;
+  }
+  if (!two) return;
+  const uint4 l4 = *reinterpret_cast<const uint4*>(lo + off);
+  const __half2* l = reinterpret_cast<const __half2*>(&l4);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float2 f = __half22float2(l[e]);
+    x[2 * e] += f.x; x[2 * e + 1] += f.y;
+  }
+}
+// the two pieces of eight entries, two entries to a word
+__device__ __forceinline__ void split8(const float* x, bool two, uint32_t* hi, uint32_t* lo) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const __half2 h = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
+    hi[e] = *reinterpret_cast<const uint32_t*>(&h);
+    if (!two) continue;
+    const float2 f = __half22float2(h);
+    const __half2 l = __floats2half2_rn(x[2 * e] - f.x, x[2 * e + 1] - f.y);
+    lo[e] = *reinterpret_cast<const uint32_t*>(&l);
+  }
+}
+
+// The caller's entry after the last product
+template <typename T>
+__device__ __forceinline__ T stored(const Store& s, T old, float v) {
+  return from_f32<T>(s.update ? __fmaf_rn(-s.rate, v, __fmul_rn(s.keep, to_f32(old))) : v);
+}
+template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
+
+// up to four neighbouring entries of a row as floats
+template <typename T>
+__device__ __forceinline__ void get4(const T* p, bool wide, int64_t left, float* x) {
+  if (wide && left >= 4) {
+    const Four<T> f = *reinterpret_cast<const Four<T>*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = to_f32(f.v[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = e < left ? to_f32(p[e]) : 0.f;
+  }
+}
+__device__ __forceinline__ void put4(float* p, bool wide, int64_t left, const float* x) {
+  if (wide && left >= 4) *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  else
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (e < left) p[e] = x[e];
+}
 #endif
 
 // X_0 lies in off_x; enqueues all products, the last of which writes R.out

@@ -25,10 +25,10 @@ namespace {
 constexpr int kBlockK = 64;                       // entries of k per slot: one 128-byte row
 constexpr int kSlotBytes = 32 * 1024;             // 128 rows of each operand
 constexpr int kSlots = 5;
-constexpr int kChunk = 2;                         // slots of k (128 entries) between two additions in registers, two pieces
+constexpr int kChunk = 2;                         // slots of k between two additions in registers, two pieces
 constexpr int kEpiWarps = 8;
 constexpr int kEpiBytes = 8 * 1024;               // per epilogue warp: 32 x 64 entries of either piece
-constexpr int kThreads = 64 + 32 * kEpiWarps;     // one warp loads, one issues the products
+constexpr int kThreads = 128 + 32 * kEpiWarps;    // warp 0 loads, warp 1 issues the products; the epilogue begins at warp 4
 constexpr int kSmemBytes = 1024 + kSlots * kSlotBytes + kEpiWarps * kEpiBytes + 256;
 constexpr int kBand = 8;                          // tile rows that are worked on side by side, for reuse in L2
 
@@ -70,56 +70,90 @@ __device__ __forceinline__ void tile_at(const ProductArgs& P, int t, bool symmet
   }
 }
 
-template <typename T>
-__device__ __forceinline__ T stored(const Store& s, T old, float v) {
-  return from_f32<T>(s.update ? __fmaf_rn(-s.rate, v, __fmul_rn(s.keep, to_f32(old))) : v);
-}
-
-// Rows r0 .. r0 + kRows of 32, 64 columns, of the caller's matrix from a buffer (row r: 256 bytes, 16-byte pieces exchanged by r & 7)
+// Rows r0 .. r0 + kRows of 32, 64 columns, of the caller's matrix from a buffer (row r: 256 bytes, 16-byte pieces exchanged by
+// r & 7).  What is updated is read in batches, so that several reads are under way.
 template <typename T, int kRows>
 __device__ __forceinline__ void store_rows(const Store& s, const float* buf, int b, int i0, int j0, int r0, int m, int n) {
   T* base = reinterpret_cast<T*>(s.to.p) + (size_t)b * s.to.batch;
   const int lane = lane_id();
-  if (s.wide) {
+  if (s.wide && j0 + 64 <= n) {
+    constexpr int kBatch = kRows / 2 < 4 ? kRows / 2 : 4;
+    const int q = lane % 16;
+#pragma unroll 1
+    for (int it0 = 0; it0 < kRows / 2; it0 += kBatch) {
+      Four<T> o[kBatch];
 #pragma unroll
-    for (int it = 0; it < kRows / 2; ++it) {
-      const int r = r0 + it * 2 + lane / 16, q = lane % 16, j = j0 + q * 4;
-      if (i0 + r >= m || j >= n) continue;
-      const float4 v = *reinterpret_cast<const float4*>(buf + r * 64 + ((q ^ (r & 7)) << 2));
-      T* p = base + (size_t)(i0 + r) * s.to.row + j;
-      struct alignas(4 * sizeof(T)) Four { T v[4]; };
-      if (j + 4 <= n) {
-        Four o = {};
-        if (s.update) o = *reinterpret_cast<const Four*>(p);
-        o = {stored(s, o.v[0], v.x), stored(s, o.v[1], v.y), stored(s, o.v[2], v.z), stored(s, o.v[3], v.w)};
-        *reinterpret_cast<Four*>(p) = o;
-      } else {
-        const float w[4] = {v.x, v.y, v.z, v.w};
-        for (int e = 0; j + e < n; ++e) p[e] = stored(s, s.update ? p[e] : T(), w[e]);
+      for (int it = 0; it < kBatch; ++it) {
+        const int r = r0 + (it0 + it) * 2 + lane / 16;
+        if (s.update && i0 + r < m) o[it] = *reinterpret_cast<const Four<T>*>(base + (size_t)(i0 + r) * s.to.row + j0 + q * 4);
+      }
+#pragma unroll
+      for (int it = 0; it < kBatch; ++it) {
+        const int r = r0 + (it0 + it) * 2 + lane / 16;
+        if (i0 + r >= m) continue;
+        const float4 v = *reinterpret_cast<const float4*>(buf + r * 64 + ((q ^ (r & 7)) << 2));
+        o[it] = {stored(s, o[it].v[0], v.x), stored(s, o[it].v[1], v.y), stored(s, o[it].v[2], v.z), stored(s, o[it].v[3], v.w)};
+        *reinterpret_cast<Four<T>*>(base + (size_t)(i0 + r) * s.to.row + j0 + q * 4) = o[it];
       }
     }
   } else {
-    for (int r = r0; r < r0 + kRows && i0 + r < m; ++r)
+    constexpr int kBatch = 4;
+#pragma unroll 1
+    for (int b0 = 0; b0 < kRows; b0 += kBatch) {
+      T o[kBatch][2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int c = h * 32 + lane;
-        if (j0 + c >= n) continue;
-        T* p = base + (size_t)(i0 + r) * s.to.row + j0 + c;
-        *p = stored(s, s.update ? *p : T(), buf[r * 64 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3)]);
+      for (int x = 0; x < kBatch * 2; ++x) {
+        const int r = r0 + b0 + x / 2, c = x % 2 * 32 + lane;
+        if (s.update && i0 + r < m && j0 + c < n) o[x / 2][x % 2] = base[(size_t)(i0 + r) * s.to.row + j0 + c];
       }
+#pragma unroll
+      for (int x = 0; x < kBatch * 2; ++x) {
+        const int r = r0 + b0 + x / 2, c = x % 2 * 32 + lane;
+        if (i0 + r < m && j0 + c < n)
+          base[(size_t)(i0 + r) * s.to.row + j0 + c] = stored(s, o[x / 2][x % 2], buf[r * 64 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3)]);
+      }
+    }
   }
 }
 
-template <typename T, int kN>
-__device__ __forceinline__ void store_columns(const Store& s, const float* v, int b, int i, int j0, int m, int n) {
-  T* base = reinterpret_cast<T*>(s.to.p) + (size_t)b * s.to.batch + i;
-  if (i >= m) return;
+// Columns c0 .. c0 + kCount of the buffer's 32 x 64 entries, which are rows of the caller's matrix.
+template <typename T, int kCount>
+__device__ __forceinline__ void store_columns(const Store& s, const float* buf, int b, int i0, int j0, int c0, int m, int n) {
+  const int lane = lane_id();
+  if (i0 + lane >= m) return;
+  T* base = reinterpret_cast<T*>(s.to.p) + (size_t)b * s.to.batch + i0 + lane;
+  const float* row = buf + lane * 64;
+#pragma unroll 1
+  for (int c = c0; c < c0 + kCount && j0 + c < n; c += 8) {
+    T* p = base + (size_t)(j0 + c) * s.to.row;
+    T old[8];
 #pragma unroll
-  for (int e = 0; e < kN; ++e)
-    if (j0 + e < n) {
-      T* p = base + (size_t)(j0 + e) * s.to.row;
-      *p = stored(s, s.update ? *p : T(), v[e]);
-    }
+    for (int e = 0; e < 8; ++e)
+      if (s.update && j0 + c + e < n) old[e] = p[(size_t)e * s.to.row];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (j0 + c + e < n) p[(size_t)e * s.to.row] = stored(s, old[e], row[((((c + e) >> 2) ^ (lane & 7)) << 2) + ((c + e) & 3)]);
+  }
+}
+
+// Eight entries of row `lane` of a 32-row part (two to a word), as column `lane` of its mirror image: row c of the image is 64
+// bytes.  Neighbouring lanes exchange half of their entries so that words are written; odd lanes go through theirs in another
+// order, which keeps the two off each other's banks.
+__device__ __forceinline__ void mirror8(char* image, int c0, const uint32_t* h) {
+  const int lane = lane_id(), odd = lane & 1;
+  const uint32_t g0 = __shfl_xor_sync(0xffffffffu, odd ? h[0] : h[2], 1), g1 = __shfl_xor_sync(0xffffffffu, odd ? h[1] : h[3], 1);
+  uint32_t* to = reinterpret_cast<uint32_t*>(image + c0 * 64) + (lane >> 1);
+  if (!odd) {
+    to[0] = __byte_perm(h[0], g0, 0x5410);
+    to[16] = __byte_perm(h[0], g0, 0x7632);
+    to[32] = __byte_perm(h[1], g1, 0x5410);
+    to[48] = __byte_perm(h[1], g1, 0x7632);
+  } else {
+    to[5 * 16] = __byte_perm(g0, h[2], 0x7632);
+    to[4 * 16] = __byte_perm(g0, h[2], 0x5410);
+    to[7 * 16] = __byte_perm(g1, h[3], 0x7632);
+    to[6 * 16] = __byte_perm(g1, h[3], 0x5410);
+  }
 }
 
 // ------------------------------------------------------------------ the three roles
@@ -166,8 +200,8 @@ struct Turn {
   }
 };
 
-// Products of `blocks` slots of k.  Two pieces: per kChunk slots first hi lo + lo hi, then hi hi, so that few additions
-// are cut off at the size of the full sum.
+// Products of `blocks` slots of k.  Two pieces: hi lo + lo hi before hi hi, so that fewer additions are cut off at the size of
+// the full sum.
 template <int kCta, bool kSplit, bool kMn>
 __device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32_t tmem, int blocks, Ring* ring, Turn* turn) {
   constexpr int kTile = 128 * kCta;
@@ -183,27 +217,19 @@ __device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32
     tcgen05_fence_after();
     const uint32_t d = tmem + turn->sum * kTile;
     if (kSplit) {
-      int hi[kChunk];
       const int n = min(kChunk, blocks - kb);
-#pragma unroll
-      for (int c = 0; c < kChunk; ++c) {
-        if (c >= n) break;
-        hi[c] = ring[0].slot;
-        const int lo = ring[1].slot;
-        if (!mbar_wait(smem_addr(&sh->full[hi[c]]), ring[0].phase)) return false;
+      for (int c = 0; c < n; ++c) {
+        const int hi = ring[0].slot, lo = ring[1].slot;
+        if (!mbar_wait(smem_addr(&sh->full[hi]), ring[0].phase)) return false;
         if (!mbar_wait(smem_addr(&sh->full[lo]), ring[1].phase)) return false;
         tcgen05_fence_after();
-        product(d, hi[c], lo, c > 0);
-        product(d, lo, hi[c], true);
+        product(d, hi, lo, c > 0);
+        product(d, lo, hi, true);
         mma_commit<kCta>(smem_addr(&sh->empty[lo]));
+        product(d, hi, hi, true);
+        mma_commit<kCta>(smem_addr(&sh->empty[hi]));
         ring[0].next();
         ring[1].next();
-      }
-#pragma unroll
-      for (int c = 0; c < kChunk; ++c) {
-        if (c >= n) break;
-        product(d, hi[c], hi[c], true);
-        mma_commit<kCta>(smem_addr(&sh->empty[hi[c]]));
       }
       kb += n;
     } else {
@@ -260,88 +286,85 @@ __device__ __forceinline__ void load_add(const ProductArgs& P, uint32_t buf_addr
   for (int piece = 0; piece < P.add_pieces; ++piece) tma_load<1>(buf_addr + piece * 4096, &P.add, j0, i0, 2 * b + piece, bar);
 }
 
-// Eight entries of a row from their sums in x, in place, and (unless they are the caller's) in the buffer at `off` as they are
-// stored; what is added lies there before.
-__device__ __forceinline__ void finish_piece(const ProductArgs& P, char* buf, int off, bool has_add, float* x) {
-  float add[8] = {};
-  if (has_add) {
-    const uint4 h4 = *reinterpret_cast<const uint4*>(buf + off);
-    const __half2* h = reinterpret_cast<const __half2*>(&h4);
+// keeps the compiler from starting all pieces of a row at once, for which there are no registers
+__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
+
+// Eight entries of a row from their sums in x, in place; what is added lies in the buffer at `off`.
+__device__ __forceinline__ void combine8(const ProductArgs& P, const char* buf, int off, float* x) {
+  if (P.kind == kGram) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float2 f = __half22float2(h[e]);
-      add[2 * e] = f.x; add[2 * e + 1] = f.y;
-    }
-    if (P.add_pieces == 2) {
-      const uint4 l4 = *reinterpret_cast<const uint4*>(buf + 4096 + off);
-      const __half2* l = reinterpret_cast<const __half2*>(&l4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float2 f = __half22float2(l[e]);
-        add[2 * e] += f.x; add[2 * e + 1] += f.y;
-      }
-    }
+    for (int e = 0; e < 8; ++e) x[e] *= P.c_acc;
+    return;
   }
+  float add[8];
+  read8(buf, buf + 4096, off, P.add_pieces == 2, add);
 #pragma unroll
   for (int e = 0; e < 8; ++e) x[e] = __fmaf_rn(P.c_add, add[e], __fmul_rn(P.c_acc, x[e]));
-  if (P.kind != kFinal) {
-    __align__(16) __half hi[8], lo[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) split_half(x[e], &hi[e], &lo[e]);
-    *reinterpret_cast<uint4*>(buf + off) = *reinterpret_cast<uint4*>(hi);
-    if (P.out_pieces == 2) *reinterpret_cast<uint4*>(buf + 4096 + off) = *reinterpret_cast<uint4*>(lo);
-  }
 }
 
 // 32 x 64 entries of the result from the sums in v: rows i0 + lane, columns j0 ..  The matrix that is added lies in the buffer.
 __device__ __forceinline__ void finish(const ProductArgs& P, char* buf, uint32_t buf_addr, int b, int i0, int j0, bool mirror, float* v) {
   const int lane = lane_id();
-  const bool has_add = P.kind != kGram;
-  if (!has_add) {
+  const bool two = P.out_pieces == 2;
+  if (P.kind == kGram) {
     if (lane == 0) tma_store_wait_read();
     __syncwarp();
   }
   // row `lane` of the buffer: 16-byte pieces exchanged by lane & 7, as TMA lays them
-#pragma unroll
-  for (int q = 0; q < 8; ++q) finish_piece(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), has_add, v + q * 8);
   if (P.kind != kFinal) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int off = lane * 128 + ((q ^ (lane & 7)) << 4);
+      uint32_t hi[4], lo[4];
+      in_order();
+      combine8(P, buf, off, v + q * 8);
+      split8(v + q * 8, two, hi, lo);
+      *reinterpret_cast<uint4*>(buf + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+      if (two) *reinterpret_cast<uint4*>(buf + 4096 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      else if (mirror) mirror8(buf + 4096, q * 8, hi);      // one piece: its mirror image fits beside it
+    }
     fence_async_smem();
     __syncwarp();
     if (lane == 0) {
-      tma_store(&P.out, j0, i0, 2 * b, buf_addr);
-      if (P.out_pieces == 2) tma_store(&P.out, j0, i0, 2 * b + 1, buf_addr + 4096);
+      for (int piece = 0; piece < P.out_pieces; ++piece) tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
+      if (mirror && !two) tma_store(&P.mirror, i0, j0, 2 * b, buf_addr + 4096);
       tma_store_commit();
     }
-    if (mirror) {                                         // rows j0 + e, columns i0 ..
+    if (mirror && two) {
       if (lane == 0) tma_store_wait_read();
       __syncwarp();
 #pragma unroll
-      for (int e = 0; e < 64; ++e) {
-        __half hi, lo;
-        split_half(v[e], &hi, &lo);
-        *reinterpret_cast<__half*>(buf + e * 64 + lane * 2) = hi;
-        if (P.out_pieces == 2) *reinterpret_cast<__half*>(buf + 4096 + e * 64 + lane * 2) = lo;
+      for (int q = 0; q < 8; ++q) {
+        uint32_t hi[4], lo[4];
+        in_order();
+        split8(v + q * 8, true, hi, lo);
+        mirror8(buf, q * 8, hi);
+        mirror8(buf + 4096, q * 8, lo);
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
-        tma_store(&P.mirror, i0, j0, 2 * b, buf_addr);
-        if (P.out_pieces == 2) tma_store(&P.mirror, i0, j0, 2 * b + 1, buf_addr + 4096);
+        for (int piece = 0; piece < 2; ++piece) tma_store(&P.mirror, i0, j0, 2 * b + piece, buf_addr + piece * 4096);
         tma_store_commit();
       }
     }
     return;
   }
-  if (P.store.transpose) {
-    if (P.store.dtype == S3GD_F32) store_columns<float, 64>(P.store, v, b, i0 + lane, j0, P.m, P.n);
-    else store_columns<__nv_bfloat16, 64>(P.store, v, b, i0 + lane, j0, P.m, P.n);
-  } else {
-    __syncwarp();
-    float* f = reinterpret_cast<float*>(buf);
 #pragma unroll
-    for (int q = 0; q < 16; ++q)
-      *reinterpret_cast<float4*>(f + lane * 64 + ((q ^ (lane & 7)) << 2)) = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-    __syncwarp();
+  for (int q = 0; q < 8; ++q) {
+    in_order();
+    combine8(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), v + q * 8);
+  }
+  __syncwarp();
+  float* f = reinterpret_cast<float*>(buf);
+#pragma unroll
+  for (int q = 0; q < 16; ++q)
+    *reinterpret_cast<float4*>(f + lane * 64 + ((q ^ (lane & 7)) << 2)) = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
+  __syncwarp();
+  if (P.store.transpose) {
+    if (P.store.dtype == S3GD_F32) store_columns<float, 64>(P.store, f, b, i0, j0, 0, P.m, P.n);
+    else store_columns<__nv_bfloat16, 64>(P.store, f, b, i0, j0, 0, P.m, P.n);
+  } else {
     if (P.store.dtype == S3GD_F32) store_rows<float, 32>(P.store, f, b, i0, j0, 0, P.m, P.n);
     else store_rows<__nv_bfloat16, 32>(P.store, f, b, i0, j0, 0, P.m, P.n);
   }
@@ -422,8 +445,8 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   } else if (warp == 1) {
     if (lane_id() == 0 && rank == 0)
       for (int t = first; t < tiles && ok; t += stride) ok = issue_products<2, kSplit, kMn>(sh, base, tmem, blocks, ring, &turn);
-  } else {
-    const int w = warp - 2, quad = warp & 3, half = w >> 2, lane = lane_id();
+  } else if (warp >= 4) {
+    const int w = warp - 4, quad = warp & 3, half = w >> 2, lane = lane_id();
     char* buf = epi + w * kEpiBytes;
     const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[w]);
     const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), 0), cluster_addr(smem_addr(&sh->sum_empty[1]), 0)};
@@ -435,20 +458,41 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int i0 = tm * kTile + (int)rank * 128 + quad * 32, jt = tn * kTile + half * kCols;
       const bool here = i0 < P.m && jt < P.n;
       if (has_add && here && lane == 0) load_add(P, buf_addr, add_bar, b, i0, jt);
-      float acc[kCols];
-      ok = take_sums<kTile, kCols>(sh, tmem, quad, half * kCols, sums_of(kSplit, blocks), empty_bar, &turn, acc);
-      if (!ok || !here) continue;
-#pragma unroll
-      for (int c = 0; c < kCols / 64; ++c) {
+      auto finish_chunk = [&](int c, float* v) {
         const int j0 = jt + c * 64;
-        if (j0 >= P.n) break;
+        if (!here || j0 >= P.n || !ok) return;
         if (has_add) {
           if (c > 0 && lane == 0) load_add(P, buf_addr, add_bar, b, i0, j0);
           ok = __all_sync(0xffffffffu, mbar_wait(add_bar, add_phase));
-          if (!ok) break;
+          if (!ok) return;
           add_phase ^= 1;
         }
-        finish(P, buf, buf_addr, b, i0, j0, symmetric && tm != tn, acc + c * 64);
+        finish(P, buf, buf_addr, b, i0, j0, symmetric && tm != tn, v);
+      };
+      if (kSplit) {
+        float acc[kCols];
+        ok = take_sums<kTile, kCols>(sh, tmem, quad, half * kCols, sums_of(true, blocks), empty_bar, &turn, acc);
+#pragma unroll
+        for (int c = 0; c < kCols / 64; ++c) finish_chunk(c, acc + c * 64);
+      } else {
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sum_full[turn.sum]), turn.phase));
+        if (!ok) break;
+        tcgen05_fence_after();
+#pragma unroll 1
+        for (int c = 0; c < kCols / 64; ++c) {               // one copy of the code: the kernels are short, instructions come late
+          float v[64];
+          const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + turn.sum * kTile + half * kCols + c * 64;
+          tmem_load32(at, v);
+          tmem_load32(at + 32, v + 32);
+          tmem_load_wait();
+          if (c + 1 == kCols / 64) {
+            tcgen05_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(empty_bar[turn.sum]);
+          }
+          finish_chunk(c, v);
+        }
+        turn.next();
       }
     }
     if (lane == 0) tma_store_wait_read();
@@ -477,14 +521,14 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
   int b, tm, tn;
   tile_at(P, blockIdx.x / kWays, symmetric, &b, &tm, &tn);
   const uint32_t tmem = set_up<1>(P, sh, 256);
-  const int w = warp - 2, quad = warp & 3, lane = lane_id();
+  const int w = warp - 4, quad = warp & 3, lane = lane_id();
   // what this warp finishes: pieces q0 .. q0 + kMine of part `part`
   const int pl = kWays == 1 ? quad * 2 + (w >> 2) : w * kMine / 8, part = (int)rank * kMine + pl, q0 = w * kMine % 8;
   const int i0 = tm * kTile + (part >> 1) * 32, j0 = tn * kTile + (part & 1) * kCols;
-  const bool here = warp >= 2 && i0 < P.m && j0 < P.n, leads = q0 == 0 && lane == 0;
-  char* buf = epi + (warp >= 2 ? pl : 0) * kEpiBytes;         // what is added, then the result
-  char* side = base_ptr + 8 * 8192 + (warp >= 2 ? pl : 0) * 8192;   // its mirror image, or the caller's rows
-  const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[warp >= 2 ? pl : 0]);
+  const bool here = warp >= 4 && i0 < P.m && j0 < P.n, leads = q0 == 0 && lane == 0;
+  char* buf = epi + (warp >= 4 ? pl : 0) * kEpiBytes;         // what is added, then the result
+  char* side = base_ptr + 8 * 8192 + (warp >= 4 ? pl : 0) * 8192;   // its mirror image, or the caller's rows
+  const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[warp >= 4 ? pl : 0]);
   Ring ring[2] = {Ring(0, kSplit ? kHiSlots : kSlots), Ring(kHiSlots, kSlots - kHiSlots)};
   Turn turn;
   bool ok = true;
@@ -493,7 +537,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
     if (lane == 0) ok = load_slots<1, kSplit, kMn>(P, sh, base, 0, b, tm * kTile, tn * kTile, from, to, ring);
   } else if (warp == 1) {
     if (lane == 0) ok = issue_products<1, kSplit, kMn>(sh, base, tmem, to - from, ring, &turn);
-  } else {
+  } else if (warp >= 4) {
     if (has_add && here && leads) load_add(P, buf_addr, add_bar, b, i0, j0);
     const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), rank), cluster_addr(smem_addr(&sh->sum_empty[1]), rank)};
     float acc[kCols];
@@ -533,7 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
   }
   if (here) {
     if (has_add) ok = __all_sync(0xffffffffu, mbar_wait(add_bar, 0)) && ok;
-    const bool mirror = symmetric && tm != tn;
+    const bool mirror = symmetric && tm != tn, two = P.out_pieces == 2;
     // the part that warps finish together: one warp (kWays 1), or 8 / kMine of them
     auto together = [&] {
       if (kWays == 1) __syncwarp();
@@ -543,25 +587,20 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
     for (int p = 0; p < kMine; ++p) {
       const int q = q0 + p, off = lane * 128 + ((q ^ (lane & 7)) << 4);
       float* x = v + p * 8;
-      finish_piece(P, buf, off, has_add, x);
-      if (mirror) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          __half hi, lo;
-          split_half(x[e], &hi, &lo);
-          *reinterpret_cast<__half*>(side + (q * 8 + e) * 64 + lane * 2) = hi;
-          if (P.out_pieces == 2) *reinterpret_cast<__half*>(side + 4096 + (q * 8 + e) * 64 + lane * 2) = lo;
+      combine8(P, buf, off, x);
+      if (P.kind != kFinal) {
+        uint32_t hi[4], lo[4];
+        split8(x, two, hi, lo);
+        *reinterpret_cast<uint4*>(buf + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        if (two) *reinterpret_cast<uint4*>(buf + 4096 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        if (mirror) {
+          mirror8(side, q * 8, hi);
+          if (two) mirror8(side + 4096, q * 8, lo);
         }
-      }
-      if (P.kind == kFinal) {
-        if (P.store.transpose) {
-          if (P.store.dtype == S3GD_F32) store_columns<float, 8>(P.store, x, b, i0 + lane, j0 + q * 8, P.m, P.n);
-          else store_columns<__nv_bfloat16, 8>(P.store, x, b, i0 + lane, j0 + q * 8, P.m, P.n);
-        } else {
-          float* f = reinterpret_cast<float*>(side) + lane * 64;
-          *reinterpret_cast<float4*>(f + (((2 * q) ^ (lane & 7)) << 2)) = make_float4(x[0], x[1], x[2], x[3]);
-          *reinterpret_cast<float4*>(f + (((2 * q + 1) ^ (lane & 7)) << 2)) = make_float4(x[4], x[5], x[6], x[7]);
-        }
+      } else {
+        float* f = reinterpret_cast<float*>(side) + lane * 64;
+        *reinterpret_cast<float4*>(f + (((2 * q) ^ (lane & 7)) << 2)) = make_float4(x[0], x[1], x[2], x[3]);
+        *reinterpret_cast<float4*>(f + (((2 * q + 1) ^ (lane & 7)) << 2)) = make_float4(x[4], x[5], x[6], x[7]);
       }
     }
     if (P.kind != kFinal) {
@@ -575,12 +614,17 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
         tma_store_commit();
         tma_store_wait_read();
       }
-    } else if (!P.store.transpose) {
+    } else {
       together();
       const float* f = reinterpret_cast<const float*>(side);
-      constexpr int kRows = 32 / kWays;                       // of the part's 32 rows, per warp
-      if (P.store.dtype == S3GD_F32) store_rows<float, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
-      else store_rows<__nv_bfloat16, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
+      if (P.store.transpose) {
+        if (P.store.dtype == S3GD_F32) store_columns<float, 8 * kMine>(P.store, f, b, i0, j0, q0 * 8, P.m, P.n);
+        else store_columns<__nv_bfloat16, 8 * kMine>(P.store, f, b, i0, j0, q0 * 8, P.m, P.n);
+      } else {
+        constexpr int kRows = 32 / kWays;                     // of the part's 32 rows, per warp
+        if (P.store.dtype == S3GD_F32) store_rows<float, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
+        else store_rows<__nv_bfloat16, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
+      }
     }
   }
   tear_down<1>(P, ok, tmem, 256, false);
@@ -664,9 +708,10 @@ int clusters_at_a_time(void (*kernel)(ProductArgs), int ways, int* cached) {
 
 struct Choice { int64_t cost; int ways; };                  // ways 0: the wide kernel
 
-// What counts is the slots of k that follow one another on an SM (both kernels take about as long for one), with kStart
-// slots' worth of time for each start of a narrow tile and kJoin for joining its parts.
-constexpr int kStart = 16, kJoin = 7;
+// What counts is the products that follow one another on an SM, in units of one 128 x 128 x 64 product (0.14 us; a 256 x 256 tile
+// takes a pair of SMs two of them), and what comes on top: kStart for a wave of narrow tiles (start, first loads, epilogue), kJoin
+// for joining parts of k, kWideStart for the wide kernel, whose last epilogue alone is not covered by products.
+constexpr int kStart = 50, kJoin = 11, kWideStart = 70;
 
 template <bool kSplit, bool kMn, int kWays>
 cudaError_t try_narrow(ProductArgs& A, Choice* best, bool launch, cudaStream_t st) {
@@ -689,7 +734,7 @@ cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
   static int done[kMaxDevices];
   const int pairs = sm_count() / 2;
   const int64_t wide = tiles_of(A, 256), blocks = (A.k + kBlockK - 1) / kBlockK;
-  Choice best = {(wide + pairs - 1) / pairs * blocks * (kSplit ? 3 : 1) + kStart, 0};
+  Choice best = {(wide + pairs - 1) / pairs * blocks * (kSplit ? 6 : 2) + kWideStart, 0};
   for (int launch = 0; launch < 2; ++launch) {
     if (launch) {
       const int tile = best.ways == 0 ? 256 : 128;

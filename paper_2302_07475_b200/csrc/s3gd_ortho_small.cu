@@ -33,42 +33,6 @@ __device__ __forceinline__ int entry_offset(int i, int j) {       // bytes, of e
   return (j >> 6) * kPanel + i * 128 + ((((j >> 3) & 7) ^ (i & 7)) << 4) + (j & 7) * 2;
 }
 
-// eight neighbouring entries of row i as floats, from one or two pieces
-__device__ __forceinline__ void read8(const char* hi, const char* lo, int off, bool two, float* x) {
-  const uint4 h4 = *reinterpret_cast<const uint4*>(hi + off);
-  const __half2* h = reinterpret_cast<const __half2*>(&h4);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 f = __half22float2(h[e]);
-    x[2 * e] = f.x; x[2 * e + 1] = f.y;
-  }
-  if (!two) return;
-  const uint4 l4 = *reinterpret_cast<const uint4*>(lo + off);
-  const __half2* l = reinterpret_cast<const __half2*>(&l4);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const float2 f = __half22float2(l[e]);
-    x[2 * e] += f.x; x[2 * e + 1] += f.y;
-  }
-}
-__device__ __forceinline__ void write8(char* hi, char* lo, int off, const float* x) {
-  __half2 h[4], l[4];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    h[e] = __floats2half2_rn(x[2 * e], x[2 * e + 1]);
-    const float2 f = __half22float2(h[e]);
-    l[e] = __floats2half2_rn(x[2 * e] - f.x, x[2 * e + 1] - f.y);
-  }
-  *reinterpret_cast<uint4*>(hi + off) = *reinterpret_cast<uint4*>(h);
-  *reinterpret_cast<uint4*>(lo + off) = *reinterpret_cast<uint4*>(l);
-}
-
-template <typename T>
-__device__ __forceinline__ T stored(const Store& s, T old, float v) {
-  return from_f32<T>(s.update ? __fmaf_rn(-s.rate, v, __fmul_rn(s.keep, to_f32(old))) : v);
-}
-template <typename T> struct alignas(4 * sizeof(T)) Four { T v[4]; };
-
 // eight neighbouring entries of row i to the caller's matrix
 template <typename T>
 __device__ __forceinline__ void put8(const Store& s, int mat, int i, int j0, int m, int n, const float* x) {
@@ -95,17 +59,11 @@ __device__ __forceinline__ void put8(const Store& s, int mat, int i, int j0, int
     if (j0 + e < n) base[e * step] = stored(s, old[e], x[e]);
 }
 
-// up to four neighbouring entries of a row as floats
-template <typename T>
-__device__ __forceinline__ void get4(const T* p, bool wide, int left, float* x) {
-  if (wide && left >= 4) {
-    const Four<T> f = *reinterpret_cast<const Four<T>*>(p);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = to_f32(f.v[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = e < left ? to_f32(p[e]) : 0.f;
-  }
+__device__ __forceinline__ void write8(char* hi, char* lo, int off, const float* x) {
+  uint32_t h[4], l[4];
+  split8(x, true, h, l);
+  *reinterpret_cast<uint4*>(hi + off) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4*>(lo + off) = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
 template <typename G, int kSmallThreads>
@@ -131,6 +89,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
   for (int o = threadIdx.x * 16; o < 2 * (P.panels_x + P.panels_s) * kPanel; o += kSmallThreads * 16)
     *reinterpret_cast<uint4*>(x_hi + o) = make_uint4(0, 0, 0, 0);            // what lies beside m and n counts as zero
   grid_dependency_wait();
+  if (mat == 0 && threadIdx.x < kHdrWords) P.hdr[threadIdx.x] = 0;           // a record, if any, comes seconds later
   // ---- momentum, norm (sum of squares in 64 bits) and X_0; u stays in registers in between
   const G* g = reinterpret_cast<const G*>(P.g.p) + (size_t)mat * P.g.batch;
   float* v = reinterpret_cast<float*>(P.v.p) + (P.has_v ? (size_t)mat * P.v.batch : 0);
@@ -163,10 +122,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
           old[k][x] = nv;
           if (c + x < P.cols) u[k0 + k][x] = P.nesterov ? __fadd_rn(u[k0 + k][x], __fmul_rn(P.mu, nv)) : nv;
         }
-        if (P.v_wide && P.cols - c >= 4) *reinterpret_cast<float4*>(p) = make_float4(old[k][0], old[k][1], old[k][2], old[k][3]);
-        else
-          for (int x = 0; x < 4; ++x)
-            if (c + x < P.cols) p[x] = old[k][x];
+        put4(p, P.v_wide, P.cols - c, old[k]);
       }
     }
   }
