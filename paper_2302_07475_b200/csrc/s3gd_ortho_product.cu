@@ -39,7 +39,8 @@ struct ProductArgs {
   Store store;
   uint32_t* hdr;
   int m, n, k, batch;
-  int tiles_m, tiles_n;
+  int tiles_m, tiles_n, ways;                     // ways: CTAs that share a tile of the narrow kernel
+  int b_mn;                                       // b is read with k down its rows
   int kind;
   int add_pieces, out_pieces;                     // 16-bit pieces of the matrix that is added, and of the result
   float c_add, c_acc;                             // result = c_add * add + c_acc * sum
@@ -170,7 +171,7 @@ struct Ring {
 };
 
 // Loads slots k of [from, to): rows row_a.. of the first operand and row_b.. of the second, 128 each.
-template <int kCta, bool kSplit, bool kMn>
+template <int kCta, bool kSplit>
 __device__ __forceinline__ bool load_slots(const ProductArgs& P, Shared* sh, uint32_t base, uint32_t rank, int b, int row_a, int row_b, int from,
                                            int to, Ring* ring) {
   for (int kb = from; kb < to; ++kb)
@@ -184,8 +185,7 @@ __device__ __forceinline__ bool load_slots(const ProductArgs& P, Shared* sh, uin
       const int k0 = kb * kBlockK, z = 2 * b + piece;
       for (int h = 0; h < 2; ++h) tma_load<kCta>(dst + h * 8192, &P.a, k0, row_a + h * 64, z, bar);
       for (int h = 0; h < 2; ++h)
-        if (kMn) tma_load<kCta>(dst + 16384 + h * 8192, &P.b, row_b + h * 64, k0, z, bar);
-        else tma_load<kCta>(dst + 16384 + h * 8192, &P.b, k0, row_b + h * 64, z, bar);
+        tma_load<kCta>(dst + 16384 + h * 8192, &P.b, P.b_mn ? row_b + h * 64 : k0, P.b_mn ? k0 : row_b + h * 64, z, bar);
       r.next();
     }
   return true;
@@ -202,15 +202,14 @@ struct Turn {
 
 // Products of `blocks` slots of k.  Two pieces: hi lo + lo hi before hi hi, so that fewer additions are cut off at the size of
 // the full sum.
-template <int kCta, bool kSplit, bool kMn>
-__device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32_t tmem, int blocks, Ring* ring, Turn* turn) {
+template <int kCta, bool kSplit>
+__device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32_t tmem, int blocks, bool b_mn, Ring* ring, Turn* turn) {
   constexpr int kTile = 128 * kCta;
-  constexpr uint32_t idesc = product_desc(kTile, kTile, kMn);
+  const uint32_t idesc = product_desc(kTile, kTile, b_mn), b_next = b_mn ? 8192 : 16, b_step = (b_mn ? 2048 : 32) / 16;
   auto product = [&](uint32_t d, int sa, int sb, bool add) {
-    const uint32_t a = base + sa * kSlotBytes, bb = base + sb * kSlotBytes + 16384;
+    const uint64_t a = operand_desc(base + sa * kSlotBytes), b = operand_desc(base + sb * kSlotBytes + 16384, b_next);
 #pragma unroll
-    for (int k = 0; k < kBlockK / 16; ++k)
-      mma_f16<kCta>(d, operand_desc(a + k * 32), kMn ? operand_desc(bb + k * 2048, 8192) : operand_desc(bb + k * 32), idesc, add || k > 0);
+    for (int k = 0; k < kBlockK / 16; ++k) mma_f16<kCta>(d, a + 2 * k, b + b_step * k, idesc, add || k > 0);
   };
   for (int kb = 0; kb < blocks;) {
     if (!mbar_wait(smem_addr(&sh->sum_empty[turn->sum]), turn->phase ^ 1)) return false;
@@ -417,7 +416,7 @@ __device__ __forceinline__ void tear_down(const ProductArgs& P, bool ok, uint32_
 }
 
 // Many tiles: persistent, two CTAs to a 256 x 256 tile.
-template <bool kSplit, bool kMn>
+template <bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant__ ProductArgs P) {
   extern __shared__ char smem_raw[];
   constexpr int kTile = 256, kCols = 128;
@@ -440,11 +439,11 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       for (int t = first; t < tiles && ok; t += stride) {
         int b, tm, tn;
         tile_at(P, t, symmetric, &b, &tm, &tn);
-        ok = load_slots<2, kSplit, kMn>(P, sh, base, rank, b, tm * kTile + (int)rank * 128, tn * kTile + (int)rank * 128, 0, blocks, ring);
+        ok = load_slots<2, kSplit>(P, sh, base, rank, b, tm * kTile + (int)rank * 128, tn * kTile + (int)rank * 128, 0, blocks, ring);
       }
   } else if (warp == 1) {
     if (lane_id() == 0 && rank == 0)
-      for (int t = first; t < tiles && ok; t += stride) ok = issue_products<2, kSplit, kMn>(sh, base, tmem, blocks, ring, &turn);
+      for (int t = first; t < tiles && ok; t += stride) ok = issue_products<2, kSplit>(sh, base, tmem, blocks, P.b_mn, ring, &turn);
   } else if (warp >= 4) {
     const int w = warp - 4, quad = warp & 3, half = w >> 2, lane = lane_id();
     char* buf = epi + w * kEpiBytes;
@@ -500,93 +499,80 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   tear_down<2>(P, ok, tmem, 512, true);
 }
 
-// Few tiles: a cluster of kWays CTAs takes one 128 x 128 tile, each a part of k.  The eight 32 x 64 parts of the tile are dealt
+// Few tiles: a cluster of P.ways CTAs takes one 128 x 128 tile, each a part of k.  The eight 32 x 64 parts of the tile are dealt
 // over the CTAs.  Every CTA lays its sums into its own shared memory (the slots are free by then) and reads those of its parts
-// from all of them, in the order of the parts of k; all eight warps of a CTA finish its parts, kMine * 8 columns each.
-template <bool kSplit, bool kMn, int kWays>
+// from all of them, in the order of the parts of k; all eight warps of a CTA finish its parts, eight columns at a time.
+// One kernel for all kinds of product and ways, with its epilogue in one short loop: the products of a step follow one another
+// within microseconds, and code that is not in the instruction cache costs each of them up to three.
+template <bool kSplit>
 __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_constant__ ProductArgs P) {
   extern __shared__ char smem_raw[];
   constexpr int kTile = 128, kCols = 64;
-  constexpr int kMine = 8 / kWays;                            // parts per CTA, and 8-column pieces per warp
   const uint32_t raw = smem_addr(smem_raw);
   const uint32_t base = (raw + 1023) & ~1023u;
   char* base_ptr = smem_raw + (base - raw);
   char* epi = base_ptr + kSlots * kSlotBytes;
   Shared* sh = reinterpret_cast<Shared*>(epi + kEpiWarps * kEpiBytes);
-  const int warp = threadIdx.x >> 5;
-  const uint32_t rank = kWays > 1 ? cluster_rank() : 0;
+  const int warp = threadIdx.x >> 5, ways = P.ways, mine = 8 / ways;     // mine: parts per CTA, and 8-column pieces per warp
+  const uint32_t rank = ways > 1 ? cluster_rank() : 0;
   const bool symmetric = P.kind <= kPoly, has_add = P.kind != kGram;
   const int blocks = (P.k + kBlockK - 1) / kBlockK;
-  const int from = (int)rank * blocks / kWays, to = ((int)rank + 1) * blocks / kWays;
+  const int from = (int)rank * blocks / ways, to = ((int)rank + 1) * blocks / ways;
   int b, tm, tn;
-  tile_at(P, blockIdx.x / kWays, symmetric, &b, &tm, &tn);
+  tile_at(P, blockIdx.x / ways, symmetric, &b, &tm, &tn);
   const uint32_t tmem = set_up<1>(P, sh, 256);
-  const int w = warp - 4, quad = warp & 3, lane = lane_id();
-  // what this warp finishes: pieces q0 .. q0 + kMine of part `part`
-  const int pl = kWays == 1 ? quad * 2 + (w >> 2) : w * kMine / 8, part = (int)rank * kMine + pl, q0 = w * kMine % 8;
+  const int w = (warp - 4) & 7, quad = warp & 3, lane = lane_id();
+  // what this warp finishes: pieces q0 .. q0 + mine of part `part` (ways 1: the part whose sums it holds)
+  const int pl = ways == 1 ? quad * 2 + (w >> 2) : w * mine / 8, part = (int)rank * mine + pl, q0 = w * mine % 8;
   const int i0 = tm * kTile + (part >> 1) * 32, j0 = tn * kTile + (part & 1) * kCols;
   const bool here = warp >= 4 && i0 < P.m && j0 < P.n, leads = q0 == 0 && lane == 0;
-  char* buf = epi + (warp >= 4 ? pl : 0) * kEpiBytes;         // what is added, then the result
-  char* side = base_ptr + 8 * 8192 + (warp >= 4 ? pl : 0) * 8192;   // its mirror image, or the caller's rows
-  const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[warp >= 4 ? pl : 0]);
+  char* buf = epi + pl * kEpiBytes;                           // what is added, then the result
+  char* side = base_ptr + 8 * 8192 + pl * 8192;               // its mirror image, or the caller's rows
+  const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[pl]);
   Ring ring[2] = {Ring(0, kSplit ? kHiSlots : kSlots), Ring(kHiSlots, kSlots - kHiSlots)};
   Turn turn;
   bool ok = true;
-  float v[8 * kMine];
   if (warp == 0) {
-    if (lane == 0) ok = load_slots<1, kSplit, kMn>(P, sh, base, 0, b, tm * kTile, tn * kTile, from, to, ring);
+    if (lane == 0) ok = load_slots<1, kSplit>(P, sh, base, 0, b, tm * kTile, tn * kTile, from, to, ring);
   } else if (warp == 1) {
-    if (lane == 0) ok = issue_products<1, kSplit, kMn>(sh, base, tmem, to - from, ring, &turn);
+    if (lane == 0) ok = issue_products<1, kSplit>(sh, base, tmem, to - from, P.b_mn, ring, &turn);
   } else if (warp >= 4) {
     if (has_add && here && leads) load_add(P, buf_addr, add_bar, b, i0, j0);
     const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), rank), cluster_addr(smem_addr(&sh->sum_empty[1]), rank)};
     float acc[kCols];
     ok = take_sums<kTile, kCols>(sh, tmem, quad, (w >> 2) * kCols, sums_of(kSplit, to - from), empty_bar, &turn, acc);
-    if (kWays == 1) {                                         // the part whose sums this warp holds
+    char* sums = base_ptr + (quad * 2 + (w >> 2)) * 8192 + lane * 16;
 #pragma unroll
-      for (int e = 0; e < 8 * kMine; ++e) v[e] = acc[e];
-    } else {
-      char* mine = base_ptr + (quad * 2 + (w >> 2)) * 8192 + lane * 16;
-#pragma unroll
-      for (int q = 0; q < 16; ++q) *reinterpret_cast<float4*>(mine + q * 512) = make_float4(acc[q * 4], acc[q * 4 + 1], acc[q * 4 + 2], acc[q * 4 + 3]);
-    }
+    for (int q = 0; q < 16; ++q) *reinterpret_cast<float4*>(sums + q * 512) = make_float4(acc[q * 4], acc[q * 4 + 1], acc[q * 4 + 2], acc[q * 4 + 3]);
   }
-  if (kWays > 1) {
+  if (ways > 1) {
     __syncwarp();
     cluster_sync();
-    if (here) {
-      float4 got[2 * kMine][kWays];
-#pragma unroll
-      for (int r = 0; r < kWays; ++r) {
-        const uint32_t at = cluster_addr(base + (uint32_t)part * 8192u + (uint32_t)(q0 * 2) * 512u + lane * 16, r);
-#pragma unroll
-        for (int l = 0; l < 2 * kMine; ++l)
-          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(got[l][r].x), "=f"(got[l][r].y), "=f"(got[l][r].z), "=f"(got[l][r].w) : "r"(at + l * 512));
-      }
-#pragma unroll
-      for (int l = 0; l < 2 * kMine; ++l) {
-        float4 sum = got[l][0];
-#pragma unroll
-        for (int r = 1; r < kWays; ++r) { sum.x += got[l][r].x; sum.y += got[l][r].y; sum.z += got[l][r].z; sum.w += got[l][r].w; }
-        v[l * 4] = sum.x; v[l * 4 + 1] = sum.y; v[l * 4 + 2] = sum.z; v[l * 4 + 3] = sum.w;
-      }
-    }
-    __syncwarp();
-    cluster_arrive();                                         // the others may go once this CTA has read their sums
   }
+  const bool mirror = symmetric && tm != tn, two = P.out_pieces == 2;
   if (here) {
     if (has_add) ok = __all_sync(0xffffffffu, mbar_wait(add_bar, 0)) && ok;
-    const bool mirror = symmetric && tm != tn, two = P.out_pieces == 2;
-    // the part that warps finish together: one warp (kWays 1), or 8 / kMine of them
-    auto together = [&] {
-      if (kWays == 1) __syncwarp();
-      else asm volatile("bar.sync %0, %1;" ::"r"(1 + pl), "r"(32 * kWays) : "memory");
-    };
+#pragma unroll 1
+    for (int q = q0; q < q0 + mine; ++q) {
+      float4 got[8][2];
+      const uint32_t at = base + (uint32_t)part * 8192u + (uint32_t)q * 1024u + lane * 16;
 #pragma unroll
-    for (int p = 0; p < kMine; ++p) {
-      const int q = q0 + p, off = lane * 128 + ((q ^ (lane & 7)) << 4);
-      float* x = v + p * 8;
+      for (int r = 0; r < 8; ++r) {
+        if (r >= ways) break;
+        const uint32_t from_r = ways > 1 ? cluster_addr(at, r) : at;
+#pragma unroll
+        for (int l = 0; l < 2; ++l)
+          asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                       : "=f"(got[r][l].x), "=f"(got[r][l].y), "=f"(got[r][l].z), "=f"(got[r][l].w) : "r"(from_r + l * 512));
+      }
+      float x[8] = {got[0][0].x, got[0][0].y, got[0][0].z, got[0][0].w, got[0][1].x, got[0][1].y, got[0][1].z, got[0][1].w};
+#pragma unroll
+      for (int r = 1; r < 8; ++r) {
+        if (r >= ways) break;
+        x[0] += got[r][0].x; x[1] += got[r][0].y; x[2] += got[r][0].z; x[3] += got[r][0].w;
+        x[4] += got[r][1].x; x[5] += got[r][1].y; x[6] += got[r][1].z; x[7] += got[r][1].w;
+      }
+      const int off = lane * 128 + ((q ^ (lane & 7)) << 4);
       combine8(P, buf, off, x);
       if (P.kind != kFinal) {
         uint32_t hi[4], lo[4];
@@ -603,9 +589,16 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
         *reinterpret_cast<float4*>(f + (((2 * q + 1) ^ (lane & 7)) << 2)) = make_float4(x[4], x[5], x[6], x[7]);
       }
     }
+  }
+  if (ways > 1) {
+    __syncwarp();
+    cluster_arrive();                                         // the others may go once this CTA has read their sums
+  }
+  if (here) {
+    if (P.kind != kFinal) fence_async_smem();
+    if (ways == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + pl), "r"(32 * ways) : "memory");   // the warps of a part
     if (P.kind != kFinal) {
-      fence_async_smem();
-      together();
       if (leads && ok) {
         for (int piece = 0; piece < P.out_pieces; ++piece) {
           tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
@@ -615,20 +608,21 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
         tma_store_wait_read();
       }
     } else {
-      together();
+      // eight columns (or four rows) at a time, `mine` of them
       const float* f = reinterpret_cast<const float*>(side);
-      if (P.store.transpose) {
-        if (P.store.dtype == S3GD_F32) store_columns<float, 8 * kMine>(P.store, f, b, i0, j0, q0 * 8, P.m, P.n);
-        else store_columns<__nv_bfloat16, 8 * kMine>(P.store, f, b, i0, j0, q0 * 8, P.m, P.n);
-      } else {
-        constexpr int kRows = 32 / kWays;                     // of the part's 32 rows, per warp
-        if (P.store.dtype == S3GD_F32) store_rows<float, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
-        else store_rows<__nv_bfloat16, kRows>(P.store, f, b, i0, j0, q0 / kMine * kRows, P.m, P.n);
+      for (int p = 0; p < mine; ++p) {
+        if (P.store.transpose) {
+          if (P.store.dtype == S3GD_F32) store_columns<float, 8>(P.store, f, b, i0, j0, (q0 + p) * 8, P.m, P.n);
+          else store_columns<__nv_bfloat16, 8>(P.store, f, b, i0, j0, (q0 + p) * 8, P.m, P.n);
+        } else {
+          if (P.store.dtype == S3GD_F32) store_rows<float, 4>(P.store, f, b, i0, j0, (q0 + p) * 4, P.m, P.n);
+          else store_rows<__nv_bfloat16, 4>(P.store, f, b, i0, j0, (q0 + p) * 4, P.m, P.n);
+        }
       }
     }
   }
   tear_down<1>(P, ok, tmem, 256, false);
-  if (kWays > 1) {
+  if (ways > 1) {
     __syncwarp();
     cluster_wait();
   }
@@ -706,53 +700,38 @@ int clusters_at_a_time(void (*kernel)(ProductArgs), int ways, int* cached) {
   return n;
 }
 
-struct Choice { int64_t cost; int ways; };                  // ways 0: the wide kernel
+// Which kernel, and over how many CTAs a narrow tile's k is dealt: what takes least time, in units of 0.14 us, by a model of
+// the measured times.  A slot of k takes two units for each product of pieces in either kernel (the wide one does four times the
+// work in it, on two SMs).  On top come, for every wave of narrow tiles, its start, first loads and epilogue, the pieces that a
+// warp finishes, and the joining of parts of k; for the wide kernel, whose epilogues run under products, the start and the last.
+constexpr int kSlotUnits = 2, kNarrowStart = 40, kWideStart = 76;
+constexpr int kJoinUnits[4] = {0, 3, 5, 14};
 
-// What counts is the products that follow one another on an SM, in units of one 128 x 128 x 64 product (0.14 us; a 256 x 256 tile
-// takes a pair of SMs two of them), and what comes on top: kStart for a wave of narrow tiles (start, first loads, epilogue), kJoin
-// for joining parts of k, kWideStart for the wide kernel, whose last epilogue alone is not covered by products.
-constexpr int kStart = 50, kJoin = 11, kWideStart = 70;
-
-template <bool kSplit, bool kMn, int kWays>
-cudaError_t try_narrow(ProductArgs& A, Choice* best, bool launch, cudaStream_t st) {
-  static int done[kMaxDevices], at_a_time[kMaxDevices];
-  auto kernel = narrow_kernel<kSplit, kMn, kWays>;
-  const int64_t tiles = tiles_of(A, 128), blocks = (A.k + kBlockK - 1) / kBlockK;
-  if (launch) return best->ways == kWays ? launch_cluster(kernel, A, (unsigned)(tiles * kWays), kWays, done, st) : cudaSuccess;
-  if (blocks < kWays || tiles * kWays >= (1ll << 31)) return cudaSuccess;
-  cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmemBytes, done);
-  if (e != cudaSuccess) return e;
-  const int room = kWays > 1 ? clusters_at_a_time(kernel, kWays, at_a_time) : sm_count();
-  const int64_t waves = (tiles + room - 1) / room;
-  const int64_t cost = waves * (kStart + (blocks + kWays - 1) / kWays * (kSplit ? 3 : 1) + (kWays > 1 ? kJoin : 0));
-  if (cost < best->cost) *best = {cost, kWays};
-  return cudaSuccess;
-}
-
-template <bool kSplit, bool kMn>
+template <bool kSplit>
 cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
-  static int done[kMaxDevices];
-  const int pairs = sm_count() / 2;
-  const int64_t wide = tiles_of(A, 256), blocks = (A.k + kBlockK - 1) / kBlockK;
-  Choice best = {(wide + pairs - 1) / pairs * blocks * (kSplit ? 6 : 2) + kWideStart, 0};
-  for (int launch = 0; launch < 2; ++launch) {
-    if (launch) {
-      const int tile = best.ways == 0 ? 256 : 128;
-      A.tiles_m = (A.m + tile - 1) / tile;
-      A.tiles_n = (A.n + tile - 1) / tile;
-      if (best.ways == 0) return launch_cluster(wide_kernel<kSplit, kMn>, A, (unsigned)(wide < pairs ? wide : pairs) * 2, 2, done, st);
-    }
-    cudaError_t e = try_narrow<kSplit, kMn, 1>(A, &best, launch, st);
-    if (e == cudaSuccess) e = try_narrow<kSplit, kMn, 2>(A, &best, launch, st);
-    if (e == cudaSuccess) e = try_narrow<kSplit, kMn, 4>(A, &best, launch, st);
-    if (e == cudaSuccess) e = try_narrow<kSplit, kMn, 8>(A, &best, launch, st);
-    if (e != cudaSuccess) return e;
+  static int done_wide[kMaxDevices], done_narrow[kMaxDevices], at_a_time[4][kMaxDevices];
+  const int pairs = sm_count() / 2, pieces = kSplit ? 3 : 1;
+  const int64_t wide = tiles_of(A, 256), narrow = tiles_of(A, 128), blocks = (A.k + kBlockK - 1) / kBlockK;
+  int64_t best = (wide + pairs - 1) / pairs * blocks * pieces * kSlotUnits + kWideStart;
+  A.ways = 0;
+  auto kernel = narrow_kernel<kSplit>;
+  cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmemBytes, done_narrow);
+  if (e != cudaSuccess) return e;
+  for (int i = 0; i < 4; ++i) {
+    const int ways = 1 << i;
+    if (blocks < ways || narrow * ways >= (1ll << 31)) break;
+    const int room = ways > 1 ? clusters_at_a_time(kernel, ways, at_a_time[i]) : sm_count();
+    const int64_t cost = (narrow + room - 1) / room * (kNarrowStart + 8 / ways + (blocks + ways - 1) / ways * pieces * kSlotUnits + kJoinUnits[i]);
+    if (cost < best) { best = cost; A.ways = ways; }
   }
-  return cudaSuccess;
+  const int tile = A.ways == 0 ? 256 : 128;
+  A.tiles_m = (A.m + tile - 1) / tile;
+  A.tiles_n = (A.n + tile - 1) / tile;
+  if (A.ways == 0) return launch_cluster(wide_kernel<kSplit>, A, (unsigned)(wide < pairs ? wide : pairs) * 2, 2, done_wide, st);
+  return launch_cluster(kernel, A, (unsigned)(narrow * A.ways), A.ways, done_narrow, st);
 }
 
-template <bool kMn>
-cudaError_t launch_by(ProductArgs& A, bool split, cudaStream_t st) { return split ? launch_product<true, kMn>(A, st) : launch_product<false, kMn>(A, st); }
+cudaError_t launch_by(ProductArgs& A, bool split, cudaStream_t st) { return split ? launch_product<true>(A, st) : launch_product<false>(A, st); }
 
 }  // namespace
 
@@ -776,24 +755,24 @@ cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws,
     A.batch = P.batch;
     A.store = R.out;
     A.add_pieces = A.out_pieces = split ? 2 : 1;
-    A.kind = kGram; A.m = m; A.n = m; A.k = n;
+    A.kind = kGram; A.m = m; A.n = m; A.k = n; A.b_mn = 0;
     A.a = A.b = x_load[from]; A.add = s_epi; A.out = s_epi; A.mirror = s_mirror;
     A.c_add = 0.f; A.c_acc = kScaleS / (kScaleX * kScaleX);
-    cudaError_t e = launch_by<false>(A, split, st);
+    cudaError_t e = launch_by(A, split, st);
     if (e != cudaSuccess) return e;
     A.kind = kPoly; A.k = m;
     A.a = A.b = s_load; A.add = s_epi; A.out = b_epi; A.mirror = b_mirror;
     A.c_add = R.b * (kScaleB / kScaleS); A.c_acc = R.c * (kScaleB / (kScaleS * kScaleS));
-    e = launch_by<false>(A, split, st);
+    e = launch_by(A, split, st);
     if (e != cudaSuccess) return e;
     const bool last = k + 1 == R.steps;
     const float unit = last ? 1.f / kScaleX : 1.f;
-    A.kind = last ? kFinal : kUpdate; A.n = n; A.k = m;
+    A.kind = last ? kFinal : kUpdate; A.n = n; A.k = m; A.b_mn = 1;
     A.a = b_load; A.b = x_load[from]; A.add = x_epi[from]; A.out = x_epi[from ^ 1];
     A.add_pieces = k < carried ? 2 : 1;
     A.out_pieces = k + 1 < carried ? 2 : 1;
     A.c_add = R.a * unit; A.c_acc = unit / kScaleB;
-    e = launch_by<true>(A, split, st);
+    e = launch_by(A, split, st);
     if (e != cudaSuccess) return e;
   }
   return cudaSuccess;
