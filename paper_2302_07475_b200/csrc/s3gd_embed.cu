@@ -6,6 +6,7 @@
 // that each row's tokens come in ascending order) and the warp finds its rows by binary search.  A token that takes more
 // than kChunk places would leave one warp with all of them: its places are summed kChunk at a time by separate warps
 // (aligned in the sorted order, so at most two such tokens meet a chunk) and joined by a last kernel in ascending order.
+// The list of these tokens is written in whatever order they are found; each is then worked on by itself.
 #include "s3gd_ops.cuh"
 
 namespace s3gd {
@@ -16,6 +17,7 @@ constexpr int kLane = 16;                          // columns per lane
 constexpr int kTileCols = 32 * kLane;              // columns per warp
 constexpr int kRows = 8;                           // rows of the table per warp
 constexpr int kDirectTokens = 512;
+constexpr int kHdrCommon = 16;                     // header word: common tokens found
 constexpr int kMinChunk = 64, kMaxChunks = 2048;   // places per partial sum at least; partial sums per worker at most
 
 // ------------------------------------------------------------------ access of kVec neighbouring entries
@@ -246,6 +248,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const I* ids
   tile_ranks(s, key, min(T - tile * kSortTile, (uint32_t)kSortTile), shift, bits, rank, &in_tile);
   const uint32_t* mine = counts + ((size_t)blockIdx.y * kBins + threadIdx.x) * tiles;
   uint32_t all = 0, before = 0;
+#pragma unroll 8
   for (uint32_t k = 0; k < tiles; ++k) {
     const uint32_t c = mine[k];
     all += c;
@@ -277,6 +280,8 @@ struct GradArgs {
   int accumulate;
   uint32_t* bad;
   const uint32_t *keys, *places;                   // sorted
+  uint4* common;                                   // {row, first place, behind the last, worker} of the common tokens, in no order
+  uint32_t* common_count;
   float* partial;                                  // [M][chunks][2][pad]: the chunk's sum for the token that enters it / that leaves it
   uint32_t chunk, chunks, pad;
 };
@@ -334,14 +339,46 @@ __device__ __forceinline__ void put_row(O* to, uint32_t c0, uint32_t dim, const 
   }
 }
 
-__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t n, uint32_t key) {
-  uint32_t lo = 0;
+__device__ __forceinline__ uint32_t lower_bound(const uint32_t* keys, uint32_t lo, uint32_t n, uint32_t key) {
   while (n > 0) {
     const uint32_t half = n / 2;
     if (__ldg(keys + lo + half) < key) { lo += half + 1; n -= half + 1; }
     else n = half;
   }
   return lo;
+}
+
+// The same by half a warp, each half for a key of its own: sixteen probes a round, so that 131072 keys take five rounds of
+// dependent loads instead of seventeen.
+__device__ __forceinline__ uint32_t lower_bound16(const uint32_t* keys, uint32_t n, uint32_t key) {
+  const uint32_t lane = lane_id(), sub = lane & 15, shift = lane & 16;
+  uint32_t lo = 0;
+  while (__any_sync(0xffffffffu, n > 0)) {
+    const uint32_t seg = (n + 17) / 17, at = (sub + 1) * seg - 1;              // probes seg apart; n == 0: none is inside
+    const bool below = n > 0 && at < n && __ldg(keys + lo + at) < key;
+    const uint32_t skip = __popc((__ballot_sync(0xffffffffu, below) >> shift) & 0xffffu) * seg;
+    lo += skip;
+    n = n > 0 ? min(seg - 1, n - skip) : 0u;
+  }
+  return lo;
+}
+
+// Lane r <= kRows gets the first place of row v0 + r.
+__device__ __forceinline__ uint32_t row_bounds(const uint32_t* keys, uint32_t T, uint64_t v0, uint32_t vocab) {
+  const uint32_t lane = lane_id();
+  const uint32_t end_key = (uint32_t)min(v0 + kRows, (uint64_t)vocab);
+  const uint32_t ends = lower_bound16(keys, T, lane < 16 ? (uint32_t)v0 : end_key);
+  const uint32_t s = __shfl_sync(0xffffffffu, ends, 0), n = __shfl_sync(0xffffffffu, ends, 16) - s;
+  const uint32_t key = (uint32_t)min(v0 + min(lane, (uint32_t)kRows), (uint64_t)vocab);
+  if (n > 32) return lower_bound(keys, s, n, key);
+  const uint32_t mine = lane < n ? __ldg(keys + s + lane) : vocab;
+  uint32_t bound = s;
+#pragma unroll
+  for (int r = 1; r <= kRows; ++r) {
+    const uint32_t below = __popc(__ballot_sync(0xffffffffu, lane < n && mine < (uint32_t)min(v0 + r, (uint64_t)vocab)));
+    if (lane >= (uint32_t)r) bound = s + below;
+  }
+  return bound;
 }
 
 // Rows of the table, few tokens: each warp looks through the ids itself.
@@ -398,8 +435,8 @@ __global__ void __launch_bounds__(kThreads) rows_sorted_kernel(GradArgs g, uint3
     for (int side = 0; side < 2; ++side) {
       const uint32_t key = side == 0 ? key0 : key1;
       if (key == g.vocab || (side == 1 && key1 == key0)) continue;
-      const uint32_t bound = lower_bound(keys, g.T, key + (lane & 1));               // lane 0: first place, lane 1: behind the last
-      const uint32_t s = __shfl_sync(0xffffffffu, bound, 0), e = __shfl_sync(0xffffffffu, bound, 1);
+      const uint32_t bound = lower_bound16(keys, g.T, key + (lane >> 4));            // first place, and behind the last
+      const uint32_t s = __shfl_sync(0xffffffffu, bound, 0), e = __shfl_sync(0xffffffffu, bound, 16);
       if (e - s <= g.chunk) continue;
       const uint32_t from = max(s, begin), n = min(e, end) - from;
       float acc[kLane] = {};
@@ -414,46 +451,46 @@ __global__ void __launch_bounds__(kThreads) rows_sorted_kernel(GradArgs g, uint3
   const uint64_t v0 = ((uint64_t)(blockIdx.x - chunk_blocks) * kWarps + w) * kRows;
   if (v0 >= g.vocab) return;
   O* grads = static_cast<O*>(g.grads) + m * g.stride;
-  const uint32_t bound = lower_bound(keys, g.T, (uint32_t)min(v0 + min(lane, (uint32_t)kRows), (uint64_t)g.vocab));
+  const uint32_t bound = row_bounds(keys, g.T, v0, g.vocab);
   for (uint32_t r = 0; r < kRows && v0 + r < g.vocab; ++r) {
     const uint32_t s = __shfl_sync(0xffffffffu, bound, r), e = __shfl_sync(0xffffffffu, bound, r + 1);
-    if (e - s > g.chunk || (e == s && g.accumulate)) continue;
+    if (e - s > g.chunk) {
+      if (tile == 0 && lane == 0) g.common[atomicAdd(g.common_count, 1u)] = make_uint4((uint32_t)(v0 + r), s, e, m);
+      continue;
+    }
+    if (e == s && g.accumulate) continue;
     float acc[kLane] = {};
     add_rows<D, kVec>(dout, g.tok_stride, [&](uint32_t i) { return __ldg(places + s + i); }, e - s, c0, g.dim, acc);
     put_row<O, kVec>(grads + (v0 + r) * g.dim, c0, g.dim, acc, g.scale, g.accumulate);
   }
 }
 
-// Common tokens: the CTA of the chunk in which one begins adds its partial sums, eight runs of them side by side.
+// Common tokens: a CTA for each and 512 columns adds its partial sums, eight runs of them side by side, in ascending order.
 template <typename O, int kVec>
 __global__ void __launch_bounds__(kThreads) join_kernel(GradArgs g) {
   __shared__ float part[kWarps][kTileCols];
-  const uint32_t w = threadIdx.x >> 5, lane = lane_id(), m = blockIdx.z, tile = blockIdx.y;
-  const uint32_t* keys = g.keys + (size_t)m * g.T;
+  const uint32_t w = threadIdx.x >> 5, lane = lane_id();
   grid_dependency_wait();
-  for (uint32_t c = blockIdx.x; c < g.chunks; c += gridDim.x) {
-    const uint32_t begin = c * g.chunk, end = min(begin + g.chunk, g.T);
-    const uint32_t key = keys[end - 1];
-    if (key == g.vocab) continue;
-    if (end == g.T || keys[end] != key) continue;          // more than `chunk` places from here on reach into the next chunk
-    const uint32_t s = lower_bound(keys, g.T, key), e = lower_bound(keys, g.T, key + 1);
-    if (e - s <= g.chunk || s < begin) continue;
-    const uint32_t last = (e - 1) / g.chunk, count = last - c + 1, each = (count + kWarps - 1) / kWarps;
-    const uint32_t c0 = tile * kTileCols + lane * kVec;
+  const uint32_t items = *g.common_count * g.tiles;
+  for (uint32_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const uint4 common = g.common[item / g.tiles];
+    const uint32_t s = common.y, e = common.z, m = common.w;
+    const uint32_t c0 = item % g.tiles * kTileCols + lane * kVec;
+    const uint32_t from = s / g.chunk, count = (e - 1) / g.chunk - from + 1, each = (count + kWarps - 1) / kWarps;
     float acc[kLane] = {};
     const float* base = g.partial + (size_t)m * g.chunks * 2 * g.pad;
     add_rows<float, kVec>(base, 1, [&](uint32_t i) -> long long {
-      const uint32_t k = c + w * each + i;
+      const uint32_t k = from + w * each + i;
       return ((long long)k * 2 + (s <= k * g.chunk ? 0 : 1)) * g.pad;
     }, w * each < count ? min(each, count - w * each) : 0u, c0, g.dim, acc);
 #pragma unroll
-    for (int e2 = 0; e2 < kLane; ++e2) part[w][e2 * 32 + lane] = acc[e2];
+    for (int x = 0; x < kLane; ++x) part[w][x * 32 + lane] = acc[x];
     __syncthreads();
     if (w == 0) {
       for (int k = 1; k < kWarps; ++k)
 #pragma unroll
-        for (int e2 = 0; e2 < kLane; ++e2) acc[e2] += part[k][e2 * 32 + lane];
-      put_row<O, kVec>(static_cast<O*>(g.grads) + m * g.stride + (uint64_t)key * g.dim, c0, g.dim, acc, g.scale, g.accumulate);
+        for (int x = 0; x < kLane; ++x) acc[x] += part[k][x * 32 + lane];
+      put_row<O, kVec>(static_cast<O*>(g.grads) + m * g.stride + (uint64_t)common.x * g.dim, c0, g.dim, acc, g.scale, g.accumulate);
     }
     __syncthreads();
   }
@@ -474,7 +511,7 @@ cudaError_t by_width(int v, F f) { return v == 8 ? f(Width<8>()) : v == 4 ? f(Wi
 struct GradLayout {
   uint32_t chunk, chunks, pad, sort_tiles;
   bool direct;
-  size_t off_keys[2], off_places[2], off_counts, off_partial, total;
+  size_t off_keys[2], off_places[2], off_counts, off_common, off_partial, total;
 };
 bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L) {
   if (M < 1 || M > 65535 || vocab == 0 || dim == 0 || vocab >= (1ull << 31) || dim >= (1ull << 31) || T >= (1ull << 31) ||
@@ -494,6 +531,7 @@ bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L)
       L->off_places[i] = off;  off = align_up(off + list, 256);
     }
     L->off_counts = off;   off = align_up(off + (size_t)M * kBins * L->sort_tiles * sizeof(uint32_t), 256);
+    L->off_common = off;   off = align_up(off + (size_t)M * L->chunks * sizeof(uint4), 256);   // each takes more than a chunk
     L->off_partial = off;  off = align_up(off + (size_t)M * L->chunks * 2 * L->pad * sizeof(float), 256);
   }
   L->total = off;
@@ -561,6 +599,8 @@ cudaError_t enqueue_grad(GradArgs g, const GradLayout& L, int dout_dtype, int id
   g.keys = reinterpret_cast<uint32_t*>(ws + L.off_keys[where]);
   g.places = reinterpret_cast<uint32_t*>(ws + L.off_places[where]);
   g.partial = reinterpret_cast<float*>(ws + L.off_partial);
+  g.common = reinterpret_cast<uint4*>(ws + L.off_common);
+  g.common_count = reinterpret_cast<uint32_t*>(ws) + kHdrCommon;
   const uint32_t chunk_blocks = (L.chunks + kWarps - 1) / kWarps;
   count_launch(2);
   e = by_real(dout_dtype, [&](auto d) { return by_real(grads_dtype, [&](auto o) { return by_width(vec, [&](auto v) {
@@ -568,9 +608,10 @@ cudaError_t enqueue_grad(GradArgs g, const GradLayout& L, int dout_dtype, int id
                         dim3(kThreads), 0, st, g, chunk_blocks);
   }); }); });
   if (e != cudaSuccess) return e;
-  const uint32_t joins = L.chunks < 128 ? L.chunks : 128;
+  const uint64_t most = (uint64_t)g.M * L.chunks * g.tiles, some = 4 * sm_count();
+  const uint32_t joins = (uint32_t)(most < some ? most : some);
   return by_real(grads_dtype, [&](auto o) { return by_width(vec, [&](auto v) {
-    return launch_after(join_kernel<decltype(o), decltype(v)::value>, dim3(joins, g.tiles, g.M), dim3(kThreads), 0, st, g);
+    return launch_after(join_kernel<decltype(o), decltype(v)::value>, dim3(joins), dim3(kThreads), 0, st, g);
   }); });
 }
 
