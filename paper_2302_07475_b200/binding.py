@@ -148,6 +148,14 @@ def _stream(t: torch.Tensor):
     return ctypes.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(index: int):
+    """The current stream of a device as an address, without a Stream object in between (1 us less per call)."""
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+
+
 def _check(call: str, code: int) -> None:
     if code != S3GD_OK:
         raise S3gdError(call, code)
@@ -502,6 +510,27 @@ def _matrices(**tensors):
     return mats, first.shape[0] if first.dim() == 3 else 1, rows, cols
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+class _on:
+    """torch.cuda.device(device) for a short call: nothing is switched where the device is current already."""
+
+    __slots__ = ("index", "before")
+
+    def __init__(self, device: torch.device):
+        self.index = device.index
+
+    def __enter__(self):
+        self.before = _current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
 def _of(t: Optional[torch.Tensor], dtypes, name: str) -> None:
     if t is not None and t.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {t.dtype}, needs one of {', '.join(str(d) for d in dtypes)}")
@@ -517,8 +546,8 @@ def s3gd_orthogonalise(g: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, ste
     _of(out, _REAL, "out")
     a, b, c = coeffs
     w = _ptr(ws, torch.uint8, name="ws")
-    with torch.cuda.device(out.device):
-        code = load().s3gd_orthogonalise(m["g"], m["out"], batch, rows, cols, steps, a, b, c, eps, split_steps, w, ws.numel(), _stream(out))
+    with _on(out.device):
+        code = load().s3gd_orthogonalise(m["g"], m["out"], batch, rows, cols, steps, a, b, c, eps, split_steps, w, ws.numel(), _stream_of(out.device.index))
     _check("s3gd_orthogonalise", code)
 
 
@@ -534,9 +563,9 @@ def s3gd_step_ortho(x: torch.Tensor, g: torch.Tensor, lr: float, ws: torch.Tenso
     _of(g, _REAL + (torch.int8,), "g")
     a, b, c = coeffs
     w = _ptr(ws, torch.uint8, name="ws")
-    with torch.cuda.device(x.device):
+    with _on(x.device):
         code = load().s3gd_step_ortho(m["x"], m["v"], m["g"], batch, rows, cols, mu, int(nesterov), lr, weight_decay, scale, steps, a, b, c,
-                                      eps, split_steps, w, ws.numel(), _stream(x))
+                                      eps, split_steps, w, ws.numel(), _stream_of(x.device.index))
     _check("s3gd_step_ortho", code)
 
 
@@ -561,22 +590,25 @@ def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale:
     """out[..., :] <- scale * table[ids[...], :]; a negative id gives a zero row.  table [vocab, dim], out ids.shape + [dim]."""
     _rows(table, _REAL, "table")
     _ids(ids)
-    if table.dim() != 2 or out.shape[:-1] != ids.shape:
+    shape = out.shape
+    if table.dim() != 2 or shape[:-1] != ids.shape:
         raise ValueError(f"table must be [vocab, dim] and out {tuple(ids.shape)} + [dim]")
     vocab, dim = table.shape
     _rows(out, _REAL, "out", dim)
-    n = ids.numel()
-    if out.dim() == 2:
-        out_stride = out.stride(0) if n > 1 else dim
-    elif out.is_contiguous():
+    if out.is_contiguous():
         out_stride = dim
+    elif len(shape) == 2:
+        out_stride = out.stride(0)
     else:
         raise ValueError("out must be contiguous, or [n, dim] with contiguous rows")
+    n = ids.numel()
     args = (table.data_ptr(), _DTYPES[table.dtype], table.stride(0) if vocab > 1 else dim, vocab, dim, ids.data_ptr(), _DTYPES[ids.dtype], n,
-            scale, out.data_ptr(), _DTYPES[out.dtype], out_stride, _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
-    with torch.cuda.device(out.device):
-        code = load().s3gd_embed(*args, _stream(out))
-    _check("s3gd_embed", code)
+            scale, out.data_ptr(), _DTYPES[out.dtype], out_stride if n > 1 else dim, _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
+    device = out.device
+    with _on(device):
+        code = load().s3gd_embed(*args, _stream_of(device.index))
+    if code:
+        _check("s3gd_embed", code)
 
 
 def s3gd_embed_grad_workspace_bytes(M: int, T: int, vocab: int, dim: int) -> int:
@@ -616,6 +648,6 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
     args = (dout.data_ptr(), _DTYPES[dout.dtype], dout.stride(-2), dout.stride(0) if ids.dim() == 2 else 0, ids.data_ptr(), _DTYPES[ids.dtype],
             M, T, vocab, dim, scale, grads.data_ptr(), _DTYPES[grads.dtype], rows_of.stride(0) if M > 1 else vocab * dim, int(accumulate),
             _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(grads.device):
-        code = load().s3gd_embed_grad(*args, _stream(grads))
+    with _on(grads.device):
+        code = load().s3gd_embed_grad(*args, _stream_of(grads.device.index))
     _check("s3gd_embed_grad", code)

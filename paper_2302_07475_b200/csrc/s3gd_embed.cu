@@ -18,7 +18,7 @@ constexpr int kTileCols = 32 * kLane;              // columns per warp
 constexpr int kRows = 8;                           // rows of the table per warp
 constexpr int kDirectTokens = 512;
 constexpr int kHdrCommon = 16;                     // header word: common tokens found
-constexpr int kMinChunk = 64, kMaxChunks = 2048;   // places per partial sum at least; partial sums per worker at most
+constexpr int kMinChunk = 32, kMaxChunks = 8192;   // places per partial sum at least; partial sums per worker at most
 
 // ------------------------------------------------------------------ access of kVec neighbouring entries
 template <typename T, int kVec>
@@ -74,9 +74,11 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(const W* table, long l
 }
 
 // ------------------------------------------------------------------ sort of the tokens by id
-// Least significant digit first, digits of at most 9 bits, tiles of 4096 tokens of one worker.  Empty places and ids out of
+// Least significant digit first, digits of at most 9 bits, tiles of 2048 or 4096 tokens of one worker.  Empty places and ids out of
 // range take the key `vocab` and end up behind all others.
-constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32, kSortEach = 8, kSortTile = kSortThreads * kSortEach;
+constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
+constexpr int kSortEach = 8, kSortTile = kSortThreads * kSortEach;   // of a long row, or the whole of a short one
+constexpr int kFewEach = 4, kFewTiles = 64;       // rows of up to 64 tiles of 2048 are cut into these: more CTAs, shorter chains
 constexpr int kMaxDigit = 9, kBins = 1 << kMaxDigit;
 
 struct SortPlan { int passes, bits; };
@@ -100,7 +102,8 @@ struct TileSort {                                  // shared memory of one tile
   uint32_t warp_total[kSortWarps];
 };
 
-// Rank of every token among those of its digit in the tile.  Warp w holds places w * 256 + r * 32 + lane in key[r].
+// Rank of every token among those of its digit in the tile.  Warp w holds places (w * kSortEach + r) * 32 + lane in key[r].
+template <int kSortEach>
 __device__ __forceinline__ void tile_ranks(TileSort& s, const uint32_t* key, uint32_t n, int shift, int bits, uint32_t* rank, uint32_t* total) {
   const uint32_t w = threadIdx.x >> 5, lane = lane_id(), mask = (1u << bits) - 1u;
   for (int i = threadIdx.x; i < kSortWarps * kBins; i += kSortThreads) s.count[i / kBins][i % kBins] = 0;
@@ -148,7 +151,7 @@ static_assert(kBins == kSortThreads, "one thread per digit");
 // All passes in shared memory: one CTA per worker, T <= kSortTile.
 template <typename I>
 __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const I* ids, uint32_t T, uint32_t vocab, SortPlan plan, uint32_t* keys,
-                                                                  uint32_t* places, uint32_t* bad) {
+                                                                  uint32_t* places, uint32_t* bad, uint32_t* hdr) {
   extern __shared__ char sort_smem[];
   TileSort& s = *reinterpret_cast<TileSort*>(sort_smem);
   uint32_t* buf_key = reinterpret_cast<uint32_t*>(sort_smem + sizeof(TileSort));
@@ -156,6 +159,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const I* ids, 
   const size_t row = (size_t)blockIdx.x * T;
   const uint32_t first = (threadIdx.x >> 5) * (kSortEach * 32) + lane_id();
   grid_dependency_wait();
+  if (blockIdx.x == 0 && threadIdx.x < kHdrWords) hdr[threadIdx.x] = 0;
   uint32_t key[kSortEach], place[kSortEach], rank[kSortEach], out_of_range = 0;
 #pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
@@ -171,7 +175,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const I* ids, 
   for (int p = 0; p < plan.passes; ++p) {
     uint32_t total;
     const int shift = p * plan.bits;
-    tile_ranks(s, key, T, shift, plan.bits, rank, &total);
+    tile_ranks<kSortEach>(s, key, T, shift, plan.bits, rank, &total);
     digit_bases(s, total);
     const bool last = p + 1 == plan.passes;
 #pragma unroll
@@ -191,19 +195,21 @@ __global__ void __launch_bounds__(kSortThreads) sort_small_kernel(const I* ids, 
   }
 }
 
-// One pass over longer rows, first half: how often each digit occurs in each tile, as count[worker][digit][tile].
-template <typename I, bool kFirst>
+// One pass over longer rows, first half: how often each digit occurs in each tile, as count[worker][tile][digit].
+template <typename I, bool kFirst, int kSortEach>
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const I* ids, const uint32_t* keys, uint32_t T, uint32_t vocab, uint32_t tiles,
-                                                                  int shift, int bits, uint32_t* counts, uint32_t* bad) {
+                                                                  int shift, int bits, uint32_t* counts, uint32_t* bad, uint32_t* hdr) {
   __shared__ uint32_t count[kBins];
   const uint32_t tile = blockIdx.x;
   const size_t row = (size_t)blockIdx.y * T;
   count[threadIdx.x] = 0;
   __syncthreads();
   grid_dependency_wait();
+  if (kFirst && tile + blockIdx.y == 0 && threadIdx.x < kHdrWords) hdr[threadIdx.x] = 0;
   uint32_t out_of_range = 0;
+#pragma unroll
   for (int r = 0; r < kSortEach; ++r) {
-    const uint32_t at = tile * kSortTile + r * kSortThreads + threadIdx.x;
+    const uint32_t at = (tile * kSortEach + r) * kSortThreads + threadIdx.x;
     uint32_t d = kBins;
     if (at < T) {
       uint32_t key;
@@ -221,17 +227,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(const I* ids, 
   }
   if (kFirst && bad != nullptr && out_of_range) atomicAdd(bad, out_of_range);
   __syncthreads();
-  counts[((size_t)blockIdx.y * kBins + threadIdx.x) * tiles + tile] = count[threadIdx.x];
+  counts[((size_t)blockIdx.y * tiles + tile) * kBins + threadIdx.x] = count[threadIdx.x];
 }
 
 // second half: every token to its place
-template <typename I, bool kFirst>
+template <typename I, bool kFirst, int kSortEach>
 __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const I* ids, const uint32_t* keys, const uint32_t* places, uint32_t T,
                                                                     uint32_t vocab, uint32_t tiles, int shift, int bits, const uint32_t* counts,
                                                                     uint32_t* to_keys, uint32_t* to_places) {
   extern __shared__ char sort_smem[];
   TileSort& s = *reinterpret_cast<TileSort*>(sort_smem);
-  const uint32_t tile = blockIdx.x, first = tile * kSortTile + (threadIdx.x >> 5) * (kSortEach * 32) + lane_id();
+  const uint32_t tile = blockIdx.x, first = tile * (kSortThreads * kSortEach) + (threadIdx.x >> 5) * (kSortEach * 32) + lane_id();
   const size_t row = (size_t)blockIdx.y * T;
   grid_dependency_wait();
   uint32_t key[kSortEach], place[kSortEach], rank[kSortEach];
@@ -245,12 +251,12 @@ __global__ void __launch_bounds__(kSortThreads) sort_scatter_kernel(const I* ids
     }
   }
   uint32_t in_tile;
-  tile_ranks(s, key, min(T - tile * kSortTile, (uint32_t)kSortTile), shift, bits, rank, &in_tile);
-  const uint32_t* mine = counts + ((size_t)blockIdx.y * kBins + threadIdx.x) * tiles;
+  tile_ranks<kSortEach>(s, key, min(T - tile * (kSortThreads * kSortEach), (uint32_t)(kSortThreads * kSortEach)), shift, bits, rank, &in_tile);
+  const uint32_t* mine = counts + (size_t)blockIdx.y * tiles * kBins + threadIdx.x;
   uint32_t all = 0, before = 0;
-#pragma unroll 8
+#pragma unroll 16
   for (uint32_t k = 0; k < tiles; ++k) {
-    const uint32_t c = mine[k];
+    const uint32_t c = mine[(size_t)k * kBins];
     all += c;
     before += k < tile ? c : 0u;
   }
@@ -278,7 +284,7 @@ struct GradArgs {
   void* grads;
   long long stride;
   int accumulate;
-  uint32_t* bad;
+  uint32_t *bad, *hdr;
   const uint32_t *keys, *places;                   // sorted
   uint4* common;                                   // {row, first place, behind the last, worker} of the common tokens, in no order
   uint32_t* common_count;
@@ -387,6 +393,7 @@ __global__ void __launch_bounds__(kThreads) rows_direct_kernel(GradArgs g) {
   __shared__ uint32_t found[kWarps][kDirectTokens];
   const uint32_t w = threadIdx.x >> 5, lane = lane_id(), m = blockIdx.z, tile = blockIdx.y;
   const uint32_t v0 = (blockIdx.x * kWarps + w) * kRows;
+  if (blockIdx.x + tile + m == 0 && threadIdx.x < kHdrWords) g.hdr[threadIdx.x] = 0;
   const I* ids = static_cast<const I*>(g.ids) + (size_t)m * g.T;
   const D* dout = static_cast<const D*>(g.dout) + m * g.worker_stride;
   O* grads = static_cast<O*>(g.grads) + m * g.stride;
@@ -510,7 +517,7 @@ cudaError_t by_width(int v, F f) { return v == 8 ? f(Width<8>()) : v == 4 ? f(Wi
 
 struct GradLayout {
   uint32_t chunk, chunks, pad, sort_tiles;
-  bool direct;
+  bool direct, few;
   size_t off_keys[2], off_places[2], off_counts, off_common, off_partial, total;
 };
 bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L) {
@@ -522,7 +529,9 @@ bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L)
   L->chunk = (uint32_t)(chunk < kMinChunk ? kMinChunk : chunk);
   L->chunks = (uint32_t)((T + L->chunk - 1) / L->chunk);
   L->pad = (uint32_t)((dim + 7) / 8 * 8);
-  L->sort_tiles = (uint32_t)((T + kSortTile - 1) / kSortTile);
+  L->few = T <= (uint64_t)kFewTiles * kSortThreads * kFewEach;
+  const uint64_t tile = kSortThreads * (L->few ? kFewEach : kSortEach);
+  L->sort_tiles = (uint32_t)((T + tile - 1) / tile);
   size_t off = align_up(kHdrWords * sizeof(uint32_t), 256);
   if (!L->direct) {
     const size_t list = (size_t)M * T * sizeof(uint32_t);
@@ -536,6 +545,26 @@ bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L)
   }
   L->total = off;
   return true;
+}
+
+template <typename I, int kEach>
+cudaError_t sort_passes(const GradArgs& g, const GradLayout& L, const SortPlan& plan, uint32_t** keys, uint32_t** places, uint32_t* counts, int* where,
+                        cudaStream_t st) {
+  const I* ids = static_cast<const I*>(g.ids);
+  const dim3 grid(L.sort_tiles, g.M), block(kSortThreads);
+  for (int p = 0; p < plan.passes; ++p) {
+    const int from = (p + 1) & 1, to = p & 1, shift = p * plan.bits;
+    auto count = p == 0 ? sort_count_kernel<I, true, kEach> : sort_count_kernel<I, false, kEach>;
+    auto scatter = p == 0 ? sort_scatter_kernel<I, true, kEach> : sort_scatter_kernel<I, false, kEach>;
+    count_launch(2);
+    cudaError_t e = launch_after(count, grid, block, 0, st, ids, keys[from], g.T, g.vocab, L.sort_tiles, shift, plan.bits, counts, g.bad, g.hdr);
+    if (e != cudaSuccess) return e;
+    e = launch_after(scatter, grid, block, sizeof(TileSort), st, ids, keys[from], places[from], g.T, g.vocab, L.sort_tiles, shift, plan.bits, counts,
+                     keys[to], places[to]);
+    if (e != cudaSuccess) return e;
+    *where = to;
+  }
+  return cudaSuccess;
 }
 
 template <typename I>
@@ -555,29 +584,9 @@ cudaError_t sort_tokens(const GradArgs& g, const GradLayout& L, char* ws, int* w
     cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(sort_small_kernel<I>), bytes, done);
     if (e != cudaSuccess) return e;
     count_launch();
-    return launch_after(sort_small_kernel<I>, dim3(g.M), dim3(kSortThreads), bytes, st, ids, g.T, g.vocab, plan, keys[0], places[0], g.bad);
+    return launch_after(sort_small_kernel<I>, dim3(g.M), dim3(kSortThreads), bytes, st, ids, g.T, g.vocab, plan, keys[0], places[0], g.bad, g.hdr);
   }
-  const dim3 grid(L.sort_tiles, g.M);
-  const int bytes = (int)sizeof(TileSort);
-  for (int p = 0; p < plan.passes; ++p) {
-    const int from = (p + 1) & 1, to = p & 1, shift = p * plan.bits;
-    count_launch(2);
-    cudaError_t e;
-    if (p == 0) {
-      e = launch_after(sort_count_kernel<I, true>, grid, dim3(kSortThreads), 0, st, ids, keys[from], g.T, g.vocab, L.sort_tiles, shift, plan.bits, counts, g.bad);
-      if (e != cudaSuccess) return e;
-      e = launch_after(sort_scatter_kernel<I, true>, grid, dim3(kSortThreads), bytes, st, ids, keys[from], places[from], g.T, g.vocab, L.sort_tiles,
-                       shift, plan.bits, counts, keys[to], places[to]);
-    } else {
-      e = launch_after(sort_count_kernel<I, false>, grid, dim3(kSortThreads), 0, st, ids, keys[from], g.T, g.vocab, L.sort_tiles, shift, plan.bits, counts, g.bad);
-      if (e != cudaSuccess) return e;
-      e = launch_after(sort_scatter_kernel<I, false>, grid, dim3(kSortThreads), bytes, st, ids, keys[from], places[from], g.T, g.vocab, L.sort_tiles,
-                       shift, plan.bits, counts, keys[to], places[to]);
-    }
-    if (e != cudaSuccess) return e;
-    *where = to;
-  }
-  return cudaSuccess;
+  return L.few ? sort_passes<I, kFewEach>(g, L, plan, keys, places, counts, where, st) : sort_passes<I, kSortEach>(g, L, plan, keys, places, counts, where, st);
 }
 
 cudaError_t enqueue_grad(GradArgs g, const GradLayout& L, int dout_dtype, int ids_dtype, int grads_dtype, char* ws, cudaStream_t st) {
@@ -600,7 +609,7 @@ cudaError_t enqueue_grad(GradArgs g, const GradLayout& L, int dout_dtype, int id
   g.places = reinterpret_cast<uint32_t*>(ws + L.off_places[where]);
   g.partial = reinterpret_cast<float*>(ws + L.off_partial);
   g.common = reinterpret_cast<uint4*>(ws + L.off_common);
-  g.common_count = reinterpret_cast<uint32_t*>(ws) + kHdrCommon;
+  g.common_count = g.hdr + kHdrCommon;
   const uint32_t chunk_blocks = (L.chunks + kWarps - 1) / kWarps;
   count_launch(2);
   e = by_real(dout_dtype, [&](auto d) { return by_real(grads_dtype, [&](auto o) { return by_width(vec, [&](auto v) {
@@ -669,12 +678,12 @@ extern "C" s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t
     return S3GD_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < L.total || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (cudaMemsetAsync(ws, 0, kHdrWords * sizeof(uint32_t), st) != cudaSuccess) return S3GD_ERR_CUDA;
   if (opt_bad_count != nullptr && cudaMemsetAsync(opt_bad_count, 0, 4, st) != cudaSuccess) return S3GD_ERR_CUDA;
   GradArgs g = {};
   g.dout = dout; g.tok_stride = dout_stride; g.worker_stride = dout_worker_stride;
   g.ids = ids; g.M = M; g.T = (uint32_t)T; g.vocab = (uint32_t)vocab; g.dim = (uint32_t)dim; g.tiles = (uint32_t)tiles;
   g.scale = scale; g.grads = grads; g.stride = grads_stride; g.accumulate = accumulate; g.bad = opt_bad_count;
   g.chunk = L.chunk; g.chunks = L.chunks; g.pad = L.pad;
+  g.hdr = static_cast<uint32_t*>(ws);
   return enqueue_grad(g, L, dout_dtype, ids_dtype, grads_dtype, static_cast<char*>(ws), st) == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
 }
