@@ -28,8 +28,11 @@ constexpr int kSlots = 5;
 constexpr int kChunk = 2;                         // slots of k between two additions in registers, two pieces
 constexpr int kEpiWarps = 8;
 constexpr int kEpiBytes = 8 * 1024;               // per epilogue warp: 32 x 64 entries of either piece
+constexpr int kImageBytes = 4 * 1024;             // and, wide kernel with two pieces, the mirror image of half of them
 constexpr int kThreads = 128 + 32 * kEpiWarps;    // warp 0 loads, warp 1 issues the products; the epilogue begins at warp 4
+template <bool kSplit> constexpr int kWideSlots = kSplit ? kSlots - 1 : kSlots;   // the images take the place of one
 constexpr int kSmemBytes = 1024 + kSlots * kSlotBytes + kEpiWarps * kEpiBytes + 256;
+static_assert(kEpiWarps * kImageBytes <= kSlotBytes, "");
 constexpr int kBand = 8;                          // tile rows that are worked on side by side, for reuse in L2
 
 enum Kind : int { kGram = 0, kPoly = 1, kUpdate = 2, kFinal = 3 };
@@ -68,72 +71,6 @@ __device__ __forceinline__ void tile_at(const ProductArgs& P, int t, bool symmet
     const int high = min(kBand, P.tiles_m - band * kBand);
     *tm = band * kBand + in % high;
     *tn = in / high;
-  }
-}
-
-// Rows r0 .. r0 + kRows of 32, 64 columns, of the caller's matrix from a buffer (row r: 256 bytes, 16-byte pieces exchanged by
-// r & 7).  What is updated is read in batches, so that several reads are under way.
-template <typename T, int kRows>
-__device__ __forceinline__ void store_rows(const Store& s, const float* buf, int b, int i0, int j0, int r0, int m, int n) {
-  T* base = reinterpret_cast<T*>(s.to.p) + (size_t)b * s.to.batch;
-  const int lane = lane_id();
-  if (s.wide && j0 + 64 <= n) {
-    constexpr int kBatch = kRows / 2 < 4 ? kRows / 2 : 4;
-    const int q = lane % 16;
-#pragma unroll 1
-    for (int it0 = 0; it0 < kRows / 2; it0 += kBatch) {
-      Four<T> o[kBatch];
-#pragma unroll
-      for (int it = 0; it < kBatch; ++it) {
-        const int r = r0 + (it0 + it) * 2 + lane / 16;
-        if (s.update && i0 + r < m) o[it] = *reinterpret_cast<const Four<T>*>(base + (size_t)(i0 + r) * s.to.row + j0 + q * 4);
-      }
-#pragma unroll
-      for (int it = 0; it < kBatch; ++it) {
-        const int r = r0 + (it0 + it) * 2 + lane / 16;
-        if (i0 + r >= m) continue;
-        const float4 v = *reinterpret_cast<const float4*>(buf + r * 64 + ((q ^ (r & 7)) << 2));
-        o[it] = {stored(s, o[it].v[0], v.x), stored(s, o[it].v[1], v.y), stored(s, o[it].v[2], v.z), stored(s, o[it].v[3], v.w)};
-        *reinterpret_cast<Four<T>*>(base + (size_t)(i0 + r) * s.to.row + j0 + q * 4) = o[it];
-      }
-    }
-  } else {
-    constexpr int kBatch = 4;
-#pragma unroll 1
-    for (int b0 = 0; b0 < kRows; b0 += kBatch) {
-      T o[kBatch][2];
-#pragma unroll
-      for (int x = 0; x < kBatch * 2; ++x) {
-        const int r = r0 + b0 + x / 2, c = x % 2 * 32 + lane;
-        if (s.update && i0 + r < m && j0 + c < n) o[x / 2][x % 2] = base[(size_t)(i0 + r) * s.to.row + j0 + c];
-      }
-#pragma unroll
-      for (int x = 0; x < kBatch * 2; ++x) {
-        const int r = r0 + b0 + x / 2, c = x % 2 * 32 + lane;
-        if (i0 + r < m && j0 + c < n)
-          base[(size_t)(i0 + r) * s.to.row + j0 + c] = stored(s, o[x / 2][x % 2], buf[r * 64 + (((c >> 2) ^ (r & 7)) << 2) + (c & 3)]);
-      }
-    }
-  }
-}
-
-// Columns c0 .. c0 + kCount of the buffer's 32 x 64 entries, which are rows of the caller's matrix.
-template <typename T, int kCount>
-__device__ __forceinline__ void store_columns(const Store& s, const float* buf, int b, int i0, int j0, int c0, int m, int n) {
-  const int lane = lane_id();
-  if (i0 + lane >= m) return;
-  T* base = reinterpret_cast<T*>(s.to.p) + (size_t)b * s.to.batch + i0 + lane;
-  const float* row = buf + lane * 64;
-#pragma unroll 1
-  for (int c = c0; c < c0 + kCount && j0 + c < n; c += 8) {
-    T* p = base + (size_t)(j0 + c) * s.to.row;
-    T old[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (s.update && j0 + c + e < n) old[e] = p[(size_t)e * s.to.row];
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (j0 + c + e < n) p[(size_t)e * s.to.row] = stored(s, old[e], row[((((c + e) >> 2) ^ (lane & 7)) << 2) + ((c + e) & 3)]);
   }
 }
 
@@ -285,90 +222,32 @@ __device__ __forceinline__ void load_add(const ProductArgs& P, uint32_t buf_addr
   for (int piece = 0; piece < P.add_pieces; ++piece) tma_load<1>(buf_addr + piece * 4096, &P.add, j0, i0, 2 * b + piece, bar);
 }
 
-// keeps the compiler from starting all pieces of a row at once, for which there are no registers
-__device__ __forceinline__ void in_order() { asm volatile("" ::: "memory"); }
-
-// Eight entries of a row from their sums in x, in place; what is added lies in the buffer at `off`.
-__device__ __forceinline__ void combine8(const ProductArgs& P, const char* buf, int off, float* x) {
+// Eight entries of row i from their sums in x: c_add * what is added (in the buffer at `off`) + c_acc * x, to the caller's matrix
+// or, in the place of what was added, as they are stored; and as column c0.. of the mirror image.
+__device__ __forceinline__ void finish8(const ProductArgs& P, char* buf, int off, char* image, int image_lo, int c0, bool mirror, int b, int i, int j,
+                                        float* x) {
   if (P.kind == kGram) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] *= P.c_acc;
-    return;
-  }
-  float add[8];
-  read8(buf, buf + 4096, off, P.add_pieces == 2, add);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = __fmaf_rn(P.c_add, add[e], __fmul_rn(P.c_acc, x[e]));
-}
-
-// 32 x 64 entries of the result from the sums in v: rows i0 + lane, columns j0 ..  The matrix that is added lies in the buffer.
-__device__ __forceinline__ void finish(const ProductArgs& P, char* buf, uint32_t buf_addr, int b, int i0, int j0, bool mirror, float* v) {
-  const int lane = lane_id();
-  const bool two = P.out_pieces == 2;
-  if (P.kind == kGram) {
-    if (lane == 0) tma_store_wait_read();
-    __syncwarp();
-  }
-  // row `lane` of the buffer: 16-byte pieces exchanged by lane & 7, as TMA lays them
-  if (P.kind != kFinal) {
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-      const int off = lane * 128 + ((q ^ (lane & 7)) << 4);
-      uint32_t hi[4], lo[4];
-      in_order();
-      combine8(P, buf, off, v + q * 8);
-      split8(v + q * 8, two, hi, lo);
-      *reinterpret_cast<uint4*>(buf + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-      if (two) *reinterpret_cast<uint4*>(buf + 4096 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-      else if (mirror) mirror8(buf + 4096, q * 8, hi);      // one piece: its mirror image fits beside it
-    }
-    fence_async_smem();
-    __syncwarp();
-    if (lane == 0) {
-      for (int piece = 0; piece < P.out_pieces; ++piece) tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
-      if (mirror && !two) tma_store(&P.mirror, i0, j0, 2 * b, buf_addr + 4096);
-      tma_store_commit();
-    }
-    if (mirror && two) {
-      if (lane == 0) tma_store_wait_read();
-      __syncwarp();
-#pragma unroll
-      for (int q = 0; q < 8; ++q) {
-        uint32_t hi[4], lo[4];
-        in_order();
-        split8(v + q * 8, true, hi, lo);
-        mirror8(buf, q * 8, hi);
-        mirror8(buf + 4096, q * 8, lo);
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) {
-        for (int piece = 0; piece < 2; ++piece) tma_store(&P.mirror, i0, j0, 2 * b + piece, buf_addr + piece * 4096);
-        tma_store_commit();
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    in_order();
-    combine8(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), v + q * 8);
-  }
-  __syncwarp();
-  float* f = reinterpret_cast<float*>(buf);
-#pragma unroll
-  for (int q = 0; q < 16; ++q)
-    *reinterpret_cast<float4*>(f + lane * 64 + ((q ^ (lane & 7)) << 2)) = make_float4(v[q * 4], v[q * 4 + 1], v[q * 4 + 2], v[q * 4 + 3]);
-  __syncwarp();
-  if (P.store.transpose) {
-    if (P.store.dtype == S3GD_F32) store_columns<float, 64>(P.store, f, b, i0, j0, 0, P.m, P.n);
-    else store_columns<__nv_bfloat16, 64>(P.store, f, b, i0, j0, 0, P.m, P.n);
   } else {
-    if (P.store.dtype == S3GD_F32) store_rows<float, 32>(P.store, f, b, i0, j0, 0, P.m, P.n);
-    else store_rows<__nv_bfloat16, 32>(P.store, f, b, i0, j0, 0, P.m, P.n);
+    float add[8];
+    read8(buf, buf + 4096, off, P.add_pieces == 2, add);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __fmaf_rn(P.c_add, add[e], __fmul_rn(P.c_acc, x[e]));
   }
-  fence_async_smem();
-  __syncwarp();
+  if (P.kind == kFinal) {
+    if (P.store.dtype == S3GD_F32) put8<float>(P.store, b, i, j, P.m, P.n, x);
+    else put8<__nv_bfloat16>(P.store, b, i, j, P.m, P.n, x);
+    return;
+  }
+  const bool two = P.out_pieces == 2;
+  uint32_t hi[4], lo[4];
+  split8(x, two, hi, lo);
+  *reinterpret_cast<uint4*>(buf + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  if (two) *reinterpret_cast<uint4*>(buf + 4096 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  if (!mirror) return;
+  mirror8(image, c0, hi);
+  if (two) mirror8(image + image_lo, c0, lo);
 }
 
 // Barriers, tensor memory, the wait for the kernel before: the same for both kernels.  Returns the tensor memory's address.
@@ -422,8 +301,9 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   constexpr int kTile = 256, kCols = 128;
   const uint32_t raw = smem_addr(smem_raw);
   const uint32_t base = (raw + 1023) & ~1023u;
-  char* epi = smem_raw + (base - raw) + kSlots * kSlotBytes;
-  Shared* sh = reinterpret_cast<Shared*>(epi + kEpiWarps * kEpiBytes);
+  constexpr int kOwnSlots = kWideSlots<kSplit>, kOwnEpi = kEpiBytes + (kSplit ? kImageBytes : 0);
+  char* epi = smem_raw + (base - raw) + kOwnSlots * kSlotBytes;
+  Shared* sh = reinterpret_cast<Shared*>(epi + kEpiWarps * kOwnEpi);
   const int warp = threadIdx.x >> 5;
   const uint32_t rank = cluster_rank();
   const bool symmetric = P.kind <= kPoly;
@@ -431,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   const int first = blockIdx.x / 2, stride = gridDim.x / 2;
   const int blocks = (P.k + kBlockK - 1) / kBlockK;
   const uint32_t tmem = set_up<2>(P, sh, 512);
-  Ring ring[2] = {Ring(0, kSplit ? kHiSlots : kSlots), Ring(kHiSlots, kSlots - kHiSlots)};
+  Ring ring[2] = {Ring(0, kSplit ? kOwnSlots / 2 : kOwnSlots), Ring(kOwnSlots / 2, kOwnSlots / 2)};
   Turn turn;
   bool ok = true;
   if (warp == 0) {
@@ -446,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       for (int t = first; t < tiles && ok; t += stride) ok = issue_products<2, kSplit>(sh, base, tmem, blocks, P.b_mn, ring, &turn);
   } else if (warp >= 4) {
     const int w = warp - 4, quad = warp & 3, half = w >> 2, lane = lane_id();
-    char* buf = epi + w * kEpiBytes;
+    char* buf = epi + w * kOwnEpi;
     const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[w]);
     const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), 0), cluster_addr(smem_addr(&sh->sum_empty[1]), 0)};
     const bool has_add = P.kind != kGram;
@@ -457,41 +337,69 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       const int i0 = tm * kTile + (int)rank * 128 + quad * 32, jt = tn * kTile + half * kCols;
       const bool here = i0 < P.m && jt < P.n;
       if (has_add && here && lane == 0) load_add(P, buf_addr, add_bar, b, i0, jt);
-      auto finish_chunk = [&](int c, float* v) {
-        const int j0 = jt + c * 64;
-        if (!here || j0 >= P.n || !ok) return;
-        if (has_add) {
-          if (c > 0 && lane == 0) load_add(P, buf_addr, add_bar, b, i0, j0);
-          ok = __all_sync(0xffffffffu, mbar_wait(add_bar, add_phase));
-          if (!ok) return;
-          add_phase ^= 1;
-        }
-        finish(P, buf, buf_addr, b, i0, j0, symmetric && tm != tn, v);
-      };
+      const bool mirror = symmetric && tm != tn;
+      float acc[kSplit ? kCols : 1];
       if (kSplit) {
-        float acc[kCols];
         ok = take_sums<kTile, kCols>(sh, tmem, quad, half * kCols, sums_of(true, blocks), empty_bar, &turn, acc);
-#pragma unroll
-        for (int c = 0; c < kCols / 64; ++c) finish_chunk(c, acc + c * 64);
       } else {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sum_full[turn.sum]), turn.phase));
-        if (!ok) break;
         tcgen05_fence_after();
+      }
+      if (!ok) break;
+      // 32 columns at a time, one copy of the code: the kernels are short and instructions come late
 #pragma unroll 1
-        for (int c = 0; c < kCols / 64; ++c) {               // one copy of the code: the kernels are short, instructions come late
-          float v[64];
-          const uint32_t at = tmem + ((uint32_t)(quad * 32) << 16) + turn.sum * kTile + half * kCols + c * 64;
-          tmem_load32(at, v);
-          tmem_load32(at + 32, v + 32);
+      for (int s = 0; s < kCols / 32; ++s) {
+        const int j0 = jt + s / 2 * 64, odd = s & 1;
+        float v[32];
+        if (kSplit) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = s < 2 ? (odd ? acc[32 + e] : acc[e]) : (odd ? acc[96 + e] : acc[64 + e]);
+        } else {
+          tmem_load32(tmem + ((uint32_t)(quad * 32) << 16) + turn.sum * kTile + half * kCols + s * 32, v);
           tmem_load_wait();
-          if (c + 1 == kCols / 64) {
+          if (s + 1 == kCols / 32) {
             tcgen05_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(empty_bar[turn.sum]);
           }
-          finish_chunk(c, v);
         }
-        turn.next();
+        if (!here || j0 >= P.n || !ok) continue;
+        if (!odd) {                                          // a new 32 x 64 part of the buffer
+          if (has_add) {
+            if (s > 0 && lane == 0) load_add(P, buf_addr, add_bar, b, i0, j0);
+            ok = __all_sync(0xffffffffu, mbar_wait(add_bar, add_phase));
+            if (!ok) continue;
+            add_phase ^= 1;
+          } else {
+            if (lane == 0) tma_store_wait_read();
+            __syncwarp();
+          }
+        } else if (kSplit && mirror) {                       // the image's buffer may still be read
+          if (lane == 0) tma_store_wait_read();
+          __syncwarp();
+        }
+        // two pieces: both pieces' images of 32 columns behind the buffer; one: they fit in its second half, in turn
+        char* image = kSplit ? buf + kEpiBytes : buf + 4096 + odd * 2048;
+#pragma unroll
+        for (int p = 0; p < 4; ++p) {
+          const int q = odd * 4 + p;
+          finish8(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), image, 2048, p * 8, mirror, b, i0 + lane, j0 + q * 8, v + p * 8);
+        }
+        if (P.kind == kFinal) continue;
+        fence_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if (odd)
+            for (int piece = 0; piece < P.out_pieces; ++piece) tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
+          if (mirror && j0 + odd * 32 < P.n)
+            for (int piece = 0; piece < P.out_pieces; ++piece) tma_store(&P.mirror, i0, j0 + odd * 32, 2 * b + piece, smem_addr(image) + piece * 2048);
+          tma_store_commit();
+        }
+      }
+      if (!kSplit) turn.next();
+      if (P.kind == kFinal) {                                // what is added next lands where this was read
+        fence_async_smem();
+        __syncwarp();
       }
     }
     if (lane == 0) tma_store_wait_read();
@@ -527,7 +435,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
   const int i0 = tm * kTile + (part >> 1) * 32, j0 = tn * kTile + (part & 1) * kCols;
   const bool here = warp >= 4 && i0 < P.m && j0 < P.n, leads = q0 == 0 && lane == 0;
   char* buf = epi + pl * kEpiBytes;                           // what is added, then the result
-  char* side = base_ptr + 8 * 8192 + pl * 8192;               // its mirror image, or the caller's rows
+  char* side = base_ptr + 8 * 8192 + pl * 8192;               // its mirror image
   const uint32_t buf_addr = smem_addr(buf), add_bar = smem_addr(&sh->add_full[pl]);
   Ring ring[2] = {Ring(0, kSplit ? kHiSlots : kSlots), Ring(kHiSlots, kSlots - kHiSlots)};
   Turn turn;
@@ -549,7 +457,7 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
     __syncwarp();
     cluster_sync();
   }
-  const bool mirror = symmetric && tm != tn, two = P.out_pieces == 2;
+  const bool mirror = symmetric && tm != tn;
   if (here) {
     if (has_add) ok = __all_sync(0xffffffffu, mbar_wait(add_bar, 0)) && ok;
 #pragma unroll 1
@@ -572,53 +480,26 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
         x[0] += got[r][0].x; x[1] += got[r][0].y; x[2] += got[r][0].z; x[3] += got[r][0].w;
         x[4] += got[r][1].x; x[5] += got[r][1].y; x[6] += got[r][1].z; x[7] += got[r][1].w;
       }
-      const int off = lane * 128 + ((q ^ (lane & 7)) << 4);
-      combine8(P, buf, off, x);
-      if (P.kind != kFinal) {
-        uint32_t hi[4], lo[4];
-        split8(x, two, hi, lo);
-        *reinterpret_cast<uint4*>(buf + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        if (two) *reinterpret_cast<uint4*>(buf + 4096 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-        if (mirror) {
-          mirror8(side, q * 8, hi);
-          if (two) mirror8(side + 4096, q * 8, lo);
-        }
-      } else {
-        float* f = reinterpret_cast<float*>(side) + lane * 64;
-        *reinterpret_cast<float4*>(f + (((2 * q) ^ (lane & 7)) << 2)) = make_float4(x[0], x[1], x[2], x[3]);
-        *reinterpret_cast<float4*>(f + (((2 * q + 1) ^ (lane & 7)) << 2)) = make_float4(x[4], x[5], x[6], x[7]);
-      }
+      finish8(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), side, 4096, q * 8, mirror, b, i0 + lane, j0 + q * 8, x);
     }
   }
   if (ways > 1) {
     __syncwarp();
     cluster_arrive();                                         // the others may go once this CTA has read their sums
   }
-  if (here) {
-    if (P.kind != kFinal) fence_async_smem();
+  if (here && P.kind != kFinal) {
+    fence_async_smem();
     if (ways == 1) __syncwarp();
     else asm volatile("bar.sync %0, %1;" ::"r"(1 + pl), "r"(32 * ways) : "memory");   // the warps of a part
-    if (P.kind != kFinal) {
-      if (leads && ok) {
-        for (int piece = 0; piece < P.out_pieces; ++piece) {
-          tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
-          if (mirror) tma_store(&P.mirror, i0, j0, 2 * b + piece, smem_addr(side) + piece * 4096);
-        }
-        tma_store_commit();
-        tma_store_wait_read();
+    if (leads && ok) {
+      for (int piece = 0; piece < P.out_pieces; ++piece) {
+        tma_store(&P.out, j0, i0, 2 * b + piece, buf_addr + piece * 4096);
+        if (!mirror) continue;
+        tma_store(&P.mirror, i0, j0, 2 * b + piece, smem_addr(side) + piece * 4096);
+        if (j0 + 32 < P.n) tma_store(&P.mirror, i0, j0 + 32, 2 * b + piece, smem_addr(side) + piece * 4096 + 2048);
       }
-    } else {
-      // eight columns (or four rows) at a time, `mine` of them
-      const float* f = reinterpret_cast<const float*>(side);
-      for (int p = 0; p < mine; ++p) {
-        if (P.store.transpose) {
-          if (P.store.dtype == S3GD_F32) store_columns<float, 8>(P.store, f, b, i0, j0, (q0 + p) * 8, P.m, P.n);
-          else store_columns<__nv_bfloat16, 8>(P.store, f, b, i0, j0, (q0 + p) * 8, P.m, P.n);
-        } else {
-          if (P.store.dtype == S3GD_F32) store_rows<float, 4>(P.store, f, b, i0, j0, (q0 + p) * 4, P.m, P.n);
-          else store_rows<__nv_bfloat16, 4>(P.store, f, b, i0, j0, (q0 + p) * 4, P.m, P.n);
-        }
-      }
+      tma_store_commit();
+      tma_store_wait_read();
     }
   }
   tear_down<1>(P, ok, tmem, 256, false);
@@ -743,8 +624,8 @@ cudaError_t launch_products(const OrthoPlan& P, const OrthoRequest& R, char* ws,
   for (int i = 0; i < 2; ++i)
     ok = ok && make_map(&x_load[i], xs[i], m, n, P.ldx, planes, 64, 64) && make_map(&x_epi[i], xs[i], m, n, P.ldx, planes, 64, 32);
   ok = ok && make_map(&s_load, ws + P.off_s, m, m, P.lds, planes, 64, 64) && make_map(&s_epi, ws + P.off_s, m, m, P.lds, planes, 64, 32) &&
-       make_map(&s_mirror, ws + P.off_s, m, m, P.lds, planes, 32, 64) && make_map(&b_load, ws + P.off_b, m, m, P.lds, planes, 64, 64) &&
-       make_map(&b_epi, ws + P.off_b, m, m, P.lds, planes, 64, 32) && make_map(&b_mirror, ws + P.off_b, m, m, P.lds, planes, 32, 64);
+       make_map(&s_mirror, ws + P.off_s, m, m, P.lds, planes, 32, 32) && make_map(&b_load, ws + P.off_b, m, m, P.lds, planes, 64, 64) &&
+       make_map(&b_epi, ws + P.off_b, m, m, P.lds, planes, 64, 32) && make_map(&b_mirror, ws + P.off_b, m, m, P.lds, planes, 32, 32);
   if (!ok) return cudaErrorInvalidValue;
   const int carried = carried_steps(R.steps, R.split);
   for (int k = 0; k < R.steps; ++k) {

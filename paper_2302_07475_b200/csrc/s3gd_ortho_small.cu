@@ -33,32 +33,6 @@ __device__ __forceinline__ int entry_offset(int i, int j) {       // bytes, of e
   return (j >> 6) * kPanel + i * 128 + ((((j >> 3) & 7) ^ (i & 7)) << 4) + (j & 7) * 2;
 }
 
-// eight neighbouring entries of row i to the caller's matrix
-template <typename T>
-__device__ __forceinline__ void put8(const Store& s, int mat, int i, int j0, int m, int n, const float* x) {
-  if (i >= m) return;
-  T* base = reinterpret_cast<T*>(s.to.p) + (size_t)mat * s.to.batch;
-  if (s.wide && !s.transpose && j0 + 8 <= n) {
-    Four<T>* p = reinterpret_cast<Four<T>*>(base + (size_t)i * s.to.row + j0);
-    Four<T> o[2] = {};
-    if (s.update) { o[0] = p[0]; o[1] = p[1]; }
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e / 4].v[e % 4] = stored(s, o[e / 4].v[e % 4], x[e]);
-    p[0] = o[0]; p[1] = o[1];
-    return;
-  }
-  const size_t step = s.transpose ? s.to.row : 1;
-  base += s.transpose ? (size_t)j0 * s.to.row + i : (size_t)i * s.to.row + j0;
-  T old[8] = {};
-  if (s.update)
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (j0 + e < n) old[e] = base[e * step];
-#pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (j0 + e < n) base[e * step] = stored(s, old[e], x[e]);
-}
-
 __device__ __forceinline__ void write8(char* hi, char* lo, int off, const float* x) {
   uint32_t h[4], l[4];
   split8(x, true, h, l);
