@@ -246,3 +246,63 @@ def test_binding_refusals():
     with pytest.raises(S.S3gdError) as e:
         S.s3gd_orthogonalise(g, out, ws, steps=0)
     assert e.value.code == 1
+
+
+# ------------------------------------------------------------------ many tiles: pairs of CTAs on 256 x 256 tiles
+def exact_on_gpu(g, steps=5):
+    """The statement in fp64 on the GPU, for sizes that take numpy minutes."""
+    y = g.double()
+    y = y / (torch.linalg.vector_norm(y, dim=(-2, -1), keepdim=True) + EPS)
+    tall = y.shape[-2] > y.shape[-1]
+    a, b, c = C
+    for _ in range(steps):
+        p = y.mT @ y if tall else y @ y.mT
+        q = b * p + c * (p @ p)
+        y = a * y + (y @ q if tall else q @ y)
+    return y
+
+
+WIDE = [(2500, 2600), (2601, 2307), (12, 1030, 1025), (5, 1400, 2000), (3, 1300, 1290), (1, 2048, 2560), (20, 520, 700)]
+
+
+@pytest.mark.parametrize("shape", WIDE)
+@pytest.mark.parametrize("src,dst", [(torch.float32, torch.float32), (torch.bfloat16, torch.bfloat16), (torch.int8, torch.float32)])
+def test_many_tiles(shape, src, dst):
+    g = rand(shape, src, 21)
+    near(ortho(g, dst), exact_on_gpu(g).cpu().numpy(), tolerance(dst))
+
+
+@pytest.mark.parametrize("shape", [(2500, 2600), (2601, 2307), (5, 1400, 1500)])
+@pytest.mark.parametrize("x_dtype", [torch.float32, torch.bfloat16])
+def test_many_tiles_step(shape, x_dtype):
+    x, g, v = rand(shape, x_dtype, 22, 0.02), rand(shape, torch.bfloat16, 23, 1e-3), rand(shape, torch.float32, 24, 1e-3)
+    mu, lr, wd, scale = 0.9, 0.01, 0.1, 0.2 * max(shape[-2:]) ** 0.5
+    # rows of x that are not a multiple of four entries apart, so that no wide access fits
+    room = torch.zeros(shape[:-1] + (shape[-1] + 3,), dtype=x_dtype, device=DEV)
+    for x1 in (x.clone(), room[..., 1:1 + shape[-1]]):
+        x1.copy_(x)
+        v1, ws = v.clone(), workspace(shape)
+        S.s3gd_step_ortho(x1, g, lr, ws, v=v1, mu=mu, nesterov=True, weight_decay=wd, scale=scale)
+        S.s3gd_device_status(ws)
+        want_v = (torch.tensor(mu, device=DEV) * v) + g.float()
+        assert torch.equal(v1, want_v)
+        moved = lr * scale * exact_on_gpu(g.double() + float(np.float32(mu)) * want_v.double())
+        want = (1 - lr * wd) * x.double() - moved
+        tol = 4 * 2.0 ** -24 * x.double().norm() + tolerance(x_dtype) * moved.norm()
+        tol += 2.0 ** -9 * want.norm() if x_dtype == torch.bfloat16 else 0.0
+        assert (x1.double() - want).norm() <= tol
+    room[..., 1:1 + shape[-1]] = 0
+    assert not room.any()
+
+
+def test_many_tiles_keep_matrices_apart():
+    shape, dst = (5, 1400, 1500), torch.bfloat16
+    g = rand(shape, torch.float32, 25)
+    alone = ortho(g, dst)
+    assert torch.equal(alone, ortho(g, dst))
+    h = g.clone()
+    h[1, 3, 5], h[3] = float("inf"), 0.0
+    got = ortho(h, dst)
+    for k in (0, 2, 4):
+        assert torch.equal(got[k], alone[k])
+    assert torch.isnan(got[1]).all() and not got[3].any()
