@@ -399,7 +399,7 @@ S3GD_API s3gd_status s3gd_step_ortho(const s3gd_matrix* x, const s3gd_matrix* op
  *
  *  table  [vocab x dim] F32 or BF16, rows table_stride elements apart      ids   [n] I32 or I64
  *  out    [n x dim] F32 or BF16, rows out_stride elements apart            opt_bad_count  dev or NULL, one uint32
- * n may be 0.  Limits: vocab, dim and n < 2^31, n * ceil(dim / 256) < 2^34.
+ * n may be 0.  Limits: vocab, dim and n < 2^31, n * ceil(dim / 512) < 2^34.
  */
 S3GD_API s3gd_status s3gd_embed(const void* table, int table_dtype, int64_t table_stride, uint64_t vocab, uint64_t dim,
                                 const void* ids, int ids_dtype, uint64_t n, float scale, void* out, int out_dtype,
@@ -418,7 +418,7 @@ S3GD_API s3gd_status s3gd_embed(const void* table, int table_dtype, int64_t tabl
  *  grads  F32 or BF16, grads_stride elements from worker to worker (>= vocab * dim; the row of s3gd_step's grads that the
  *         table is a part of), already pointing at the table's first coordinate
  *  ws     >= s3gd_embed_grad_workspace_bytes(M, T, vocab, dim), 256-byte aligned
- * T may be 0.  M = 1 is the ordinary gradient.  Limits: M <= 65535, M * T < 2^31, vocab < 2^31, dim < 2^24.
+ * T may be 0.  M = 1 is the ordinary gradient.  Limits: M <= 65535, M * T < 2^31, vocab < 2^31, dim <= 2^25 - 512.
  */
 S3GD_API size_t s3gd_embed_grad_workspace_bytes(int M, uint64_t T, uint64_t vocab, uint64_t dim);
 S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t dout_stride, int64_t dout_worker_stride,

@@ -1,12 +1,19 @@
 // Embedding table: scaled lookup, and the gradient of M workers written into their rows (see include/s3gd.h).
 //
+// Lookup.  A warp takes 512 columns of one token's row, all loads under way before the first store.  Bound by memory: 65536
+// rows of 1000 from fp32 to bf16 take 39 us, 331 MB if every row were read once (51 us at 6.5 TB/s); common words are read
+// from L2.
+//
 // Gradient.  Every entry of a worker's vocab x dim block is written once: a warp takes kRows neighbouring rows and 512
-// columns, finds the tokens of its rows, sums their gradients in registers and stores sums or zeros.  Up to kDirectTokens
-// tokens per worker the warp scans the ids itself (one launch); beyond that the tokens are first sorted by id (stable, so
-// that each row's tokens come in ascending order) and the warp finds its rows by binary search.  A token that takes more
-// than kChunk places would leave one warp with all of them: its places are summed kChunk at a time by separate warps
-// (aligned in the sorted order, so at most two such tokens meet a chunk) and joined by a last kernel in ascending order.
-// The list of these tokens is written in whatever order they are found; each is then worked on by itself.
+// columns, finds the tokens of its rows, sums their gradients in registers and stores sums or zeros.  Few tokens per worker
+// (kDirectTokens, kDirectWork) the warp looks through itself, in one launch; more are first sorted by id (stable, so that
+// each row's tokens come in ascending order) and the warp finds its rows by search.  A token that takes more than a chunk of
+// places would leave one warp with all of them: its places are summed a chunk at a time by separate warps (aligned in the
+// sorted order, so at most two such tokens meet a chunk) and joined by a last kernel in ascending order.  The list of these
+// tokens is written in whatever order they are found; each is then worked on by itself.
+// Bound by memory and, for few tokens to a row, by the chain search - place - gradient: 131072 tokens bf16 into 65536 x 2048
+// fp32 take 246 us (1064 MB: 163 us at 6.5 TB/s; sort 37, rows 193, joining 20 by themselves), eight workers of 4096 tokens
+// into 16000 x 512 each 91 us (326 MB: 50 us).
 #include "s3gd_ops.cuh"
 
 namespace s3gd {
@@ -16,9 +23,13 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kLane = 16;                          // columns per lane
 constexpr int kTileCols = 32 * kLane;              // columns per warp
 constexpr int kRows = 8;                           // rows of the table per warp
+// Tokens per worker, and tokens times rows, that warps look through themselves: 512 tokens, 8000 rows of 768: 14.6 us, sorted
+// 18.5 us; 64 tokens: 12.4 and 15.9 us; 1024 tokens: 18.5 us either way; 512 tokens, 100000 rows: 88 us, sorted 72 us.
 constexpr int kDirectTokens = 512;
+constexpr uint64_t kDirectWork = 1ull << 24;
 constexpr int kHdrCommon = 16;                     // header word: common tokens found
-constexpr int kMinChunk = 32, kMaxChunks = 8192;   // places per partial sum at least; partial sums per worker at most
+constexpr int kMinChunk = 32, kMaxChunks = 8192;   // places per partial sum at least (64: 107 instead of 94 us for the eight
+                                                   // workers above); partial sums per worker at most
 
 // ------------------------------------------------------------------ access of kVec neighbouring entries
 template <typename T, int kVec>
@@ -78,7 +89,8 @@ __global__ void __launch_bounds__(kThreads) lookup_kernel(const W* table, long l
 // range take the key `vocab` and end up behind all others.
 constexpr int kSortThreads = 512, kSortWarps = kSortThreads / 32;
 constexpr int kSortEach = 8, kSortTile = kSortThreads * kSortEach;   // of a long row, or the whole of a short one
-constexpr int kFewEach = 4, kFewTiles = 64;       // rows of up to 64 tiles of 2048 are cut into these: more CTAs, shorter chains
+constexpr int kFewEach = 4, kFewTiles = 64;       // rows of up to 64 tiles of 2048 are cut into these: more
+                                                   // CTAs, shorter chains (131072 tokens: 246 instead of 273 us)
 constexpr int kMaxDigit = 9, kBins = 1 << kMaxDigit;
 
 struct SortPlan { int passes, bits; };
@@ -524,7 +536,7 @@ bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L)
   if (M < 1 || M > 65535 || vocab == 0 || dim == 0 || vocab >= (1ull << 31) || dim >= (1ull << 31) || T >= (1ull << 31) ||
       (uint64_t)M * T >= (1ull << 31))
     return false;
-  L->direct = T <= kDirectTokens;
+  L->direct = T <= kDirectTokens && T * vocab <= kDirectWork;
   uint64_t chunk = (T + kMaxChunks - 1) / kMaxChunks;
   L->chunk = (uint32_t)(chunk < kMinChunk ? kMinChunk : chunk);
   L->chunks = (uint32_t)((T + L->chunk - 1) / L->chunk);

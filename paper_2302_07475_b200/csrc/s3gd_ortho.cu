@@ -1,4 +1,7 @@
-// Orthogonalised updates: momentum, Newton-Schulz products, update of the matrices (see include/s3gd.h).
+// Orthogonalised updates: argument checks, momentum, norm and the first 16-bit matrix (see include/s3gd.h).
+// Two passes over the gradient, because the norm must be known before anything can be rounded to 16 bits: momentum and sum of
+// squares (32 us for 4 x 2048 x 2048 with bf16 gradients: 168 MB, 26 us at 6.5 TB/s), then u over the norm as fp16 pieces
+// (50 us; its blocks live too briefly to keep more loads under way).
 #include <math.h>
 
 #include "s3gd_ortho.cuh"

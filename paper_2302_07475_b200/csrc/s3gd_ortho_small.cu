@@ -2,7 +2,8 @@
 // update.  X (up to 128 x 256) and S stay in shared memory, as two fp16 pieces each, in the layout that the tensor cores read
 // both ways: rows of 64 entries in 128 swizzled bytes serve as K-major operand for X X^T and S S^T and as MN-major operand for
 // B X.  A step is three products, each followed by all sixteen warps taking the sums out of tensor memory and writing the next
-// operand in place; the chain of these (about 3 us a step for 64 x 128), not bytes or operations, is what the time is made of.
+// operand in place.  The chain of these, not bytes or operations, is what the time is made of: 32 matrices of 64 x 128 fp32 take
+// 31 us (2 MB, 0.9 GFLOP), about 5 us a step of three products; 16 x 16 still 20 us.
 #include "s3gd_ortho.cuh"
 #include "s3gd_tcgen05.cuh"
 
@@ -271,6 +272,8 @@ cudaError_t launch_by(const SmallArgs& A, int batch, int bytes, cudaStream_t st)
 
 }  // namespace
 
+// What one CTA's shared memory holds.  One 64 x 128 fp32: 31 us, by the kernels for large matrices 90 us; 128 x 256: 60 and 97 us;
+// 400 of them: 186 and 816 us.
 bool is_small(const OrthoPlan& P) { return P.m <= 128 && P.n <= 256; }
 
 cudaError_t launch_small(const OrthoPlan& P, const OrthoRequest& R, char* ws, cudaStream_t st) {
