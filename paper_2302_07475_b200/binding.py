@@ -462,6 +462,8 @@ def s3gd_step_randk(x: torch.Tensor, grads: torch.Tensor, K: int, lr: float, see
 
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.int8: 2, torch.int32: 3, torch.int64: 4}
 _REAL = (torch.float32, torch.bfloat16)
+_REAL_CODES = {d: _DTYPES[d] for d in _REAL}
+_INDEX_CODES = {d: _DTYPES[d] for d in (torch.int32, torch.int64)}
 #: Coefficients of the quintic that five steps of are usually taken.
 ORTHO_COEFFS = (3.4445, -4.7750, 2.0315)
 
@@ -588,25 +590,37 @@ def _ids(ids: torch.Tensor):
 def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale: float = 1.0,
                opt_bad_count: Optional[torch.Tensor] = None) -> None:
     """out[..., :] <- scale * table[ids[...], :]; a negative id gives a zero row.  table [vocab, dim], out ids.shape + [dim]."""
-    _rows(table, _REAL, "table")
-    _ids(ids)
-    shape = out.shape
+    try:                                   # a call for one token takes 8 us, half of it here: look once, name the fault afterwards
+        whole = table.is_cuda and ids.is_cuda and out.is_cuda and ids.is_contiguous()
+        codes = _REAL_CODES[table.dtype], _INDEX_CODES[ids.dtype], _REAL_CODES[out.dtype]
+    except (AttributeError, KeyError):
+        whole = False
+    if not whole:
+        _rows(table, _REAL, "table")
+        _ids(ids)
+        _rows(out, _REAL, "out")
+        raise TypeError("table, ids and out must be CUDA tensors")
+    shape, n = out.shape, ids.numel()
     if table.dim() != 2 or shape[:-1] != ids.shape:
         raise ValueError(f"table must be [vocab, dim] and out {tuple(ids.shape)} + [dim]")
     vocab, dim = table.shape
-    _rows(out, _REAL, "out", dim)
-    if out.is_contiguous():
-        out_stride = dim
-    elif len(shape) == 2:
+    table_stride = out_stride = dim
+    if not table.is_contiguous():
+        _rows(table, _REAL, "table")
+        table_stride = table.stride(0)
+    if shape[-1] != dim or not out.is_contiguous():
+        _rows(out, _REAL, "out", dim)
+        if len(shape) != 2:
+            raise ValueError("out must be contiguous, or [n, dim] with contiguous rows")
         out_stride = out.stride(0)
+    bad = None if opt_bad_count is None else _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count")
+    index = out.get_device()
+    args = (table.data_ptr(), codes[0], table_stride, vocab, dim, ids.data_ptr(), codes[1], n, scale, out.data_ptr(), codes[2], out_stride, bad)
+    if _current_device() == index:
+        code = load().s3gd_embed(*args, _stream_of(index))
     else:
-        raise ValueError("out must be contiguous, or [n, dim] with contiguous rows")
-    n = ids.numel()
-    args = (table.data_ptr(), _DTYPES[table.dtype], table.stride(0) if vocab > 1 else dim, vocab, dim, ids.data_ptr(), _DTYPES[ids.dtype], n,
-            scale, out.data_ptr(), _DTYPES[out.dtype], out_stride if n > 1 else dim, _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
-    device = out.device
-    with _on(device):
-        code = load().s3gd_embed(*args, _stream_of(device.index))
+        with _on(out.device):
+            code = load().s3gd_embed(*args, _stream_of(index))
     if code:
         _check("s3gd_embed", code)
 
@@ -629,25 +643,37 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
 
     grads is [M, >= vocab * dim] (a column slice of the step's gradient buffer), [M, vocab, dim], or [vocab, dim] where dout is
     [T, dim] and ids [T] (one worker).  Negative ids are skipped; accumulate adds to what grads holds."""
-    _rows(dout, _REAL, "dout")
-    _ids(ids)
-    if dout.dim() != ids.dim() + 1 or dout.shape[:-1] != ids.shape or ids.dim() not in (1, 2):
+    try:
+        whole = dout.is_cuda and ids.is_cuda and grads.is_cuda and ids.is_contiguous() and dout.shape[:-1] == ids.shape and ids.dim() in (1, 2)
+        codes = _REAL_CODES[dout.dtype], _INDEX_CODES[ids.dtype], _REAL_CODES[grads.dtype]
+    except (AttributeError, KeyError):
+        whole = False
+    if not whole:
+        _rows(dout, _REAL, "dout")
+        _ids(ids)
+        _rows(grads, _REAL, "grads")
         raise ValueError("dout must be [M, T, dim] with ids [M, T], or [T, dim] with ids [T]")
-    M, T, dim = (ids.shape[0] if ids.dim() == 2 else 1), ids.shape[-1], dout.shape[-1]
-    _of(grads, _REAL, "grads")
-    if not (grads.is_cuda and grads.dim() >= 2):
-        raise TypeError("grads must be a CUDA tensor of two or three axes")
-    if grads.shape[-2:] == (vocab, dim) and grads.dim() == ids.dim() + 1:
-        per, rows_of = vocab * dim, grads if grads.dim() == 3 else grads.unsqueeze(0)
-        whole = (dim == 1 or grads.stride(-1) == 1) and (vocab == 1 or grads.stride(-2) == dim)
+    several = ids.dim() == 2
+    M, T, dim = (ids.shape[0] if several else 1), ids.shape[-1], dout.shape[-1]
+    if dim > 1 and dout.stride(-1) != 1:
+        raise ValueError("dout must be contiguous along its last axis")
+    shape = grads.shape
+    if len(shape) == ids.dim() + 1 and shape[-2:] == (vocab, dim):
+        per, given, stride = vocab * dim, shape[0] if several else 1, grads.stride(0) if several else 0
+        packed = grads.is_contiguous() or ((dim == 1 or grads.stride(-1) == 1) and (vocab == 1 or grads.stride(-2) == dim))
     else:
-        per, rows_of = grads.shape[-1], grads
-        whole = grads.dim() == 2 and (per == 1 or grads.stride(-1) == 1)
-    if not whole or rows_of.shape[0] != M or per < vocab * dim:
+        per, given, stride = shape[-1], shape[0], grads.stride(0)
+        packed = len(shape) == 2 and (per == 1 or grads.stride(-1) == 1)
+    if not packed or given != M or per < vocab * dim:
         raise ValueError(f"grads must be [{M}, >= {vocab * dim}] or [{M}, {vocab}, {dim}], contiguous within a worker")
-    args = (dout.data_ptr(), _DTYPES[dout.dtype], dout.stride(-2), dout.stride(0) if ids.dim() == 2 else 0, ids.data_ptr(), _DTYPES[ids.dtype],
-            M, T, vocab, dim, scale, grads.data_ptr(), _DTYPES[grads.dtype], rows_of.stride(0) if M > 1 else vocab * dim, int(accumulate),
-            _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with _on(grads.device):
-        code = load().s3gd_embed_grad(*args, _stream_of(grads.device.index))
-    _check("s3gd_embed_grad", code)
+    bad = None if opt_bad_count is None else _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count")
+    index = grads.get_device()
+    args = (dout.data_ptr(), codes[0], dout.stride(-2), dout.stride(0) if several else 0, ids.data_ptr(), codes[1], M, T, vocab, dim, scale,
+            grads.data_ptr(), codes[2], stride if M > 1 else vocab * dim, accumulate, bad, _ptr(ws, torch.uint8, name="ws"), ws.numel())
+    if _current_device() == index:
+        code = load().s3gd_embed_grad(*args, _stream_of(index))
+    else:
+        with _on(grads.device):
+            code = load().s3gd_embed_grad(*args, _stream_of(index))
+    if code:
+        _check("s3gd_embed_grad", code)

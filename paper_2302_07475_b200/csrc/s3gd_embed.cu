@@ -12,8 +12,8 @@
 // sorted order, so at most two such tokens meet a chunk) and joined by a last kernel in ascending order.  The list of these
 // tokens is written in whatever order they are found; each is then worked on by itself.
 // Bound by memory and, for few tokens to a row, by the chain search - place - gradient: 131072 tokens bf16 into 65536 x 2048
-// fp32 take 246 us (1064 MB: 163 us at 6.5 TB/s; sort 37, rows 193, joining 20 by themselves), eight workers of 4096 tokens
-// into 16000 x 512 each 91 us (326 MB: 50 us).
+// fp32 take 252 us (1064 MB: 163 us at 6.5 TB/s; sort 37, rows 193, joining 20 by themselves), eight workers of 4096 tokens
+// into 16000 x 512 each 86 us (326 MB: 50 us).
 #include "s3gd_ops.cuh"
 
 namespace s3gd {
@@ -471,6 +471,8 @@ __global__ void __launch_bounds__(kThreads) rows_sorted_kernel(GradArgs g, uint3
   if (v0 >= g.vocab) return;
   O* grads = static_cast<O*>(g.grads) + m * g.stride;
   const uint32_t bound = row_bounds(keys, g.T, v0, g.vocab);
+  uint32_t window = __shfl_sync(0xffffffffu, bound, 0);      // 32 places from here on are in the lanes' `place`
+  uint32_t place = window + lane < g.T ? __ldg(places + window + lane) : 0u;
   for (uint32_t r = 0; r < kRows && v0 + r < g.vocab; ++r) {
     const uint32_t s = __shfl_sync(0xffffffffu, bound, r), e = __shfl_sync(0xffffffffu, bound, r + 1);
     if (e - s > g.chunk) {
@@ -479,7 +481,14 @@ __global__ void __launch_bounds__(kThreads) rows_sorted_kernel(GradArgs g, uint3
     }
     if (e == s && g.accumulate) continue;
     float acc[kLane] = {};
-    add_rows<D, kVec>(dout, g.tok_stride, [&](uint32_t i) { return __ldg(places + s + i); }, e - s, c0, g.dim, acc);
+    for (uint32_t at = s; at < e; at += 32) {
+      const uint32_t n = min(32u, e - at);
+      if (at + n > window + 32) {
+        window = at;
+        place = window + lane < g.T ? __ldg(places + window + lane) : 0u;
+      }
+      add_rows<D, kVec>(dout, g.tok_stride, [&](uint32_t i) { return __shfl_sync(0xffffffffu, place, at - window + i); }, n, c0, g.dim, acc);
+    }
     put_row<O, kVec>(grads + (v0 + r) * g.dim, c0, g.dim, acc, g.scale, g.accumulate);
   }
 }
