@@ -23,8 +23,8 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kLane = 16;                          // columns per lane
 constexpr int kTileCols = 32 * kLane;              // columns per warp
 constexpr int kRows = 8;                           // rows of the table per warp
-// Tokens per worker, and tokens times rows, that warps look through themselves: 512 tokens, 8000 rows of 768: 14.6 us, sorted
-// 18.5 us; 64 tokens: 12.4 and 15.9 us; 1024 tokens: 18.5 us either way; 512 tokens, 100000 rows: 88 us, sorted 72 us.
+// Tokens per worker, and tokens times rows, that warps look through themselves: 512 tokens, 8000 rows of 768: 14.2 us, sorted
+// 18.5 us; 64 tokens: 12.4 and 15.9 us; 1024 tokens: 18.5 us either way; 512 tokens, 100000 rows: 87 us, sorted 70 us.
 constexpr int kDirectTokens = 512;
 constexpr uint64_t kDirectWork = 1ull << 24;
 constexpr int kHdrCommon = 16;                     // header word: common tokens found
@@ -410,16 +410,25 @@ __global__ void __launch_bounds__(kThreads) rows_direct_kernel(GradArgs g) {
   const D* dout = static_cast<const D*>(g.dout) + m * g.worker_stride;
   O* grads = static_cast<O*>(g.grads) + m * g.stride;
   if (v0 >= g.vocab) return;
-  uint32_t n = 0, out_of_range = 0;
-  for (uint32_t t0 = 0; t0 < g.T; t0 += 32) {
-    const uint32_t t = t0 + lane;
-    const uint32_t key = t < g.T ? key_of(ids[t], g.vocab) : g.vocab;
-    if (v0 == 0 && tile == 0) out_of_range += t < g.T && ids[t] >= 0 && key == g.vocab;
-    const bool mine = key < g.vocab && key >= v0 && key < v0 + kRows;
+  uint32_t n = 0, out_of_range = 0, keys[kDirectTokens / 32];
+#pragma unroll
+  for (int k = 0; k < kDirectTokens / 32; ++k) {                               // all ids under way at once
+    const uint32_t t = k * 32 + lane;
+    keys[k] = g.vocab;
+    if (t >= g.T) continue;
+    const I id = ids[t];
+    keys[k] = key_of(id, g.vocab);
+    out_of_range += id >= 0 && keys[k] == g.vocab;
+  }
+#pragma unroll
+  for (int k = 0; k < kDirectTokens / 32; ++k) {
+    if (k * 32 >= g.T) break;
+    const bool mine = keys[k] < g.vocab && keys[k] >= v0 && keys[k] < v0 + kRows;
     const uint32_t votes = __ballot_sync(0xffffffffu, mine);
-    if (mine) found[w][n + __popc(votes & lanemask_lt())] = (key - v0) << 16 | t;
+    if (mine) found[w][n + __popc(votes & lanemask_lt())] = (keys[k] - v0) << 16 | (k * 32 + lane);
     n += __popc(votes);
   }
+  if (v0 != 0 || tile != 0) out_of_range = 0;                                  // counted once
   if (g.bad != nullptr && out_of_range) atomicAdd(g.bad, out_of_range);
   __syncwarp();
   const uint32_t c0 = tile * kTileCols + lane * kVec;
