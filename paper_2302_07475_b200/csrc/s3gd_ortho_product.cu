@@ -50,6 +50,7 @@ struct ProductArgs {
   uint32_t* hdr;
   int m, n, k, batch;
   int tiles_m, tiles_n, ways;                     // ways: CTAs that share a tile of the narrow kernel
+  int whole;                                      // wide kernel: tiles that are not cut in two
   int b_mn;                                       // b is read with k down its rows
   int kind;
   int add_pieces, out_pieces;                     // 16-bit pieces of the matrix that is added, and of the result
@@ -114,22 +115,23 @@ struct Ring {
   }
 };
 
-// Loads slots k of [from, to): rows row_a.. of the first operand and row_b.. of the second, 128 each.
+// Loads slots k of [from, to): 128 rows of the first operand from row_a, and 64 * boxes_b of the second from row_b.
 template <int kCta, bool kSplit>
-__device__ __forceinline__ bool load_slots(const ProductArgs& P, Shared* sh, uint32_t base, uint32_t rank, int b, int row_a, int row_b, int from,
-                                           int to, Ring* ring) {
+__device__ __forceinline__ bool load_slots(const ProductArgs& P, Shared* sh, uint32_t base, uint32_t rank, int b, int row_a, int row_b, int boxes_b,
+                                           int from, int to, Ring* ring) {
   for (int kb = from; kb < to; ++kb)
     for (int piece = 0; piece < (kSplit ? 2 : 1); ++piece) {
       Ring& r = ring[piece];
       if (!mbar_wait(smem_addr(&sh->empty[r.slot]), r.phase ^ 1)) return false;
       uint32_t bar = smem_addr(&sh->full[r.slot]);
-      if (rank == 0) mbar_expect_tx(bar, kCta * kSlotBytes);
+      if (rank == 0) mbar_expect_tx(bar, kCta * (16384 + boxes_b * 8192));
       if (kCta == 2) bar = cluster_addr(bar, 0);
       const uint32_t dst = base + r.slot * kSlotBytes;
       const int k0 = kb * kBlockK, z = 2 * b + piece;
       for (int h = 0; h < 2; ++h) tma_load<kCta>(dst + h * 8192, &P.a, k0, row_a + h * 64, z, bar);
-      for (int h = 0; h < 2; ++h)
-        tma_load<kCta>(dst + 16384 + h * 8192, &P.b, P.b_mn ? row_b + h * 64 : k0, P.b_mn ? k0 : row_b + h * 64, z, bar);
+      const int xb = P.b_mn ? row_b : k0, yb = P.b_mn ? k0 : row_b;
+      tma_load<kCta>(dst + 16384, &P.b, xb, yb, z, bar);    // written out: a loop of a length not known costs 4 % of the large products
+      if (boxes_b == 2) tma_load<kCta>(dst + 16384 + 8192, &P.b, P.b_mn ? xb + 64 : xb, P.b_mn ? yb : yb + 64, z, bar);
       r.next();
     }
   return true;
@@ -144,12 +146,13 @@ struct Turn {
   }
 };
 
-// Products of `blocks` slots of k.  Two pieces: hi lo + lo hi before hi hi, so that fewer additions are cut off at the size of
+// Products of `blocks` slots of k into `columns` columns.  Two pieces: hi lo + lo hi before hi hi, so that fewer additions are cut off at the size of
 // the full sum.
 template <int kCta, bool kSplit>
-__device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32_t tmem, int blocks, bool b_mn, Ring* ring, Turn* turn) {
+__device__ __forceinline__ bool issue_products(Shared* sh, uint32_t base, uint32_t tmem, int blocks, int columns, bool b_mn, Ring* ring,
+                                               Turn* turn) {
   constexpr int kTile = 128 * kCta;
-  const uint32_t idesc = product_desc(kTile, kTile, b_mn), b_next = b_mn ? 8192 : 16, b_step = (b_mn ? 2048 : 32) / 16;
+  const uint32_t idesc = product_desc(kTile, columns, b_mn), b_next = b_mn ? 8192 : 16, b_step = (b_mn ? 2048 : 32) / 16;
   auto product = [&](uint32_t d, int sa, int sb, bool add) {
     const uint64_t a = operand_desc(base + sa * kSlotBytes), b = operand_desc(base + sb * kSlotBytes + 16384, b_next);
 #pragma unroll
@@ -317,20 +320,29 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
   const int tiles = P.batch * (symmetric ? P.tiles_m * (P.tiles_m + 1) / 2 : P.tiles_m * P.tiles_n);
   const int first = blockIdx.x / 2, stride = gridDim.x / 2;
   const int blocks = (P.k + kBlockK - 1) / kBlockK;
+  // Tiles beyond P.whole are worked on as two halves of 128 columns each.
+  const int items = P.whole + 2 * (tiles - P.whole);
+  auto item_at = [&](int t, int* b, int* tm, int* tn, int* column) {
+    const int over = t - P.whole;
+    tile_at(P, over < 0 ? t : P.whole + over / 2, symmetric, b, tm, tn);
+    *column = *tn * kTile + (over < 0 ? 0 : (over & 1) * 128);
+    return over < 0 ? kTile : kTile / 2;
+  };
   const uint32_t tmem = set_up<2>(P, sh, 512);
   Ring ring[2] = {Ring(0, kSplit ? kOwnSlots / 2 : kOwnSlots), Ring(kOwnSlots / 2, kOwnSlots / 2)};
   Turn turn;
   bool ok = true;
   if (warp == 0) {
     if (lane_id() == 0)
-      for (int t = first; t < tiles && ok; t += stride) {
-        int b, tm, tn;
-        tile_at(P, t, symmetric, &b, &tm, &tn);
-        ok = load_slots<2, kSplit>(P, sh, base, rank, b, tm * kTile + (int)rank * 128, tn * kTile + (int)rank * 128, 0, blocks, ring);
+      for (int t = first; t < items && ok; t += stride) {
+        int b, tm, tn, column;
+        const int columns = item_at(t, &b, &tm, &tn, &column);
+        ok = load_slots<2, kSplit>(P, sh, base, rank, b, tm * kTile + (int)rank * 128, column + (int)rank * columns / 2, columns / 128, 0, blocks, ring);
       }
   } else if (warp == 1) {
     if (lane_id() == 0 && rank == 0)
-      for (int t = first; t < tiles && ok; t += stride) ok = issue_products<2, kSplit>(sh, base, tmem, blocks, P.b_mn, ring, &turn);
+      for (int t = first; t < items && ok; t += stride)
+        ok = issue_products<2, kSplit>(sh, base, tmem, blocks, t < P.whole ? kTile : kTile / 2, P.b_mn, ring, &turn);
   } else if (warp >= 4) {
     const int w = warp - 4, quad = warp & 3, half = w >> 2, lane = lane_id();
     char* buf = epi + w * kOwnEpi;
@@ -338,16 +350,16 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
     const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), 0), cluster_addr(smem_addr(&sh->sum_empty[1]), 0)};
     const bool has_add = P.kind != kGram;
     uint32_t add_phase = 0;
-    for (int t = first; t < tiles && ok; t += stride) {
-      int b, tm, tn;
-      tile_at(P, t, symmetric, &b, &tm, &tn);
-      const int i0 = tm * kTile + (int)rank * 128 + quad * 32, jt = tn * kTile + half * kCols;
+    for (int t = first; t < items && ok; t += stride) {
+      int b, tm, tn, column;
+      const int own = item_at(t, &b, &tm, &tn, &column) / 2;   // columns of this warp
+      const int i0 = tm * kTile + (int)rank * 128 + quad * 32, jt = column + half * own;
       const bool here = i0 < P.m && jt < P.n;
       if (has_add && here && lane == 0) load_add(P, buf_addr, add_bar, b, i0, jt);
       const bool mirror = symmetric && tm != tn;
       float acc[kSplit ? kCols : 1];
       if (kSplit) {
-        ok = take_sums<kTile, kCols>(sh, tmem, quad, half * kCols, sums_of(true, blocks), empty_bar, &turn, acc);
+        ok = take_sums<kTile, kCols>(sh, tmem, quad, half * own, sums_of(true, blocks), empty_bar, &turn, acc);
       } else {
         ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->sum_full[turn.sum]), turn.phase));
         tcgen05_fence_after();
@@ -355,16 +367,16 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
       if (!ok) break;
       // 32 columns at a time, one copy of the code: the kernels are short and instructions come late
 #pragma unroll 1
-      for (int s = 0; s < kCols / 32; ++s) {
+      for (int s = 0; s < own / 32; ++s) {
         const int j0 = jt + s / 2 * 64, odd = s & 1;
         float v[32];
         if (kSplit) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = s < 2 ? (odd ? acc[32 + e] : acc[e]) : (odd ? acc[96 + e] : acc[64 + e]);
         } else {
-          tmem_load32(tmem + ((uint32_t)(quad * 32) << 16) + turn.sum * kTile + half * kCols + s * 32, v);
+          tmem_load32(tmem + ((uint32_t)(quad * 32) << 16) + turn.sum * kTile + half * own + s * 32, v);
           tmem_load_wait();
-          if (s + 1 == kCols / 32) {
+          if (s + 1 == own / 32) {
             tcgen05_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(empty_bar[turn.sum]);
@@ -448,9 +460,9 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
   Turn turn;
   bool ok = true;
   if (warp == 0) {
-    if (lane == 0) ok = load_slots<1, kSplit>(P, sh, base, 0, b, tm * kTile, tn * kTile, from, to, ring);
+    if (lane == 0) ok = load_slots<1, kSplit>(P, sh, base, 0, b, tm * kTile, tn * kTile, 2, from, to, ring);
   } else if (warp == 1) {
-    if (lane == 0) ok = issue_products<1, kSplit>(sh, base, tmem, to - from, P.b_mn, ring, &turn);
+    if (lane == 0) ok = issue_products<1, kSplit>(sh, base, tmem, to - from, kTile, P.b_mn, ring, &turn);
   } else if (warp >= 4) {
     if (has_add && here && leads) load_add(P, buf_addr, add_bar, b, i0, j0);
     const uint32_t empty_bar[2] = {cluster_addr(smem_addr(&sh->sum_empty[0]), rank), cluster_addr(smem_addr(&sh->sum_empty[1]), rank)};
@@ -600,7 +612,9 @@ cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
   static int done_wide[kMaxDevices], done_narrow[kMaxDevices], at_a_time[4][kMaxDevices];
   const int pairs = sm_count() / 2, pieces = kSplit ? 3 : 1;
   const int64_t wide = tiles_of(A, 256), narrow = tiles_of(A, 128), blocks = (A.k + kBlockK - 1) / kBlockK;
-  int64_t best = (wide + pairs - 1) / pairs * blocks * pieces * kSlotUnits + kWideStart;
+  // The last round of wide tiles is cut into halves where they fit into one: it takes half as long then.
+  const int64_t over = wide % pairs, whole = over * 2 <= pairs ? wide - over : wide;
+  int64_t best = (whole / pairs * 2 + (whole % pairs != 0 ? 2 : 0) + (whole < wide ? 1 : 0)) * blocks * pieces * kSlotUnits / 2 + kWideStart;
   A.ways = 0;
   auto kernel = narrow_kernel<kSplit>;
   cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kSmemBytes, done_narrow);
@@ -615,7 +629,11 @@ cudaError_t launch_product(ProductArgs& A, cudaStream_t st) {
   const int tile = A.ways == 0 ? 256 : 128;
   A.tiles_m = (A.m + tile - 1) / tile;
   A.tiles_n = (A.n + tile - 1) / tile;
-  if (A.ways == 0) return launch_cluster(wide_kernel<kSplit>, A, (unsigned)(wide < pairs ? wide : pairs) * 2, 2, done_wide, st);
+  if (A.ways == 0) {
+    A.whole = (int)whole;
+    const int64_t items = whole + 2 * (wide - whole);
+    return launch_cluster(wide_kernel<kSplit>, A, (unsigned)(items < pairs ? items : pairs) * 2, 2, done_wide, st);
+  }
   return launch_cluster(kernel, A, (unsigned)(narrow * A.ways), A.ways, done_narrow, st);
 }
 
