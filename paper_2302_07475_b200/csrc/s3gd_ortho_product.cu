@@ -15,9 +15,10 @@
 // diagonal of S); with two pieces the sum is therefore taken out of tensor memory every kChunk slots of k and added in
 // registers, and the small products go first.
 //
-// Bounds.  Large: the tensor cores under the power cap; 8192 x 8192 bf16 runs five steps in 9.2 to 9.8 ms, 1.12 to 1.19 PFLOP/s
+// Bounds.  Large: the tensor cores under the power cap; 8192 x 8192 bf16 runs five steps in 9.0 to 10.1 ms, 1.09 to 1.22 PFLOP/s
 // of m^2 n + m^3 + 2 m^2 n operations a step (a plain bf16 product of the library sustains 1.37 here), fp32 results 28 ms with
-// three times the products.  Tile counts that do not fill the last round cost up to a seventh.  Middle: the chain of kernels; a
+// three times the products.  Tiles of a last round that fill half of it or less are cut in two (4 x 2048 x 2048 fp32: 2.09 ->
+// 1.99 ms); a last round between half and full is lost time.  Middle: the chain of kernels; a
 // product of 1024 x 1024 takes 9 us, of which 1.3 pass between two kernels, 1.5 until the first operands arrive, 3 to 5 in the
 // products (bound by L2: 64 KB per CTA and 64 entries of k, 12.6 TB/s over 128 CTAs with two pieces) and 3 in the epilogue.
 #include <atomic>
