@@ -368,7 +368,8 @@ typedef struct s3gd_matrix {
  *  steps  1..32       a, b, c, eps  finite, eps >= 0; refused where some s in [0, 1] would leave [-2, 2] on its way, or
  *                     |b s^2 + c s^4| pass 24, which the internal 16-bit forms are not made for
  *  split_steps  how many of the first steps take their products from two 16-bit pieces of each operand (22 bits) instead
- *                     of one (11 bits): 0..steps, or -1: all for an F32 result and for matrices with a side below 32, else none
+ *                     of one (11 bits): 0..steps, or -1: all, which is what fp32 products give.  A third of the products and
+ *                     about 1e-3 (in the norm) off with 0, for callers to whom a bf16 update of that accuracy is enough
  *  ws           >= s3gd_orthogonalise_workspace_bytes(batch, rows, cols), 256-byte aligned, not preserved
  * Sums are held in 32 bits, norms in 64.  s3gd_device_status(ws) reports a kernel that gave up (S3GD_ERR_INTERNAL).
  * Limits: 1 <= batch <= 65535, rows and cols < 2^24, batch * rows * cols <= 10^12.
@@ -385,7 +386,7 @@ S3GD_API s3gd_status s3gd_orthogonalise(const s3gd_matrix* g, const s3gd_matrix*
  *
  *  x      F32 or BF16, updated       opt_v  F32, updated, or NULL: u = g (mu and nesterov are not used)
  *  g      F32, BF16 or I8 (the vote of s3gd_majority_vote / s3gd_step as the gradient), const
- *  the rest as for s3gd_orthogonalise; split_steps = -1 goes by the type of x
+ *  the rest as for s3gd_orthogonalise
  */
 S3GD_API s3gd_status s3gd_step_ortho(const s3gd_matrix* x, const s3gd_matrix* opt_v, const s3gd_matrix* g, int batch,
                                      uint64_t rows, uint64_t cols, float mu, int nesterov, float lr, float weight_decay,

@@ -542,7 +542,8 @@ def s3gd_orthogonalise(g: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, ste
                        eps: float = 1e-7, split_steps: int = -1) -> None:
     """out <- g with its singular values moved towards 1 by `steps` Newton-Schulz products, per matrix of the batch.
 
-    g fp32, bf16 or an int8 vote; out fp32 or bf16, g itself allowed.  split_steps: see include/s3gd.h (-1: by out's type)."""
+    g fp32, bf16 or an int8 vote; out fp32 or bf16, g itself allowed.  split_steps: of how many steps the products take
+    operands of 22 bits instead of 11 (-1: all)."""
     m, batch, rows, cols = _matrices(g=g, out=out)
     _of(g, _REAL + (torch.int8,), "g")
     _of(out, _REAL, "out")

@@ -201,14 +201,9 @@ s3gd_status common_checks(const s3gd_matrix* g, int batch, uint64_t rows, uint64
 
 Mat as_mat(const s3gd_matrix* a) { return {static_cast<char*>(a->data), (long long)a->row_stride, (long long)a->batch_stride}; }
 
-// Products of one-piece operands are off by up to 2^-12 per entry and step; over the sums of a matrix's rows such errors
-// average out to well below what rounding to bf16 leaves (2^-9), but not where a row has a few entries only: a 1 x 7 matrix
-// came out 5.5e-3 off.  Matrices that small cost the same either way.
-constexpr int kFewRows = 32;
-int split_rule(int split_steps, int steps, int dtype, int m) {
-  if (split_steps >= 0) return split_steps;
-  return dtype == S3GD_F32 || m < kFewRows ? steps : 0;
-}
+// Two pieces in every product unless the caller asks for fewer, whatever the result's type: a bf16 result is then the fp32
+// one rounded once (1.7e-3 from the definition, all of it rounding; with one piece 2.0e-3 to 2.3e-3).
+int split_rule(int split_steps, int steps) { return split_steps >= 0 ? split_steps : steps; }
 
 }  // namespace
 }  // namespace s3gd
@@ -231,7 +226,7 @@ extern "C" s3gd_status s3gd_orthogonalise(const s3gd_matrix* g, const s3gd_matri
   OrthoRequest R = {};
   R.g = as_mat(g); R.g_dtype = g->dtype;
   R.out = as_store(out, batch, rows > cols, false, 0.f, 0.f);
-  R.steps = steps; R.split = split_rule(split_steps, steps, out->dtype, P.m);
+  R.steps = steps; R.split = split_rule(split_steps, steps);
   R.a = a; R.b = b; R.c = c; R.eps = eps;
   return run(P, R, static_cast<char*>(ws), static_cast<cudaStream_t>(stream)) == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
 }
@@ -251,7 +246,7 @@ extern "C" s3gd_status s3gd_step_ortho(const s3gd_matrix* x, const s3gd_matrix* 
   if (R.has_v) R.v = as_mat(opt_v);
   R.mu = mu; R.nesterov = nesterov;
   R.out = as_store(x, batch, rows > cols, true, 1.f - lr * weight_decay, lr * scale);
-  R.steps = steps; R.split = split_rule(split_steps, steps, x->dtype, P.m);
+  R.steps = steps; R.split = split_rule(split_steps, steps);
   R.a = a; R.b = b; R.c = c; R.eps = eps;
   return run(P, R, static_cast<char*>(ws), static_cast<cudaStream_t>(stream)) == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
 }

@@ -46,11 +46,12 @@ struct OrthoRequest {
   float a, b, c, eps;
 };
 
-// For how many of the first steps X is held in two pieces: where the products take two, and otherwise for the a X term
-// alone in all but the last two steps.  The products of one-piece operands lose little where singular values are small
-// (B is of second order in them), while X itself must keep them through the steps that raise them: with a part of rank 16
-// ten times above the rest the result is off by 5e-4 this way, 3.6e-3 with X in one piece, and 1e-3 with two full steps of
-// three products.  In the last steps the rounding of X in both terms cancels in part, so one piece is as good there.
+// For how many of the first steps X is held in two pieces: where the products take two, and in steps whose products the
+// caller wants of one piece for the a X term alone, in all but the last two.  The products of one-piece operands lose little
+// where singular values are small (B is of second order in them), while X itself must keep them through the steps that raise
+// them: with a part of rank 16 ten times above the rest and no split step the result is off by 5e-4 this way, 3.6e-3 with X in
+// one piece, and 1e-3 with X in one piece but two split steps.  In the last steps the rounding of X in both terms cancels in
+// part, so one piece is as good there.
 inline int carried_steps(int steps, int split) {
   const int c = steps > 3 ? steps - 2 : 1;
   return c > split ? c : split;

@@ -10,7 +10,8 @@
 // under the products of the next.  narrow_kernel, where there are fewer tiles than SMs: 128 x 128 tiles, each by a cluster of
 // up to eight CTAs that share out k and join their sums through distributed shared memory.
 //
-// Precision.  One fp16 piece per entry (11 bits), or two (kSplit, 22 bits): then hi hi + hi lo + lo hi, three products.
+// Precision.  Two fp16 pieces per entry (kSplit, 22 bits): hi hi + hi lo + lo hi, three products.  Or, in steps for which the
+// caller asks for it, one (11 bits).
 // The tensor cores cut off, rather than round, what falls below the running fp32 sum, which biases a long sum of squares (the
 // diagonal of S); with two pieces the sum is therefore taken out of tensor memory every kChunk slots of k and added in
 // registers, and the small products go first.
