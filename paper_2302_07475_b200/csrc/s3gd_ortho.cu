@@ -112,14 +112,14 @@ __global__ void __launch_bounds__(kPrepThreads) normalise_kernel(Mat g, Mat v, b
   }
   double s = 0.0;
   for (int i = threadIdx.x; i < norm_blocks; i += kPrepThreads) s += partial[b * norm_blocks + i];
-  const float inv = (float)((double)kScaleX / (sqrt(block_sum(s, warp_sums)) + (double)eps));
+  const Normaliser normalised(sqrt(block_sum(s, warp_sums)), eps);
 #pragma unroll
   for (int k = 0; k < 4; ++k) {
     const int dr = k * 16 + (threadIdx.x >> 4), dc = (threadIdx.x & 15) * 4;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float w = has_v && nesterov ? __fadd_rn(u[k][e], __fmul_rn(mu, old[k][e])) : u[k][e];
-      tile[tall ? dc + e : dr][tall ? dr : dc + e] = w * inv;
+      tile[tall ? dc + e : dr][tall ? dr : dc + e] = normalised(w);
     }
   }
   __syncthreads();

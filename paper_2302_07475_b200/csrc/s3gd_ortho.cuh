@@ -58,6 +58,17 @@ inline int carried_steps(int steps, int split) {
 }
 
 #ifdef __CUDACC__
+// X_0 = u / (|u| + eps), times 2^10, as (u pre) inv.  2^10 over a norm below 2^-118 would not fit fp32, and one over 2^136
+// would lose bits in its subnormals: such matrices are first moved by a power of two, which changes no bit of theirs.
+struct Normaliser {
+  float pre, inv;
+  __device__ __forceinline__ Normaliser(double norm, float eps) {
+    const double d = norm + (double)eps;
+    pre = d < 0x1p-96 ? 0x1p96f : d > 0x1p96 ? 0x1p-96f : 1.f;
+    inv = (float)((double)kScaleX / (d * (double)pre));
+  }
+  __device__ __forceinline__ float operator()(float u) const { return __fmul_rn(__fmul_rn(u, pre), inv); }
+};
 // a value as two fp16 pieces, 22 bits together
 __device__ __forceinline__ void split_half(float v, __half* hi, __half* lo) {
   *hi = __float2half_rn(v);

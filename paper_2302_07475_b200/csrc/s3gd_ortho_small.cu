@@ -117,7 +117,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
   __syncthreads();
   sum = 0.0;
   for (int k = 0; k < kSmallThreads / 32; ++k) sum += sh->warp_sums[k];
-  const float inv = (float)((double)kScaleX / (sqrt(sum) + (double)P.eps));
+  const Normaliser normalised(sqrt(sum), P.eps);
   const bool tall = P.rows > P.cols;
 #pragma unroll
   for (int k = 0; k < kGroups; ++k) {
@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
     if (e >= groups) continue;
     __align__(8) __half hi[4], lo[4];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) split_half(u[k][x] * inv, &hi[x], &lo[x]);
+    for (int x = 0; x < 4; ++x) split_half(normalised(u[k][x]), &hi[x], &lo[x]);
     if (!tall) {
       const int off = entry_offset(r, c);                    // four entries from a multiple of four: eight bytes
       *reinterpret_cast<uint2*>(x_hi + off) = *reinterpret_cast<uint2*>(hi);
