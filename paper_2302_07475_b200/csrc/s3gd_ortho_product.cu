@@ -406,7 +406,13 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
           const int q = odd * 4 + p;
           finish8(P, buf, lane * 128 + ((q ^ (lane & 7)) << 4), image, 2048, p * 8, mirror, b, i0 + lane, j0 + q * 8, v + p * 8);
         }
-        if (P.kind == kFinal) continue;
+        if (P.kind == kFinal) {                              // what is added next lands where this was read
+          if (odd) {
+            fence_async_smem();
+            __syncwarp();
+          }
+          continue;
+        }
         fence_async_smem();
         __syncwarp();
         if (lane == 0) {
@@ -418,10 +424,6 @@ __global__ void __launch_bounds__(kThreads, 1) wide_kernel(const __grid_constant
         }
       }
       if (!kSplit) turn.next();
-      if (P.kind == kFinal) {                                // what is added next lands where this was read
-        fence_async_smem();
-        __syncwarp();
-      }
     }
     if (lane == 0) tma_store_wait_read();
   }
