@@ -494,7 +494,8 @@ __global__ void __launch_bounds__(kThreads, 1) narrow_kernel(const __grid_consta
 #pragma unroll
         for (int l = 0; l < 2; ++l)
           asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                       : "=f"(got[r][l].x), "=f"(got[r][l].y), "=f"(got[r][l].z), "=f"(got[r][l].w) : "r"(from_r + l * 512));
+                       : "=f"(got[r][l].x), "=f"(got[r][l].y), "=f"(got[r][l].z), "=f"(got[r][l].w) : "r"(from_r + l * 512)
+                       : "memory");                           // ways 1: after this lane's own stores above
       }
       float x[8] = {got[0][0].x, got[0][0].y, got[0][0].z, got[0][0].w, got[0][1].x, got[0][1].y, got[0][1].z, got[0][1].w};
 #pragma unroll
