@@ -366,7 +366,8 @@ typedef struct s3gd_matrix {
  *
  *  g      F32, BF16 or I8 (a vote), const        out    F32 or BF16; may be g itself (same type and strides)
  *  steps  1..32       a, b, c, eps  finite, eps >= 0; refused where some s in [0, 1] would leave [-2, 2] on its way, or
- *                     |b s^2 + c s^4| pass 24, which the internal 16-bit forms are not made for
+ *                     |b s^2 + c s^4| pass 24, which the internal 16-bit forms are not made for, and where errors of 2^-9 a
+ *                     step could take one an eighth beyond these
  *  split_steps  how many of the first steps take their products from two 16-bit pieces of each operand (22 bits) instead
  *                     of one (11 bits): 0..steps, or -1: all, which is what fp32 products give.  A third of the products and
  *                     about 1e-3 (in the norm) off with 0, for callers to whom a bf16 update of that accuracy is enough
