@@ -156,6 +156,31 @@ def _stream_of(index: int):
     return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+class _on:
+    """torch.cuda.device of the tensors of a short call, which have to share one (None: not given); nothing is switched where it is
+    current already."""
+
+    __slots__ = ("index", "before")
+
+    def __init__(self, t: torch.Tensor, *others: Optional[torch.Tensor]):
+        self.index = index = t.get_device()
+        for o in others:
+            if o is not None and o.get_device() != index:
+                raise TypeError(f"tensors of one call must be on one device, not on {t.device} and {o.device}")
+
+    def __enter__(self):
+        self.before = _current_device()
+        if self.before != self.index:
+            torch.cuda.set_device(self.index)
+
+    def __exit__(self, *exc):
+        if self.before != self.index:
+            torch.cuda.set_device(self.before)
+
+
 def _check(call: str, code: int) -> None:
     if code != S3GD_OK:
         raise S3gdError(call, code)
@@ -512,27 +537,6 @@ def _matrices(**tensors):
     return mats, first.shape[0] if first.dim() == 3 else 1, rows, cols
 
 
-_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-
-
-class _on:
-    """torch.cuda.device(device) for a short call: nothing is switched where the device is current already."""
-
-    __slots__ = ("index", "before")
-
-    def __init__(self, device: torch.device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.before = _current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
-
-
 def _of(t: Optional[torch.Tensor], dtypes, name: str) -> None:
     if t is not None and t.dtype not in dtypes:
         raise TypeError(f"{name} has dtype {t.dtype}, needs one of {', '.join(str(d) for d in dtypes)}")
@@ -549,7 +553,7 @@ def s3gd_orthogonalise(g: torch.Tensor, out: torch.Tensor, ws: torch.Tensor, ste
     _of(out, _REAL, "out")
     a, b, c = coeffs
     w = _ptr(ws, torch.uint8, name="ws")
-    with _on(out.device):
+    with _on(out, ws):
         code = load().s3gd_orthogonalise(m["g"], m["out"], batch, rows, cols, steps, a, b, c, eps, split_steps, w, ws.numel(), _stream_of(out.device.index))
     _check("s3gd_orthogonalise", code)
 
@@ -566,7 +570,7 @@ def s3gd_step_ortho(x: torch.Tensor, g: torch.Tensor, lr: float, ws: torch.Tenso
     _of(g, _REAL + (torch.int8,), "g")
     a, b, c = coeffs
     w = _ptr(ws, torch.uint8, name="ws")
-    with _on(x.device):
+    with _on(x, ws):
         code = load().s3gd_step_ortho(m["x"], m["v"], m["g"], batch, rows, cols, mu, int(nesterov), lr, weight_decay, scale, steps, a, b, c,
                                       eps, split_steps, w, ws.numel(), _stream_of(x.device.index))
     _check("s3gd_step_ortho", code)
@@ -592,7 +596,8 @@ def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale:
                opt_bad_count: Optional[torch.Tensor] = None) -> None:
     """out[..., :] <- scale * table[ids[...], :]; a negative id gives a zero row.  table [vocab, dim], out ids.shape + [dim]."""
     try:                                   # a call for one token takes 8 us, half of it here: look once, name the fault afterwards
-        whole = table.is_cuda and ids.is_cuda and out.is_cuda and ids.is_contiguous()
+        index = out.get_device()
+        whole = index >= 0 and table.get_device() == index and ids.get_device() == index and ids.is_contiguous()
         codes = _REAL_CODES[table.dtype], _INDEX_CODES[ids.dtype], _REAL_CODES[out.dtype]
     except (AttributeError, KeyError):
         whole = False
@@ -600,7 +605,7 @@ def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale:
         _rows(table, _REAL, "table")
         _ids(ids)
         _rows(out, _REAL, "out")
-        raise TypeError("table, ids and out must be CUDA tensors")
+        raise TypeError(f"table, ids and out must be on one device, not on {table.device}, {ids.device} and {out.device}")
     shape, n = out.shape, ids.numel()
     if table.dim() != 2 or shape[:-1] != ids.shape:
         raise ValueError(f"table must be [vocab, dim] and out {tuple(ids.shape)} + [dim]")
@@ -615,12 +620,13 @@ def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale:
             raise ValueError("out must be contiguous, or [n, dim] with contiguous rows")
         out_stride = out.stride(0)
     bad = None if opt_bad_count is None else _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count")
-    index = out.get_device()
+    if bad is not None and opt_bad_count.get_device() != index:
+        raise TypeError(f"opt_bad_count must be on the device of out, {out.device}")
     args = (table.data_ptr(), codes[0], table_stride, vocab, dim, ids.data_ptr(), codes[1], n, scale, out.data_ptr(), codes[2], out_stride, bad)
     if _current_device() == index:
         code = load().s3gd_embed(*args, _stream_of(index))
     else:
-        with _on(out.device):
+        with _on(out):
             code = load().s3gd_embed(*args, _stream_of(index))
     if code:
         _check("s3gd_embed", code)
@@ -645,7 +651,9 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
     grads is [M, >= vocab * dim] (a column slice of the step's gradient buffer), [M, vocab, dim], or [vocab, dim] where dout is
     [T, dim] and ids [T] (one worker).  Negative ids are skipped; accumulate adds to what grads holds."""
     try:
-        whole = dout.is_cuda and ids.is_cuda and grads.is_cuda and ids.is_contiguous() and dout.shape[:-1] == ids.shape and ids.dim() in (1, 2)
+        index = grads.get_device()
+        whole = (index >= 0 and dout.get_device() == index and ids.get_device() == index and ids.is_contiguous() and dout.shape[:-1] == ids.shape
+                 and ids.dim() in (1, 2))
         codes = _REAL_CODES[dout.dtype], _INDEX_CODES[ids.dtype], _REAL_CODES[grads.dtype]
     except (AttributeError, KeyError):
         whole = False
@@ -653,6 +661,8 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
         _rows(dout, _REAL, "dout")
         _ids(ids)
         _rows(grads, _REAL, "grads")
+        if not dout.device == ids.device == grads.device:
+            raise TypeError(f"dout, ids and grads must be on one device, not on {dout.device}, {ids.device} and {grads.device}")
         raise ValueError("dout must be [M, T, dim] with ids [M, T], or [T, dim] with ids [T]")
     several = ids.dim() == 2
     M, T, dim = (ids.shape[0] if several else 1), ids.shape[-1], dout.shape[-1]
@@ -668,13 +678,15 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
     if not packed or given != M or per < vocab * dim:
         raise ValueError(f"grads must be [{M}, >= {vocab * dim}] or [{M}, {vocab}, {dim}], contiguous within a worker")
     bad = None if opt_bad_count is None else _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count")
-    index = grads.get_device()
+    w = _ptr(ws, torch.uint8, name="ws")
+    if ws.get_device() != index or (bad is not None and opt_bad_count.get_device() != index):
+        raise TypeError(f"ws and opt_bad_count must be on the device of grads, {grads.device}")
     args = (dout.data_ptr(), codes[0], dout.stride(-2), dout.stride(0) if several else 0, ids.data_ptr(), codes[1], M, T, vocab, dim, scale,
-            grads.data_ptr(), codes[2], stride if M > 1 else vocab * dim, accumulate, bad, _ptr(ws, torch.uint8, name="ws"), ws.numel())
+            grads.data_ptr(), codes[2], stride if M > 1 else vocab * dim, accumulate, bad, w, ws.numel())
     if _current_device() == index:
         code = load().s3gd_embed_grad(*args, _stream_of(index))
     else:
-        with _on(grads.device):
+        with _on(grads):
             code = load().s3gd_embed_grad(*args, _stream_of(index))
     if code:
         _check("s3gd_embed_grad", code)
