@@ -214,7 +214,7 @@ def s3gd_topk_sign(grads: torch.Tensor, K: int, out_idx: torch.Tensor, out_signb
     args = (g, M, d, K, _ptr(out_idx, torch.int32, M * K, "out_idx"),
             _ptr(out_signbits, torch.int32, M * words(K), "out_signbits"),
             _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(grads.device):
+    with _on(grads, out_idx, out_signbits, ws):
         code = load().s3gd_topk_sign(*args, _stream(grads))
     _check("s3gd_topk_sign", code)
 
@@ -224,7 +224,7 @@ def s3gd_majority_vote(idx: torch.Tensor, signbits: torch.Tensor, M: int, K: int
     """idx [M, K], signbits [M, ceil(K/32)] -> out_vote [d] int8 in {-1, 0, +1}."""
     args = (_ptr(idx, torch.int32, M * K, "idx"), _ptr(signbits, torch.int32, M * words(K), "signbits"), M, K, d,
             _ptr(out_vote, torch.int8, d, "out_vote"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(out_vote.device):
+    with _on(out_vote, idx, signbits, ws):
         code = load().s3gd_majority_vote(*args, _stream(out_vote))
     _check("s3gd_majority_vote", code)
 
@@ -233,7 +233,7 @@ def s3gd_apply(x: torch.Tensor, vote: torch.Tensor, lr: float) -> None:
     """x [d] fp32 updated in place by -lr * vote."""
     d = x.numel()
     args = (_ptr(x, torch.float32, name="x"), _ptr(vote, torch.int8, d, "vote"), d, ctypes.c_float(lr))
-    with torch.cuda.device(x.device):
+    with _on(x, vote):
         code = load().s3gd_apply(*args, _stream(x))
     _check("s3gd_apply", code)
 
@@ -247,7 +247,7 @@ def s3gd_step(x: torch.Tensor, grads: torch.Tensor, K: int, lr: float, ws: torch
     args = (_ptr(x, torch.float32, d, "x"), g, M, d, K, ctypes.c_float(lr),
             _ptr(opt_idx, torch.int32, M * K, "opt_idx"), _ptr(opt_signbits, torch.int32, M * words(K), "opt_signbits"),
             _ptr(opt_vote, torch.int8, d, "opt_vote"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(x.device):
+    with _on(x, grads, opt_idx, opt_signbits, opt_vote, ws):
         code = load().s3gd_step(*args, _stream(x))
     _check("s3gd_step", code)
 
@@ -278,7 +278,7 @@ def s3gd_debug_topk_sign(grads: torch.Tensor, K: int, out_idx: torch.Tensor, out
     args = (g, M, d, K, _ptr(out_idx, torch.int32, M * K, "out_idx"),
             _ptr(out_signbits, torch.int32, M * words(K), "out_signbits"),
             _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(grads.device):
+    with _on(grads, out_idx, out_signbits, ws):
         code = load().s3gd_debug_topk_sign(*args, _stream(grads), int(sample_rank))
     _check("s3gd_debug_topk_sign", code)
 
@@ -292,7 +292,7 @@ def s3gd_debug_step(x: torch.Tensor, grads: torch.Tensor, K: int, lr: float, ws:
     args = (_ptr(x, torch.float32, d, "x"), g, M, d, K, ctypes.c_float(lr),
             _ptr(opt_idx, torch.int32, M * K, "opt_idx"), _ptr(opt_signbits, torch.int32, M * words(K), "opt_signbits"),
             _ptr(opt_vote, torch.int8, d, "opt_vote"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(x.device):
+    with _on(x, grads, opt_idx, opt_signbits, opt_vote, ws):
         code = load().s3gd_debug_step(*args, _stream(x), int(sample_rank), int(prevote_rank))
     _check("s3gd_debug_step", code)
 
@@ -304,7 +304,7 @@ def s3gd_vote_apply(x: torch.Tensor, msg: torch.Tensor, n_groups: int, group_str
     need = (n_groups - 1) * group_stride + M_group * (K + words(K)) if n_groups > 0 else 0
     args = (_ptr(x, torch.float32, name="x"), _ptr(msg, torch.int32, need, "msg"), n_groups, group_stride, M_group, K, d,
             ctypes.c_float(lr), _ptr(opt_vote, torch.int8, d, "opt_vote"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(x.device):
+    with _on(x, msg, opt_vote, ws):
         code = load().s3gd_vote_apply(*args, _stream(x))
     _check("s3gd_vote_apply", code)
 
@@ -318,7 +318,7 @@ def s3gd_vote_counts(idx: torch.Tensor, signbits: torch.Tensor, M: int, K: int, 
         per, p = 4, _ptr(out_counts, torch.int32, d, "out_counts")
     args = (_ptr(idx, torch.int32, M * K, "idx"), _ptr(signbits, torch.int32, M * words(K), "signbits"), M, K, d,
             out_counts.numel(), p, per, _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
-    with torch.cuda.device(out_counts.device):
+    with _on(out_counts, idx, signbits, opt_bad_count):
         code = load().s3gd_vote_counts(*args, _stream(out_counts))
     _check("s3gd_vote_counts", code)
 
@@ -333,7 +333,7 @@ def s3gd_encode_vote2(src: torch.Tensor, out_words: torch.Tensor, n_summed: int 
     else:
         kind, p = 2, _ptr(src, torch.int8, name="src")
     args = (p, kind, n_summed, n, _ptr(out_words, torch.int32, (n + 15) // 16, "out_words"))
-    with torch.cuda.device(src.device):
+    with _on(src, out_words):
         code = load().s3gd_encode_vote2(*args, _stream(src))
     _check("s3gd_encode_vote2", code)
 
@@ -343,7 +343,7 @@ def s3gd_apply_vote2(x: torch.Tensor, words2: torch.Tensor, lr: float, opt_vote:
     d = x.numel()
     args = (_ptr(x, torch.float32, name="x"), _ptr(words2, torch.int32, (d + 15) // 16, "words"), d, ctypes.c_float(lr),
             _ptr(opt_vote, torch.int8, d, "opt_vote"))
-    with torch.cuda.device(x.device):
+    with _on(x, words2, opt_vote):
         code = load().s3gd_apply_vote2(*args, _stream(x))
     _check("s3gd_apply_vote2", code)
 
@@ -369,7 +369,7 @@ def s3gd_encode_vote_sparse(src: torch.Tensor, out_piece: torch.Tensor, cap: int
         kind, p = 2, _ptr(src, torch.int8, name="src")
     args = (p, kind, n_summed, n, index_base, cap, _ptr(out_piece, torch.int32, sparse_piece_words(cap), "out_piece"),
             _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(src.device):
+    with _on(src, out_piece, ws):
         code = load().s3gd_encode_vote_sparse(*args, _stream(src))
     _check("s3gd_encode_vote_sparse", code)
 
@@ -381,7 +381,7 @@ def s3gd_apply_vote_sparse(x: torch.Tensor, pieces: torch.Tensor, n_pieces: int,
     need = (n_pieces - 1) * piece_stride + sparse_piece_words(cap)
     args = (_ptr(x, torch.float32, name="x"), _ptr(pieces, torch.int32, need, "pieces"), n_pieces, piece_stride, cap, d,
             ctypes.c_float(lr), _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
-    with torch.cuda.device(x.device):
+    with _on(x, pieces, opt_bad_count):
         code = load().s3gd_apply_vote_sparse(*args, _stream(x))
     _check("s3gd_apply_vote_sparse", code)
 
@@ -426,7 +426,7 @@ def s3gd_majority_vote_noalloc(idx: torch.Tensor, signbits: torch.Tensor, M: int
     """
     args = (_ptr(idx, torch.int32, M * K, "idx"), _ptr(signbits, torch.int32, M * words(K), "signbits"), M, K, d,
             _ptr(out_vote, torch.int8, d, "out_vote"), _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count"))
-    with torch.cuda.device(out_vote.device):
+    with _on(out_vote, idx, signbits, opt_bad_count):
         code = load().s3gd_majority_vote_noalloc(*args, _stream(out_vote))
     _check("s3gd_majority_vote_noalloc", code)
 
@@ -443,7 +443,7 @@ def s3gd_step_ex(x: torch.Tensor, grads: torch.Tensor, K: int, lr: float, ws: to
             _ptr(v, torch.float32, d, "v"), ctypes.c_float(mu), M, d, K, ctypes.c_float(lr),
             _ptr(opt_idx, torch.int32, M * K, "opt_idx"), _ptr(opt_signbits, torch.int32, M * words(K), "opt_signbits"),
             _ptr(opt_vote, torch.int8, d, "opt_vote"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(x.device):
+    with _on(x, grads, err, v, opt_idx, opt_signbits, opt_vote, ws):
         code = load().s3gd_step_ex(*args, _stream(x))
     _check("s3gd_step_ex", code)
 
@@ -453,7 +453,7 @@ def s3gd_apply_momentum(x: torch.Tensor, v: torch.Tensor, vote: torch.Tensor, mu
     d = x.numel()
     args = (_ptr(x, torch.float32, name="x"), _ptr(v, torch.float32, d, "v"), _ptr(vote, torch.int8, d, "vote"), d,
             ctypes.c_float(mu), ctypes.c_float(lr))
-    with torch.cuda.device(x.device):
+    with _on(x, v, vote):
         code = load().s3gd_apply_momentum(*args, _stream(x))
     _check("s3gd_apply_momentum", code)
 
@@ -466,7 +466,7 @@ def s3gd_randk_sign(grads: torch.Tensor, K: int, seed: int, step: int, out_idx: 
     args = (g, M, d, K, seed & 0xFFFFFFFF, step & 0xFFFFFFFF, _ptr(out_idx, torch.int32, M * K, "out_idx"),
             _ptr(out_signbits, torch.int32, M * words(K), "out_signbits"),
             _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(grads.device):
+    with _on(grads, out_idx, out_signbits, ws):
         code = load().s3gd_randk_sign(*args, _stream(grads))
     _check("s3gd_randk_sign", code)
 
@@ -480,7 +480,7 @@ def s3gd_step_randk(x: torch.Tensor, grads: torch.Tensor, K: int, lr: float, see
     args = (_ptr(x, torch.float32, d, "x"), g, M, d, K, ctypes.c_float(lr), seed & 0xFFFFFFFF, step & 0xFFFFFFFF,
             _ptr(opt_idx, torch.int32, M * K, "opt_idx"), _ptr(opt_signbits, torch.int32, M * words(K), "opt_signbits"),
             _ptr(opt_vote, torch.int8, d, "opt_vote"), _ptr(ws, torch.uint8, name="ws"), ws.numel())
-    with torch.cuda.device(x.device):
+    with _on(x, grads, opt_idx, opt_signbits, opt_vote, ws):
         code = load().s3gd_step_randk(*args, _stream(x))
     _check("s3gd_step_randk", code)
 
