@@ -5,6 +5,7 @@
 #include <atomic>
 
 #include "s3gd_common.cuh"
+#include "s3gd_opt_in.h"
 
 namespace s3gd {
 
@@ -92,16 +93,7 @@ int sm_count() {
   return n;
 }
 
-cudaError_t opt_in_dynamic_smem(const void* func, int bytes, int* done) {
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  const bool cached = dev >= 0 && dev < kMaxDevices;
-  if (cached && __atomic_load_n(&done[dev], __ATOMIC_RELAXED) >= bytes) return cudaSuccess;
-  e = cudaFuncSetAttribute(func, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess && cached) __atomic_store_n(&done[dev], bytes, __ATOMIC_RELAXED);
-  return e;
-}
+cudaError_t opt_in_dynamic_smem(const void* func, int bytes, int* done) { return raise_dynamic_smem(func, bytes, done, kMaxDevices); }
 
 // ---------------------------------------------------------------- profiling
 namespace {

@@ -30,8 +30,8 @@ constexpr int kMaxDevices = 64;                    // per-device host caches are
 
 // SMs of the current device (asked once per device).  Grids are sized in multiples of it.
 int sm_count();
-// cudaFuncSetAttribute(func, MaxDynamicSharedMemorySize, bytes), issued once per device and
-// kernel: `done` is a zero-initialised array of kMaxDevices flags owned by the call site.
+// cudaFuncSetAttribute(func, MaxDynamicSharedMemorySize, bytes), issued once per device, kernel and larger size
+// (s3gd_opt_in.h): `done` is a zero-initialised array of kMaxDevices sizes owned by the call site.
 cudaError_t opt_in_dynamic_smem(const void* func, int bytes, int* done);
 
 // --------------------------------------------------------------- device state
