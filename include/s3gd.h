@@ -419,7 +419,7 @@ S3GD_API s3gd_status s3gd_embed(const void* table, int table_dtype, int64_t tabl
  *  ids    [M x T] I32 or I64
  *  grads  F32 or BF16, grads_stride elements from worker to worker (>= vocab * dim; the row of s3gd_step's grads that the
  *         table is a part of), already pointing at the table's first coordinate
- *  ws     >= s3gd_embed_grad_workspace_bytes(M, T, vocab, dim), 256-byte aligned
+ *  ws     >= s3gd_embed_grad_workspace_bytes(M, T, vocab, dim), 256-byte aligned; one for larger numbers serves smaller ones
  * T may be 0.  M = 1 is the ordinary gradient.  Limits: M <= 65535, M * T < 2^31, vocab < 2^31, dim <= 2^25 - 512.
  */
 S3GD_API size_t s3gd_embed_grad_workspace_bytes(int M, uint64_t T, uint64_t vocab, uint64_t dim);

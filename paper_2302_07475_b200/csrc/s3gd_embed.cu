@@ -569,9 +569,13 @@ bool grad_layout(int M, uint64_t T, uint64_t vocab, uint64_t dim, GradLayout* L)
       L->off_keys[i] = off;    off = align_up(off + list, 256);
       L->off_places[i] = off;  off = align_up(off + list, 256);
     }
-    L->off_counts = off;   off = align_up(off + (size_t)M * kBins * L->sort_tiles * sizeof(uint32_t), 256);
-    L->off_common = off;   off = align_up(off + (size_t)M * L->chunks * sizeof(uint4), 256);   // each takes more than a chunk
-    L->off_partial = off;  off = align_up(off + (size_t)M * L->chunks * 2 * L->pad * sizeof(float), 256);
+    // Room that does not shrink where T grows past the point at which tiles or chunks become longer, so that a workspace for
+    // many tokens serves fewer.
+    const size_t tiles = !L->few && L->sort_tiles < kFewTiles ? kFewTiles : L->sort_tiles;
+    const size_t chunks = L->chunk > kMinChunk ? kMaxChunks : L->chunks;
+    L->off_counts = off;   off = align_up(off + (size_t)M * kBins * tiles * sizeof(uint32_t), 256);
+    L->off_common = off;   off = align_up(off + (size_t)M * chunks * sizeof(uint4), 256);   // each takes more than a chunk
+    L->off_partial = off;  off = align_up(off + (size_t)M * chunks * 2 * L->pad * sizeof(float), 256);
   }
   L->total = off;
   return true;
