@@ -607,7 +607,7 @@ def s3gd_embed(table: torch.Tensor, ids: torch.Tensor, out: torch.Tensor, scale:
         _rows(out, _REAL, "out")
         raise TypeError(f"table, ids and out must be on one device, not on {table.device}, {ids.device} and {out.device}")
     shape, n = out.shape, ids.numel()
-    if table.dim() != 2 or shape[:-1] != ids.shape:
+    if table.dim() != 2 or len(shape) == 0 or shape[:-1] != ids.shape:
         raise ValueError(f"table must be [vocab, dim] and out {tuple(ids.shape)} + [dim]")
     vocab, dim = table.shape
     table_stride = out_stride = dim
@@ -672,9 +672,12 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
     if len(shape) == ids.dim() + 1 and shape[-2:] == (vocab, dim):
         per, given, stride = vocab * dim, shape[0] if several else 1, grads.stride(0) if several else 0
         packed = grads.is_contiguous() or ((dim == 1 or grads.stride(-1) == 1) and (vocab == 1 or grads.stride(-2) == dim))
+    elif len(shape) == 2:
+        per, given, stride = shape[1], shape[0], grads.stride(0)
+        packed = per == 1 or grads.stride(1) == 1
     else:
-        per, given, stride = shape[-1], shape[0], grads.stride(0)
-        packed = len(shape) == 2 and (per == 1 or grads.stride(-1) == 1)
+        per = given = stride = 0
+        packed = False
     if not packed or given != M or per < vocab * dim:
         raise ValueError(f"grads must be [{M}, >= {vocab * dim}] or [{M}, {vocab}, {dim}], contiguous within a worker")
     bad = None if opt_bad_count is None else _ptr(opt_bad_count, torch.int32, 1, "opt_bad_count")
