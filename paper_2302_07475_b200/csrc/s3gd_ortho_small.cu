@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
       mma_commit_elect(smem_addr(&sh->done));
     }
     __syncwarp();
-    ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->done), phase)) && ok;
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_addr(&sh->done), phase));   // a warp that gave up keeps to the barriers
     phase ^= 1;
     tcgen05_fence_after();
   };
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
       tmem_load_wait();
     }
   };
-  for (int step = 0; step < P.steps && ok; ++step) {
+  for (int step = 0; step < P.steps; ++step) {
     const bool split = step < P.split;
     float acc[16];
     product(xa, xa, false, m16 * 16, n16, split);
@@ -239,6 +239,7 @@ __global__ void __launch_bounds__(kSmallThreads, 512 / kSmallThreads) small_kern
         } else {
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] *= 1.f / kScaleX;
+          if (!ok) continue;
           if (P.store.dtype == S3GD_F32) put8<float>(P.store, mat, i, j, P.m, P.n, x);
           else put8<__nv_bfloat16>(P.store, mat, i, j, P.m, P.n, x);
         }
