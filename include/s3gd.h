@@ -372,7 +372,8 @@ typedef struct s3gd_matrix {
  *                     of one (11 bits): 0..steps, or -1: all, which is what fp32 products give.  A third of the products and
  *                     about 1e-3 (in the norm) off with 0, for callers to whom a bf16 update of that accuracy is enough
  *  ws           >= s3gd_orthogonalise_workspace_bytes(batch, rows, cols), 256-byte aligned, not preserved
- * Sums are held in 32 bits, norms in 64.  s3gd_device_status(ws) reports a kernel that gave up (S3GD_ERR_INTERNAL).
+ * Sums are held in 32 bits, norms in 64.  Entries of Y_0 below 2^-34 (6e-11) count as zero: where |G| << eps, all of them may.
+ * s3gd_device_status(ws) reports a kernel that gave up (S3GD_ERR_INTERNAL).
  * Limits: 1 <= batch <= 65535, rows and cols < 2^24, batch * rows * cols <= 10^12.
  */
 S3GD_API size_t s3gd_orthogonalise_workspace_bytes(int batch, uint64_t rows, uint64_t cols);

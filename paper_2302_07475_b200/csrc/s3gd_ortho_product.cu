@@ -7,8 +7,9 @@
 // One kernel per product.  Operands are fp16 tiles brought by TMA into slots; one thread issues tcgen05.mma with fp32 sums in
 // tensor memory, two sums in turn, and eight warps take the sums out and finish the tile.  wide_kernel: two CTAs share a
 // 256 x 256 tile (cta_group::2), each with half of either operand, and go from tile to tile, so that the epilogue of one runs
-// under the products of the next.  narrow_kernel, where there are fewer tiles than SMs: 128 x 128 tiles, each by a cluster of
-// up to eight CTAs that share out k and join their sums through distributed shared memory.
+// under the products of the next.  narrow_kernel: 128 x 128 tiles, each by a cluster of up to eight CTAs that share out k and
+// join their sums through distributed shared memory.  launch_product's model of their times chooses, in effect the second where
+// its tiles are fewer than SMs.
 //
 // Precision.  Two fp16 pieces per entry (kSplit, 22 bits): hi hi + hi lo + lo hi, three products.  Or, in steps for which the
 // caller asks for it, one (11 bits).
@@ -16,12 +17,13 @@
 // diagonal of S); with two pieces the sum is therefore taken out of tensor memory every kChunk slots of k and added in
 // registers, and the small products go first.
 //
-// Bounds.  Large: the tensor cores under the power cap; 8192 x 8192 bf16 runs five steps in 9.0 to 10.1 ms, 1.09 to 1.22 PFLOP/s
-// of m^2 n + m^3 + 2 m^2 n operations a step (a plain bf16 product of the library sustains 1.37 here), fp32 results 28 ms with
-// three times the products.  Tiles of a last round that fill half of it or less are cut in two (4 x 2048 x 2048 fp32: 2.09 ->
-// 1.99 ms); a last round between half and full is lost time.  Middle: the chain of kernels; a
-// product of 1024 x 1024 takes 9 us, of which 1.3 pass between two kernels, 1.5 until the first operands arrive, 3 to 5 in the
-// products (bound by L2: 64 KB per CTA and 64 entries of k, 12.6 TB/s over 128 CTAs with two pieces) and 3 in the epilogue.
+// Bounds.  Large: the tensor cores under the power cap; 8192 x 8192 runs five steps in 28.9 to 30.4 ms, 1.08 to 1.14 PFLOP/s of
+// three products for each of the m^2 n + m^3 + 2 m^2 n operations a step (a plain bf16 product of the library sustains 1.37 here;
+// the tensor pipes are active 64 to 67 % of the cycles at 4096 x 4096); with one piece 9.2 to 10.1 ms.  Tiles of a last round
+// that fill half of it or less are cut in two (4 x 2048 x 2048 fp32: 2.09 -> 1.99 ms); a last round between half and full is
+// lost time.  Middle: the chain of kernels; a product of 1024 x 1024 takes 12 to 13 us, of which 1.3 pass between two kernels, 1.5
+// until the first operands arrive, 5 in the products (bound by L2: 64 KB per CTA and 64 entries of k, 12.6 TB/s over 128 CTAs)
+// and 3 to 4 in the epilogue; with one piece 9 us.
 #include <atomic>
 
 #include "s3gd_ortho.cuh"
@@ -609,6 +611,13 @@ int clusters_at_a_time(void (*kernel)(ProductArgs), int ways, int* cached) {
 // the measured times.  A slot of k takes two units for each product of pieces in either kernel (the wide one does four times the
 // work in it, on two SMs).  On top come, for every wave of narrow tiles, its start, first loads and epilogue, the pieces that a
 // warp finishes, and the joining of parts of k; for the wide kernel, whose epilogues run under products, the start and the last.
+// Five steps in us with the choice left to the model | all products wide | narrow with 1, 2, 4, 8 CTAs to a tile, two pieces:
+//   256 x 256      109 |  172 |  154  121  108  108        2731 x 1000      367 |  540 |  502  389  537  852
+//   512 x 512      123 |  253 |  200  147  123  164        2048 x 2048      629 |  637 |  635  760 1089 1870
+//   512 x 4608     184 |  516 |  421  309  333  515        3000 x 3000     1986 | 2085 | 2488 2614 3139 4936
+//   1024 x 1024    196 |  351 |  286  197  281  472        12 x 600 x 900   613 |  613 |  705  805 1275 2499
+// It takes several waves of narrow tiles for slower than they are where there are two: 1500 x 1500 runs in 469 (wide) and would
+// in 382 (narrow, one CTA), 30 x 300 x 300 in 447 and 335.
 constexpr int kSlotUnits = 2, kNarrowStart = 40, kWideStart = 76;
 constexpr int kJoinUnits[4] = {0, 3, 5, 14};
 

@@ -3,7 +3,8 @@
 // both ways: rows of 64 entries in 128 swizzled bytes serve as K-major operand for X X^T and S S^T and as MN-major operand for
 // B X.  A step is three products, each followed by all sixteen warps taking the sums out of tensor memory and writing the next
 // operand in place.  The chain of these, not bytes or operations, is what the time is made of: 32 matrices of 64 x 128 fp32 take
-// 31 us (2 MB, 0.9 GFLOP), about 5 us a step of three products; 16 x 16 still 20 us.
+// 31 us (2 MB, 0.9 GFLOP), about 5 us a step of three products; 16 x 16 still 19 us, from a CUDA graph too (the host's part of a
+// call, 15 us, runs beside it).
 #include "s3gd_ortho.cuh"
 #include "s3gd_tcgen05.cuh"
 
