@@ -339,8 +339,9 @@ S3GD_API s3gd_status s3gd_majority_vote_noalloc(const uint32_t* idx, const uint3
 
 /*
  * Operators for the parameters of a language model that is trained with the calls above: its matrices
- * (orthogonalised updates, which take the workers' vote or any other gradient) and its embedding table
- * (lookup, and the gradient that a worker's row of `grads` holds for it).
+ * (orthogonalised updates, which take the workers' vote or any other gradient), its embedding table
+ * (lookup, and the gradient that a worker's row of `grads` holds for it), its layer norms (forward, and backward with the
+ * weights' gradients in the workers' rows) and the workers' gradients as a whole (norm over all tensors, clipping).
  *
  * Element types.  Every tensor argument names its own; which are accepted stands at each call.
  */
@@ -428,6 +429,84 @@ S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t d
                                      const void* ids, int ids_dtype, int M, uint64_t T, uint64_t vocab, uint64_t dim,
                                      float scale, void* grads, int grads_dtype, int64_t grads_stride, int accumulate,
                                      uint32_t* opt_bad_count, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Layer norm of M workers' rows of `dim` entries, with the sum of a residual stream taken on the way:
+ *     total = x + add, rounded to x's type (without opt_add: total is x),
+ *     y = (total - mean) / sqrt(variance + eps) * weight + bias,
+ * mean and variance (divided by dim) over the dim entries of a row; opt_weight NULL: ones, opt_bias NULL: zeros.
+ * A row whose id is negative is an empty place (as in s3gd_embed): its rows of y and total are zero, whatever x and add hold.
+ *
+ *  x, add, total  [M x T x dim] F32 or BF16, one type; *_stride elements from token to token, *_worker_stride from worker to
+ *                 worker (only read where there are several).  opt_add and opt_total come together
+ *  opt_weight, opt_bias  [dim], both param_dtype: F32 or BF16
+ *  opt_ids        [M x T] I32 or I64 (ids_dtype; any of the two where opt_ids is NULL)
+ *  y              [M x T x dim] F32 or BF16.  y may be x itself, total may be x or add itself (same type and strides); outputs
+ *                 otherwise overlap nothing.  An input's stride may be 0: the same row repeated
+ * An Inf or NaN makes its own row NaN.  Sums, mean and variance are held in 32 bits or more and rows far from zero keep their digits;
+ * entries beyond about 1e18 in magnitude, whose squares pass fp32's range, are not provided for.
+ * T may be 0.  Limits: M <= 65535, M * T < 2^31, dim < 2^24, 0 <= eps < Inf.
+ */
+S3GD_API s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_add,
+                                     int64_t add_stride, int64_t add_worker_stride, void* opt_total, int64_t total_stride,
+                                     int64_t total_worker_stride, const void* opt_weight, const void* opt_bias, int param_dtype,
+                                     const void* opt_ids, int ids_dtype, int M, uint64_t T, uint64_t dim, float eps, void* y,
+                                     int y_dtype, int64_t y_stride, int64_t y_worker_stride, void* stream);
+
+/*
+ * Gradient of s3gd_layer_norm, with each worker's gradient of weight and bias in its own row of the gradient buffer.  With
+ * xhat = (x - mean) / sqrt(variance + eps), computed again from x, and g = dy * weight:
+ *     dx = (g - mean(g) - xhat * mean(g * xhat)) / sqrt(variance + eps) + dtotal
+ *     dweight[m][j] = sum over t of dy[m][t][j] * xhat[m][t][j],   dbias[m][j] = sum over t of dy[m][t][j]
+ *
+ *  dy         [M x T x dim] F32 or BF16, the gradient of y
+ *  x          [M x T x dim] F32 or BF16, what was normalised (total, where there was one)
+ *  opt_dtotal [M x T x dim] of x's type: gradient that reaches the sum from elsewhere, or NULL; needs opt_dx
+ *  opt_weight [dim] F32 or BF16, or NULL: ones
+ *  opt_ids    as above: empty places have zero rows in dx and give nothing to the weights, whatever dy, x and dtotal hold
+ *  opt_dx     [M x T x dim] of x's type, or NULL; may be dy, x or dtotal itself (same type and strides)
+ *  opt_dweight, opt_dbias  F32 or BF16, dim entries per worker, grads_stride elements from worker to worker (>= dim); either may
+ *             be NULL.  Every entry is written; with accumulate != 0 the sum is added to what is there (one rounding)
+ *  ws         >= s3gd_layer_norm_grad_workspace_bytes(M, T, dim), 256-byte aligned, not preserved; one for larger numbers serves
+ *             smaller ones
+ * Sums over tokens are taken in an order that depends on the sizes alone.  T may be 0.  Limits as for s3gd_layer_norm.
+ */
+S3GD_API size_t s3gd_layer_norm_grad_workspace_bytes(int M, uint64_t T, uint64_t dim);
+S3GD_API s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_t dy_stride, int64_t dy_worker_stride, const void* x,
+                                          int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_dtotal,
+                                          int64_t dtotal_stride, int64_t dtotal_worker_stride, const void* opt_weight,
+                                          int weight_dtype, const void* opt_ids, int ids_dtype, int M, uint64_t T, uint64_t dim,
+                                          float eps, void* opt_dx, int64_t dx_stride, int64_t dx_worker_stride, void* opt_dweight,
+                                          void* opt_dbias, int grads_dtype, int64_t grads_stride, int accumulate, void* ws,
+                                          size_t ws_bytes, void* stream);
+
+/*
+ * The norm of each worker's gradients over a list of tensors, and clipping by it:
+ *     norm[m] = sqrt(sum over tensors i and entries j of data_i[m][j]^2)
+ *     c[m] = 1 where norm[m] + eps <= max_norm, else max_norm / (norm[m] + eps);   out_i[m][j] = c[m] * data_i[m][j], rounded
+ *
+ * parts (host, read before the call returns): `count` tensors, each `n` entries per worker in one piece, `stride` elements from
+ * worker to worker (only read for M > 1; 0: the same for all).  out may be data itself (same type and stride: in place, and rows
+ * that need no clipping are not written) or overlaps no tensor of the call, e.g. the tensor's columns of the workers' rows of a
+ * gradient buffer.  s3gd_grad_norm reads neither out nor out_dtype.  Tensors with n = 0 and an empty list are allowed.
+ *
+ *  out_norm  dev  [M] fp32        ws  >= s3gd_clip_workspace_bytes(M), 256-byte aligned, not preserved
+ * Squares are summed in 64 bits, c is rounded to 32: entries at either end of fp32's range count as they should.  A worker that holds a NaN has norm and
+ * outputs NaN; one that holds an Inf has norm Inf and c = 0, so that its infinite entries become NaN and the others 0.  Results depend on
+ * the sizes alone, not on the run.  Limits: 1 <= M <= 65535, n < 2^40, 0 <= max_norm < Inf, 0 <= eps < Inf.
+ */
+typedef struct s3gd_part {
+  const void* data; /* F32 or BF16, aligned to its type */
+  void* out;
+  uint64_t n;
+  int64_t stride, out_stride; /* out_stride >= n */
+  int dtype, out_dtype;       /* s3gd_dtype */
+} s3gd_part;
+S3GD_API size_t s3gd_clip_workspace_bytes(int M);
+S3GD_API s3gd_status s3gd_grad_norm(const s3gd_part* parts, int count, int M, float* out_norm, void* ws, size_t ws_bytes,
+                                    void* stream);
+S3GD_API s3gd_status s3gd_clip(const s3gd_part* parts, int count, int M, float max_norm, float eps, float* out_norm, void* ws,
+                               size_t ws_bytes, void* stream);
 
 /*
  * Measurement aid (the paper reports no timings; this has no counterpart there).

@@ -13,4 +13,6 @@ from .binding import (  # noqa: F401
     s3gd_sparse_workspace_bytes, s3gd_encode_vote_sparse, s3gd_apply_vote_sparse,
     alloc_embed_workspace, alloc_ortho_workspace, s3gd_embed, s3gd_embed_grad, s3gd_embed_grad_workspace_bytes,
     s3gd_orthogonalise, s3gd_orthogonalise_workspace_bytes, s3gd_step_ortho,
+    alloc_clip_workspace, alloc_layer_norm_workspace, s3gd_clip, s3gd_clip_workspace_bytes, s3gd_grad_norm,
+    s3gd_layer_norm, s3gd_layer_norm_grad, s3gd_layer_norm_grad_workspace_bytes,
 )

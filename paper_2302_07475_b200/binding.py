@@ -7,6 +7,7 @@ dtype the call raises -- there is no CPU fallback.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Optional
@@ -30,7 +31,8 @@ EXPORTS = ("s3gd_status_string", "s3gd_workspace_bytes", "s3gd_topk_sign", "s3gd
            "s3gd_debug_topk_sign", "s3gd_debug_step", "s3gd_vote_apply", "s3gd_vote_counts", "s3gd_encode_vote2",
            "s3gd_apply_vote2", "s3gd_sparse_workspace_bytes", "s3gd_encode_vote_sparse", "s3gd_apply_vote_sparse",
            "s3gd_profile_begin_filter_every", "s3gd_orthogonalise_workspace_bytes", "s3gd_orthogonalise", "s3gd_step_ortho",
-           "s3gd_embed", "s3gd_embed_grad_workspace_bytes", "s3gd_embed_grad")
+           "s3gd_embed", "s3gd_embed_grad_workspace_bytes", "s3gd_embed_grad", "s3gd_layer_norm",
+           "s3gd_layer_norm_grad_workspace_bytes", "s3gd_layer_norm_grad", "s3gd_clip_workspace_bytes", "s3gd_grad_norm", "s3gd_clip")
 
 
 class S3gdError(RuntimeError):
@@ -129,6 +131,19 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.s3gd_embed_grad_workspace_bytes.argtypes = [i32, u64, u64, u64]
     lib.s3gd_embed_grad.restype = i32
     lib.s3gd_embed_grad.argtypes = [vp, i32, i64, i64, vp, i32, i32, u64, u64, u64, f32, vp, i32, i64, i32, vp, vp, sz, vp]
+    lib.s3gd_layer_norm.restype = i32
+    lib.s3gd_layer_norm.argtypes = [vp, i32, i64, i64, vp, i64, i64, vp, i64, i64, vp, vp, i32, vp, i32, i32, u64, u64, f32, vp, i32, i64, i64, vp]
+    lib.s3gd_layer_norm_grad_workspace_bytes.restype = sz
+    lib.s3gd_layer_norm_grad_workspace_bytes.argtypes = [i32, u64, u64]
+    lib.s3gd_layer_norm_grad.restype = i32
+    lib.s3gd_layer_norm_grad.argtypes = [vp, i32, i64, i64, vp, i32, i64, i64, vp, i64, i64, vp, i32, vp, i32, i32, u64, u64, f32, vp, i64, i64,
+                                         vp, vp, i32, i64, i32, vp, sz, vp]
+    lib.s3gd_clip_workspace_bytes.restype = sz
+    lib.s3gd_clip_workspace_bytes.argtypes = [i32]
+    lib.s3gd_grad_norm.restype = i32
+    lib.s3gd_grad_norm.argtypes = [vp, i32, i32, vp, vp, sz, vp]
+    lib.s3gd_clip.restype = i32
+    lib.s3gd_clip.argtypes = [vp, i32, i32, f32, f32, vp, vp, sz, vp]
     if path is None:
         _lib = lib
     return lib
@@ -693,3 +708,280 @@ def s3gd_embed_grad(dout: torch.Tensor, ids: torch.Tensor, grads: torch.Tensor, 
             code = load().s3gd_embed_grad(*args, _stream_of(index))
     if code:
         _check("s3gd_embed_grad", code)
+
+
+def _norm_shape(x: torch.Tensor):
+    """(M, T, dim) of rows [T, dim] or [M, T, dim], or of any contiguous [..., dim]."""
+    shape = x.shape
+    if len(shape) == 2:
+        return 1, shape[0], shape[1]
+    if len(shape) == 3:
+        return shape
+    if len(shape) == 0:
+        raise ValueError("x must be [..., dim]")
+    return 1, x.numel() // shape[-1] if shape[-1] else 0, shape[-1]
+
+
+def _norm_strides(t: Optional[torch.Tensor], like: torch.Tensor, name: str):
+    """Elements from row to row and from worker to worker; (0, 0) where the tensor is not given."""
+    if t is None:
+        return 0, 0
+    shape = t.shape
+    if shape != like.shape:
+        raise ValueError(f"{name} has shape {tuple(shape)}, needs {tuple(like.shape)}")
+    if t.is_contiguous():
+        return shape[-1], shape[-1] * shape[-2] if len(shape) > 2 else 0
+    if len(shape) not in (2, 3):
+        raise ValueError(f"{name} must be contiguous, or [T, dim] or [M, T, dim]")
+    _rows(t, _REAL, name)
+    return t.stride(-2), t.stride(0) if len(shape) == 3 else 0
+
+
+def _norm_device(index: int, **tensors: Optional[torch.Tensor]):
+    """Checks that the tensors given are CUDA tensors on one device, of types that the calls take."""
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not (isinstance(t, torch.Tensor) and t.is_cuda):
+            raise TypeError(f"{name} must be a CUDA tensor")
+        if t.get_device() != index:
+            raise TypeError(f"{name} must be on the device of the others, cuda:{index}, not on {t.device}")
+
+
+def _norm_ids(ids: Optional[torch.Tensor], like: torch.Tensor):
+    if ids is None:
+        return None, 3
+    _ids(ids)
+    if ids.shape != like.shape[:-1]:
+        raise ValueError(f"ids has shape {tuple(ids.shape)}, needs {tuple(like.shape[:-1])}")
+    return ids.data_ptr(), _INDEX_CODES[ids.dtype]
+
+
+def _param(t: Optional[torch.Tensor], dim: int, name: str):
+    if t is None:
+        return None
+    if t.dim() != 1 or t.shape[0] != dim or (dim > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be [{dim}], contiguous")
+    return t.data_ptr()
+
+
+def s3gd_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                    eps: float = 1e-5, ids: Optional[torch.Tensor] = None, add: Optional[torch.Tensor] = None,
+                    total: Optional[torch.Tensor] = None) -> None:
+    """y[..., :] <- layer norm of x[..., :], or of total <- x + add where add and total are given.
+
+    x, y (and add, total) are [T, dim] or [M, T, dim] with contiguous rows, or contiguous [..., dim]; fp32 or bf16, add and total
+    of x's type.  ids (shape of x without its last axis): rows whose id is negative become zero."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda):
+        raise TypeError("x must be a CUDA tensor")
+    index = x.get_device()
+    _norm_device(index, y=y, weight=weight, bias=bias, ids=ids, add=add, total=total)
+    try:
+        xd, yd = _REAL_CODES[x.dtype], _REAL_CODES[y.dtype]
+        pd = 0 if weight is None and bias is None else _REAL_CODES[(bias if weight is None else weight).dtype]
+    except KeyError:
+        for t, name in ((x, "x"), (y, "y"), (weight, "weight"), (bias, "bias")):
+            _of(t, _REAL, name)
+    if weight is not None and bias is not None and weight.dtype != bias.dtype:
+        raise TypeError(f"weight and bias must have one dtype, not {weight.dtype} and {bias.dtype}")
+    if (add is None) != (total is None):
+        raise ValueError("add and total come together")
+    _of(add, (x.dtype,), "add")
+    _of(total, (x.dtype,), "total")
+    M, T, dim = _norm_shape(x)
+    xs, xw = _norm_strides(x, x, "x")
+    ys, yw = _norm_strides(y, x, "y")
+    as_, aw = _norm_strides(add, x, "add")
+    ts, tw = _norm_strides(total, x, "total")
+    idp, idt = _norm_ids(ids, x)
+    args = (x.data_ptr(), xd, xs, xw, None if add is None else add.data_ptr(), as_, aw, None if total is None else total.data_ptr(), ts, tw,
+            _param(weight, dim, "weight"), _param(bias, dim, "bias"), pd, idp, idt, M, T, dim, eps, y.data_ptr(), yd, ys, yw)
+    if _current_device() == index:
+        code = load().s3gd_layer_norm(*args, _stream_of(index))
+    else:
+        with _on(x):
+            code = load().s3gd_layer_norm(*args, _stream_of(index))
+    if code:
+        _check("s3gd_layer_norm", code)
+
+
+def s3gd_layer_norm_grad_workspace_bytes(M: int, T: int, dim: int) -> int:
+    return int(load().s3gd_layer_norm_grad_workspace_bytes(int(M), int(T), int(dim)))
+
+
+def alloc_layer_norm_workspace(M: int, T: int, dim: int, device="cuda") -> torch.Tensor:
+    """A uint8 CUDA tensor for s3gd_layer_norm_grad of M workers with T rows of dim each."""
+    n = s3gd_layer_norm_grad_workspace_bytes(M, T, dim)
+    if n == 0:
+        raise ValueError("invalid (M, T, dim)")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _worker_rows(t: Optional[torch.Tensor], M: int, dim: int, several: bool, name: str):
+    """Elements from worker to worker of a gradient [M, dim] (or [dim] for one worker)."""
+    if t is None:
+        return None, 0
+    shape = t.shape
+    if shape == (M, dim):
+        stride = t.stride(0)
+    elif shape == (dim,) and not several:
+        stride = dim
+    else:
+        raise ValueError(f"{name} has shape {tuple(shape)}, needs {(M, dim)}" + ("" if several else f" or {(dim,)}"))
+    if dim > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name} must be contiguous along its last axis")
+    return t.data_ptr(), stride if M > 1 else dim
+
+
+def s3gd_layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, dx: Optional[torch.Tensor], weight: Optional[torch.Tensor],
+                         dweight: Optional[torch.Tensor], dbias: Optional[torch.Tensor], ws: torch.Tensor, eps: float = 1e-5,
+                         ids: Optional[torch.Tensor] = None, dtotal: Optional[torch.Tensor] = None, accumulate: bool = False) -> None:
+    """Gradient of s3gd_layer_norm: dx (+ dtotal), and each worker's gradient of weight and bias.
+
+    dy, x, dx, dtotal are [T, dim] or [M, T, dim]; x is what was normalised (total, where there was one); dx and dtotal have its
+    type.  dweight and dbias are [M, dim] (columns of the workers' rows of a gradient buffer) or [dim] for one worker, of one
+    type; accumulate adds to what they hold.  dx, or dweight and dbias, may be None; dx may be dy, x or dtotal itself."""
+    if not (isinstance(x, torch.Tensor) and x.is_cuda):
+        raise TypeError("x must be a CUDA tensor")
+    index = x.get_device()
+    w = _ptr(ws, torch.uint8, name="ws")
+    _norm_device(index, dy=dy, dx=dx, weight=weight, dweight=dweight, dbias=dbias, ws=ws, ids=ids, dtotal=dtotal)
+    given = dbias if dweight is None else dweight
+    try:
+        dyd, xd = _REAL_CODES[dy.dtype], _REAL_CODES[x.dtype]
+        wd = 0 if weight is None else _REAL_CODES[weight.dtype]
+        gd = 0 if given is None else _REAL_CODES[given.dtype]
+    except KeyError:
+        for t, name in ((dy, "dy"), (x, "x"), (weight, "weight"), (dweight, "dweight"), (dbias, "dbias")):
+            _of(t, _REAL, name)
+    if dweight is not None and dbias is not None and dweight.dtype != dbias.dtype:
+        raise TypeError(f"dweight and dbias must have one dtype, not {dweight.dtype} and {dbias.dtype}")
+    _of(dx, (x.dtype,), "dx")
+    _of(dtotal, (x.dtype,), "dtotal")
+    if x.dim() not in (2, 3):
+        raise ValueError("x must be [T, dim] or [M, T, dim]")
+    if dx is None and (given is None or dtotal is not None):
+        raise ValueError("dx must be given" + (" with dtotal" if dtotal is not None else ", or dweight or dbias"))
+    M, T, dim = _norm_shape(x)
+    xs, xw = _norm_strides(x, x, "x")
+    ds, dw = _norm_strides(dy, x, "dy")
+    os, ow = _norm_strides(dx, x, "dx")
+    ts, tw = _norm_strides(dtotal, x, "dtotal")
+    idp, idt = _norm_ids(ids, x)
+    wp, stride = _worker_rows(dweight, M, dim, x.dim() == 3, "dweight")
+    bp, bstride = _worker_rows(dbias, M, dim, x.dim() == 3, "dbias")
+    if dweight is not None and dbias is not None and stride != bstride:
+        raise ValueError(f"dweight and dbias must have one distance from worker to worker, not {stride} and {bstride}")
+    args = (dy.data_ptr(), dyd, ds, dw, x.data_ptr(), xd, xs, xw, None if dtotal is None else dtotal.data_ptr(), ts, tw,
+            _param(weight, dim, "weight"), wd, idp, idt, M, T, dim, eps, None if dx is None else dx.data_ptr(), os, ow, wp, bp, gd,
+            stride or bstride, accumulate, w, ws.numel())
+    if _current_device() == index:
+        code = load().s3gd_layer_norm_grad(*args, _stream_of(index))
+    else:
+        with _on(x):
+            code = load().s3gd_layer_norm_grad(*args, _stream_of(index))
+    if code:
+        _check("s3gd_layer_norm_grad", code)
+
+
+def s3gd_clip_workspace_bytes(M: int) -> int:
+    return int(load().s3gd_clip_workspace_bytes(int(M)))
+
+
+def alloc_clip_workspace(M: int = 1, device="cuda") -> torch.Tensor:
+    """A uint8 CUDA tensor for s3gd_grad_norm and s3gd_clip of M workers, whatever their tensors."""
+    n = s3gd_clip_workspace_bytes(M)
+    if n == 0:
+        raise ValueError("invalid M")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _in_one_piece(shape, strides) -> bool:
+    """Whether the entries fill one piece of memory, in whatever order of axes."""
+    expected = 1
+    for stride, size in sorted(zip(strides, shape)):
+        if size != 1:
+            if stride != expected:
+                return False
+            expected *= size
+    return True
+
+
+def _parts(grads, out, index: int, M: int, several: bool):
+    """The tensors as an array of s3gd_part, and their number."""
+    if isinstance(grads, torch.Tensor):
+        grads, out = (grads,), (out,) if isinstance(out, torch.Tensor) else out
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
+    packed, first = array.array("Q"), 1 if several else 0
+    for i, (g, o) in enumerate(zip(grads, outs)):
+        try:
+            if g.get_device() != index or o.get_device() != index:
+                raise TypeError(f"tensors of one call must be on one device: gradient {i} or its output is not on cuda:{index}")
+            code = _REAL_CODES[g.dtype] | _REAL_CODES[o.dtype] << 32
+        except (AttributeError, KeyError):
+            for t in (g, o):
+                if not (isinstance(t, torch.Tensor) and t.is_cuda):
+                    raise TypeError(f"gradient {i} and its output must be CUDA tensors") from None
+                _of(t, _REAL, f"gradient {i} or its output")
+        shape = g.shape
+        if several and (len(shape) == 0 or shape[0] != M):
+            raise ValueError(f"gradient {i} has shape {tuple(shape)}, needs {M} workers in front")
+        n = g.numel() // M
+        if n == 0:
+            continue
+        strides = g.stride()
+        if not g.is_contiguous() and not _in_one_piece(shape[first:], strides[first:]):
+            raise ValueError(f"gradient {i} is not in one piece" + (" within a worker" if several else ""))
+        out_strides = strides
+        if o is not g:
+            out_strides = o.stride()
+            if o.shape != shape:
+                raise ValueError(f"output {i} has shape {tuple(o.shape)}, needs {tuple(shape)}")
+            if out_strides[first:] != strides[first:] and any(a != b and s != 1 for a, b, s in zip(out_strides[first:], strides[first:], shape[first:])):
+                raise ValueError(f"output {i} does not lie like its gradient: strides {out_strides} and {strides}")
+        packed.extend((g.data_ptr(), o.data_ptr(), n, strides[0] if several else 0, out_strides[0] if several else 0, code))
+    return packed, len(packed) // 6
+
+
+def _norms(norm: torch.Tensor):
+    if not (isinstance(norm, torch.Tensor) and norm.is_cuda and norm.dtype == torch.float32 and norm.dim() <= 1 and norm.is_contiguous()):
+        raise TypeError("norm must be a contiguous CUDA tensor of dtype float32, [] or [M]")
+    several = norm.dim() == 1
+    if norm.numel() == 0:
+        raise ValueError("norm must have an entry for each of at least one worker")
+    return norm.get_device(), norm.numel(), several
+
+
+def s3gd_grad_norm(grads, norm: torch.Tensor, ws: torch.Tensor) -> None:
+    """norm <- the norm over all entries of the tensors in grads (one tensor, or a sequence).
+
+    norm is fp32: [] for one norm over everything, or [M] for one per worker, where every tensor's first axis is the M workers.
+    Tensors are fp32 or bf16, each in one piece (within a worker)."""
+    index, M, several = _norms(norm)
+    packed, count = _parts(grads, None, index, M, several)
+    w = _ptr(ws, torch.uint8, name="ws")
+    if ws.get_device() != index:
+        raise TypeError(f"ws must be on the device of norm, {norm.device}")
+    args = (packed.buffer_info()[0] if count else None, count, M, norm.data_ptr(), w, ws.numel())
+    with _on(norm):
+        code = load().s3gd_grad_norm(*args, _stream_of(index))
+    _check("s3gd_grad_norm", code)
+
+
+def s3gd_clip(grads, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, out=None, eps: float = 1e-6) -> None:
+    """out <- grads * min(1, max_norm / (norm + eps)), norm as s3gd_grad_norm gives it; per worker where norm is [M].
+
+    out (None: in place) has a tensor for each of grads, of the same shape and order of axes, fp32 or bf16: e.g. the columns of a
+    gradient buffer, out[i] = rows[:, a:b].view_as(grads[i]).  Outputs overlap no other tensor of the call."""
+    index, M, several = _norms(norm)
+    packed, count = _parts(grads, out, index, M, several)
+    w = _ptr(ws, torch.uint8, name="ws")
+    if ws.get_device() != index:
+        raise TypeError(f"ws must be on the device of norm, {norm.device}")
+    args = (packed.buffer_info()[0] if count else None, count, M, max_norm, eps, norm.data_ptr(), w, ws.numel())
+    with _on(norm):
+        code = load().s3gd_clip(*args, _stream_of(index))
+    _check("s3gd_clip", code)

@@ -14,7 +14,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libs3gd.so")
 SOURCES = ["s3gd_api.cu", "s3gd_vote.cu", "s3gd_signplane.cu", "s3gd_filter.cu", "s3gd_select.cu", "s3gd_select_small.cu", "s3gd_noalloc.cu", "s3gd_randk.cu", "s3gd_exchange.cu",
-           "s3gd_ortho.cu", "s3gd_ortho_product.cu", "s3gd_ortho_small.cu", "s3gd_embed.cu"]
+           "s3gd_ortho.cu", "s3gd_ortho_product.cu", "s3gd_ortho_small.cu", "s3gd_embed.cu", "s3gd_layer_norm.cu", "s3gd_clip.cu"]
 HEADERS = ["s3gd_common.cuh", "s3gd_opt_in.h", "s3gd_tile.cuh", "s3gd_select_emit.inl", "s3gd_ops.cuh", "s3gd_ortho.cuh", "s3gd_tcgen05.cuh"]
 
 

@@ -1,0 +1,277 @@
+// The norm of each worker's gradients over many tensors, and clipping by it (see include/s3gd.h).
+//
+//     norm[m] = sqrt(sum over tensors i and entries j of g_i[m][j]^2),   c[m] = min(1, max_norm / (norm[m] + eps)),
+//     out_i[m][j] = c[m] g_i[m][j].
+//
+// The tensors' addresses and sizes travel as the kernels' arguments (no copy to the device, nothing that a captured graph would
+// have to keep alive), in groups where there are very many.  Each worker's tensors are cut into tiles of 8192 entries that begin on 16-byte boundaries; a CTA sums
+// a run of tiles in 64 bits and writes one partial sum.  Whoever needs the norm adds the worker's partial sums in ascending
+// order: no atomics, and the result depends on the sizes alone.
+#include "s3gd_ops.cuh"
+
+namespace s3gd {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr uint32_t kTile = 8192;                   // entries of a tile
+constexpr int kFewParts = 64, kMostParts = 640;    // tensors of one launch: kernel arguments of up to 32 KB
+constexpr uint32_t kRunsAll = 2368, kRunsEach = 128;  // partial sums over all workers, and of each worker, at least
+
+struct Part {
+  const void* src;
+  void* dst;
+  uint64_t n;
+  long long src_worker, dst_worker;
+  uint32_t first_tile;
+  uint32_t src_bf16 : 1, dst_bf16 : 1, in_place : 1;
+};
+struct ClipArgs {
+  double* partial;     // [M x runs]
+  float* norm;
+  uint32_t* hdr;
+  uint32_t count, tiles, per, runs, add, sum_only;
+  float max_norm, eps;
+};
+template <int kMax> struct Parts { Part p[kMax]; };
+
+template <int kMax>
+__device__ __forceinline__ uint32_t part_of(const Parts<kMax>& parts, uint32_t count, uint32_t tile) {
+  uint32_t lo = 0, hi = count;
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (parts.p[mid].first_tile <= tile) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// entries of a 16-byte access, and how many entries the address lies behind such a boundary
+template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
+template <typename T>
+__device__ __forceinline__ uint32_t behind(const T* p, int v) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) % v; }
+
+template <typename T>
+__device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t tile) {
+  constexpr int kVec = kWide<T>;
+  const long long begin = (long long)tile * kTile - behind(g, kVec);
+  double sum = 0;
+#pragma unroll
+  for (uint32_t i = 0; i < kTile / (kThreads * kVec); ++i) {
+    const long long at = begin + (i * kThreads + threadIdx.x) * kVec;
+    if (at >= 0 && (uint64_t)at + kVec <= n) {
+      const Pack<T, kVec> v = *reinterpret_cast<const Pack<T, kVec>*>(g + at);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) { const double d = to_f32(v.v[e]); sum += d * d; }
+    } else {
+      for (int e = 0; e < kVec; ++e)
+        if (at + e >= 0 && (uint64_t)(at + e) < n) { const double d = to_f32(g[at + e]); sum += d * d; }
+    }
+  }
+  return sum;
+}
+
+// the CTA's sum, in every thread
+__device__ __forceinline__ double cta_sum(double v) {
+  __shared__ double room[kWarps];
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  __syncthreads();
+  if (lane_id() == 0) room[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0;
+  for (int w = 0; w < kWarps; ++w) v += room[w];
+  return v;
+}
+__device__ __forceinline__ double norm_of(const ClipArgs& a, uint32_t m) {
+  double sum = 0;
+  for (uint32_t i = threadIdx.x; i < a.runs; i += kThreads) sum += a.partial[(size_t)m * a.runs + i];
+  return sqrt(cta_sum(sum));
+}
+
+// blockIdx.x: run of tiles, blockIdx.y: worker
+template <int kMax>
+__global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a) {
+  grid_dependency_wait();
+  const uint32_t m = blockIdx.y, begin = blockIdx.x * a.per, end = min(begin + a.per, a.tiles);
+  double sum = 0;
+  uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
+  for (uint32_t tile = begin; tile < end; ++tile) {
+    while (k + 1 < a.count && parts.p[k + 1].first_tile <= tile) ++k;
+    const Part& p = parts.p[k];
+    const uint32_t in = tile - p.first_tile;
+    sum += p.src_bf16 ? tile_squares(static_cast<const __nv_bfloat16*>(p.src) + m * p.src_worker, p.n, in)
+                      : tile_squares(static_cast<const float*>(p.src) + m * p.src_worker, p.n, in);
+  }
+  sum = cta_sum(sum);
+  double* to = a.partial + (size_t)m * a.runs + blockIdx.x;
+  if (threadIdx.x == 0) *to = a.add ? *to + sum : sum;
+}
+
+__global__ void __launch_bounds__(kThreads) norm_kernel(const ClipArgs a) {
+  grid_dependency_wait();
+  const double norm = norm_of(a, blockIdx.x);
+  if (threadIdx.x == 0) a.norm[blockIdx.x] = (float)norm;
+  if (blockIdx.x == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+}
+
+template <typename S, typename D, int kVec>
+__device__ __forceinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
+  const long long begin = (long long)tile * kTile - behind(g, kVec);
+#pragma unroll 8
+  for (uint32_t i = 0; i < kTile / (kThreads * kVec); ++i) {
+    const long long at = begin + (i * kThreads + threadIdx.x) * kVec;
+    if (at >= 0 && (uint64_t)at + kVec <= n) {
+      const Pack<S, kVec> v = *reinterpret_cast<const Pack<S, kVec>*>(g + at);
+      float o[kVec];
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) o[e] = __fmul_rn(to_f32(v.v[e]), c);
+      store_pack<D, kVec>(out + at, o);
+    } else {
+      for (int e = 0; e < kVec; ++e)
+        if (at + e >= 0 && (uint64_t)(at + e) < n) out[at + e] = from_f32<D>(__fmul_rn(to_f32(g[at + e]), c));
+    }
+  }
+}
+template <typename S, typename D>
+__device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t tile, float c) {
+  const S* g = static_cast<const S*>(p.src) + m * p.src_worker;
+  D* out = static_cast<D*>(p.dst) + m * p.dst_worker;
+  // four entries at a time where both sides lie alike, two or one where they do not
+  if (behind(g, 4) == behind(out, 4)) tile_scaled<S, D, 4>(g, out, p.n, tile, c);
+  else if (behind(g, 2) == behind(out, 2)) tile_scaled<S, D, 2>(g, out, p.n, tile, c);
+  else tile_scaled<S, D, 1>(g, out, p.n, tile, c);
+}
+
+template <int kMax>
+__global__ void __launch_bounds__(kThreads) scale_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a, uint32_t runs) {
+  grid_dependency_wait();
+  const uint32_t m = blockIdx.y, run = runs - 1 - blockIdx.x;      // what was read last is in the L2
+  const double norm = norm_of(a, m), held = norm + (double)a.eps;
+  const float c = held <= (double)a.max_norm ? 1.f : (float)((double)a.max_norm / held);   // NaN stays NaN
+  if (run == 0 && threadIdx.x == 0) a.norm[m] = (float)norm;
+  if (run == 0 && m == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+  const uint32_t begin = run * a.per, end = min(begin + a.per, a.tiles);
+  uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
+  for (uint32_t tile = begin; tile < end; ++tile) {
+    while (k + 1 < a.count && parts.p[k + 1].first_tile <= tile) ++k;
+    const Part& p = parts.p[k];
+    if (c == 1.f && p.in_place) continue;
+    const uint32_t in = tile - p.first_tile;
+    if (p.src_bf16)
+      p.dst_bf16 ? tile_clipped<__nv_bfloat16, __nv_bfloat16>(p, m, in, c) : tile_clipped<__nv_bfloat16, float>(p, m, in, c);
+    else
+      p.dst_bf16 ? tile_clipped<float, __nv_bfloat16>(p, m, in, c) : tile_clipped<float, float>(p, m, in, c);
+  }
+}
+
+// ------------------------------------------------------------------ host
+uint32_t runs_each(int M) {
+  const uint32_t even = (kRunsAll + M - 1) / M;
+  return even > kRunsEach ? even : kRunsEach;
+}
+size_t workspace_bytes(int M) { return 256 + align_up(((size_t)kRunsAll + (size_t)M * (kRunsEach + 1)) * sizeof(double), 256); }
+
+// tiles that n entries take wherever the first one lies
+uint64_t tiles_of(uint64_t n) { return n == 0 ? 0 : (n + 8 - 1 + kTile - 1) / kTile; }
+
+bool valid(const s3gd_part* parts, int count, int M, bool clip) {
+  if (count < 0 || (count > 0 && parts == nullptr) || M < 1 || M > 65535) return false;
+  for (int i = 0; i < count; ++i) {
+    const s3gd_part& p = parts[i];
+    if (!is_real(p.dtype) || (clip && !is_real(p.out_dtype)) || p.n >= (1ull << 40)) return false;
+    if (p.n == 0) continue;
+    if (p.data == nullptr || !is_aligned(p.data, dtype_bytes(p.dtype)) || (M > 1 && p.stride < 0)) return false;
+    if (!clip) continue;
+    if (p.out == nullptr || !is_aligned(p.out, dtype_bytes(p.out_dtype)) || (M > 1 && (p.out_stride < 0 || (uint64_t)p.out_stride < p.n))) return false;
+    // in place: the same entries, not others of the same memory
+    if (p.out == p.data && (p.dtype != p.out_dtype || (M > 1 && p.stride != p.out_stride))) return false;
+  }
+  return true;
+}
+
+// Calls f(Parts, ClipArgs of the group) for groups of at most kMax tensors.
+template <int kMax, typename F>
+cudaError_t by_group(const s3gd_part* parts, int count, int M, ClipArgs a, F f) {
+  a.runs = runs_each(M);
+  for (int i = 0;;) {
+    Parts<kMax> group;
+    a.count = 0;
+    uint64_t tiles = 0;
+    for (; i < count && a.count < kMax; ++i) {
+      const s3gd_part& p = parts[i];
+      const uint64_t more = tiles_of(p.n);
+      if (more == 0) continue;
+      if (tiles + more >= (1ull << 31)) break;
+      Part& q = group.p[a.count++];
+      q.src = p.data; q.dst = p.out; q.n = p.n; q.src_worker = M > 1 ? p.stride : 0; q.dst_worker = M > 1 ? p.out_stride : 0;
+      q.first_tile = (uint32_t)tiles;
+      q.src_bf16 = p.dtype == S3GD_BF16; q.dst_bf16 = p.out_dtype == S3GD_BF16; q.in_place = p.out == p.data;
+      tiles += more;
+    }
+    a.tiles = (uint32_t)tiles;
+    a.per = (uint32_t)((tiles + a.runs - 1) / a.runs);
+    if (a.per == 0) a.per = 1;
+    const cudaError_t e = f(group, a);
+    if (e != cudaSuccess || i >= count) return e;
+    a.add = 1;
+  }
+}
+
+template <int kMax>
+cudaError_t enqueue_squares(const s3gd_part* parts, int count, int M, const ClipArgs& base, cudaStream_t st) {
+  return by_group<kMax>(parts, count, M, base, [&](const Parts<kMax>& group, const ClipArgs& a) {
+    count_launch();
+    return launch_after(squares_kernel<kMax>, dim3(a.runs, M), dim3(kThreads), 0, st, group, a);
+  });
+}
+template <int kMax>
+cudaError_t enqueue_clip(const s3gd_part* parts, int count, int M, const ClipArgs& base, cudaStream_t st) {
+  const cudaError_t e = enqueue_squares<kMax>(parts, count, M, base, st);
+  if (e != cudaSuccess) return e;
+  return by_group<kMax>(parts, count, M, base, [&](const Parts<kMax>& group, const ClipArgs& a) {
+    const uint32_t busy = (a.tiles + a.per - 1) / a.per, runs = busy < 1 ? 1 : busy;
+    count_launch();
+    return launch_after(scale_kernel<kMax>, dim3(runs, M), dim3(kThreads), 0, st, group, a, runs);
+  });
+}
+
+ClipArgs clip_args(void* ws, float* norm) {
+  ClipArgs a = {};
+  a.hdr = static_cast<uint32_t*>(ws);
+  a.partial = reinterpret_cast<double*>(static_cast<char*>(ws) + 256);
+  a.norm = norm;
+  return a;
+}
+
+}  // namespace
+}  // namespace s3gd
+
+using namespace s3gd;
+
+extern "C" size_t s3gd_clip_workspace_bytes(int M) { return M < 1 || M > 65535 ? 0 : workspace_bytes(M); }
+
+extern "C" s3gd_status s3gd_grad_norm(const s3gd_part* parts, int count, int M, float* out_norm, void* ws, size_t ws_bytes, void* stream) {
+  if (!valid(parts, count, M, false) || out_norm == nullptr || !is_aligned(out_norm, 4)) return S3GD_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < workspace_bytes(M) || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
+  const ClipArgs a = clip_args(ws, out_norm);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = count <= kFewParts ? enqueue_squares<kFewParts>(parts, count, M, a, st) : enqueue_squares<kMostParts>(parts, count, M, a, st);
+  if (e == cudaSuccess) {
+    ClipArgs last = a;
+    last.runs = runs_each(M);
+    count_launch();
+    e = launch_after(norm_kernel, dim3(M), dim3(kThreads), 0, st, last);
+  }
+  return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
+}
+
+extern "C" s3gd_status s3gd_clip(const s3gd_part* parts, int count, int M, float max_norm, float eps, float* out_norm, void* ws,
+                                 size_t ws_bytes, void* stream) {
+  if (!valid(parts, count, M, true) || out_norm == nullptr || !is_aligned(out_norm, 4)) return S3GD_ERR_INVALID_ARG;
+  if (!(max_norm >= 0.f && max_norm < INFINITY) || !(eps >= 0.f && eps < INFINITY)) return S3GD_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < workspace_bytes(M) || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
+  ClipArgs a = clip_args(ws, out_norm);
+  a.max_norm = max_norm;
+  a.eps = eps;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = count <= kFewParts ? enqueue_clip<kFewParts>(parts, count, M, a, st) : enqueue_clip<kMostParts>(parts, count, M, a, st);
+  return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
+}

@@ -31,30 +31,6 @@ constexpr int kHdrCommon = 16;                     // header word: common tokens
 constexpr int kMinChunk = 32, kMaxChunks = 8192;   // places per partial sum at least (64: 107 instead of 94 us for the eight
                                                    // workers above); partial sums per worker at most
 
-// ------------------------------------------------------------------ access of kVec neighbouring entries
-template <typename T, int kVec>
-struct alignas((kVec * sizeof(T) > 16 ? 16 : kVec * sizeof(T))) Pack { T v[kVec]; };
-
-template <typename T, int kVec>
-__device__ __forceinline__ void store_pack(T* p, const float* v) {
-  Pack<T, kVec> o;
-#pragma unroll
-  for (int e = 0; e < kVec; ++e) o.v[e] = from_f32<T>(v[e]);
-  *reinterpret_cast<Pack<T, kVec>*>(p) = o;
-}
-
-// the widest access that base and distances allow, no wider than what keeps 32 lanes busy on `dim` columns
-int widest(uint64_t dim) {
-  int v = 8;
-  while (v > 1 && (dim % v != 0 || dim < 32u * v)) v /= 2;
-  return v;
-}
-int allowed(int v, const void* p, int dtype, int64_t stride_a, int64_t stride_b) {
-  const size_t size = dtype_bytes(dtype);
-  while (v > 1 && (!is_aligned(p, v * size < 16 ? v * size : 16) || stride_a % v != 0 || stride_b % v != 0)) v /= 2;
-  return v;
-}
-
 // ------------------------------------------------------------------ lookup
 template <typename W, typename I, typename O, int kVec>
 __global__ void __launch_bounds__(kThreads) lookup_kernel(const W* table, long long table_stride, uint64_t vocab, uint32_t dim, const I* ids,
@@ -534,17 +510,6 @@ __global__ void __launch_bounds__(kThreads) join_kernel(GradArgs g) {
 }
 
 // ------------------------------------------------------------------ host
-bool is_real(int dt) { return dt == S3GD_F32 || dt == S3GD_BF16; }
-bool is_index(int dt) { return dt == S3GD_I32 || dt == S3GD_I64; }
-
-template <typename F>
-cudaError_t by_real(int dt, F f) { return dt == S3GD_F32 ? f(float()) : f(__nv_bfloat16()); }
-template <typename F>
-cudaError_t by_index(int dt, F f) { return dt == S3GD_I32 ? f(int32_t()) : f(int64_t()); }
-template <int kN> struct Width { static constexpr int value = kN; };
-template <typename F>
-cudaError_t by_width(int v, F f) { return v == 8 ? f(Width<8>()) : v == 4 ? f(Width<4>()) : v == 2 ? f(Width<2>()) : f(Width<1>()); }
-
 struct GradLayout {
   uint32_t chunk, chunks, pad, sort_tiles;
   bool direct, few;

@@ -1,0 +1,394 @@
+// Layer norm over rows of a batch of workers, and its gradient with the workers' weight gradients (see include/s3gd.h).
+//
+// Forward: y = (x - mean) rstd w + b.  Backward, with xhat = (x - mean) rstd and g = dy w:
+//     dx = rstd (g - mean(g) - xhat mean(g xhat)),   dw = sum over a worker's rows of dy xhat,   db = sum of dy.
+// Mean and rstd are computed again from x, which the backward pass reads anyway: nothing is saved between the passes.
+//
+// Sums over a row.  The mean is taken first, then the sums of d = x - mean and d^2 (and of g and g d): the sum of d, which
+// would be zero but for the mean's rounding, corrects both mean and variance, so that rows far from zero keep their digits.
+//
+// Weight gradients.  The rows of all workers, one worker after the other, are dealt to CTAs in runs of `per` rows.  A CTA
+// writes a partial sum for each worker that its run touches; run k and worker m meet in slot k + m (from one slot to the next
+// in that order either k or m grows).  A last kernel adds a worker's slots in 64 bits, in ascending order: no atomics, and the
+// result depends on the sizes alone.
+#include "s3gd_ops.cuh"
+
+namespace s3gd {
+namespace {
+
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr uint64_t kMaxDim = (1ull << 24) - 1;
+constexpr int kRuns = kDefaultSMs;                 // runs of rows at least, where there are as many rows
+constexpr uint64_t kMaxRun = 4096;                 // rows of a run at most: 32-bit sums stay short
+
+struct Rows {                                      // [M x T] rows of `dim` entries; p NULL: not given
+  const void* p;
+  long long tok, worker;
+};
+struct NormArgs {
+  Rows x, add, total, y;
+  const void *weight, *bias;
+  bool param_bf16, ids64;
+  const void* ids;
+  uint32_t T, N, dim;
+  float eps;
+};
+struct NormGradArgs {
+  Rows dy, x, dtotal, dx;
+  const void *weight, *ids;
+  bool weight_bf16, ids64, grads_bf16, accumulate;
+  uint32_t M, T, N, dim, pad, per, runs;
+  float eps;
+  void *dweight, *dbias;
+  long long grads_stride;
+  uint32_t* hdr;
+  float4* stats;
+  float* partial;
+};
+
+template <typename T>
+__device__ __forceinline__ T* row_of(const Rows& r, uint32_t m, uint32_t t) {
+  return static_cast<T*>(const_cast<void*>(r.p)) + m * r.worker + t * r.tok;
+}
+__device__ __forceinline__ bool is_empty(const void* ids, bool ids64, uint32_t r) {
+  if (ids == nullptr) return false;
+  return ids64 ? static_cast<const long long*>(ids)[r] < 0 : static_cast<const int*>(ids)[r] < 0;
+}
+__device__ __forceinline__ float param_at(const void* p, bool bf16, uint32_t c, float otherwise) {
+  if (p == nullptr) return otherwise;
+  return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[c]) : static_cast<const float*>(p)[c];
+}
+template <typename T, int kVec>
+__device__ __forceinline__ void load_pack(const T* p, float* v) {
+  const Pack<T, kVec> o = *reinterpret_cast<const Pack<T, kVec>*>(p);
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) v[e] = to_f32(o.v[e]);
+}
+
+// the CTA's sums of kCount values, in every thread
+template <int kCount>
+__device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCount][kWarps]) {
+#pragma unroll
+  for (int i = 0; i < kCount; ++i)
+    for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  __syncthreads();
+  if (lane_id() == 0)
+    for (int i = 0; i < kCount; ++i) room[i][threadIdx.x >> 5] = v[i];
+  __syncthreads();
+  for (int i = 0; i < kCount; ++i) {
+    v[i] = 0;
+    for (int w = 0; w < kWarps; ++w) v[i] += room[i][w];
+  }
+}
+
+// ------------------------------------------------------------------ rows of any length, read once for each sum
+template <typename X, typename Y, int kVec>
+__global__ void __launch_bounds__(kThreads) norm_long_kernel(NormArgs a) {
+  __shared__ double room1[1][kWarps], room2[2][kWarps];
+  for (uint32_t r = blockIdx.x; r < a.N; r += gridDim.x) {
+    const uint32_t m = r / a.T, t = r % a.T;
+    const X* x = row_of<X>(a.x, m, t);
+    X* total = a.total.p == nullptr ? nullptr : row_of<X>(a.total, m, t);
+    Y* y = row_of<Y>(a.y, m, t);
+    if (is_empty(a.ids, a.ids64, r)) {
+      const float zero[kVec] = {};
+      for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
+        store_pack<Y, kVec>(y + c, zero);
+        if (total != nullptr) store_pack<X, kVec>(total + c, zero);
+      }
+      continue;
+    }
+    double sum[1] = {};
+    for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
+      float v[kVec], u[kVec];
+      load_pack<X, kVec>(x + c, v);
+      if (a.add.p != nullptr) {
+        load_pack<X, kVec>(row_of<X>(a.add, m, t) + c, u);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = to_f32(from_f32<X>(v[e] + u[e]));
+        store_pack<X, kVec>(total + c, v);
+      }
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) sum[0] += v[e];
+    }
+    cta_sums(sum, room1);
+    if (total != nullptr) x = total;               // each thread reads back what it wrote itself
+    const float mean = (float)(sum[0] / a.dim);
+    double sums[2] = {};
+    for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
+      float v[kVec];
+      load_pack<X, kVec>(x + c, v);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const double d = v[e] - mean;
+        sums[0] += d;
+        sums[1] += d * d;
+      }
+    }
+    cta_sums(sums, room2);
+    const double rest = sums[0] / a.dim;
+    const float shift = (float)rest, rstd = (float)(1.0 / sqrt(fmax(sums[1] / a.dim - rest * rest, 0.0) + a.eps));
+    for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
+      float v[kVec];
+      load_pack<X, kVec>(x + c, v);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        v[e] = fmaf((v[e] - mean - shift) * rstd, param_at(a.weight, a.param_bf16, c + e, 1.f), param_at(a.bias, a.param_bf16, c + e, 0.f));
+      store_pack<Y, kVec>(y + c, v);
+    }
+  }
+}
+
+// Two times four numbers for every row: the mean in two pieces, rstd; mean of g, mean of g xhat.
+template <typename D, typename X, int kVec>
+__global__ void __launch_bounds__(kThreads) stats_long_kernel(NormGradArgs a) {
+  __shared__ double room1[1][kWarps], room4[4][kWarps];
+  for (uint32_t r = blockIdx.x; r < a.N; r += gridDim.x) {
+    if (is_empty(a.ids, a.ids64, r)) continue;
+    const uint32_t m = r / a.T, t = r % a.T;
+    const X* x = row_of<X>(a.x, m, t);
+    const D* dy = row_of<D>(a.dy, m, t);
+    double sum[1] = {};
+    for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
+      float v[kVec];
+      load_pack<X, kVec>(x + c, v);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) sum[0] += v[e];
+    }
+    cta_sums(sum, room1);
+    const float mean = (float)(sum[0] / a.dim);
+    double s[4] = {};
+    for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
+      float v[kVec], g[kVec];
+      load_pack<X, kVec>(x + c, v);
+      load_pack<D, kVec>(dy + c, g);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const double d = v[e] - mean, w = g[e] * param_at(a.weight, a.weight_bf16, c + e, 1.f);
+        s[0] += d;
+        s[1] += d * d;
+        s[2] += w;
+        s[3] += w * d;
+      }
+    }
+    cta_sums(s, room4);
+    const double rest = s[0] / a.dim, rstd = 1.0 / sqrt(fmax(s[1] / a.dim - rest * rest, 0.0) + a.eps);
+    if (threadIdx.x == 0) {
+      a.stats[2 * (size_t)r] = make_float4(mean, (float)rest, (float)rstd, 0.f);
+      a.stats[2 * (size_t)r + 1] = make_float4((float)(s[2] / a.dim), (float)((s[3] - rest * s[2]) * rstd / a.dim), 0.f, 0.f);
+    }
+  }
+}
+
+// blockIdx.x: run of rows, blockIdx.y: tile of columns.  dx of the tile, and its partial sums of the weight gradients.
+template <typename D, typename X, int kVec>
+__global__ void __launch_bounds__(kThreads) grad_long_kernel(NormGradArgs a) {
+  grid_dependency_wait();
+  const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N), c = (blockIdx.y * kThreads + threadIdx.x) * kVec;
+  if (c >= a.dim) return;
+  float w[kVec], dw[kVec] = {}, db[kVec] = {};
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) w[e] = param_at(a.weight, a.weight_bf16, c + e, 1.f);
+  for (uint32_t r = r0; r < r1; ++r) {
+    const uint32_t m = r / a.T, t = r % a.T;
+    float o[kVec] = {};
+    if (!is_empty(a.ids, a.ids64, r)) {
+      const float4 s = a.stats[2 * (size_t)r], q = a.stats[2 * (size_t)r + 1];
+      float x[kVec], g[kVec];
+      load_pack<X, kVec>(row_of<X>(a.x, m, t) + c, x);
+      load_pack<D, kVec>(row_of<D>(a.dy, m, t) + c, g);
+      if (a.dtotal.p != nullptr) load_pack<X, kVec>(row_of<X>(a.dtotal, m, t) + c, o);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        const float xhat = (x[e] - s.x - s.y) * s.z;
+        dw[e] = fmaf(g[e], xhat, dw[e]);
+        db[e] += g[e];
+        o[e] = fmaf(s.z, fmaf(-xhat, q.y, fmaf(g[e], w[e], -q.x)), o[e]);
+      }
+    }
+    if (a.dx.p != nullptr) store_pack<X, kVec>(row_of<X>(a.dx, m, t) + c, o);
+    if (a.partial != nullptr && (r + 1 == r1 || t + 1 == a.T)) {
+      float* to = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad + c;
+      store_pack<float, kVec>(to, dw);
+      store_pack<float, kVec>(to + a.pad, db);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) dw[e] = db[e] = 0.f;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ weight gradients from the partial sums
+// blockIdx.x: 32 columns of [dw | db] (pad entries each), blockIdx.y: worker.  The warps take neighbouring slots in turn.
+constexpr int kJoinWarps = 16;
+__global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(NormGradArgs a) {
+  __shared__ double room[kJoinWarps][32];
+  const uint32_t w = threadIdx.x >> 5, lane = lane_id(), m = blockIdx.y, col = blockIdx.x * 32 + lane;
+  grid_dependency_wait();
+  if (blockIdx.x == 0 && m == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+  if (a.dweight == nullptr && a.dbias == nullptr) return;
+  double sum = 0;
+  if (a.T > 0 && col < 2 * a.pad) {
+    const uint32_t first = (uint32_t)((uint64_t)m * a.T / a.per), last = (uint32_t)(((uint64_t)(m + 1) * a.T - 1) / a.per);
+    const float* from = a.partial + (size_t)m * 2 * a.pad + col;
+#pragma unroll 8
+    for (uint32_t k = first + w; k <= last; k += kJoinWarps) sum += from[(size_t)k * 2 * a.pad];
+  }
+  room[w][lane] = sum;
+  __syncthreads();
+  if (w != 0 || col >= 2 * a.pad) return;
+  for (int k = 1; k < kJoinWarps; ++k) sum += room[k][lane];
+  const uint32_t c = col < a.pad ? col : col - a.pad;
+  void* base = col < a.pad ? a.dweight : a.dbias;
+  if (base == nullptr || c >= a.dim) return;
+  if (a.grads_bf16) {
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(base) + m * a.grads_stride + c;
+    *to = __float2bfloat16_rn((float)(a.accumulate ? sum + (double)__bfloat162float(*to) : sum));
+  } else {
+    float* to = static_cast<float*>(base) + m * a.grads_stride + c;
+    *to = (float)(a.accumulate ? sum + (double)*to : sum);
+  }
+}
+
+// ------------------------------------------------------------------ host
+struct NormGradLayout {
+  uint32_t per, runs, pad;
+  size_t off_stats, off_partial, total;
+};
+bool norm_grad_layout(int M, uint64_t T, uint64_t dim, NormGradLayout* L) {
+  if (M < 1 || M > 65535 || dim == 0 || dim > kMaxDim || T >= (1ull << 31) || (uint64_t)M * T >= (1ull << 31)) return false;
+  const uint64_t N = (uint64_t)M * T;
+  uint64_t per = (N + kRuns - 1) / kRuns;
+  per = per < 1 ? 1 : per > kMaxRun ? kMaxRun : per;
+  L->per = (uint32_t)per;
+  L->runs = (uint32_t)((N + per - 1) / per);
+  L->pad = (uint32_t)((dim + 3) / 4 * 4);
+  L->off_stats = align_up(kHdrWords * sizeof(uint32_t), 256);
+  L->off_partial = align_up(L->off_stats + N * 2 * sizeof(float4), 256);
+  // slots: runs + M, which never shrinks as N grows if runs is counted as follows
+  const uint64_t most = (N < kRuns ? N : (uint64_t)kRuns) + N / kMaxRun + M + 1;
+  L->total = align_up(L->off_partial + most * 2 * L->pad * sizeof(float), 256);
+  return true;
+}
+
+// widest access of rows: 4 entries where base and distances of every tensor allow it
+struct Given { Rows r; int dtype; };
+int row_width(const Given* g, int n, uint64_t dim, int M, uint64_t T) {
+  int v = dim % 4 == 0 ? 4 : 1;
+  for (int i = 0; i < n; ++i)
+    if (g[i].r.p != nullptr && allowed(v, g[i].r.p, g[i].dtype, T > 1 ? g[i].r.tok : 0, M > 1 ? g[i].r.worker : 0) != v) v = 1;
+  return v;
+}
+// inputs may repeat a row (distance 0); what is written must not overlap itself
+bool readable(const Rows& r, int dtype) { return is_aligned(r.p, dtype_bytes(dtype)) && r.tok >= 0 && r.worker >= 0; }
+bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
+  if (!is_aligned(r.p, dtype_bytes(dtype)) || r.tok < 0 || r.worker < 0) return false;
+  const uint64_t tok = (uint64_t)r.tok, worker = (uint64_t)r.worker;
+  if (T > 1 && tok < dim) return false;
+  if (M == 1) return true;
+  // workers one behind the other, or interleaved (each token's row of all workers side by side)
+  return worker >= (T > 1 ? (T - 1) * tok : 0) + dim || (worker >= dim && (T == 1 || tok >= (uint64_t)(M - 1) * worker + dim));
+}
+template <typename F>
+cudaError_t by_row_width(int v, F f) { return v == 4 ? f(Width<4>()) : f(Width<1>()); }
+
+}  // namespace
+}  // namespace s3gd
+
+using namespace s3gd;
+
+extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_add,
+                                       int64_t add_stride, int64_t add_worker_stride, void* opt_total, int64_t total_stride,
+                                       int64_t total_worker_stride, const void* opt_weight, const void* opt_bias, int param_dtype,
+                                       const void* opt_ids, int ids_dtype, int M, uint64_t T, uint64_t dim, float eps, void* y, int y_dtype,
+                                       int64_t y_stride, int64_t y_worker_stride, void* stream) {
+  if (!is_real(x_dtype) || !is_real(y_dtype) || !is_real(param_dtype) || !is_index(ids_dtype)) return S3GD_ERR_INVALID_ARG;
+  if (M < 1 || M > 65535 || dim == 0 || dim > kMaxDim || T >= (1ull << 31) || (uint64_t)M * T >= (1ull << 31)) return S3GD_ERR_INVALID_ARG;
+  if (!(eps >= 0.f && eps < INFINITY) || (opt_add == nullptr) != (opt_total == nullptr)) return S3GD_ERR_INVALID_ARG;
+  NormArgs a = {};
+  a.x = {x, x_stride, x_worker_stride};
+  a.add = {opt_add, add_stride, add_worker_stride};
+  a.total = {opt_total, total_stride, total_worker_stride};
+  a.y = {y, y_stride, y_worker_stride};
+  if (!is_aligned(opt_weight, dtype_bytes(param_dtype)) || !is_aligned(opt_bias, dtype_bytes(param_dtype)) ||
+      !is_aligned(opt_ids, dtype_bytes(ids_dtype)))
+    return S3GD_ERR_INVALID_ARG;
+  if (T == 0) return S3GD_OK;
+  if (x == nullptr || y == nullptr || !readable(a.x, x_dtype) || !writable(a.y, y_dtype, M, T, dim)) return S3GD_ERR_INVALID_ARG;
+  if (opt_add != nullptr && (!readable(a.add, x_dtype) || !writable(a.total, x_dtype, M, T, dim))) return S3GD_ERR_INVALID_ARG;
+  a.weight = opt_weight; a.bias = opt_bias; a.param_bf16 = param_dtype == S3GD_BF16;
+  a.ids = opt_ids; a.ids64 = ids_dtype == S3GD_I64;
+  a.T = (uint32_t)T; a.N = (uint32_t)((uint64_t)M * T); a.dim = (uint32_t)dim; a.eps = eps;
+  const Given all[] = {{a.x, x_dtype}, {a.add, x_dtype}, {a.total, x_dtype}, {a.y, y_dtype}};
+  const int vec = row_width(all, 4, dim, M, T);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const unsigned most = 8u * sm_count(), grid = a.N < most ? a.N : most;
+  count_launch();
+  const cudaError_t e = by_real(x_dtype, [&](auto xt) { return by_real(y_dtype, [&](auto yt) { return by_row_width(vec, [&](auto v) {
+    norm_long_kernel<decltype(xt), decltype(yt), decltype(v)::value><<<grid, kThreads, 0, st>>>(a);
+    return cudaGetLastError();
+  }); }); });
+  return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
+}
+
+extern "C" size_t s3gd_layer_norm_grad_workspace_bytes(int M, uint64_t T, uint64_t dim) {
+  NormGradLayout L;
+  return norm_grad_layout(M, T, dim, &L) ? L.total : 0;
+}
+
+extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_t dy_stride, int64_t dy_worker_stride, const void* x,
+                                            int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_dtotal,
+                                            int64_t dtotal_stride, int64_t dtotal_worker_stride, const void* opt_weight, int weight_dtype,
+                                            const void* opt_ids, int ids_dtype, int M, uint64_t T, uint64_t dim, float eps, void* opt_dx,
+                                            int64_t dx_stride, int64_t dx_worker_stride, void* opt_dweight, void* opt_dbias,
+                                            int grads_dtype, int64_t grads_stride, int accumulate, void* ws, size_t ws_bytes,
+                                            void* stream) {
+  NormGradLayout L;
+  if (!norm_grad_layout(M, T, dim, &L) || !is_real(dy_dtype) || !is_real(x_dtype) || !is_real(weight_dtype) || !is_index(ids_dtype) ||
+      !is_real(grads_dtype) || !(eps >= 0.f && eps < INFINITY))
+    return S3GD_ERR_INVALID_ARG;
+  const bool weights = opt_dweight != nullptr || opt_dbias != nullptr;
+  if ((opt_dx == nullptr && !weights) || (opt_dtotal != nullptr && opt_dx == nullptr)) return S3GD_ERR_INVALID_ARG;
+  if (weights && M > 1 && (grads_stride < 0 || (uint64_t)grads_stride < dim)) return S3GD_ERR_INVALID_ARG;
+  NormGradArgs a = {};
+  a.dy = {dy, dy_stride, dy_worker_stride};
+  a.x = {x, x_stride, x_worker_stride};
+  a.dtotal = {opt_dtotal, dtotal_stride, dtotal_worker_stride};
+  a.dx = {opt_dx, dx_stride, dx_worker_stride};
+  if (!is_aligned(opt_weight, dtype_bytes(weight_dtype)) || !is_aligned(opt_ids, dtype_bytes(ids_dtype)) ||
+      !is_aligned(opt_dweight, dtype_bytes(grads_dtype)) || !is_aligned(opt_dbias, dtype_bytes(grads_dtype)))
+    return S3GD_ERR_INVALID_ARG;
+  if (T > 0 && (dy == nullptr || x == nullptr || !readable(a.dy, dy_dtype) || !readable(a.x, x_dtype) ||
+                (opt_dtotal != nullptr && !readable(a.dtotal, x_dtype)) || (opt_dx != nullptr && !writable(a.dx, x_dtype, M, T, dim))))
+    return S3GD_ERR_INVALID_ARG;
+  if (ws == nullptr || ws_bytes < L.total || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
+  a.weight = opt_weight; a.weight_bf16 = weight_dtype == S3GD_BF16;
+  a.ids = opt_ids; a.ids64 = ids_dtype == S3GD_I64;
+  a.grads_bf16 = grads_dtype == S3GD_BF16; a.accumulate = accumulate != 0;
+  a.M = M; a.T = (uint32_t)T; a.N = (uint32_t)((uint64_t)M * T); a.dim = (uint32_t)dim; a.pad = L.pad; a.per = L.per; a.runs = L.runs;
+  a.eps = eps; a.dweight = opt_dweight; a.dbias = opt_dbias; a.grads_stride = M > 1 ? grads_stride : 0;
+  char* base = static_cast<char*>(ws);
+  a.hdr = reinterpret_cast<uint32_t*>(base);
+  a.stats = reinterpret_cast<float4*>(base + L.off_stats);
+  a.partial = weights ? reinterpret_cast<float*>(base + L.off_partial) : nullptr;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  cudaError_t e = cudaSuccess;
+  if (a.N > 0) {
+    const Given all[] = {{a.dy, dy_dtype}, {a.x, x_dtype}, {a.dtotal, x_dtype}, {a.dx, x_dtype}};
+    const int vec = row_width(all, 4, dim, M, T);
+    const unsigned most = 8u * sm_count(), grid = a.N < most ? a.N : most;
+    const unsigned tiles = (unsigned)((dim + kThreads * vec - 1) / (kThreads * vec));
+    if (tiles > 65535) return S3GD_ERR_INVALID_ARG;
+    count_launch(2);
+    e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) { return by_row_width(vec, [&](auto v) {
+      stats_long_kernel<decltype(dt), decltype(xt), decltype(v)::value><<<grid, kThreads, 0, st>>>(a);
+      const cudaError_t first = cudaGetLastError();
+      if (first != cudaSuccess) return first;
+      return launch_after(grad_long_kernel<decltype(dt), decltype(xt), decltype(v)::value>, dim3(a.runs, tiles), dim3(kThreads), 0, st, a);
+    }); }); });
+  }
+  if (e == cudaSuccess) {
+    count_launch();
+    e = launch_after(norm_join_kernel, dim3(weights ? (2 * a.pad + 31) / 32 : 1, weights ? M : 1), dim3(kJoinWarps * 32), 0, st, a);
+  }
+  return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
+}

@@ -20,6 +20,9 @@ inline size_t dtype_bytes(int dt) {
   return 0;
 }
 
+inline bool is_real(int dt) { return dt == S3GD_F32 || dt == S3GD_BF16; }
+inline bool is_index(int dt) { return dt == S3GD_I32 || dt == S3GD_I64; }
+
 #ifdef __CUDACC__
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
@@ -27,6 +30,39 @@ __device__ __forceinline__ float to_f32(int8_t v) { return (float)v; }
 template <typename T> __device__ __forceinline__ T from_f32(float v);
 template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// ------------------------------------------------------------------ access of kVec neighbouring entries
+template <typename T, int kVec>
+struct alignas((kVec * sizeof(T) > 16 ? 16 : kVec * sizeof(T))) Pack { T v[kVec]; };
+
+template <typename T, int kVec>
+__device__ __forceinline__ void store_pack(T* p, const float* v) {
+  Pack<T, kVec> o;
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) o.v[e] = from_f32<T>(v[e]);
+  *reinterpret_cast<Pack<T, kVec>*>(p) = o;
+}
+
+// the widest access that base and distances allow, no wider than what keeps 32 lanes busy on `dim` columns
+inline int widest(uint64_t dim) {
+  int v = 8;
+  while (v > 1 && (dim % v != 0 || dim < 32u * v)) v /= 2;
+  return v;
+}
+inline int allowed(int v, const void* p, int dtype, int64_t stride_a, int64_t stride_b) {
+  const size_t size = dtype_bytes(dtype);
+  while (v > 1 && (!is_aligned(p, v * size < 16 ? v * size : 16) || stride_a % v != 0 || stride_b % v != 0)) v /= 2;
+  return v;
+}
+
+// f is called with a value of the element type, or with the number as a type
+template <typename F>
+cudaError_t by_real(int dt, F f) { return dt == S3GD_F32 ? f(float()) : f(__nv_bfloat16()); }
+template <typename F>
+cudaError_t by_index(int dt, F f) { return dt == S3GD_I32 ? f(int32_t()) : f(int64_t()); }
+template <int kN> struct Width { static constexpr int value = kN; };
+template <typename F>
+cudaError_t by_width(int v, F f) { return v == 8 ? f(Width<8>()) : v == 4 ? f(Width<4>()) : v == 2 ? f(Width<2>()) : f(Width<1>()); }
 #endif
 
 }  // namespace s3gd
