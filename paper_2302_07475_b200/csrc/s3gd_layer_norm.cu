@@ -81,6 +81,285 @@ __device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCo
   }
 }
 
+// ------------------------------------------------------------------ rows that threads hold in registers
+// A group of `tpr` threads (a power of two; part of a warp, a warp, or several) takes a row, kEach entries a thread: of neighbouring
+// kVec entries, `tpr * kVec` apart.  Rows to come are on their way into shared memory meanwhile: every thread copies the entries
+// that it will read itself (cp.async), so the ring needs no barrier, rows may lie anywhere and empty places are not read.
+constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
+constexpr int kEach = 16;
+constexpr uint64_t kMaxRowDim = (uint64_t)kRowThreads * kEach;
+
+template <int kBytes>
+__device__ __forceinline__ void copy_async(void* to, const void* from) {
+  const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+  if (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+// What a thread holds of a row of one tensor: slots in shared memory, or (entries that cp.async cannot move) the row itself.
+template <typename T, int kVec>
+struct Slots {
+  static constexpr int kBytes = kVec * (int)sizeof(T), kChunks = kEach / kVec;
+  static constexpr bool kAsync = kBytes >= 4;
+  static constexpr int kStage = kAsync ? kEach * (int)sizeof(T) * kRowThreads : 0;      // bytes of a stage, all threads
+  static __device__ __forceinline__ void issue(char* stage, const T* row, uint32_t c, uint32_t step, uint32_t dim) {
+    if (!kAsync) return;
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k)
+      if (c + k * step < dim) copy_async<kAsync ? kBytes : 4>(stage + (k * kRowThreads + threadIdx.x) * kBytes, row + c + k * step);
+  }
+  static __device__ __forceinline__ void read(const char* stage, const T* row, uint32_t c, uint32_t step, uint32_t dim, float* v) {
+#pragma unroll
+    for (int k = 0; k < kChunks; ++k) {
+      const T* from = kAsync ? reinterpret_cast<const T*>(stage + (k * kRowThreads + threadIdx.x) * kBytes) : row + c + k * step;
+      if (c + k * step < dim) load_pack<T, kVec>(from, v + k * kVec);
+      else
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[k * kVec + e] = 0.f;
+    }
+  }
+};
+__host__ __device__ constexpr int stages_of(int bytes, int room) { return bytes == 0 ? 1 : room / bytes > 5 ? 5 : room / bytes; }
+
+// sums over the group, in every thread of it; `room` holds kCount values of every warp
+template <int kCount>
+__device__ __forceinline__ void group_sums(float (&v)[kCount], float (&room)[kRowWarps][4], uint32_t tpr) {
+#pragma unroll
+  for (uint32_t o = 1; o < 32; o *= 2) {
+    if (o >= tpr) break;
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  }
+  if (tpr <= 32) return;
+  const uint32_t w = threadIdx.x / 32, warps = tpr / 32, first = w / warps * warps;
+  if (lane_id() == 0)
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) room[w][i] = v[i];
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + w / warps), "r"(tpr) : "memory");
+#pragma unroll
+  for (int i = 0; i < kCount; ++i) {
+    v[i] = room[first][i];
+    for (uint32_t k = 1; k < warps; ++k) v[i] += room[first + k][i];
+  }
+}
+
+template <typename T, int kVec>
+__device__ __forceinline__ void store_row(T* row, uint32_t c, uint32_t step, uint32_t dim, const float* v) {
+#pragma unroll
+  for (int k = 0; k < kEach / kVec; ++k)
+    if (c + k * step < dim) store_pack<T, kVec>(row + c + k * step, v + k * kVec);
+}
+template <int kVec>
+__device__ __forceinline__ void load_param(const void* p, bool bf16, uint32_t c, uint32_t step, uint32_t dim, float otherwise, float* v) {
+#pragma unroll
+  for (int k = 0; k < kEach / kVec; ++k)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[k * kVec + e] = c + k * step < dim ? param_at(p, bf16, c + k * step + e, otherwise) : 0.f;
+}
+
+constexpr int kNormRoom = 100 * 1024;              // shared memory of the ring: two CTAs an SM where the ring is that small
+template <typename X, int kVec, bool kAdd>
+constexpr int kNormStages = stages_of(Slots<X, kVec>::kStage * (kAdd ? 2 : 1), kNormRoom) >= 2
+                                ? stages_of(Slots<X, kVec>::kStage * (kAdd ? 2 : 1), kNormRoom)
+                                : stages_of(Slots<X, kVec>::kStage * (kAdd ? 2 : 1), 2 * kNormRoom);
+
+template <typename X, typename Y, int kVec, bool kAdd>
+__global__ void __launch_bounds__(kRowThreads) norm_row_kernel(NormArgs a, uint32_t tpr) {
+  using Slot = Slots<X, kVec>;
+  constexpr int kStages = kNormStages<X, kVec, kAdd>, kStage = Slot::kStage * (kAdd ? 2 : 1);
+  extern __shared__ __align__(16) char ring[];
+  __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
+  const uint32_t group = threadIdx.x / tpr, groups = kRowThreads / tpr, c = threadIdx.x % tpr * kVec, step = tpr * kVec;
+  const uint32_t first = blockIdx.x * groups, stride = gridDim.x * groups;
+  const uint32_t turns = first < a.N ? (a.N - first + stride - 1) / stride : 0;
+  auto row_at = [&](uint32_t k) { return (uint64_t)first + group + (uint64_t)k * stride; };
+  auto there = [&](uint32_t k) { const uint64_t r = row_at(k); return r < a.N && !is_empty(a.ids, a.ids64, (uint32_t)r); };
+  auto issue = [&](uint32_t k, bool real) {
+    if (Slot::kAsync && real) {
+      const uint32_t r = (uint32_t)row_at(k), m = r / a.T, t = r % a.T;
+      char* stage = ring + k % kStages * kStage;
+      Slot::issue(stage, row_of<X>(a.x, m, t), c, step, a.dim);
+      if (kAdd) Slot::issue(stage + Slot::kStage, row_of<X>(a.add, m, t), c, step, a.dim);
+    }
+    copy_commit();
+  };
+  float w[kEach], b[kEach];
+  uint32_t flags = 0;                                                // bit k: the row k turns ahead is there
+  for (uint32_t k = 0; k + 1 < (uint32_t)kStages; ++k) {
+    const bool real = there(k);
+    issue(k, real);
+    flags |= (uint32_t)real << k;
+  }
+  bool coming = there(kStages - 1);
+  load_param<kVec>(a.weight, a.param_bf16, c, step, a.dim, 1.f, w);
+  load_param<kVec>(a.bias, a.param_bf16, c, step, a.dim, 0.f, b);
+  for (uint32_t k = 0; k < turns; ++k) {
+    issue(k + kStages - 1, coming);                                  // (the slot that the turn before read)
+    flags |= (uint32_t)coming << (kStages - 1);
+    coming = there(k + kStages);
+    copy_wait<kStages - 1>();
+    const bool real = flags & 1;
+    flags >>= 1;
+    const uint64_t at = row_at(k);
+    const uint32_t r = at < a.N ? (uint32_t)at : 0, m = r / a.T, t = r % a.T;
+    const char* stage = ring + k % kStages * kStage;
+    float v[kEach];
+    if (real) {
+      Slot::read(stage, row_of<X>(a.x, m, t), c, step, a.dim, v);
+      if (kAdd) {
+        float u[kEach];
+        Slot::read(stage + Slot::kStage, row_of<X>(a.add, m, t), c, step, a.dim, u);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) v[e] = to_f32(from_f32<X>(v[e] + u[e]));
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) v[e] = 0.f;
+    }
+    if (kAdd && at < a.N) store_row<X, kVec>(row_of<X>(a.total, m, t), c, step, a.dim, v);
+    const float over = 1.f / a.dim;
+    float sum[1] = {0.f};
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) sum[0] += v[e];
+    group_sums(sum, room1, tpr);
+    const float mean = sum[0] * over;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      v[e] = c + e / kVec * step < a.dim ? v[e] - mean : 0.f;
+      s[0] += v[e];
+      s[1] = fmaf(v[e], v[e], s[1]);
+    }
+    group_sums(s, room2, tpr);
+    const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) v[e] = real ? fmaf((v[e] - shift) * rstd, w[e], b[e]) : 0.f;
+    if (at < a.N) store_row<Y, kVec>(row_of<Y>(a.y, m, t), c, step, a.dim, v);
+  }
+}
+
+constexpr int kGradRoom = 200 * 1024;
+template <typename D, typename X, int kVec, bool kMore>
+constexpr int kGradStage = Slots<D, kVec>::kStage + Slots<X, kVec>::kStage * (kMore ? 2 : 1);
+constexpr int kFlushBytes = kRowThreads * 2 * 4 * (int)sizeof(float);
+
+template <typename D, typename X, int kVec, bool kMore>
+__global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a, uint32_t tpr) {
+  using SlotD = Slots<D, kVec>; using SlotX = Slots<X, kVec>;
+  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kStages = stages_of(kStage, kGradRoom);
+  extern __shared__ __align__(16) char ring[];
+  float* flush = reinterpret_cast<float*>(ring + kStages * kStage);
+  __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
+  const uint32_t group = threadIdx.x / tpr, groups = kRowThreads / tpr, c = threadIdx.x % tpr * kVec, step = tpr * kVec;
+  grid_dependency_wait();
+  const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
+  float w[kEach], dw[kEach], db[kEach];
+  load_param<kVec>(a.weight, a.weight_bf16, c, step, a.dim, 1.f, w);
+  for (uint32_t begin = r0; begin < r1;) {                           // one worker's rows of the run at a time
+    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T), turns = (end - begin + groups - 1) / groups;
+    const uint32_t t0 = begin - m * a.T + group;                     // the group's first token
+    auto there = [&](uint32_t k) { const uint32_t r = begin + group + k * groups; return r < end && !is_empty(a.ids, a.ids64, r); };
+    auto issue = [&](uint32_t k, bool real) {
+      if (real) {
+        char* stage = ring + k % kStages * kStage;
+        SlotD::issue(stage, row_of<D>(a.dy, m, t0 + k * groups), c, step, a.dim);
+        SlotX::issue(stage + SlotD::kStage, row_of<X>(a.x, m, t0 + k * groups), c, step, a.dim);
+        if (kMore) SlotX::issue(stage + SlotD::kStage + SlotX::kStage, row_of<X>(a.dtotal, m, t0 + k * groups), c, step, a.dim);
+      }
+      copy_commit();
+    };
+    uint32_t flags = 0;
+    for (uint32_t k = 0; k + 1 < (uint32_t)kStages; ++k) {
+      const bool real = there(k);
+      issue(k, real);
+      flags |= (uint32_t)real << k;
+    }
+    bool coming = there(kStages - 1);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) dw[e] = db[e] = 0.f;
+    for (uint32_t k = 0; k < turns; ++k) {
+      issue(k + kStages - 1, coming);
+      flags |= (uint32_t)coming << (kStages - 1);
+      coming = there(k + kStages);
+      copy_wait<kStages - 1>();
+      const bool real = flags & 1;
+      flags >>= 1;
+      const uint32_t t = t0 + k * groups;
+      const char* stage = ring + k % kStages * kStage;
+      float v[kEach], g[kEach];
+      if (real) {
+        SlotD::read(stage, row_of<D>(a.dy, m, t), c, step, a.dim, g);
+        SlotX::read(stage + SlotD::kStage, row_of<X>(a.x, m, t), c, step, a.dim, v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) v[e] = g[e] = 0.f;
+      }
+      const float over = 1.f / a.dim;
+      float sum[1] = {0.f};
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) sum[0] += v[e];
+      group_sums(sum, room1, tpr);
+      const float mean = sum[0] * over;
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        v[e] = c + e / kVec * step < a.dim ? v[e] - mean : 0.f;
+        const float gw = g[e] * w[e];
+        s[0] += v[e];
+        s[1] = fmaf(v[e], v[e], s[1]);
+        s[2] += gw;
+        s[3] = fmaf(gw, v[e], s[3]);
+      }
+      group_sums(s, room2, tpr);
+      const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
+      const float mg = s[2] * over, mgx = fmaf(-shift, s[2], s[3]) * over * rstd;
+      if (real) {
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const float xhat = (v[e] - shift) * rstd;
+          dw[e] = fmaf(g[e], xhat, dw[e]);
+          db[e] += g[e];
+          v[e] = rstd * fmaf(-xhat, mgx, fmaf(g[e], w[e], -mg));
+        }
+        if (kMore) {
+          float o[kEach];
+          SlotX::read(stage + SlotD::kStage + SlotX::kStage, row_of<X>(a.dtotal, m, t), c, step, a.dim, o);
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) v[e] += o[e];
+        }
+      }
+      if (a.dx.p != nullptr && begin + group + k * groups < end) {
+        if (!real)
+#pragma unroll
+          for (int e = 0; e < kEach; ++e) v[e] = 0.f;
+        store_row<X, kVec>(row_of<X>(a.dx, m, t), c, step, a.dim, v);
+      }
+    }
+    if (a.partial != nullptr) {                                      // the groups' sums, four entries a thread at a time
+      float* to = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad;
+#pragma unroll
+      for (int q = 0; q < kEach / 4; ++q) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          flush[e * kRowThreads + threadIdx.x] = dw[q * 4 + e];
+          flush[(4 + e) * kRowThreads + threadIdx.x] = db[q * 4 + e];
+        }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < 8 * tpr; i += kRowThreads) {
+          const uint32_t part = i / tpr, l = i % tpr, e = q * 4 + part % 4, col = l * kVec + e / kVec * step + e % kVec;
+          float sum = 0.f;
+          for (uint32_t j = 0; j < groups; ++j) sum += flush[part * kRowThreads + j * tpr + l];
+          if (col < a.dim) to[(part < 4 ? 0 : a.pad) + col] = sum;
+        }
+      }
+    }
+    begin = end;
+  }
+}
+
 // ------------------------------------------------------------------ rows of any length, read once for each sum
 template <typename X, typename Y, int kVec>
 __global__ void __launch_bounds__(kThreads) norm_long_kernel(NormArgs a) {
@@ -263,7 +542,7 @@ bool norm_grad_layout(int M, uint64_t T, uint64_t dim, NormGradLayout* L) {
   L->runs = (uint32_t)((N + per - 1) / per);
   L->pad = (uint32_t)((dim + 3) / 4 * 4);
   L->off_stats = align_up(kHdrWords * sizeof(uint32_t), 256);
-  L->off_partial = align_up(L->off_stats + N * 2 * sizeof(float4), 256);
+  L->off_partial = align_up(L->off_stats + (dim > kMaxRowDim ? N * 2 * sizeof(float4) : 0), 256);
   // slots: runs + M, which never shrinks as N grows if runs is counted as follows
   const uint64_t most = (N < kRuns ? N : (uint64_t)kRuns) + N / kMaxRun + M + 1;
   L->total = align_up(L->off_partial + most * 2 * L->pad * sizeof(float), 256);
@@ -287,6 +566,33 @@ bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
   if (M == 1) return true;
   // workers one behind the other, or interleaved (each token's row of all workers side by side)
   return worker >= (T > 1 ? (T - 1) * tok : 0) + dim || (worker >= dim && (T == 1 || tok >= (uint64_t)(M - 1) * worker + dim));
+}
+// threads of a row: the fewest (4 at least) that hold it
+uint32_t threads_per_row(uint64_t dim) {
+  uint32_t n = 4;
+  while (n * kEach < dim) n *= 2;
+  return n;
+}
+template <typename X, typename Y, int kVec, bool kAdd>
+cudaError_t enqueue_norm_rows(const NormArgs& a, cudaStream_t st) {
+  static int done[kMaxDevices];
+  constexpr int kBytes = kNormStages<X, kVec, kAdd> * Slots<X, kVec>::kStage * (kAdd ? 2 : 1);
+  auto kernel = norm_row_kernel<X, Y, kVec, kAdd>;
+  const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
+  if (e != cudaSuccess) return e;
+  const uint32_t tpr = threads_per_row(a.dim), groups = kRowThreads / tpr, most = (kBytes <= kNormRoom ? 2 : 1) * sm_count();
+  const uint32_t blocks = (a.N + groups - 1) / groups;
+  kernel<<<blocks < most ? blocks : most, kRowThreads, kBytes, st>>>(a, tpr);
+  return cudaGetLastError();
+}
+template <typename D, typename X, int kVec, bool kMore>
+cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
+  static int done[kMaxDevices];
+  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage + kFlushBytes;
+  auto kernel = grad_row_kernel<D, X, kVec, kMore>;
+  const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
+  if (e != cudaSuccess) return e;
+  return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, threads_per_row(a.dim));
 }
 template <typename F>
 cudaError_t by_row_width(int v, F f) { return v == 4 ? f(Width<4>()) : f(Width<1>()); }
@@ -321,11 +627,16 @@ extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_str
   const Given all[] = {{a.x, x_dtype}, {a.add, x_dtype}, {a.total, x_dtype}, {a.y, y_dtype}};
   const int vec = row_width(all, 4, dim, M, T);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const unsigned most = 8u * sm_count(), grid = a.N < most ? a.N : most;
   count_launch();
   const cudaError_t e = by_real(x_dtype, [&](auto xt) { return by_real(y_dtype, [&](auto yt) { return by_row_width(vec, [&](auto v) {
-    norm_long_kernel<decltype(xt), decltype(yt), decltype(v)::value><<<grid, kThreads, 0, st>>>(a);
-    return cudaGetLastError();
+    using X = decltype(xt); using Y = decltype(yt);
+    constexpr int kVec = decltype(v)::value;
+    if (dim > kMaxRowDim) {
+      const unsigned most = 8u * sm_count();
+      norm_long_kernel<X, Y, kVec><<<a.N < most ? a.N : most, kThreads, 0, st>>>(a);
+      return cudaGetLastError();
+    }
+    return opt_add != nullptr ? enqueue_norm_rows<X, Y, kVec, true>(a, st) : enqueue_norm_rows<X, Y, kVec, false>(a, st);
   }); }); });
   return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
 }
@@ -378,12 +689,15 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
     const unsigned most = 8u * sm_count(), grid = a.N < most ? a.N : most;
     const unsigned tiles = (unsigned)((dim + kThreads * vec - 1) / (kThreads * vec));
     if (tiles > 65535) return S3GD_ERR_INVALID_ARG;
-    count_launch(2);
+    count_launch(dim > kMaxRowDim ? 2 : 1);
     e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) { return by_row_width(vec, [&](auto v) {
-      stats_long_kernel<decltype(dt), decltype(xt), decltype(v)::value><<<grid, kThreads, 0, st>>>(a);
+      using D = decltype(dt); using X = decltype(xt);
+      constexpr int kVec = decltype(v)::value;
+      if (dim <= kMaxRowDim) return opt_dtotal != nullptr ? enqueue_grad_rows<D, X, kVec, true>(a, st) : enqueue_grad_rows<D, X, kVec, false>(a, st);
+      stats_long_kernel<D, X, kVec><<<grid, kThreads, 0, st>>>(a);
       const cudaError_t first = cudaGetLastError();
       if (first != cudaSuccess) return first;
-      return launch_after(grad_long_kernel<decltype(dt), decltype(xt), decltype(v)::value>, dim3(a.runs, tiles), dim3(kThreads), 0, st, a);
+      return launch_after(grad_long_kernel<D, X, kVec>, dim3(a.runs, tiles), dim3(kThreads), 0, st, a);
     }); }); });
   }
   if (e == cudaSuccess) {
