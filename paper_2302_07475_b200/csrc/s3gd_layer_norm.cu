@@ -30,7 +30,7 @@ struct NormArgs {
   const void *weight, *bias;
   bool param_bf16, ids64;
   const void* ids;
-  uint32_t T, N, dim;
+  uint32_t T, N, dim, per;
   float eps;
 };
 struct NormGradArgs {
@@ -86,7 +86,7 @@ __device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCo
 // kVec entries, `tpr * kVec` apart.  Rows to come are on their way into shared memory meanwhile: every thread copies the entries
 // that it will read itself (cp.async), so the ring needs no barrier, rows may lie anywhere and empty places are not read.
 constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
-constexpr int kEach = 16;
+constexpr int kEach = 16, kPairs = kEach / 2;
 constexpr uint64_t kMaxRowDim = (uint64_t)kRowThreads * kEach;
 
 template <int kBytes>
@@ -98,30 +98,92 @@ __device__ __forceinline__ void copy_async(void* to, const void* from) {
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// What a thread holds of a row of one tensor: slots in shared memory, or (entries that cp.async cannot move) the row itself.
-template <typename T, int kVec>
+// Two entries at a time (one instruction for both).
+__device__ __forceinline__ unsigned long long bits(float2 a) { return *reinterpret_cast<unsigned long long*>(&a); }
+__device__ __forceinline__ float2 pair(unsigned long long a) { return *reinterpret_cast<float2*>(&a); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  unsigned long long d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)), "l"(bits(c)));
+  return pair(d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
+  return pair(d);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  unsigned long long d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
+  return pair(d);
+}
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+
+// Which of its chunks of kVec columns a thread has.  A row is longer than half of what its group can hold, but for rows of up to
+// eight entries (kAnyDim), so only the upper half of the chunks is ever missing; none where the row fills the group (kFullDim).
+enum Fill : int { kAnyDim = 0, kMoreThanHalf = 1, kFullDim = 2 };
+template <int kVec, int kFill>
+struct Columns {
+  static constexpr int kChunks = kEach / kVec;
+  uint32_t c, step, dim;
+  __device__ __forceinline__ bool has(int k) const {
+    if (kFill == kFullDim || (kFill == kMoreThanHalf && k < kChunks / 2)) return true;
+    return c + k * step < dim;
+  }
+};
+
+// What a thread holds of a row of one tensor: slots in shared memory, or (16-bit entries one by one, which cp.async cannot move)
+// the row itself.  `row` points at the thread's first column.
+template <typename T, int kVec, int kFill>
 struct Slots {
+  using Cols = Columns<kVec, kFill>;
   static constexpr int kBytes = kVec * (int)sizeof(T), kChunks = kEach / kVec;
   static constexpr bool kAsync = kBytes >= 4;
   static constexpr int kStage = kAsync ? kEach * (int)sizeof(T) * kRowThreads : 0;      // bytes of a stage, all threads
-  static __device__ __forceinline__ void issue(char* stage, const T* row, uint32_t c, uint32_t step, uint32_t dim) {
+  // stage: the thread's first slot
+  static __device__ __forceinline__ void issue(char* stage, const T* row, const Cols& at) {
     if (!kAsync) return;
 #pragma unroll
     for (int k = 0; k < kChunks; ++k)
-      if (c + k * step < dim) copy_async<kAsync ? kBytes : 4>(stage + (k * kRowThreads + threadIdx.x) * kBytes, row + c + k * step);
+      if (at.has(k)) copy_async<kAsync ? kBytes : 4>(stage + k * kRowThreads * kBytes, row + k * at.step);
   }
-  static __device__ __forceinline__ void read(const char* stage, const T* row, uint32_t c, uint32_t step, uint32_t dim, float* v) {
+  static __device__ __forceinline__ void read(const char* stage, const T* row, const Cols& at, float2* v) {
+    float* f = reinterpret_cast<float*>(v);
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      const T* from = kAsync ? reinterpret_cast<const T*>(stage + (k * kRowThreads + threadIdx.x) * kBytes) : row + c + k * step;
-      if (c + k * step < dim) load_pack<T, kVec>(from, v + k * kVec);
+      const T* from = kAsync ? reinterpret_cast<const T*>(stage + k * kRowThreads * kBytes) : row + k * at.step;
+      if (at.has(k)) load_pack<T, kVec>(from, f + k * kVec);
       else
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[k * kVec + e] = 0.f;
+        for (int e = 0; e < kVec; ++e) f[k * kVec + e] = 0.f;
     }
   }
+  static __device__ __forceinline__ char* first(char* ring) { return ring + threadIdx.x * (kAsync ? kBytes : 0); }
 };
 __host__ __device__ constexpr int stages_of(int bytes, int room) { return bytes == 0 ? 1 : room / bytes > 5 ? 5 : room / bytes; }
+
+template <typename T, int kVec, int kFill>
+__device__ __forceinline__ void store_row(T* row, const Columns<kVec, kFill>& at, const float2* v) {
+#pragma unroll
+  for (int k = 0; k < kEach / kVec; ++k)
+    if (at.has(k)) store_pack<T, kVec>(row + k * at.step, reinterpret_cast<const float*>(v) + k * kVec);
+}
+template <int kVec, int kFill>
+__device__ __forceinline__ void load_param(const void* p, bool bf16, const Columns<kVec, kFill>& at, float otherwise, float2* v) {
+#pragma unroll
+  for (int k = 0; k < kEach / kVec; ++k)
+#pragma unroll
+    for (int e = 0; e < kVec; ++e)
+      reinterpret_cast<float*>(v)[k * kVec + e] = at.has(k) ? param_at(p, bf16, at.c + k * at.step + e, otherwise) : 0.f;
+}
+// v - mean, zero in columns that the thread does not have
+template <int kVec, int kFill>
+__device__ __forceinline__ void centre(float2* v, float mean, const Columns<kVec, kFill>& at) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], both(-mean));
+#pragma unroll
+  for (int e = 0; e < kEach; ++e)
+    if (!at.has(e / kVec)) reinterpret_cast<float*>(v)[e] = 0.f;
+}
 
 // sums over the group, in every thread of it; `room` holds kCount values of every warp
 template <int kCount>
@@ -133,226 +195,272 @@ __device__ __forceinline__ void group_sums(float (&v)[kCount], float (&room)[kRo
     for (int i = 0; i < kCount; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   }
   if (tpr <= 32) return;
-  const uint32_t w = threadIdx.x / 32, warps = tpr / 32, first = w / warps * warps;
+  const uint32_t w = threadIdx.x / 32, warps = tpr / 32, first = w & ~(warps - 1);
   if (lane_id() == 0)
 #pragma unroll
     for (int i = 0; i < kCount; ++i) room[w][i] = v[i];
-  asm volatile("bar.sync %0, %1;" ::"r"(1 + w / warps), "r"(tpr) : "memory");
+  asm volatile("bar.sync %0, %1;" ::"r"(1 + first / warps), "r"(tpr) : "memory");
 #pragma unroll
-  for (int i = 0; i < kCount; ++i) {
-    v[i] = room[first][i];
-    for (uint32_t k = 1; k < warps; ++k) v[i] += room[first + k][i];
+  for (int i = 0; i < kCount; ++i) v[i] = room[first][i];
+  for (uint32_t k = 1; k < warps; ++k)
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) v[i] += room[first + k][i];
+}
+
+// Walks a run of rows, one worker's rows at a time; a group takes every groups-th of them.
+struct Walk {
+  uint32_t groups, group, m, t, left;              // the group's row: worker, token, rows of the segment from it on (0: none)
+  __device__ __forceinline__ void start(uint32_t begin, uint32_t end, uint32_t worker, uint32_t T) {
+    m = worker;
+    t = begin - worker * T + group;
+    left = end - begin > group ? end - begin - group : 0;
   }
-}
+  __device__ __forceinline__ bool in(uint32_t k) const { return k * groups < left; }     // is there a row k turns from the first?
+};
 
-template <typename T, int kVec>
-__device__ __forceinline__ void store_row(T* row, uint32_t c, uint32_t step, uint32_t dim, const float* v) {
-#pragma unroll
-  for (int k = 0; k < kEach / kVec; ++k)
-    if (c + k * step < dim) store_pack<T, kVec>(row + c + k * step, v + k * kVec);
-}
-template <int kVec>
-__device__ __forceinline__ void load_param(const void* p, bool bf16, uint32_t c, uint32_t step, uint32_t dim, float otherwise, float* v) {
-#pragma unroll
-  for (int k = 0; k < kEach / kVec; ++k)
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) v[k * kVec + e] = c + k * step < dim ? param_at(p, bf16, c + k * step + e, otherwise) : 0.f;
-}
+constexpr int kNormRoom = 200 * 1024;              // shared memory of the ring
+template <typename X, int kVec, int kFill, bool kAdd>
+constexpr int kNormStage = Slots<X, kVec, kFill>::kStage * (kAdd ? 2 : 1);
 
-constexpr int kNormRoom = 100 * 1024;              // shared memory of the ring: two CTAs an SM where the ring is that small
-template <typename X, int kVec, bool kAdd>
-constexpr int kNormStages = stages_of(Slots<X, kVec>::kStage * (kAdd ? 2 : 1), kNormRoom) >= 2
-                                ? stages_of(Slots<X, kVec>::kStage * (kAdd ? 2 : 1), kNormRoom)
-                                : stages_of(Slots<X, kVec>::kStage * (kAdd ? 2 : 1), 2 * kNormRoom);
-
-template <typename X, typename Y, int kVec, bool kAdd>
-__global__ void __launch_bounds__(kRowThreads) norm_row_kernel(NormArgs a, uint32_t tpr) {
-  using Slot = Slots<X, kVec>;
-  constexpr int kStages = kNormStages<X, kVec, kAdd>, kStage = Slot::kStage * (kAdd ? 2 : 1);
+template <typename X, typename Y, int kVec, int kFill, bool kAdd>
+__global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, uint32_t tpr) {
+  using Slot = Slots<X, kVec, kFill>;
+  constexpr int kStage = kNormStage<X, kVec, kFill, kAdd>, kStages = stages_of(kStage, kNormRoom);
   extern __shared__ __align__(16) char ring[];
   __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
-  const uint32_t group = threadIdx.x / tpr, groups = kRowThreads / tpr, c = threadIdx.x % tpr * kVec, step = tpr * kVec;
-  const uint32_t first = blockIdx.x * groups, stride = gridDim.x * groups;
-  const uint32_t turns = first < a.N ? (a.N - first + stride - 1) / stride : 0;
-  auto row_at = [&](uint32_t k) { return (uint64_t)first + group + (uint64_t)k * stride; };
-  auto there = [&](uint32_t k) { const uint64_t r = row_at(k); return r < a.N && !is_empty(a.ids, a.ids64, (uint32_t)r); };
-  auto issue = [&](uint32_t k, bool real) {
-    if (Slot::kAsync && real) {
-      const uint32_t r = (uint32_t)row_at(k), m = r / a.T, t = r % a.T;
-      char* stage = ring + k % kStages * kStage;
-      Slot::issue(stage, row_of<X>(a.x, m, t), c, step, a.dim);
-      if (kAdd) Slot::issue(stage + Slot::kStage, row_of<X>(a.add, m, t), c, step, a.dim);
-    }
-    copy_commit();
-  };
-  float w[kEach], b[kEach];
-  uint32_t flags = 0;                                                // bit k: the row k turns ahead is there
-  for (uint32_t k = 0; k + 1 < (uint32_t)kStages; ++k) {
-    const bool real = there(k);
-    issue(k, real);
-    flags |= (uint32_t)real << k;
-  }
-  bool coming = there(kStages - 1);
-  load_param<kVec>(a.weight, a.param_bf16, c, step, a.dim, 1.f, w);
-  load_param<kVec>(a.bias, a.param_bf16, c, step, a.dim, 0.f, b);
-  for (uint32_t k = 0; k < turns; ++k) {
-    issue(k + kStages - 1, coming);                                  // (the slot that the turn before read)
-    flags |= (uint32_t)coming << (kStages - 1);
-    coming = there(k + kStages);
-    copy_wait<kStages - 1>();
-    const bool real = flags & 1;
-    flags >>= 1;
-    const uint64_t at = row_at(k);
-    const uint32_t r = at < a.N ? (uint32_t)at : 0, m = r / a.T, t = r % a.T;
-    const char* stage = ring + k % kStages * kStage;
-    float v[kEach];
-    if (real) {
-      Slot::read(stage, row_of<X>(a.x, m, t), c, step, a.dim, v);
-      if (kAdd) {
-        float u[kEach];
-        Slot::read(stage + Slot::kStage, row_of<X>(a.add, m, t), c, step, a.dim, u);
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) v[e] = to_f32(from_f32<X>(v[e] + u[e]));
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) v[e] = 0.f;
-    }
-    if (kAdd && at < a.N) store_row<X, kVec>(row_of<X>(a.total, m, t), c, step, a.dim, v);
-    const float over = 1.f / a.dim;
-    float sum[1] = {0.f};
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) sum[0] += v[e];
-    group_sums(sum, room1, tpr);
-    const float mean = sum[0] * over;
-    float s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      v[e] = c + e / kVec * step < a.dim ? v[e] - mean : 0.f;
-      s[0] += v[e];
-      s[1] = fmaf(v[e], v[e], s[1]);
-    }
-    group_sums(s, room2, tpr);
-    const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) v[e] = real ? fmaf((v[e] - shift) * rstd, w[e], b[e]) : 0.f;
-    if (at < a.N) store_row<Y, kVec>(row_of<Y>(a.y, m, t), c, step, a.dim, v);
-  }
-}
-
-constexpr int kGradRoom = 200 * 1024;
-template <typename D, typename X, int kVec, bool kMore>
-constexpr int kGradStage = Slots<D, kVec>::kStage + Slots<X, kVec>::kStage * (kMore ? 2 : 1);
-constexpr int kFlushBytes = kRowThreads * 2 * 4 * (int)sizeof(float);
-
-template <typename D, typename X, int kVec, bool kMore>
-__global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a, uint32_t tpr) {
-  using SlotD = Slots<D, kVec>; using SlotX = Slots<X, kVec>;
-  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kStages = stages_of(kStage, kGradRoom);
-  extern __shared__ __align__(16) char ring[];
-  float* flush = reinterpret_cast<float*>(ring + kStages * kStage);
-  __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
-  const uint32_t group = threadIdx.x / tpr, groups = kRowThreads / tpr, c = threadIdx.x % tpr * kVec, step = tpr * kVec;
-  grid_dependency_wait();
+  const uint32_t groups = kRowThreads / tpr;
+  const Columns<kVec, kFill> at = {threadIdx.x % tpr * kVec, tpr * kVec, a.dim};
+  Walk walk = {groups, threadIdx.x / tpr};
+  char* slots = Slot::first(ring);
+  const float over = 1.f / a.dim;
   const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
-  float w[kEach], dw[kEach], db[kEach];
-  load_param<kVec>(a.weight, a.weight_bf16, c, step, a.dim, 1.f, w);
-  for (uint32_t begin = r0; begin < r1;) {                           // one worker's rows of the run at a time
+  float2 w[kPairs], b[kPairs];
+  bool params = false;
+  for (uint32_t begin = r0; begin < r1;) {
     const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T), turns = (end - begin + groups - 1) / groups;
-    const uint32_t t0 = begin - m * a.T + group;                     // the group's first token
-    auto there = [&](uint32_t k) { const uint32_t r = begin + group + k * groups; return r < end && !is_empty(a.ids, a.ids64, r); };
-    auto issue = [&](uint32_t k, bool real) {
+    walk.start(begin, end, m, a.T);
+    auto there = [&](uint32_t k) { return walk.in(k) && !is_empty(a.ids, a.ids64, begin + walk.group + k * groups); };
+    const X* ahead_x = row_of<X>(a.x, m, walk.t) + at.c;            // the row that is copied next
+    const X* ahead_a = kAdd ? row_of<X>(a.add, m, walk.t) + at.c : nullptr;
+    const X* row_x = ahead_x; const X* row_a = ahead_a;
+    Y* row_y = row_of<Y>(a.y, m, walk.t) + at.c;
+    X* row_t = kAdd ? row_of<X>(a.total, m, walk.t) + at.c : nullptr;
+    int to = 0, from = 0;
+    auto issue = [&](bool real) {
       if (real) {
-        char* stage = ring + k % kStages * kStage;
-        SlotD::issue(stage, row_of<D>(a.dy, m, t0 + k * groups), c, step, a.dim);
-        SlotX::issue(stage + SlotD::kStage, row_of<X>(a.x, m, t0 + k * groups), c, step, a.dim);
-        if (kMore) SlotX::issue(stage + SlotD::kStage + SlotX::kStage, row_of<X>(a.dtotal, m, t0 + k * groups), c, step, a.dim);
+        Slot::issue(slots + to * kStage, ahead_x, at);
+        if (kAdd) Slot::issue(slots + to * kStage + Slot::kStage, ahead_a, at);
       }
       copy_commit();
+      ahead_x += groups * a.x.tok;
+      if (kAdd) ahead_a += groups * a.add.tok;
+      to = to + 1 == kStages ? 0 : to + 1;
     };
-    uint32_t flags = 0;
-    for (uint32_t k = 0; k + 1 < (uint32_t)kStages; ++k) {
+    uint32_t flags = 0;                                              // bit k: the row k turns ahead is there
+#pragma unroll
+    for (int k = 0; k + 1 < kStages; ++k) {
       const bool real = there(k);
-      issue(k, real);
+      issue(real);
       flags |= (uint32_t)real << k;
     }
     bool coming = there(kStages - 1);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) dw[e] = db[e] = 0.f;
+    if (!params) {
+      load_param(a.weight, a.param_bf16, at, 1.f, w);
+      load_param(a.bias, a.param_bf16, at, 0.f, b);
+      params = true;
+    }
     for (uint32_t k = 0; k < turns; ++k) {
-      issue(k + kStages - 1, coming);
+      issue(coming);                                                 // (into the slot that the turn before read)
       flags |= (uint32_t)coming << (kStages - 1);
       coming = there(k + kStages);
       copy_wait<kStages - 1>();
       const bool real = flags & 1;
       flags >>= 1;
-      const uint32_t t = t0 + k * groups;
-      const char* stage = ring + k % kStages * kStage;
-      float v[kEach], g[kEach];
+      const char* stage = slots + from * kStage;
+      float2 v[kPairs];
       if (real) {
-        SlotD::read(stage, row_of<D>(a.dy, m, t), c, step, a.dim, g);
-        SlotX::read(stage + SlotD::kStage, row_of<X>(a.x, m, t), c, step, a.dim, v);
+        Slot::read(stage, row_x, at, v);
+        if (kAdd) {
+          float2 u[kPairs];
+          Slot::read(stage + Slot::kStage, row_a, at, u);
+#pragma unroll
+          for (int i = 0; i < kPairs; ++i) {
+            v[i] = add2(v[i], u[i]);
+            v[i] = make_float2(to_f32(from_f32<X>(v[i].x)), to_f32(from_f32<X>(v[i].y)));
+          }
+        }
       } else {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) v[e] = g[e] = 0.f;
+        for (int i = 0; i < kPairs; ++i) v[i] = both(0.f);
       }
-      const float over = 1.f / a.dim;
-      float sum[1] = {0.f};
+      if (kAdd && walk.in(k)) store_row(row_t, at, v);
+      float2 q = v[0];
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) sum[0] += v[e];
+      for (int i = 1; i < kPairs; ++i) q = add2(q, v[i]);
+      float sum[1] = {q.x + q.y};
       group_sums(sum, room1, tpr);
-      const float mean = sum[0] * over;
-      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      centre(v, sum[0] * over, at);
+      float2 s0 = v[0], s1 = mul2(v[0], v[0]);
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        v[e] = c + e / kVec * step < a.dim ? v[e] - mean : 0.f;
-        const float gw = g[e] * w[e];
-        s[0] += v[e];
-        s[1] = fmaf(v[e], v[e], s[1]);
-        s[2] += gw;
-        s[3] = fmaf(gw, v[e], s[3]);
+      for (int i = 1; i < kPairs; ++i) {
+        s0 = add2(s0, v[i]);
+        s1 = fma2(v[i], v[i], s1);
       }
+      float s[2] = {s0.x + s0.y, s1.x + s1.y};
+      group_sums(s, room2, tpr);
+      const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
+      if (walk.in(k)) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = real ? fma2(mul2(add2(v[i], both(-shift)), both(rstd)), w[i], b[i]) : both(0.f);
+        store_row(row_y, at, v);
+      }
+      row_x += groups * a.x.tok;
+      row_y += groups * a.y.tok;
+      if (kAdd) { row_a += groups * a.add.tok; row_t += groups * a.total.tok; }
+      from = from + 1 == kStages ? 0 : from + 1;
+    }
+    begin = end;
+  }
+}
+
+constexpr int kGradRoom = 200 * 1024;
+template <typename D, typename X, int kVec, int kFill, bool kMore>
+constexpr int kGradStage = Slots<D, kVec, kFill>::kStage + Slots<X, kVec, kFill>::kStage * (kMore ? 2 : 1);
+constexpr int kFlushBytes = kRowThreads * 2 * 4 * (int)sizeof(float);
+
+template <typename D, typename X, int kVec, int kFill, bool kMore>
+__global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a, uint32_t tpr) {
+  using SlotD = Slots<D, kVec, kFill>; using SlotX = Slots<X, kVec, kFill>;
+  constexpr int kStage = kGradStage<D, X, kVec, kFill, kMore>, kStages = stages_of(kStage, kGradRoom);
+  extern __shared__ __align__(16) char ring[];
+  float* flush = reinterpret_cast<float*>(ring + kStages * kStage);
+  __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
+  const uint32_t groups = kRowThreads / tpr;
+  const Columns<kVec, kFill> at = {threadIdx.x % tpr * kVec, tpr * kVec, a.dim};
+  Walk walk = {groups, threadIdx.x / tpr};
+  char* slots_d = SlotD::first(ring);
+  char* slots_x = SlotX::first(ring) + SlotD::kStage;
+  const float over = 1.f / a.dim;
+  grid_dependency_wait();
+  const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
+  float2 w[kPairs], dw[kPairs], db[kPairs];
+  load_param(a.weight, a.weight_bf16, at, 1.f, w);
+  for (uint32_t begin = r0; begin < r1;) {
+    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T), turns = (end - begin + groups - 1) / groups;
+    walk.start(begin, end, m, a.T);
+    auto there = [&](uint32_t k) { return walk.in(k) && !is_empty(a.ids, a.ids64, begin + walk.group + k * groups); };
+    const D* ahead_d = row_of<D>(a.dy, m, walk.t) + at.c;           // the row that is copied next
+    const X* ahead_x = row_of<X>(a.x, m, walk.t) + at.c;
+    const X* ahead_m = kMore ? row_of<X>(a.dtotal, m, walk.t) + at.c : nullptr;
+    const D* row_d = ahead_d; const X* row_x = ahead_x; const X* row_m = ahead_m;
+    X* row_o = row_of<X>(a.dx, m, walk.t) + at.c;
+    int to = 0, from = 0;
+    auto issue = [&](bool real) {
+      if (real) {
+        SlotD::issue(slots_d + to * kStage, ahead_d, at);
+        SlotX::issue(slots_x + to * kStage, ahead_x, at);
+        if (kMore) SlotX::issue(slots_x + to * kStage + SlotX::kStage, ahead_m, at);
+      }
+      copy_commit();
+      ahead_d += groups * a.dy.tok;
+      ahead_x += groups * a.x.tok;
+      if (kMore) ahead_m += groups * a.dtotal.tok;
+      to = to + 1 == kStages ? 0 : to + 1;
+    };
+    uint32_t flags = 0;                                              // bit k: the row k turns ahead is there
+#pragma unroll
+    for (int k = 0; k + 1 < kStages; ++k) {
+      const bool real = there(k);
+      issue(real);
+      flags |= (uint32_t)real << k;
+    }
+    bool coming = there(kStages - 1);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) dw[i] = db[i] = both(0.f);
+    for (uint32_t k = 0; k < turns; ++k) {
+      issue(coming);                                                 // (into the slot that the turn before read)
+      flags |= (uint32_t)coming << (kStages - 1);
+      coming = there(k + kStages);
+      copy_wait<kStages - 1>();
+      const bool real = flags & 1;
+      flags >>= 1;
+      float2 v[kPairs], g[kPairs];
+      if (real) {
+        SlotD::read(slots_d + from * kStage, row_d, at, g);
+        SlotX::read(slots_x + from * kStage, row_x, at, v);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = g[i] = both(0.f);
+      }
+      float2 q = v[0];
+#pragma unroll
+      for (int i = 1; i < kPairs; ++i) q = add2(q, v[i]);
+      float sum[1] = {q.x + q.y};
+      group_sums(sum, room1, tpr);
+      centre(v, sum[0] * over, at);
+      float2 s0 = both(0.f), s1 = s0, s2 = s0, s3 = s0;
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const float2 gw = mul2(g[i], w[i]);
+        s0 = add2(s0, v[i]);
+        s1 = fma2(v[i], v[i], s1);
+        s2 = add2(s2, gw);
+        s3 = fma2(gw, v[i], s3);
+      }
+      float s[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
       group_sums(s, room2, tpr);
       const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
       const float mg = s[2] * over, mgx = fmaf(-shift, s[2], s[3]) * over * rstd;
       if (real) {
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-          const float xhat = (v[e] - shift) * rstd;
-          dw[e] = fmaf(g[e], xhat, dw[e]);
-          db[e] += g[e];
-          v[e] = rstd * fmaf(-xhat, mgx, fmaf(g[e], w[e], -mg));
+        for (int i = 0; i < kPairs; ++i) {
+          const float2 xhat = mul2(add2(v[i], both(-shift)), both(rstd));
+          dw[i] = fma2(g[i], xhat, dw[i]);
+          db[i] = add2(db[i], g[i]);
+          v[i] = mul2(fma2(xhat, both(-mgx), fma2(g[i], w[i], both(-mg))), both(rstd));
         }
         if (kMore) {
-          float o[kEach];
-          SlotX::read(stage + SlotD::kStage + SlotX::kStage, row_of<X>(a.dtotal, m, t), c, step, a.dim, o);
+          float2 o[kPairs];
+          SlotX::read(slots_x + from * kStage + SlotX::kStage, row_m, at, o);
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) v[e] += o[e];
+          for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], o[i]);
         }
       }
-      if (a.dx.p != nullptr && begin + group + k * groups < end) {
+      if (a.dx.p != nullptr && walk.in(k)) {
         if (!real)
 #pragma unroll
-          for (int e = 0; e < kEach; ++e) v[e] = 0.f;
-        store_row<X, kVec>(row_of<X>(a.dx, m, t), c, step, a.dim, v);
+          for (int i = 0; i < kPairs; ++i) v[i] = both(0.f);
+        store_row(row_o, at, v);
       }
+      row_d += groups * a.dy.tok;
+      row_x += groups * a.x.tok;
+      row_o += groups * a.dx.tok;
+      if (kMore) row_m += groups * a.dtotal.tok;
+      from = from + 1 == kStages ? 0 : from + 1;
     }
     if (a.partial != nullptr) {                                      // the groups' sums, four entries a thread at a time
-      float* to = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad;
+      float* out = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad;
 #pragma unroll
-      for (int q = 0; q < kEach / 4; ++q) {
+      for (int i = 0; i < kPairs; ++i)                               // groups of one warp
+        for (uint32_t o = tpr; o < 32; o *= 2) {
+          dw[i] = add2(dw[i], pair(__shfl_xor_sync(0xffffffffu, bits(dw[i]), o)));
+          db[i] = add2(db[i], pair(__shfl_xor_sync(0xffffffffu, bits(db[i]), o)));
+        }
+      const uint32_t apart = tpr < 32 ? 32 : tpr;                    // threads from one sum of a column to the next
+#pragma unroll
+      for (int part = 0; part < kEach / 4; ++part) {
         __syncthreads();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          flush[e * kRowThreads + threadIdx.x] = dw[q * 4 + e];
-          flush[(4 + e) * kRowThreads + threadIdx.x] = db[q * 4 + e];
+          flush[e * kRowThreads + threadIdx.x] = reinterpret_cast<float*>(dw)[part * 4 + e];
+          flush[(4 + e) * kRowThreads + threadIdx.x] = reinterpret_cast<float*>(db)[part * 4 + e];
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 8 * tpr; i += kRowThreads) {
-          const uint32_t part = i / tpr, l = i % tpr, e = q * 4 + part % 4, col = l * kVec + e / kVec * step + e % kVec;
+          const uint32_t row = i / tpr, l = i % tpr, e = part * 4 + row % 4, col = l * kVec + e / kVec * at.step + e % kVec;
           float sum = 0.f;
-          for (uint32_t j = 0; j < groups; ++j) sum += flush[part * kRowThreads + j * tpr + l];
-          if (col < a.dim) to[(part < 4 ? 0 : a.pad) + col] = sum;
+          for (uint32_t j = l; j < kRowThreads; j += apart) sum += flush[row * kRowThreads + j];
+          if (col < a.dim) out[(row < 4 ? 0 : a.pad) + col] = sum;
         }
       }
     }
@@ -552,7 +660,7 @@ bool norm_grad_layout(int M, uint64_t T, uint64_t dim, NormGradLayout* L) {
 // widest access of rows: 4 entries where base and distances of every tensor allow it
 struct Given { Rows r; int dtype; };
 int row_width(const Given* g, int n, uint64_t dim, int M, uint64_t T) {
-  int v = dim % 4 == 0 ? 4 : 1;
+  int v = dim % 4 == 0 && dim > kEach / 2 ? 4 : 1;
   for (int i = 0; i < n; ++i)
     if (g[i].r.p != nullptr && allowed(v, g[i].r.p, g[i].dtype, T > 1 ? g[i].r.tok : 0, M > 1 ? g[i].r.worker : 0) != v) v = 1;
   return v;
@@ -567,29 +675,35 @@ bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
   // workers one behind the other, or interleaved (each token's row of all workers side by side)
   return worker >= (T > 1 ? (T - 1) * tok : 0) + dim || (worker >= dim && (T == 1 || tok >= (uint64_t)(M - 1) * worker + dim));
 }
-// threads of a row: the fewest (4 at least) that hold it
+// threads of a row: the fewest that hold it
 uint32_t threads_per_row(uint64_t dim) {
-  uint32_t n = 4;
+  uint32_t n = 1;
   while (n * kEach < dim) n *= 2;
   return n;
 }
-template <typename X, typename Y, int kVec, bool kAdd>
-cudaError_t enqueue_norm_rows(const NormArgs& a, cudaStream_t st) {
+// f is called with the width of an access and how a row fills its group, as types
+template <typename F>
+cudaError_t by_row_form(int vec, uint64_t dim, F f) {
+  if (vec == 1) return dim <= kEach / 2 ? f(Width<1>(), Width<kAnyDim>()) : f(Width<1>(), Width<kMoreThanHalf>());
+  return dim == threads_per_row(dim) * kEach ? f(Width<4>(), Width<kFullDim>()) : f(Width<4>(), Width<kMoreThanHalf>());
+}
+template <typename X, typename Y, int kVec, int kFill, bool kAdd>
+cudaError_t enqueue_norm_rows(NormArgs a, cudaStream_t st) {
   static int done[kMaxDevices];
-  constexpr int kBytes = kNormStages<X, kVec, kAdd> * Slots<X, kVec>::kStage * (kAdd ? 2 : 1);
-  auto kernel = norm_row_kernel<X, Y, kVec, kAdd>;
+  constexpr int kStage = kNormStage<X, kVec, kFill, kAdd>, kBytes = stages_of(kStage, kNormRoom) * kStage;
+  auto kernel = norm_row_kernel<X, Y, kVec, kFill, kAdd>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
-  const uint32_t tpr = threads_per_row(a.dim), groups = kRowThreads / tpr, most = (kBytes <= kNormRoom ? 2 : 1) * sm_count();
-  const uint32_t blocks = (a.N + groups - 1) / groups;
-  kernel<<<blocks < most ? blocks : most, kRowThreads, kBytes, st>>>(a, tpr);
+  const uint32_t runs = sm_count();
+  a.per = (a.N + runs - 1) / runs;
+  kernel<<<(a.N + a.per - 1) / a.per, kRowThreads, kBytes, st>>>(a, threads_per_row(a.dim));
   return cudaGetLastError();
 }
-template <typename D, typename X, int kVec, bool kMore>
+template <typename D, typename X, int kVec, int kFill, bool kMore>
 cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   static int done[kMaxDevices];
-  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage + kFlushBytes;
-  auto kernel = grad_row_kernel<D, X, kVec, kMore>;
+  constexpr int kStage = kGradStage<D, X, kVec, kFill, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage + kFlushBytes;
+  auto kernel = grad_row_kernel<D, X, kVec, kFill, kMore>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
   return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, threads_per_row(a.dim));
@@ -628,16 +742,19 @@ extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_str
   const int vec = row_width(all, 4, dim, M, T);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   count_launch();
-  const cudaError_t e = by_real(x_dtype, [&](auto xt) { return by_real(y_dtype, [&](auto yt) { return by_row_width(vec, [&](auto v) {
+  const cudaError_t e = by_real(x_dtype, [&](auto xt) { return by_real(y_dtype, [&](auto yt) {
     using X = decltype(xt); using Y = decltype(yt);
-    constexpr int kVec = decltype(v)::value;
-    if (dim > kMaxRowDim) {
+    if (dim <= kMaxRowDim)
+      return by_row_form(vec, dim, [&](auto v, auto f) {
+        constexpr int kVec = decltype(v)::value, kFill = decltype(f)::value;
+        return opt_add != nullptr ? enqueue_norm_rows<X, Y, kVec, kFill, true>(a, st) : enqueue_norm_rows<X, Y, kVec, kFill, false>(a, st);
+      });
+    return by_row_width(vec, [&](auto v) {
       const unsigned most = 8u * sm_count();
-      norm_long_kernel<X, Y, kVec><<<a.N < most ? a.N : most, kThreads, 0, st>>>(a);
+      norm_long_kernel<X, Y, decltype(v)::value><<<a.N < most ? a.N : most, kThreads, 0, st>>>(a);
       return cudaGetLastError();
-    }
-    return opt_add != nullptr ? enqueue_norm_rows<X, Y, kVec, true>(a, st) : enqueue_norm_rows<X, Y, kVec, false>(a, st);
-  }); }); });
+    });
+  }); });
   return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
 }
 
@@ -690,15 +807,21 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
     const unsigned tiles = (unsigned)((dim + kThreads * vec - 1) / (kThreads * vec));
     if (tiles > 65535) return S3GD_ERR_INVALID_ARG;
     count_launch(dim > kMaxRowDim ? 2 : 1);
-    e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) { return by_row_width(vec, [&](auto v) {
+    e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) {
       using D = decltype(dt); using X = decltype(xt);
-      constexpr int kVec = decltype(v)::value;
-      if (dim <= kMaxRowDim) return opt_dtotal != nullptr ? enqueue_grad_rows<D, X, kVec, true>(a, st) : enqueue_grad_rows<D, X, kVec, false>(a, st);
-      stats_long_kernel<D, X, kVec><<<grid, kThreads, 0, st>>>(a);
-      const cudaError_t first = cudaGetLastError();
-      if (first != cudaSuccess) return first;
-      return launch_after(grad_long_kernel<D, X, kVec>, dim3(a.runs, tiles), dim3(kThreads), 0, st, a);
-    }); }); });
+      if (dim <= kMaxRowDim)
+        return by_row_form(vec, dim, [&](auto v, auto f) {
+          constexpr int kVec = decltype(v)::value, kFill = decltype(f)::value;
+          return opt_dtotal != nullptr ? enqueue_grad_rows<D, X, kVec, kFill, true>(a, st) : enqueue_grad_rows<D, X, kVec, kFill, false>(a, st);
+        });
+      return by_row_width(vec, [&](auto v) {
+        constexpr int kVec = decltype(v)::value;
+        stats_long_kernel<D, X, kVec><<<grid, kThreads, 0, st>>>(a);
+        const cudaError_t first = cudaGetLastError();
+        if (first != cudaSuccess) return first;
+        return launch_after(grad_long_kernel<D, X, kVec>, dim3(a.runs, tiles), dim3(kThreads), 0, st, a);
+      });
+    }); });
   }
   if (e == cudaSuccess) {
     count_launch();
