@@ -24,6 +24,7 @@ constexpr uint64_t kMaxRun = 4096;                 // rows of a run at most: 32-
 struct Rows {                                      // [M x T] rows of `dim` entries; p NULL: not given
   const void* p;
   long long tok, worker;
+  long long last;                                  // entries from the first to behind the last
 };
 struct NormArgs {
   Rows x, add, total, y;
@@ -58,13 +59,6 @@ __device__ __forceinline__ float param_at(const void* p, bool bf16, uint32_t c, 
   if (p == nullptr) return otherwise;
   return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[c]) : static_cast<const float*>(p)[c];
 }
-template <typename T, int kVec>
-__device__ __forceinline__ void load_pack(const T* p, float* v) {
-  const Pack<T, kVec> o = *reinterpret_cast<const Pack<T, kVec>*>(p);
-#pragma unroll
-  for (int e = 0; e < kVec; ++e) v[e] = to_f32(o.v[e]);
-}
-
 // the CTA's sums of kCount values, in every thread
 template <int kCount>
 __device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCount][kWarps]) {
@@ -83,8 +77,8 @@ __device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCo
 
 // ------------------------------------------------------------------ rows that threads hold in registers
 // A group of `tpr` threads (a power of two; part of a warp, a warp, or several) takes a row, kEach entries a thread: of neighbouring
-// kVec entries, `tpr * kVec` apart.  Rows to come are on their way into shared memory meanwhile: every thread copies the entries
-// that it will read itself (cp.async), so the ring needs no barrier, rows may lie anywhere and empty places are not read.
+// kVec entries, `tpr * kVec` apart.  Rows to come are on their way into a ring in shared memory meanwhile (cp.async; empty places are
+// not read).
 constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
 constexpr int kEach = 16, kPairs = kEach / 2;
 constexpr uint64_t kMaxRowDim = (uint64_t)kRowThreads * kEach;
@@ -116,10 +110,27 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits(a)), "l"(bits(b)));
   return pair(d);
 }
+template <typename T>
+__device__ __forceinline__ float2 rounded(float2 a) {
+  if constexpr (sizeof(T) == 4) return a;
+  const __nv_bfloat162 o = __floats2bfloat162_rn(a.x, a.y);
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(&o);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
 __device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+__device__ __forceinline__ void clear(float2* v) {
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) v[i] = both(0.f);
+}
+__device__ __forceinline__ float total_of(const float2* v) {
+  float2 q = v[0];
+#pragma unroll
+  for (int i = 1; i < kPairs; ++i) q = add2(q, v[i]);
+  return q.x + q.y;
+}
 
-// Which of its chunks of kVec columns a thread has.  A row is longer than half of what its group can hold, but for rows of up to
-// eight entries (kAnyDim), so only the upper half of the chunks is ever missing; none where the row fills the group (kFullDim).
+// Which of its chunks of kVec columns a thread has.  A row is longer than half of what its group can hold, but for very short rows
+// (kAnyDim), so only the upper half of the chunks is ever missing; none where the row fills the group (kFullDim).
 enum Fill : int { kAnyDim = 0, kMoreThanHalf = 1, kFullDim = 2 };
 template <int kVec, int kFill>
 struct Columns {
@@ -131,41 +142,74 @@ struct Columns {
   }
 };
 
-// What a thread holds of a row of one tensor: slots in shared memory, or (16-bit entries one by one, which cp.async cannot move)
-// the row itself.  `row` points at the thread's first column.
+__device__ __forceinline__ void group_sync(uint32_t tpr) {
+  if (tpr <= 32) __syncwarp();
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.x / tpr), "r"(tpr) : "memory");
+}
+
+// A tensor's part of a ring stage.  Rows that wide accesses fit (kVec > 1): every thread copies the entries that it will read itself,
+// and nobody waits for anybody.  Other rows (kVec 1): the group copies the row's 16-byte granules, whatever lies in them beside the
+// row, and reads entries after a barrier.
 template <typename T, int kVec, int kFill>
-struct Slots {
+struct Ring {
   using Cols = Columns<kVec, kFill>;
+  static constexpr bool kShared = kVec == 1;
   static constexpr int kBytes = kVec * (int)sizeof(T), kChunks = kEach / kVec;
-  static constexpr bool kAsync = kBytes >= 4;
-  static constexpr int kStage = kAsync ? kEach * (int)sizeof(T) * kRowThreads : 0;      // bytes of a stage, all threads
-  // stage: the thread's first slot
-  static __device__ __forceinline__ void issue(char* stage, const T* row, const Cols& at) {
-    if (!kAsync) return;
-#pragma unroll
-    for (int k = 0; k < kChunks; ++k)
-      if (at.has(k)) copy_async<kAsync ? kBytes : 4>(stage + k * kRowThreads * kBytes, row + k * at.step);
+  static constexpr int kStage = kEach * (int)sizeof(T) * kRowThreads + (kShared ? kRowThreads / 4 * 16 : 0);
+  const T* next;                                   // the group's row that is copied next, from the thread's first column (kShared: from the first)
+  long long turn;                                  // entries from a row to the group's next
+  uintptr_t begin, end;                            // what the tensor's entries lie between
+  uint32_t own, low;                               // where the thread's (group's) entries begin in a stage; address of the row that is read next
+
+  __device__ __forceinline__ void start(const Rows& r, uint32_t m, uint32_t t, uint32_t groups, uint32_t tpr, const Cols& at) {
+    next = row_of<T>(r, m, t);
+    turn = groups * r.tok;
+    begin = reinterpret_cast<uintptr_t>(r.p);
+    end = reinterpret_cast<uintptr_t>(static_cast<const T*>(r.p) + r.last);
+    low = (uint32_t)reinterpret_cast<uintptr_t>(next);
+    if (kShared) own = threadIdx.x / tpr * (tpr * kEach * (uint32_t)sizeof(T) + 16);
+    else { own = threadIdx.x * kBytes; next += at.c; }
   }
-  static __device__ __forceinline__ void read(const char* stage, const T* row, const Cols& at, float2* v) {
+  __device__ __forceinline__ void copy(char* stage, const Cols& at, uint32_t tpr) const {
+    if (kShared) {
+      const uintptr_t from = reinterpret_cast<uintptr_t>(next), to = from + at.dim * sizeof(T), first = from & ~(uintptr_t)15;
+      for (uint32_t i = at.c * 16; first + i < to; i += tpr * 16) {
+        if (first + i >= begin && first + i + 16 <= end) copy_async<16>(stage + own + i, reinterpret_cast<const void*>(first + i));
+        else                                       // at the ends of the tensor: only its own entries
+          for (uint32_t e = 0; e < 16; e += sizeof(T))
+            if (first + i + e >= from && first + i + e < to)
+              *reinterpret_cast<T*>(stage + own + i + e) = *reinterpret_cast<const T*>(first + i + e);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < kChunks; ++k)
+        if (at.has(k)) copy_async<kShared ? 16 : kBytes>(stage + own + k * kRowThreads * kBytes, next + k * at.step);
+    }
+  }
+  __device__ __forceinline__ void advance() { next += turn; }
+  __device__ __forceinline__ void done() { if (kShared) low += (uint32_t)turn * (uint32_t)sizeof(T); }
+  // ahead: 1 for the row after the one that is read next
+  __device__ __forceinline__ void read(const char* stage, const Cols& at, float2* v, int ahead = 0) const {
     float* f = reinterpret_cast<float*>(v);
+    const char* from = stage + own;
+    if (kShared) from += ((low + (ahead ? (uint32_t)turn * (uint32_t)sizeof(T) : 0u)) & 15) + at.c * (uint32_t)sizeof(T);
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      const T* from = kAsync ? reinterpret_cast<const T*>(stage + k * kRowThreads * kBytes) : row + k * at.step;
-      if (at.has(k)) load_pack<T, kVec>(from, f + k * kVec);
+      const T* chunk = reinterpret_cast<const T*>(from + (kShared ? k * at.step * (uint32_t)sizeof(T) : k * kRowThreads * kBytes));
+      if (at.has(k)) load_floats<T, kVec>(chunk, f + k * kVec);
       else
 #pragma unroll
         for (int e = 0; e < kVec; ++e) f[k * kVec + e] = 0.f;
     }
   }
-  static __device__ __forceinline__ char* first(char* ring) { return ring + threadIdx.x * (kAsync ? kBytes : 0); }
 };
-__host__ __device__ constexpr int stages_of(int bytes, int room) { return bytes == 0 ? 1 : room / bytes > 5 ? 5 : room / bytes; }
+__host__ __device__ constexpr int stages_of(int bytes, int room) { return room / bytes > 5 ? 5 : room / bytes; }
 
 template <typename T, int kVec, int kFill>
 __device__ __forceinline__ void store_row(T* row, const Columns<kVec, kFill>& at, const float2* v) {
 #pragma unroll
   for (int k = 0; k < kEach / kVec; ++k)
-    if (at.has(k)) store_pack<T, kVec>(row + k * at.step, reinterpret_cast<const float*>(v) + k * kVec);
+    if (at.has(k)) store_floats<T, kVec>(row + k * at.step, reinterpret_cast<const float*>(v) + k * kVec);
 }
 template <int kVec, int kFill>
 __device__ __forceinline__ void load_param(const void* p, bool bf16, const Columns<kVec, kFill>& at, float otherwise, float2* v) {
@@ -185,219 +229,282 @@ __device__ __forceinline__ void centre(float2* v, float mean, const Columns<kVec
     if (!at.has(e / kVec)) reinterpret_cast<float*>(v)[e] = 0.f;
 }
 
-// sums over the group, in every thread of it; `room` holds kCount values of every warp
-template <int kCount>
-__device__ __forceinline__ void group_sums(float (&v)[kCount], float (&room)[kRowWarps][4], uint32_t tpr) {
+// Sums over the group, in every thread of it: kCount values and, with kNext, one more.  Over a warp two or four sums share the
+// exchanges: each step leaves a lane with half as many sums of twice as many lanes.  Calls in turn take another room each.
+struct Room { float4 sums[kRowWarps]; float next[kRowWarps]; };
+template <int kCount, bool kNext>
+__device__ __forceinline__ void group_sums(float (&v)[kCount == 0 ? 1 : kCount], float& next, Room& room, uint32_t tpr) {
+  constexpr uint32_t kAll = 0xffffffffu;
+  if (tpr < 32) {
+#pragma unroll
+    for (uint32_t o = 1; o < 32; o *= 2) {
+      if (o >= tpr) break;
+#pragma unroll
+      for (int i = 0; i < kCount; ++i) v[i] += __shfl_xor_sync(kAll, v[i], o);
+      if (kNext) next += __shfl_xor_sync(kAll, next, o);
+    }
+    return;
+  }
+  const uint32_t lane = lane_id();
+  float one = 0.f;                                 // lane l: sum number l % kCount
+  if constexpr (kCount == 2) {
+    const bool odd = lane & 1;
+    one = (odd ? v[1] : v[0]) + __shfl_xor_sync(kAll, odd ? v[0] : v[1], 1);
+  } else if constexpr (kCount == 4) {
+    const bool odd = lane & 1, high = lane & 2;
+    const float a = (odd ? v[1] : v[0]) + __shfl_xor_sync(kAll, odd ? v[0] : v[1], 1);
+    const float b = (odd ? v[3] : v[2]) + __shfl_xor_sync(kAll, odd ? v[2] : v[3], 1);
+    one = (high ? b : a) + __shfl_xor_sync(kAll, high ? a : b, 2);
+  }
 #pragma unroll
   for (uint32_t o = 1; o < 32; o *= 2) {
-    if (o >= tpr) break;
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+    if (kCount > 0 && o >= kCount) one += __shfl_xor_sync(kAll, one, o);
+    if (kNext) next += __shfl_xor_sync(kAll, next, o);
   }
-  if (tpr <= 32) return;
+  if (tpr == 32) {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) v[i] = __shfl_sync(kAll, one, i);
+    return;
+  }
   const uint32_t w = threadIdx.x / 32, warps = tpr / 32, first = w & ~(warps - 1);
-  if (lane_id() == 0)
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) room[w][i] = v[i];
-  asm volatile("bar.sync %0, %1;" ::"r"(1 + first / warps), "r"(tpr) : "memory");
-#pragma unroll
-  for (int i = 0; i < kCount; ++i) v[i] = room[first][i];
-  for (uint32_t k = 1; k < warps; ++k)
-#pragma unroll
-    for (int i = 0; i < kCount; ++i) v[i] += room[first + k][i];
+  if (kCount > 0 && lane < kCount) reinterpret_cast<float*>(room.sums + w)[lane] = one;
+  if (kNext && lane == 0) room.next[w] = next;
+  group_sync(tpr);
+  float4 all = make_float4(0.f, 0.f, 0.f, 0.f);
+  next = 0.f;
+  for (uint32_t k = 0; k < warps; ++k) {
+    if constexpr (kCount == 4) {
+      const float4 more = room.sums[first + k];
+      all.x += more.x; all.y += more.y; all.z += more.z; all.w += more.w;
+    } else if constexpr (kCount == 2) {
+      const float2 more = *reinterpret_cast<const float2*>(room.sums + first + k);
+      all.x += more.x; all.y += more.y;
+    }
+    if (kNext) next += room.next[first + k];
+  }
+  if constexpr (kCount > 0) { v[0] = all.x; v[1] = all.y; }
+  if constexpr (kCount > 2) { v[2] = all.z; v[3] = all.w; }
 }
 
-// Walks a run of rows, one worker's rows at a time; a group takes every groups-th of them.
-struct Walk {
-  uint32_t groups, group, m, t, left;              // the group's row: worker, token, rows of the segment from it on (0: none)
-  __device__ __forceinline__ void start(uint32_t begin, uint32_t end, uint32_t worker, uint32_t T) {
-    m = worker;
-    t = begin - worker * T + group;
-    left = end - begin > group ? end - begin - group : 0;
+// One worker's rows begin .. end of a run, of which the group takes every groups-th.
+struct Segment {
+  uint32_t m, t, turns, row, groups;
+  int left;                                        // rows from the group's next one on
+  const void* ids;
+  bool ids64;
+  __device__ __forceinline__ bool there(uint32_t k) const {          // is there a token k turns from the first?
+    return k * groups < (uint32_t)left && !is_empty(ids, ids64, row + k * groups);
   }
-  __device__ __forceinline__ bool in(uint32_t k) const { return k * groups < left; }     // is there a row k turns from the first?
 };
+__device__ __forceinline__ Segment segment(uint32_t begin, uint32_t end, uint32_t m, uint32_t T, uint32_t groups, uint32_t group, const void* ids, bool ids64) {
+  return {m, begin - m * T + group, (end - begin + groups - 1) / groups, begin + group, groups, end - begin > group ? (int)(end - begin - group) : 0, ids, ids64};
+}
 
-constexpr int kNormRoom = 200 * 1024;              // shared memory of the ring
+// The two kernels have the same course.  Turn k: wait until its row has arrived, send for row k + kStages - 1 (into the stage that
+// turn k - 1 read), take the row's sums.  With four stages or more the sum of row k + 1 is taken in turn k and travels with the
+// others, which leaves one exchange a row (65536 x 2048 bf16 with residual: see below); with fewer, waiting for row k + 1 would leave
+// too little on its way.
+constexpr int kNormRoom = 204 * 1024;              // shared memory of the ring
 template <typename X, int kVec, int kFill, bool kAdd>
-constexpr int kNormStage = Slots<X, kVec, kFill>::kStage * (kAdd ? 2 : 1);
+constexpr int kNormStage = Ring<X, kVec, kFill>::kStage * (kAdd ? 2 : 1);
 
 template <typename X, typename Y, int kVec, int kFill, bool kAdd>
 __global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, uint32_t tpr) {
-  using Slot = Slots<X, kVec, kFill>;
+  using RingX = Ring<X, kVec, kFill>;
   constexpr int kStage = kNormStage<X, kVec, kFill, kAdd>, kStages = stages_of(kStage, kNormRoom);
+  constexpr bool kAhead = kStages >= 4;
   extern __shared__ __align__(16) char ring[];
-  __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
+  __shared__ Room rooms[2];
   const uint32_t groups = kRowThreads / tpr;
   const Columns<kVec, kFill> at = {threadIdx.x % tpr * kVec, tpr * kVec, a.dim};
-  Walk walk = {groups, threadIdx.x / tpr};
-  char* slots = Slot::first(ring);
   const float over = 1.f / a.dim;
   const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
   float2 w[kPairs], b[kPairs];
   bool params = false;
   for (uint32_t begin = r0; begin < r1;) {
-    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T), turns = (end - begin + groups - 1) / groups;
-    walk.start(begin, end, m, a.T);
-    auto there = [&](uint32_t k) { return walk.in(k) && !is_empty(a.ids, a.ids64, begin + walk.group + k * groups); };
-    const X* ahead_x = row_of<X>(a.x, m, walk.t) + at.c;            // the row that is copied next
-    const X* ahead_a = kAdd ? row_of<X>(a.add, m, walk.t) + at.c : nullptr;
-    const X* row_x = ahead_x; const X* row_a = ahead_a;
-    Y* row_y = row_of<Y>(a.y, m, walk.t) + at.c;
-    X* row_t = kAdd ? row_of<X>(a.total, m, walk.t) + at.c : nullptr;
-    int to = 0, from = 0;
+    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T);
+    Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
+    RingX x, add;
+    x.start(a.x, m, s.t, groups, tpr, at);
+    if (kAdd) add.start(a.add, m, s.t, groups, tpr, at);
+    Y* row_y = row_of<Y>(a.y, m, s.t) + at.c;
+    X* row_t = kAdd ? row_of<X>(a.total, m, s.t) + at.c : nullptr;
+    char *to = ring, *from = ring;
+    auto after = [&](char* stage) { return stage + kStage == ring + kStages * kStage ? ring : stage + kStage; };
     auto issue = [&](bool real) {
       if (real) {
-        Slot::issue(slots + to * kStage, ahead_x, at);
-        if (kAdd) Slot::issue(slots + to * kStage + Slot::kStage, ahead_a, at);
+        x.copy(to, at, tpr);
+        if (kAdd) add.copy(to + RingX::kStage, at, tpr);
       }
       copy_commit();
-      ahead_x += groups * a.x.tok;
-      if (kAdd) ahead_a += groups * a.add.tok;
-      to = to + 1 == kStages ? 0 : to + 1;
+      x.advance();
+      if (kAdd) add.advance();
+      to = after(to);
     };
+    auto read = [&](const char* stage, float2* v, int ahead) {
+      x.read(stage, at, v, ahead);
+      if (!kAdd) return;
+      float2 u[kPairs];
+      add.read(stage + RingX::kStage, at, u, ahead);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) v[i] = rounded<X>(add2(v[i], u[i]));
+    };
+    group_sync(tpr);                                                 // the segment before is read: ring and rooms are free
     uint32_t flags = 0;                                              // bit k: the row k turns ahead is there
 #pragma unroll
     for (int k = 0; k + 1 < kStages; ++k) {
-      const bool real = there(k);
+      const bool real = s.there(k);
       issue(real);
       flags |= (uint32_t)real << k;
     }
-    bool coming = there(kStages - 1);
+    bool coming = s.there(kStages - 1);
     if (!params) {
       load_param(a.weight, a.param_bf16, at, 1.f, w);
       load_param(a.bias, a.param_bf16, at, 0.f, b);
       params = true;
     }
-    for (uint32_t k = 0; k < turns; ++k) {
-      issue(coming);                                                 // (into the slot that the turn before read)
-      flags |= (uint32_t)coming << (kStages - 1);
-      coming = there(k + kStages);
-      copy_wait<kStages - 1>();
-      const bool real = flags & 1;
-      flags >>= 1;
-      const char* stage = slots + from * kStage;
-      float2 v[kPairs];
-      if (real) {
-        Slot::read(stage, row_x, at, v);
-        if (kAdd) {
-          float2 u[kPairs];
-          Slot::read(stage + Slot::kStage, row_a, at, u);
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) {
-            v[i] = add2(v[i], u[i]);
-            v[i] = make_float2(to_f32(from_f32<X>(v[i].x)), to_f32(from_f32<X>(v[i].y)));
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = both(0.f);
+    float2 v[kPairs];
+    float sum = 0.f, none[1];
+    if (kAhead) {
+      copy_wait<kStages - 2>();
+      if (RingX::kShared) group_sync(tpr);
+      if (flags & 1) {
+        read(from, v, 0);
+        sum = total_of(v);
       }
-      if (kAdd && walk.in(k)) store_row(row_t, at, v);
-      float2 q = v[0];
-#pragma unroll
-      for (int i = 1; i < kPairs; ++i) q = add2(q, v[i]);
-      float sum[1] = {q.x + q.y};
-      group_sums(sum, room1, tpr);
-      centre(v, sum[0] * over, at);
+      group_sums<0, true>(none, sum, rooms[1], tpr);
+    }
+    for (uint32_t k = 0; k < s.turns; ++k) {
+      copy_wait<kAhead ? kStages - 3 : kStages - 2>();
+      if (RingX::kShared) group_sync(tpr);
+      issue(coming);
+      flags |= (uint32_t)coming << (kStages - 1);
+      coming = s.there(k + kStages);
+      const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
+      flags >>= 1;
+      clear(v);
+      if (real) read(from, v, 0);
+      if (kAdd && in) store_row(row_t, at, v);
+      if (!kAhead) {
+        sum = total_of(v);
+        group_sums<0, true>(none, sum, rooms[1], tpr);
+      }
+      centre(v, sum * over, at);
       float2 s0 = v[0], s1 = mul2(v[0], v[0]);
 #pragma unroll
       for (int i = 1; i < kPairs; ++i) {
         s0 = add2(s0, v[i]);
         s1 = fma2(v[i], v[i], s1);
       }
-      float s[2] = {s0.x + s0.y, s1.x + s1.y};
-      group_sums(s, room2, tpr);
-      const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
-      if (walk.in(k)) {
+      float sums[2] = {s0.x + s0.y, s1.x + s1.y};
+      sum = 0.f;
+      if (kAhead && more) {
+        float2 u[kPairs];
+        read(after(from), u, 1);
+        sum = total_of(u);
+      }
+      group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
+      const float shift = sums[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+      if (in) {
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = real ? fma2(mul2(add2(v[i], both(-shift)), both(rstd)), w[i], b[i]) : both(0.f);
+        for (int i = 0; i < kPairs; ++i) v[i] = fma2(mul2(add2(v[i], both(-shift)), both(rstd)), w[i], b[i]);
+        if (!real) clear(v);
         store_row(row_y, at, v);
       }
-      row_x += groups * a.x.tok;
       row_y += groups * a.y.tok;
-      if (kAdd) { row_a += groups * a.add.tok; row_t += groups * a.total.tok; }
-      from = from + 1 == kStages ? 0 : from + 1;
+      if (kAdd) row_t += groups * a.total.tok;
+      x.done();
+      if (kAdd) add.done();
+      from = after(from);
     }
     begin = end;
   }
 }
 
-constexpr int kGradRoom = 200 * 1024;
+constexpr int kGradRoom = 204 * 1024;
 template <typename D, typename X, int kVec, int kFill, bool kMore>
-constexpr int kGradStage = Slots<D, kVec, kFill>::kStage + Slots<X, kVec, kFill>::kStage * (kMore ? 2 : 1);
+constexpr int kGradStage = Ring<D, kVec, kFill>::kStage + Ring<X, kVec, kFill>::kStage * (kMore ? 2 : 1);
 constexpr int kFlushBytes = kRowThreads * 2 * 4 * (int)sizeof(float);
 
 template <typename D, typename X, int kVec, int kFill, bool kMore>
 __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a, uint32_t tpr) {
-  using SlotD = Slots<D, kVec, kFill>; using SlotX = Slots<X, kVec, kFill>;
+  using RingD = Ring<D, kVec, kFill>; using RingX = Ring<X, kVec, kFill>;
   constexpr int kStage = kGradStage<D, X, kVec, kFill, kMore>, kStages = stages_of(kStage, kGradRoom);
+  constexpr bool kAhead = kStages >= 4;
   extern __shared__ __align__(16) char ring[];
   float* flush = reinterpret_cast<float*>(ring + kStages * kStage);
-  __shared__ float room1[kRowWarps][4], room2[kRowWarps][4];
+  __shared__ Room rooms[2];
   const uint32_t groups = kRowThreads / tpr;
   const Columns<kVec, kFill> at = {threadIdx.x % tpr * kVec, tpr * kVec, a.dim};
-  Walk walk = {groups, threadIdx.x / tpr};
-  char* slots_d = SlotD::first(ring);
-  char* slots_x = SlotX::first(ring) + SlotD::kStage;
   const float over = 1.f / a.dim;
   grid_dependency_wait();
   const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
   float2 w[kPairs], dw[kPairs], db[kPairs];
   load_param(a.weight, a.weight_bf16, at, 1.f, w);
   for (uint32_t begin = r0; begin < r1;) {
-    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T), turns = (end - begin + groups - 1) / groups;
-    walk.start(begin, end, m, a.T);
-    auto there = [&](uint32_t k) { return walk.in(k) && !is_empty(a.ids, a.ids64, begin + walk.group + k * groups); };
-    const D* ahead_d = row_of<D>(a.dy, m, walk.t) + at.c;           // the row that is copied next
-    const X* ahead_x = row_of<X>(a.x, m, walk.t) + at.c;
-    const X* ahead_m = kMore ? row_of<X>(a.dtotal, m, walk.t) + at.c : nullptr;
-    const D* row_d = ahead_d; const X* row_x = ahead_x; const X* row_m = ahead_m;
-    X* row_o = row_of<X>(a.dx, m, walk.t) + at.c;
-    int to = 0, from = 0;
+    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T);
+    Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
+    RingD dy;
+    RingX x, dt;
+    dy.start(a.dy, m, s.t, groups, tpr, at);
+    x.start(a.x, m, s.t, groups, tpr, at);
+    if (kMore) dt.start(a.dtotal, m, s.t, groups, tpr, at);
+    X* row_o = row_of<X>(a.dx, m, s.t) + at.c;
+    char *to = ring, *from = ring;
+    auto after = [&](char* stage) { return stage + kStage == ring + kStages * kStage ? ring : stage + kStage; };
     auto issue = [&](bool real) {
       if (real) {
-        SlotD::issue(slots_d + to * kStage, ahead_d, at);
-        SlotX::issue(slots_x + to * kStage, ahead_x, at);
-        if (kMore) SlotX::issue(slots_x + to * kStage + SlotX::kStage, ahead_m, at);
+        x.copy(to, at, tpr);
+        dy.copy(to + RingX::kStage, at, tpr);
+        if (kMore) dt.copy(to + RingX::kStage + RingD::kStage, at, tpr);
       }
       copy_commit();
-      ahead_d += groups * a.dy.tok;
-      ahead_x += groups * a.x.tok;
-      if (kMore) ahead_m += groups * a.dtotal.tok;
-      to = to + 1 == kStages ? 0 : to + 1;
+      dy.advance();
+      x.advance();
+      if (kMore) dt.advance();
+      to = after(to);
     };
+    group_sync(tpr);                                                 // the segment before is read: ring and rooms are free
     uint32_t flags = 0;                                              // bit k: the row k turns ahead is there
 #pragma unroll
     for (int k = 0; k + 1 < kStages; ++k) {
-      const bool real = there(k);
+      const bool real = s.there(k);
       issue(real);
       flags |= (uint32_t)real << k;
     }
-    bool coming = there(kStages - 1);
-#pragma unroll
-    for (int i = 0; i < kPairs; ++i) dw[i] = db[i] = both(0.f);
-    for (uint32_t k = 0; k < turns; ++k) {
-      issue(coming);                                                 // (into the slot that the turn before read)
-      flags |= (uint32_t)coming << (kStages - 1);
-      coming = there(k + kStages);
-      copy_wait<kStages - 1>();
-      const bool real = flags & 1;
-      flags >>= 1;
-      float2 v[kPairs], g[kPairs];
-      if (real) {
-        SlotD::read(slots_d + from * kStage, row_d, at, g);
-        SlotX::read(slots_x + from * kStage, row_x, at, v);
-      } else {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = g[i] = both(0.f);
+    bool coming = s.there(kStages - 1);
+    clear(dw);
+    clear(db);
+    float2 v[kPairs], g[kPairs];
+    float sum = 0.f, none[1];
+    if (kAhead) {
+      copy_wait<kStages - 2>();
+      if (RingX::kShared) group_sync(tpr);
+      if (flags & 1) {
+        x.read(from, at, v);
+        sum = total_of(v);
       }
-      float2 q = v[0];
-#pragma unroll
-      for (int i = 1; i < kPairs; ++i) q = add2(q, v[i]);
-      float sum[1] = {q.x + q.y};
-      group_sums(sum, room1, tpr);
-      centre(v, sum[0] * over, at);
+      group_sums<0, true>(none, sum, rooms[1], tpr);
+    }
+    for (uint32_t k = 0; k < s.turns; ++k) {
+      copy_wait<kAhead ? kStages - 3 : kStages - 2>();
+      if (RingX::kShared) group_sync(tpr);
+      issue(coming);
+      flags |= (uint32_t)coming << (kStages - 1);
+      coming = s.there(k + kStages);
+      const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
+      flags >>= 1;
+      clear(v);
+      clear(g);
+      if (real) {
+        x.read(from, at, v);
+        dy.read(from + RingX::kStage, at, g);
+      }
+      if (!kAhead) {
+        sum = total_of(v);
+        group_sums<0, true>(none, sum, rooms[1], tpr);
+      }
+      centre(v, sum * over, at);
       float2 s0 = both(0.f), s1 = s0, s2 = s0, s3 = s0;
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {
@@ -407,10 +514,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
         s2 = add2(s2, gw);
         s3 = fma2(gw, v[i], s3);
       }
-      float s[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
-      group_sums(s, room2, tpr);
-      const float shift = s[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, s[1] * over), 0.f) + a.eps);
-      const float mg = s[2] * over, mgx = fmaf(-shift, s[2], s[3]) * over * rstd;
+      float sums[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
+      sum = 0.f;
+      if (kAhead && more) {
+        float2 u[kPairs];
+        x.read(after(from), at, u, 1);
+        sum = total_of(u);
+      }
+      group_sums<4, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
+      const float shift = sums[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+      const float mg = sums[2] * over, mgx = fmaf(-shift, sums[2], sums[3]) * over * rstd;
       if (real) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
@@ -421,22 +534,20 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
         }
         if (kMore) {
           float2 o[kPairs];
-          SlotX::read(slots_x + from * kStage + SlotX::kStage, row_m, at, o);
+          dt.read(from + RingX::kStage + RingD::kStage, at, o);
 #pragma unroll
           for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], o[i]);
         }
       }
-      if (a.dx.p != nullptr && walk.in(k)) {
-        if (!real)
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) v[i] = both(0.f);
+      if (a.dx.p != nullptr && in) {
+        if (!real) clear(v);
         store_row(row_o, at, v);
       }
-      row_d += groups * a.dy.tok;
-      row_x += groups * a.x.tok;
       row_o += groups * a.dx.tok;
-      if (kMore) row_m += groups * a.dtotal.tok;
-      from = from + 1 == kStages ? 0 : from + 1;
+      dy.done();
+      x.done();
+      if (kMore) dt.done();
+      from = after(from);
     }
     if (a.partial != nullptr) {                                      // the groups' sums, four entries a thread at a time
       float* out = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad;
@@ -480,20 +591,20 @@ __global__ void __launch_bounds__(kThreads) norm_long_kernel(NormArgs a) {
     if (is_empty(a.ids, a.ids64, r)) {
       const float zero[kVec] = {};
       for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
-        store_pack<Y, kVec>(y + c, zero);
-        if (total != nullptr) store_pack<X, kVec>(total + c, zero);
+        store_floats<Y, kVec>(y + c, zero);
+        if (total != nullptr) store_floats<X, kVec>(total + c, zero);
       }
       continue;
     }
     double sum[1] = {};
     for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
       float v[kVec], u[kVec];
-      load_pack<X, kVec>(x + c, v);
+      load_floats<X, kVec>(x + c, v);
       if (a.add.p != nullptr) {
-        load_pack<X, kVec>(row_of<X>(a.add, m, t) + c, u);
+        load_floats<X, kVec>(row_of<X>(a.add, m, t) + c, u);
 #pragma unroll
         for (int e = 0; e < kVec; ++e) v[e] = to_f32(from_f32<X>(v[e] + u[e]));
-        store_pack<X, kVec>(total + c, v);
+        store_floats<X, kVec>(total + c, v);
       }
 #pragma unroll
       for (int e = 0; e < kVec; ++e) sum[0] += v[e];
@@ -504,7 +615,7 @@ __global__ void __launch_bounds__(kThreads) norm_long_kernel(NormArgs a) {
     double sums[2] = {};
     for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
       float v[kVec];
-      load_pack<X, kVec>(x + c, v);
+      load_floats<X, kVec>(x + c, v);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const double d = v[e] - mean;
@@ -517,11 +628,11 @@ __global__ void __launch_bounds__(kThreads) norm_long_kernel(NormArgs a) {
     const float shift = (float)rest, rstd = (float)(1.0 / sqrt(fmax(sums[1] / a.dim - rest * rest, 0.0) + a.eps));
     for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
       float v[kVec];
-      load_pack<X, kVec>(x + c, v);
+      load_floats<X, kVec>(x + c, v);
 #pragma unroll
       for (int e = 0; e < kVec; ++e)
         v[e] = fmaf((v[e] - mean - shift) * rstd, param_at(a.weight, a.param_bf16, c + e, 1.f), param_at(a.bias, a.param_bf16, c + e, 0.f));
-      store_pack<Y, kVec>(y + c, v);
+      store_floats<Y, kVec>(y + c, v);
     }
   }
 }
@@ -538,7 +649,7 @@ __global__ void __launch_bounds__(kThreads) stats_long_kernel(NormGradArgs a) {
     double sum[1] = {};
     for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
       float v[kVec];
-      load_pack<X, kVec>(x + c, v);
+      load_floats<X, kVec>(x + c, v);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) sum[0] += v[e];
     }
@@ -547,8 +658,8 @@ __global__ void __launch_bounds__(kThreads) stats_long_kernel(NormGradArgs a) {
     double s[4] = {};
     for (uint32_t c = threadIdx.x * kVec; c < a.dim; c += kThreads * kVec) {
       float v[kVec], g[kVec];
-      load_pack<X, kVec>(x + c, v);
-      load_pack<D, kVec>(dy + c, g);
+      load_floats<X, kVec>(x + c, v);
+      load_floats<D, kVec>(dy + c, g);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const double d = v[e] - mean, w = g[e] * param_at(a.weight, a.weight_bf16, c + e, 1.f);
@@ -582,9 +693,9 @@ __global__ void __launch_bounds__(kThreads) grad_long_kernel(NormGradArgs a) {
     if (!is_empty(a.ids, a.ids64, r)) {
       const float4 s = a.stats[2 * (size_t)r], q = a.stats[2 * (size_t)r + 1];
       float x[kVec], g[kVec];
-      load_pack<X, kVec>(row_of<X>(a.x, m, t) + c, x);
-      load_pack<D, kVec>(row_of<D>(a.dy, m, t) + c, g);
-      if (a.dtotal.p != nullptr) load_pack<X, kVec>(row_of<X>(a.dtotal, m, t) + c, o);
+      load_floats<X, kVec>(row_of<X>(a.x, m, t) + c, x);
+      load_floats<D, kVec>(row_of<D>(a.dy, m, t) + c, g);
+      if (a.dtotal.p != nullptr) load_floats<X, kVec>(row_of<X>(a.dtotal, m, t) + c, o);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         const float xhat = (x[e] - s.x - s.y) * s.z;
@@ -593,11 +704,11 @@ __global__ void __launch_bounds__(kThreads) grad_long_kernel(NormGradArgs a) {
         o[e] = fmaf(s.z, fmaf(-xhat, q.y, fmaf(g[e], w[e], -q.x)), o[e]);
       }
     }
-    if (a.dx.p != nullptr) store_pack<X, kVec>(row_of<X>(a.dx, m, t) + c, o);
+    if (a.dx.p != nullptr) store_floats<X, kVec>(row_of<X>(a.dx, m, t) + c, o);
     if (a.partial != nullptr && (r + 1 == r1 || t + 1 == a.T)) {
       float* to = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad + c;
-      store_pack<float, kVec>(to, dw);
-      store_pack<float, kVec>(to + a.pad, db);
+      store_floats<float, kVec>(to, dw);
+      store_floats<float, kVec>(to + a.pad, db);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) dw[e] = db[e] = 0.f;
     }
@@ -657,14 +768,19 @@ bool norm_grad_layout(int M, uint64_t T, uint64_t dim, NormGradLayout* L) {
   return true;
 }
 
-// widest access of rows: 4 entries where base and distances of every tensor allow it
+// widest access of rows: 8 (16-bit types only) or 4 entries where base and distances of every tensor allow it, else single ones
 struct Given { Rows r; int dtype; };
 int row_width(const Given* g, int n, uint64_t dim, int M, uint64_t T) {
-  int v = dim % 4 == 0 && dim > kEach / 2 ? 4 : 1;
-  for (int i = 0; i < n; ++i)
-    if (g[i].r.p != nullptr && allowed(v, g[i].r.p, g[i].dtype, T > 1 ? g[i].r.tok : 0, M > 1 ? g[i].r.worker : 0) != v) v = 1;
-  return v;
+  int v = dim % 8 == 0 ? 8 : dim % 4 == 0 && dim > kEach / 2 ? 4 : 1;
+  for (int i = 0; i < n; ++i) {
+    if (g[i].r.p == nullptr) continue;
+    if (g[i].dtype != S3GD_BF16 && v == 8) v = 4;
+    v = allowed(v, g[i].r.p, g[i].dtype, T > 1 ? g[i].r.tok : 0, M > 1 ? g[i].r.worker : 0);
+  }
+  return v >= 4 ? v : 1;
 }
+// entries from the first to behind the last
+void measure(Rows* r, int M, uint64_t T, uint64_t dim) { r->last = (M - 1) * r->worker + (long long)(T - 1) * r->tok + (long long)dim; }
 // inputs may repeat a row (distance 0); what is written must not overlap itself
 bool readable(const Rows& r, int dtype) { return is_aligned(r.p, dtype_bytes(dtype)) && r.tok >= 0 && r.worker >= 0; }
 bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
@@ -675,17 +791,19 @@ bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
   // workers one behind the other, or interleaved (each token's row of all workers side by side)
   return worker >= (T > 1 ? (T - 1) * tok : 0) + dim || (worker >= dim && (T == 1 || tok >= (uint64_t)(M - 1) * worker + dim));
 }
-// threads of a row: the fewest that hold it
-uint32_t threads_per_row(uint64_t dim) {
-  uint32_t n = 1;
+// threads of a row: the fewest that hold it, but four where groups copy rows together
+uint32_t threads_per_row(uint64_t dim, int vec) {
+  uint32_t n = vec == 1 ? 4 : 1;
   while (n * kEach < dim) n *= 2;
   return n;
 }
-// f is called with the width of an access and how a row fills its group, as types
-template <typename F>
+// f is called with the width of an access and how a row fills its group, as types.  16-bit rows alone may be read eight entries at a time.
+template <bool kWide, typename F>
 cudaError_t by_row_form(int vec, uint64_t dim, F f) {
-  if (vec == 1) return dim <= kEach / 2 ? f(Width<1>(), Width<kAnyDim>()) : f(Width<1>(), Width<kMoreThanHalf>());
-  return dim == threads_per_row(dim) * kEach ? f(Width<4>(), Width<kFullDim>()) : f(Width<4>(), Width<kMoreThanHalf>());
+  const uint32_t tpr = threads_per_row(dim, vec);
+  if (vec == 1) return dim <= tpr * kEach / 2 ? f(Width<1>(), Width<kAnyDim>()) : f(Width<1>(), Width<kMoreThanHalf>());
+  if (kWide && vec == 8) return dim == tpr * kEach ? f(Width<kWide ? 8 : 4>(), Width<kFullDim>()) : f(Width<kWide ? 8 : 4>(), Width<kMoreThanHalf>());
+  return dim == tpr * kEach ? f(Width<4>(), Width<kFullDim>()) : f(Width<4>(), Width<kMoreThanHalf>());
 }
 template <typename X, typename Y, int kVec, int kFill, bool kAdd>
 cudaError_t enqueue_norm_rows(NormArgs a, cudaStream_t st) {
@@ -696,7 +814,7 @@ cudaError_t enqueue_norm_rows(NormArgs a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const uint32_t runs = sm_count();
   a.per = (a.N + runs - 1) / runs;
-  kernel<<<(a.N + a.per - 1) / a.per, kRowThreads, kBytes, st>>>(a, threads_per_row(a.dim));
+  kernel<<<(a.N + a.per - 1) / a.per, kRowThreads, kBytes, st>>>(a, threads_per_row(a.dim, kVec));
   return cudaGetLastError();
 }
 template <typename D, typename X, int kVec, int kFill, bool kMore>
@@ -706,10 +824,10 @@ cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   auto kernel = grad_row_kernel<D, X, kVec, kFill, kMore>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
-  return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, threads_per_row(a.dim));
+  return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, threads_per_row(a.dim, kVec));
 }
 template <typename F>
-cudaError_t by_row_width(int v, F f) { return v == 4 ? f(Width<4>()) : f(Width<1>()); }
+cudaError_t by_row_width(int v, F f) { return v >= 4 ? f(Width<4>()) : f(Width<1>()); }
 
 }  // namespace
 }  // namespace s3gd
@@ -738,6 +856,7 @@ extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_str
   a.weight = opt_weight; a.bias = opt_bias; a.param_bf16 = param_dtype == S3GD_BF16;
   a.ids = opt_ids; a.ids64 = ids_dtype == S3GD_I64;
   a.T = (uint32_t)T; a.N = (uint32_t)((uint64_t)M * T); a.dim = (uint32_t)dim; a.eps = eps;
+  for (Rows* r : {&a.x, &a.add}) measure(r, M, T, dim);
   const Given all[] = {{a.x, x_dtype}, {a.add, x_dtype}, {a.total, x_dtype}, {a.y, y_dtype}};
   const int vec = row_width(all, 4, dim, M, T);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
@@ -745,7 +864,7 @@ extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_str
   const cudaError_t e = by_real(x_dtype, [&](auto xt) { return by_real(y_dtype, [&](auto yt) {
     using X = decltype(xt); using Y = decltype(yt);
     if (dim <= kMaxRowDim)
-      return by_row_form(vec, dim, [&](auto v, auto f) {
+      return by_row_form<sizeof(X) == 2 && sizeof(Y) == 2>(vec, dim, [&](auto v, auto f) {
         constexpr int kVec = decltype(v)::value, kFill = decltype(f)::value;
         return opt_add != nullptr ? enqueue_norm_rows<X, Y, kVec, kFill, true>(a, st) : enqueue_norm_rows<X, Y, kVec, kFill, false>(a, st);
       });
@@ -801,16 +920,17 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (a.N > 0) {
+    for (Rows* r : {&a.dy, &a.x, &a.dtotal}) measure(r, M, T, dim);
     const Given all[] = {{a.dy, dy_dtype}, {a.x, x_dtype}, {a.dtotal, x_dtype}, {a.dx, x_dtype}};
     const int vec = row_width(all, 4, dim, M, T);
     const unsigned most = 8u * sm_count(), grid = a.N < most ? a.N : most;
-    const unsigned tiles = (unsigned)((dim + kThreads * vec - 1) / (kThreads * vec));
+    const unsigned wide = vec >= 4 ? 4 : 1, tiles = (unsigned)((dim + kThreads * wide - 1) / (kThreads * wide));
     if (tiles > 65535) return S3GD_ERR_INVALID_ARG;
     count_launch(dim > kMaxRowDim ? 2 : 1);
     e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) {
       using D = decltype(dt); using X = decltype(xt);
       if (dim <= kMaxRowDim)
-        return by_row_form(vec, dim, [&](auto v, auto f) {
+        return by_row_form<sizeof(D) == 2 && sizeof(X) == 2>(vec, dim, [&](auto v, auto f) {
           constexpr int kVec = decltype(v)::value, kFill = decltype(f)::value;
           return opt_dtotal != nullptr ? enqueue_grad_rows<D, X, kVec, kFill, true>(a, st) : enqueue_grad_rows<D, X, kVec, kFill, false>(a, st);
         });

@@ -43,6 +43,34 @@ __device__ __forceinline__ void store_pack(T* p, const float* v) {
   *reinterpret_cast<Pack<T, kVec>*>(p) = o;
 }
 
+// kVec neighbouring entries as 32-bit floats, and back (rounded to nearest); 16-bit entries two at a time
+template <typename T, int kVec>
+__device__ __forceinline__ void load_floats(const T* p, float* v) {
+  if constexpr (sizeof(T) == 2 && kVec % 2 == 0) {
+    const Pack<uint32_t, kVec / 2> o = *reinterpret_cast<const Pack<uint32_t, kVec / 2>*>(p);
+#pragma unroll
+    for (int i = 0; i < kVec / 2; ++i) {
+      v[2 * i] = __uint_as_float(o.v[i] << 16);
+      v[2 * i + 1] = __uint_as_float(o.v[i] & 0xffff0000u);
+    }
+  } else {
+    const Pack<T, kVec> o = *reinterpret_cast<const Pack<T, kVec>*>(p);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = to_f32(o.v[e]);
+  }
+}
+template <typename T, int kVec>
+__device__ __forceinline__ void store_floats(T* p, const float* v) {
+  if constexpr (sizeof(T) == 2 && kVec % 2 == 0) {
+    Pack<__nv_bfloat162, kVec / 2> o;
+#pragma unroll
+    for (int i = 0; i < kVec / 2; ++i) o.v[i] = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<Pack<__nv_bfloat162, kVec / 2>*>(p) = o;
+  } else {
+    store_pack<T, kVec>(p, v);
+  }
+}
+
 // the widest access that base and distances allow, no wider than what keeps 32 lanes busy on `dim` columns
 inline int widest(uint64_t dim) {
   int v = 8;
