@@ -84,8 +84,7 @@ constexpr int kEach = 16, kPairs = kEach / 2;
 constexpr uint64_t kMaxRowDim = (uint64_t)kRowThreads * kEach;
 
 template <int kBytes>
-__device__ __forceinline__ void copy_async(void* to, const void* from) {
-  const uint32_t at = (uint32_t)__cvta_generic_to_shared(to);
+__device__ __forceinline__ void copy_async(uint32_t at, const void* from) {   // at: shared memory
   if (kBytes == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(at), "l"(from) : "memory");
   else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(at), "l"(from), "n"(kBytes) : "memory");
 }
@@ -170,32 +169,34 @@ struct Ring {
     if (kShared) own = threadIdx.x / tpr * (tpr * kEach * (uint32_t)sizeof(T) + 16);
     else { own = threadIdx.x * kBytes; next += at.c; }
   }
-  __device__ __forceinline__ void copy(char* stage, const Cols& at, uint32_t tpr) const {
+  // stage: offset of the tensor's part in the ring
+  __device__ __forceinline__ void copy(char* ring, uint32_t stage, const Cols& at, uint32_t tpr) const {
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring) + stage + own;
     if (kShared) {
-      const uintptr_t from = reinterpret_cast<uintptr_t>(next), to = from + at.dim * sizeof(T), first = from & ~(uintptr_t)15;
-      for (uint32_t i = at.c * 16; first + i < to; i += tpr * 16) {
-        if (first + i >= begin && first + i + 16 <= end) copy_async<16>(stage + own + i, reinterpret_cast<const void*>(first + i));
+      const uintptr_t from = reinterpret_cast<uintptr_t>(next), past = from + at.dim * sizeof(T), first = from & ~(uintptr_t)15;
+      for (uint32_t i = at.c * 16; first + i < past; i += tpr * 16) {
+        if (first + i >= begin && first + i + 16 <= end) copy_async<16>(to + i, reinterpret_cast<const void*>(first + i));
         else                                       // at the ends of the tensor: only its own entries
           for (uint32_t e = 0; e < 16; e += sizeof(T))
-            if (first + i + e >= from && first + i + e < to)
-              *reinterpret_cast<T*>(stage + own + i + e) = *reinterpret_cast<const T*>(first + i + e);
+            if (first + i + e >= from && first + i + e < past)
+              *reinterpret_cast<T*>(ring + stage + own + i + e) = *reinterpret_cast<const T*>(first + i + e);
       }
     } else {
 #pragma unroll
       for (int k = 0; k < kChunks; ++k)
-        if (at.has(k)) copy_async<kShared ? 16 : kBytes>(stage + own + k * kRowThreads * kBytes, next + k * at.step);
+        if (at.has(k)) copy_async<kShared ? 16 : kBytes>(to + k * kRowThreads * kBytes, next + k * at.step);
     }
   }
   __device__ __forceinline__ void advance() { next += turn; }
   __device__ __forceinline__ void done() { if (kShared) low += (uint32_t)turn * (uint32_t)sizeof(T); }
   // ahead: 1 for the row after the one that is read next
-  __device__ __forceinline__ void read(const char* stage, const Cols& at, float2* v, int ahead = 0) const {
+  __device__ __forceinline__ void read(const char* ring, uint32_t stage, const Cols& at, float2* v, int ahead = 0) const {
     float* f = reinterpret_cast<float*>(v);
-    const char* from = stage + own;
+    uint32_t from = stage + own;
     if (kShared) from += ((low + (ahead ? (uint32_t)turn * (uint32_t)sizeof(T) : 0u)) & 15) + at.c * (uint32_t)sizeof(T);
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      const T* chunk = reinterpret_cast<const T*>(from + (kShared ? k * at.step * (uint32_t)sizeof(T) : k * kRowThreads * kBytes));
+      const T* chunk = reinterpret_cast<const T*>(ring + from + (kShared ? k * at.step * (uint32_t)sizeof(T) : k * kRowThreads * kBytes));
       if (at.has(k)) load_floats<T, kVec>(chunk, f + k * kVec);
       else
 #pragma unroll
@@ -329,23 +330,23 @@ __global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, ui
     if (kAdd) add.start(a.add, m, s.t, groups, tpr, at);
     Y* row_y = row_of<Y>(a.y, m, s.t) + at.c;
     X* row_t = kAdd ? row_of<X>(a.total, m, s.t) + at.c : nullptr;
-    char *to = ring, *from = ring;
-    auto after = [&](char* stage) { return stage + kStage == ring + kStages * kStage ? ring : stage + kStage; };
+    uint32_t to = 0, from = 0;
+    auto after = [](uint32_t stage) { return stage == (kStages - 1) * kStage ? 0u : stage + kStage; };
     auto issue = [&](bool real) {
       if (real) {
-        x.copy(to, at, tpr);
-        if (kAdd) add.copy(to + RingX::kStage, at, tpr);
+        x.copy(ring, to, at, tpr);
+        if (kAdd) add.copy(ring, to + RingX::kStage, at, tpr);
       }
       copy_commit();
       x.advance();
       if (kAdd) add.advance();
       to = after(to);
     };
-    auto read = [&](const char* stage, float2* v, int ahead) {
-      x.read(stage, at, v, ahead);
+    auto read = [&](uint32_t stage, float2* v, int ahead) {
+      x.read(ring, stage, at, v, ahead);
       if (!kAdd) return;
       float2 u[kPairs];
-      add.read(stage + RingX::kStage, at, u, ahead);
+      add.read(ring, stage + RingX::kStage, at, u, ahead);
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) v[i] = rounded<X>(add2(v[i], u[i]));
     };
@@ -363,15 +364,14 @@ __global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, ui
       load_param(a.bias, a.param_bf16, at, 0.f, b);
       params = true;
     }
-    float2 v[kPairs];
+    float2 v[kPairs], u[kPairs];                                     // this row, the next one
     float sum = 0.f, none[1];
     if (kAhead) {
       copy_wait<kStages - 2>();
       if (RingX::kShared) group_sync(tpr);
-      if (flags & 1) {
-        read(from, v, 0);
-        sum = total_of(v);
-      }
+      if (flags & 1) read(from, u, 0);
+      else clear(u);
+      sum = total_of(u);
       group_sums<0, true>(none, sum, rooms[1], tpr);
     }
     for (uint32_t k = 0; k < s.turns; ++k) {
@@ -382,13 +382,18 @@ __global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, ui
       coming = s.there(k + kStages);
       const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
       flags >>= 1;
-      clear(v);
-      if (real) read(from, v, 0);
-      if (kAdd && in) store_row(row_t, at, v);
-      if (!kAhead) {
+      if (kAhead) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = u[i];
+        if (more) read(after(from), u, 1);
+        else clear(u);
+      } else {
+        if (real) read(from, v, 0);
+        else clear(v);
         sum = total_of(v);
         group_sums<0, true>(none, sum, rooms[1], tpr);
       }
+      if (kAdd && in) store_row(row_t, at, v);
       centre(v, sum * over, at);
       float2 s0 = v[0], s1 = mul2(v[0], v[0]);
 #pragma unroll
@@ -397,14 +402,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, ui
         s1 = fma2(v[i], v[i], s1);
       }
       float sums[2] = {s0.x + s0.y, s1.x + s1.y};
-      sum = 0.f;
-      if (kAhead && more) {
-        float2 u[kPairs];
-        read(after(from), u, 1);
-        sum = total_of(u);
-      }
+      if (kAhead) sum = total_of(u);
       group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-      const float shift = sums[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+      const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
       if (in) {
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) v[i] = fma2(mul2(add2(v[i], both(-shift)), both(rstd)), w[i], b[i]);
@@ -450,13 +450,13 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
     x.start(a.x, m, s.t, groups, tpr, at);
     if (kMore) dt.start(a.dtotal, m, s.t, groups, tpr, at);
     X* row_o = row_of<X>(a.dx, m, s.t) + at.c;
-    char *to = ring, *from = ring;
-    auto after = [&](char* stage) { return stage + kStage == ring + kStages * kStage ? ring : stage + kStage; };
+    uint32_t to = 0, from = 0;
+    auto after = [](uint32_t stage) { return stage == (kStages - 1) * kStage ? 0u : stage + kStage; };
     auto issue = [&](bool real) {
       if (real) {
-        x.copy(to, at, tpr);
-        dy.copy(to + RingX::kStage, at, tpr);
-        if (kMore) dt.copy(to + RingX::kStage + RingD::kStage, at, tpr);
+        x.copy(ring, to, at, tpr);
+        dy.copy(ring, to + RingX::kStage, at, tpr);
+        if (kMore) dt.copy(ring, to + RingX::kStage + RingD::kStage, at, tpr);
       }
       copy_commit();
       dy.advance();
@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
       copy_wait<kStages - 2>();
       if (RingX::kShared) group_sync(tpr);
       if (flags & 1) {
-        x.read(from, at, v);
+        x.read(ring, from, at, v);
         sum = total_of(v);
       }
       group_sums<0, true>(none, sum, rooms[1], tpr);
@@ -494,11 +494,12 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
       coming = s.there(k + kStages);
       const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
       flags >>= 1;
-      clear(v);
-      clear(g);
       if (real) {
-        x.read(from, at, v);
-        dy.read(from + RingX::kStage, at, g);
+        x.read(ring, from, at, v);
+        dy.read(ring, from + RingX::kStage, at, g);
+      } else {
+        clear(v);
+        clear(g);
       }
       if (!kAhead) {
         sum = total_of(v);
@@ -518,11 +519,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
       sum = 0.f;
       if (kAhead && more) {
         float2 u[kPairs];
-        x.read(after(from), at, u, 1);
+        x.read(ring, after(from), at, u, 1);
         sum = total_of(u);
       }
       group_sums<4, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-      const float shift = sums[0] * over, rstd = __frsqrt_rn(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+      const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
       const float mg = sums[2] * over, mgx = fmaf(-shift, sums[2], sums[3]) * over * rstd;
       if (real) {
 #pragma unroll
@@ -534,7 +535,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
         }
         if (kMore) {
           float2 o[kPairs];
-          dt.read(from + RingX::kStage + RingD::kStage, at, o);
+          dt.read(ring, from + RingX::kStage + RingD::kStage, at, o);
 #pragma unroll
           for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], o[i]);
         }
