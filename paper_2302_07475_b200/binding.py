@@ -9,7 +9,9 @@ from __future__ import annotations
 
 import array
 import ctypes
+import operator
 import os
+from itertools import chain, repeat
 from typing import Optional
 
 import torch
@@ -772,16 +774,54 @@ def s3gd_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Ten
 
     x, y (and add, total) are [T, dim] or [M, T, dim] with contiguous rows, or contiguous [..., dim]; fp32 or bf16, add and total
     of x's type.  ids (shape of x without its last axis): rows whose id is negative become zero."""
+    args = _norm_args(x, y, weight, bias, eps, ids, add, total)
+    index = x.get_device()
+    if _current_device() == index:
+        code = load().s3gd_layer_norm(*args, _stream_of(index))
+    else:
+        with _on(x):
+            code = load().s3gd_layer_norm(*args, _stream_of(index))
+    if code:
+        _check("s3gd_layer_norm", code)
+
+
+def _like(t: torch.Tensor, index: int, shape) -> bool:
+    return t.get_device() == index and t.is_contiguous() and t.shape == shape
+
+
+def _vector(t: Optional[torch.Tensor], index: int, dim: int):
+    """The address of a contiguous [dim] on the device; None where it is not given; -1 where it is something else."""
+    if t is None:
+        return None
+    return t.data_ptr() if t.get_device() == index and t.dim() == 1 and t.numel() == dim and t.is_contiguous() else -1
+
+
+def _norm_args(x, y, weight, bias, eps, ids, add, total):
+    """Arguments of s3gd_layer_norm.  A call for a few tokens is over in some microseconds: contiguous tensors are looked at once here,
+    everything else, and what is wrong, below."""
+    try:
+        index, shape, kind = x.get_device(), x.shape, x.dtype
+        dim = shape[-1]
+        w, b = _vector(weight, index, dim), _vector(bias, index, dim)
+        xd, yd = _REAL_CODES[kind], _REAL_CODES[y.dtype]
+        pd = _REAL_CODES[weight.dtype if weight is not None else bias.dtype] if w or b else 0
+        if (index >= 0 and dim > 0 and w != -1 and b != -1 and x.is_contiguous() and _like(y, index, shape)
+                and (weight is None or bias is None or weight.dtype is bias.dtype)
+                and ((add is None and total is None) or (add.dtype is kind and total.dtype is kind and _like(add, index, shape) and _like(total, index, shape)))
+                and (ids is None or _like(ids, index, shape[:-1]))):
+            i, it = (None, 3) if ids is None else (ids.data_ptr(), _INDEX_CODES[ids.dtype])
+            p, q = (None, None) if add is None else (add.data_ptr(), total.data_ptr())
+            return (x.data_ptr(), xd, dim, 0, p, dim, 0, q, dim, 0, w, b, pd, i, it, 1, x.numel() // dim, dim, eps, y.data_ptr(), yd, dim, 0)
+    except (AttributeError, KeyError, IndexError):
+        pass
     if not (isinstance(x, torch.Tensor) and x.is_cuda):
         raise TypeError("x must be a CUDA tensor")
     index = x.get_device()
     _norm_device(index, y=y, weight=weight, bias=bias, ids=ids, add=add, total=total)
-    try:
-        xd, yd = _REAL_CODES[x.dtype], _REAL_CODES[y.dtype]
-        pd = 0 if weight is None and bias is None else _REAL_CODES[(bias if weight is None else weight).dtype]
-    except KeyError:
-        for t, name in ((x, "x"), (y, "y"), (weight, "weight"), (bias, "bias")):
-            _of(t, _REAL, name)
+    for t, name in ((x, "x"), (y, "y"), (weight, "weight"), (bias, "bias")):
+        _of(t, _REAL, name)
+    if y is None:
+        raise TypeError("y must be a CUDA tensor")
     if weight is not None and bias is not None and weight.dtype != bias.dtype:
         raise TypeError(f"weight and bias must have one dtype, not {weight.dtype} and {bias.dtype}")
     if (add is None) != (total is None):
@@ -794,15 +834,10 @@ def s3gd_layer_norm(x: torch.Tensor, y: torch.Tensor, weight: Optional[torch.Ten
     as_, aw = _norm_strides(add, x, "add")
     ts, tw = _norm_strides(total, x, "total")
     idp, idt = _norm_ids(ids, x)
-    args = (x.data_ptr(), xd, xs, xw, None if add is None else add.data_ptr(), as_, aw, None if total is None else total.data_ptr(), ts, tw,
-            _param(weight, dim, "weight"), _param(bias, dim, "bias"), pd, idp, idt, M, T, dim, eps, y.data_ptr(), yd, ys, yw)
-    if _current_device() == index:
-        code = load().s3gd_layer_norm(*args, _stream_of(index))
-    else:
-        with _on(x):
-            code = load().s3gd_layer_norm(*args, _stream_of(index))
-    if code:
-        _check("s3gd_layer_norm", code)
+    given = bias if weight is None else weight
+    return (x.data_ptr(), _REAL_CODES[x.dtype], xs, xw, None if add is None else add.data_ptr(), as_, aw,
+            None if total is None else total.data_ptr(), ts, tw, _param(weight, dim, "weight"), _param(bias, dim, "bias"),
+            0 if given is None else _REAL_CODES[given.dtype], idp, idt, M, T, dim, eps, y.data_ptr(), _REAL_CODES[y.dtype], ys, yw)
 
 
 def s3gd_layer_norm_grad_workspace_bytes(M: int, T: int, dim: int) -> int:
@@ -841,23 +876,50 @@ def s3gd_layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, dx: Optional[torch.T
     dy, x, dx, dtotal are [T, dim] or [M, T, dim]; x is what was normalised (total, where there was one); dx and dtotal have its
     type.  dweight and dbias are [M, dim] (columns of the workers' rows of a gradient buffer) or [dim] for one worker, of one
     type; accumulate adds to what they hold.  dx, or dweight and dbias, may be None; dx may be dy, x or dtotal itself."""
+    args = _norm_grad_args(dy, x, dx, weight, dweight, dbias, ws, eps, ids, dtotal, accumulate)
+    index = x.get_device()
+    if _current_device() == index:
+        code = load().s3gd_layer_norm_grad(*args, _stream_of(index))
+    else:
+        with _on(x):
+            code = load().s3gd_layer_norm_grad(*args, _stream_of(index))
+    if code:
+        _check("s3gd_layer_norm_grad", code)
+
+
+def _norm_grad_args(dy, x, dx, weight, dweight, dbias, ws, eps, ids, dtotal, accumulate):
+    """Arguments of s3gd_layer_norm_grad, by the same two ways as _norm_args."""
+    try:
+        index, shape, kind = x.get_device(), x.shape, x.dtype
+        M, T, dim = shape if len(shape) == 3 else (1, *shape)
+        w, rows = _vector(weight, index, dim), (M, dim)
+        stride = dweight.stride(0)
+        if (index >= 0 and w != -1 and x.is_contiguous() and _like(dy, index, shape) and _like(dx, index, shape) and dx.dtype is kind
+                and (dtotal is None or (_like(dtotal, index, shape) and dtotal.dtype is kind)) and (ids is None or _like(ids, index, shape[:-1]))
+                and dweight.get_device() == index and dbias.get_device() == index and dweight.shape == rows and dbias.shape == rows
+                and (dim == 1 or dweight.stride(1) == 1 == dbias.stride(1)) and dbias.stride(0) == stride and dweight.dtype is dbias.dtype
+                and ws.get_device() == index and ws.dtype is torch.uint8 and ws.is_contiguous()):
+            i, it = (None, 3) if ids is None else (ids.data_ptr(), _INDEX_CODES[ids.dtype])
+            return (dy.data_ptr(), _REAL_CODES[dy.dtype], dim, T * dim, x.data_ptr(), _REAL_CODES[kind], dim, T * dim,
+                    None if dtotal is None else dtotal.data_ptr(), dim, T * dim, w, 0 if w is None else _REAL_CODES[weight.dtype], i, it, M, T, dim,
+                    eps, dx.data_ptr(), dim, T * dim, dweight.data_ptr(), dbias.data_ptr(), _REAL_CODES[dweight.dtype], stride if M > 1 else dim,
+                    accumulate, ws.data_ptr(), ws.numel())
+    except (AttributeError, KeyError, IndexError, ValueError):
+        pass
     if not (isinstance(x, torch.Tensor) and x.is_cuda):
         raise TypeError("x must be a CUDA tensor")
     index = x.get_device()
     w = _ptr(ws, torch.uint8, name="ws")
+    if dy is None or w is None:
+        raise TypeError("dy and ws must be CUDA tensors")
     _norm_device(index, dy=dy, dx=dx, weight=weight, dweight=dweight, dbias=dbias, ws=ws, ids=ids, dtotal=dtotal)
-    given = dbias if dweight is None else dweight
-    try:
-        dyd, xd = _REAL_CODES[dy.dtype], _REAL_CODES[x.dtype]
-        wd = 0 if weight is None else _REAL_CODES[weight.dtype]
-        gd = 0 if given is None else _REAL_CODES[given.dtype]
-    except KeyError:
-        for t, name in ((dy, "dy"), (x, "x"), (weight, "weight"), (dweight, "dweight"), (dbias, "dbias")):
-            _of(t, _REAL, name)
+    for t, name in ((dy, "dy"), (x, "x"), (weight, "weight"), (dweight, "dweight"), (dbias, "dbias")):
+        _of(t, _REAL, name)
     if dweight is not None and dbias is not None and dweight.dtype != dbias.dtype:
         raise TypeError(f"dweight and dbias must have one dtype, not {dweight.dtype} and {dbias.dtype}")
     _of(dx, (x.dtype,), "dx")
     _of(dtotal, (x.dtype,), "dtotal")
+    given = dbias if dweight is None else dweight
     if x.dim() not in (2, 3):
         raise ValueError("x must be [T, dim] or [M, T, dim]")
     if dx is None and (given is None or dtotal is not None):
@@ -872,16 +934,9 @@ def s3gd_layer_norm_grad(dy: torch.Tensor, x: torch.Tensor, dx: Optional[torch.T
     bp, bstride = _worker_rows(dbias, M, dim, x.dim() == 3, "dbias")
     if dweight is not None and dbias is not None and stride != bstride:
         raise ValueError(f"dweight and dbias must have one distance from worker to worker, not {stride} and {bstride}")
-    args = (dy.data_ptr(), dyd, ds, dw, x.data_ptr(), xd, xs, xw, None if dtotal is None else dtotal.data_ptr(), ts, tw,
-            _param(weight, dim, "weight"), wd, idp, idt, M, T, dim, eps, None if dx is None else dx.data_ptr(), os, ow, wp, bp, gd,
-            stride or bstride, accumulate, w, ws.numel())
-    if _current_device() == index:
-        code = load().s3gd_layer_norm_grad(*args, _stream_of(index))
-    else:
-        with _on(x):
-            code = load().s3gd_layer_norm_grad(*args, _stream_of(index))
-    if code:
-        _check("s3gd_layer_norm_grad", code)
+    return (dy.data_ptr(), _REAL_CODES[dy.dtype], ds, dw, x.data_ptr(), _REAL_CODES[x.dtype], xs, xw, None if dtotal is None else dtotal.data_ptr(), ts, tw,
+            _param(weight, dim, "weight"), 0 if weight is None else _REAL_CODES[weight.dtype], idp, idt, M, T, dim, eps,
+            None if dx is None else dx.data_ptr(), os, ow, wp, bp, 0 if given is None else _REAL_CODES[given.dtype], stride or bstride, accumulate, w, ws.numel())
 
 
 def s3gd_clip_workspace_bytes(M: int) -> int:
@@ -907,6 +962,35 @@ def _in_one_piece(shape, strides) -> bool:
     return True
 
 
+_T = torch.Tensor
+_dtype_of = operator.attrgetter("dtype")
+
+
+def _plain_parts(grads, outs, index: int, M: int, several: bool):
+    """As _parts for lists of contiguous gradients of one type (and outputs of one type that lie alike); None for others.
+
+    A list has hundreds of tensors and its kernels take some ten microseconds: each question is put to all tensors at once."""
+    dtypes, devices = set(map(_dtype_of, grads)), set(map(_T.get_device, grads))
+    sizes = list(map(_T.size, grads))
+    if len(dtypes) != 1 or devices != {index} or not all(map(_T.is_contiguous, grads)) or (several and not all(s and s[0] == M for s in sizes)):
+        return None
+    code = _REAL_CODES[dtypes.pop()]
+    entries, pointers = [n // M for n in map(_T.numel, grads)] if M > 1 else list(map(_T.numel, grads)), list(map(_T.data_ptr, grads))
+    if outs is grads:
+        return array.array("Q", chain.from_iterable(zip(pointers, pointers, entries, entries, entries, repeat(code | code << 32)))), len(pointers)
+    dtypes = set(map(_dtype_of, outs))
+    if len(dtypes) != 1 or set(map(_T.get_device, outs)) != devices or sizes != list(map(_T.size, outs)):
+        return None
+    apart = entries
+    if not all(map(_T.is_contiguous, outs)):
+        strides = list(map(_T.stride, outs))
+        if not several or any(a[1:] != b[1:] for a, b in zip(strides, map(_T.stride, grads))):
+            return None
+        apart = [s[0] for s in strides]
+    code |= _REAL_CODES[dtypes.pop()] << 32
+    return array.array("Q", chain.from_iterable(zip(pointers, map(_T.data_ptr, outs), entries, entries, apart, repeat(code)))), len(pointers)
+
+
 def _parts(grads, out, index: int, M: int, several: bool):
     """The tensors as an array of s3gd_part, and their number."""
     if isinstance(grads, torch.Tensor):
@@ -915,6 +999,12 @@ def _parts(grads, out, index: int, M: int, several: bool):
     outs = grads if out is None else list(out)
     if len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
+    try:
+        plain = _plain_parts(grads, outs, index, M, several)
+    except (TypeError, AttributeError, KeyError):        # something that is no tensor, or of another type: named below
+        plain = None
+    if plain is not None:
+        return plain
     packed, first = array.array("Q"), 1 if several else 0
     for i, (g, o) in enumerate(zip(grads, outs)):
         try:

@@ -46,26 +46,85 @@ __device__ __forceinline__ uint32_t part_of(const Parts<kMax>& parts, uint32_t c
 
 // entries of a 16-byte access, and how many entries the address lies behind such a boundary
 template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
+
+// Accesses of 16, 8, 4 or 2 bytes with a hint to the L2 on what will be read again.
+__device__ __forceinline__ uint64_t keep_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+__device__ __forceinline__ uint64_t drop_policy() {
+  uint64_t p;
+  asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+  return p;
+}
+template <typename P>
+__device__ __forceinline__ P load_hint(const void* from, uint64_t policy) {
+  P v;
+  if constexpr (sizeof(P) == 16) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(from), "l"(policy) : "memory");
+  } else if constexpr (sizeof(P) == 8) {
+    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+    asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v2.u32 {%0,%1}, [%2], %3;" : "=r"(w[0]), "=r"(w[1]) : "l"(from), "l"(policy) : "memory");
+  } else {
+    v = *static_cast<const P*>(from);
+  }
+  return v;
+}
+template <typename P>
+__device__ __forceinline__ void store_hint(void* to, const P& v, uint64_t policy) {
+  if constexpr (sizeof(P) == 16) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+    asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(policy) : "memory");
+  } else if constexpr (sizeof(P) == 8) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
+    asm volatile("st.global.L2::cache_hint.v2.u32 [%0], {%1,%2}, %3;" ::"l"(to), "r"(w[0]), "r"(w[1]), "l"(policy) : "memory");
+  } else {
+    *static_cast<P*>(to) = v;
+  }
+}
 template <typename T>
 __device__ __forceinline__ uint32_t behind(const T* p, int v) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) % v; }
 
-template <typename T>
-__device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t tile) {
-  constexpr int kVec = kWide<T>;
-  const long long begin = (long long)tile * kTile - behind(g, kVec);
+// Squares of up to eight neighbours are added in 32 bits (off by 8 half steps of their sum at most), everything else in 64: one
+// conversion for eight entries (where the conversions would otherwise take as long as the reads).  Sums that may have lost small
+// squares, or overflowed, are taken again in 64 bits.
+constexpr float kLeast = 8.2718061e-25f, kMost = 8.5070592e37f;                  // 2^-80, 2^126
+template <int kN>
+__device__ __forceinline__ double squares(const float* v) {
+  float s = v[0] * v[0];
+#pragma unroll
+  for (int e = 1; e < kN; ++e) s = fmaf(v[e], v[e], s);
+  if (s >= kLeast && s <= kMost) return s;
   double sum = 0;
 #pragma unroll
-  for (uint32_t i = 0; i < kTile / (kThreads * kVec); ++i) {
-    const long long at = begin + (i * kThreads + threadIdx.x) * kVec;
-    if (at >= 0 && (uint64_t)at + kVec <= n) {
-      const Pack<T, kVec> v = *reinterpret_cast<const Pack<T, kVec>*>(g + at);
+  for (int e = 0; e < kN; ++e) sum += (double)v[e] * v[e];
+  return sum;
+}
+template <typename T>
+__device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t tile, uint64_t policy) {
+  constexpr int kVec = kWide<T>, kLoads = kTile / (kThreads * kVec);
+  const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec;
+  double sum = 0;
+  if (begin >= 0 && (uint64_t)begin + kTile <= n) {
+    Pack<T, kVec> raw[kLoads];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) { const double d = to_f32(v.v[e]); sum += d * d; }
-    } else {
-      for (int e = 0; e < kVec; ++e)
-        if (at + e >= 0 && (uint64_t)(at + e) < n) { const double d = to_f32(g[at + e]); sum += d * d; }
+    for (int i = 0; i < kLoads; ++i) raw[i] = load_hint<Pack<T, kVec>>(g + at + i * kThreads * kVec, policy);
+#pragma unroll
+    for (int i = 0; i < kLoads * kVec / 8; ++i) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; e += kVec) load_floats<T, kVec>(raw[i * 8 / kVec + e / kVec].v, v + e);
+      sum += squares<8>(v);
     }
+    return sum;
   }
+  for (int i = 0; i < kLoads; ++i)
+    for (int e = 0; e < kVec; ++e) {
+      const long long c = at + i * kThreads * kVec + e;
+      if (c >= 0 && (uint64_t)c < n) { const double d = to_f32(g[c]); sum += d * d; }
+    }
   return sum;
 }
 
@@ -91,14 +150,15 @@ template <int kMax>
 __global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a) {
   grid_dependency_wait();
   const uint32_t m = blockIdx.y, begin = blockIdx.x * a.per, end = min(begin + a.per, a.tiles);
+  const uint64_t policy = keep_policy();
   double sum = 0;
   uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
   for (uint32_t tile = begin; tile < end; ++tile) {
     while (k + 1 < a.count && parts.p[k + 1].first_tile <= tile) ++k;
     const Part& p = parts.p[k];
     const uint32_t in = tile - p.first_tile;
-    sum += p.src_bf16 ? tile_squares(static_cast<const __nv_bfloat16*>(p.src) + m * p.src_worker, p.n, in)
-                      : tile_squares(static_cast<const float*>(p.src) + m * p.src_worker, p.n, in);
+    sum += p.src_bf16 ? tile_squares(static_cast<const __nv_bfloat16*>(p.src) + m * p.src_worker, p.n, in, policy)
+                      : tile_squares(static_cast<const float*>(p.src) + m * p.src_worker, p.n, in, policy);
   }
   sum = cta_sum(sum);
   double* to = a.partial + (size_t)m * a.runs + blockIdx.x;
@@ -114,21 +174,33 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const ClipArgs a) {
 
 template <typename S, typename D, int kVec>
 __device__ __forceinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
-  const long long begin = (long long)tile * kTile - behind(g, kVec);
-#pragma unroll 8
-  for (uint32_t i = 0; i < kTile / (kThreads * kVec); ++i) {
-    const long long at = begin + (i * kThreads + threadIdx.x) * kVec;
-    if (at >= 0 && (uint64_t)at + kVec <= n) {
-      const Pack<S, kVec> v = *reinterpret_cast<const Pack<S, kVec>*>(g + at);
-      float o[kVec];
+  constexpr int kLoads = kTile / (kThreads * kVec), kBatch = kLoads < 8 ? kLoads : 8;
+  const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec;
+  if (begin >= 0 && (uint64_t)begin + kTile <= n) {
+    const uint64_t policy = drop_policy();
+#pragma unroll 1
+    for (int b = 0; b < kLoads; b += kBatch) {
+      Pack<S, kVec> raw[kBatch];
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) o[e] = __fmul_rn(to_f32(v.v[e]), c);
-      store_pack<D, kVec>(out + at, o);
-    } else {
-      for (int e = 0; e < kVec; ++e)
-        if (at + e >= 0 && (uint64_t)(at + e) < n) out[at + e] = from_f32<D>(__fmul_rn(to_f32(g[at + e]), c));
+      for (int i = 0; i < kBatch; ++i) raw[i] = load_hint<Pack<S, kVec>>(g + at + (b + i) * kThreads * kVec, policy);
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        float v[kVec];
+        load_floats<S, kVec>(raw[i].v, v);
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[e] = __fmul_rn(v[e], c);
+        Pack<D, kVec> o;
+        store_floats<D, kVec>(o.v, v);
+        store_hint(out + at + (b + i) * kThreads * kVec, o, policy);
+      }
     }
+    return;
   }
+  for (int i = 0; i < kLoads; ++i)
+    for (int e = 0; e < kVec; ++e) {
+      const long long j = at + i * kThreads * kVec + e;
+      if (j >= 0 && (uint64_t)j < n) out[j] = from_f32<D>(__fmul_rn(to_f32(g[j]), c));
+    }
 }
 template <typename S, typename D>
 __device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t tile, float c) {
