@@ -76,8 +76,8 @@ __device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCo
 }
 
 // ------------------------------------------------------------------ rows that threads hold in registers
-// A group of `tpr` threads (a power of two; part of a warp, a warp, or several) takes a row, kEach entries a thread: of neighbouring
-// kVec entries, `tpr * kVec` apart.  Rows to come are on their way into a ring in shared memory meanwhile (cp.async; empty places are
+// A group of `tpr` threads (part of a warp, a power of two, or whole warps) takes a row, kEach entries a thread: chunks of
+// neighbouring kVec entries.  Rows to come are on their way into a ring in shared memory meanwhile (cp.async; empty places are
 // not read).
 constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
 constexpr int kEach = 16, kPairs = kEach / 2;
@@ -128,53 +128,66 @@ __device__ __forceinline__ float total_of(const float2* v) {
   return q.x + q.y;
 }
 
-// Which of its chunks of kVec columns a thread has.  A row is longer than half of what its group can hold, but for very short rows
-// (kAnyDim), so only the upper half of the chunks is ever missing; none where the row fills the group (kFullDim).
-enum Fill : int { kAnyDim = 0, kMoreThanHalf = 1, kFullDim = 2 };
-template <int kVec, int kFill>
+// The columns of a thread: kEach / kVec chunks, `step` apart.  Rows of more than 256 entries (kTiles) are dealt out evenly to the warps
+// of the group, up to 512 to a warp, with a step that is known beforehand; shorter ones take a part of a warp, the smallest that holds
+// them.  Either way the lower half of the chunks is there in every thread, but for a few entries by themselves (kTiny).
+enum Form : int { kTiny = 0, kShort = 1, kTiles = 2, kFullTiles = 3 };      // kFullTiles: 512 columns to every warp
+template <int kVec, int kForm>
 struct Columns {
   static constexpr int kChunks = kEach / kVec;
-  uint32_t c, step, dim;
-  __device__ __forceinline__ bool has(int k) const {
-    if (kFill == kFullDim || (kFill == kMoreThanHalf && k < kChunks / 2)) return true;
-    return c + k * step < dim;
-  }
+  uint32_t c, any_step, limit;                     // first column; step; column behind the last one of the warp (of the row)
+  __device__ __forceinline__ uint32_t step() const { return kForm >= kTiles ? 32 * kVec : any_step; }
+  __device__ __forceinline__ bool has(int k) const { return kForm == kFullTiles || (kForm != kTiny && k < kChunks / 2) || c + k * step() < limit; }
 };
+// columns of a warp: the row's, dealt out evenly
+template <int kVec>
+__device__ __forceinline__ uint32_t tile_columns(uint32_t tpr, uint32_t dim) {
+  const uint32_t warps = tpr / 32;
+  return (dim + warps * kVec - 1) / (warps * kVec) * kVec;
+}
+template <int kVec, int kForm>
+__device__ __forceinline__ Columns<kVec, kForm> columns(uint32_t tpr, uint32_t dim) {
+  const uint32_t l = threadIdx.x % tpr;
+  if (kForm < kTiles) return {l * kVec, tpr * kVec, dim};
+  const uint32_t tile = tile_columns<kVec>(tpr, dim), first = l / 32 * tile;
+  return {first + l % 32 * kVec, 32 * kVec, min(first + tile, dim)};
+}
 
 __device__ __forceinline__ void group_sync(uint32_t tpr) {
   if (tpr <= 32) __syncwarp();
-  else asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.x / tpr), "r"(tpr) : "memory");
+  else asm volatile("bar.sync %0, %1;" ::"r"(1 + threadIdx.x / tpr), "r"(tpr) : "memory");     // at most eight groups
 }
 
 // A tensor's part of a ring stage.  Rows that wide accesses fit (kVec > 1): every thread copies the entries that it will read itself,
 // and nobody waits for anybody.  Other rows (kVec 1): the group copies the row's 16-byte granules, whatever lies in them beside the
 // row, and reads entries after a barrier.
-template <typename T, int kVec, int kFill>
+template <typename T, int kVec>
 struct Ring {
-  using Cols = Columns<kVec, kFill>;
   static constexpr bool kShared = kVec == 1;
   static constexpr int kBytes = kVec * (int)sizeof(T), kChunks = kEach / kVec;
   static constexpr int kStage = kEach * (int)sizeof(T) * kRowThreads + (kShared ? kRowThreads / 4 * 16 : 0);
   const T* next;                                   // the group's row that is copied next, from the thread's first column (kShared: from the first)
   long long turn;                                  // entries from a row to the group's next
   uintptr_t begin, end;                            // what the tensor's entries lie between
-  uint32_t own, low;                               // where the thread's (group's) entries begin in a stage; address of the row that is read next
+  uint32_t own, low, bytes;                        // where the thread's (group's) entries begin in a stage; address of the row that is read next; of a row
 
-  __device__ __forceinline__ void start(const Rows& r, uint32_t m, uint32_t t, uint32_t groups, uint32_t tpr, const Cols& at) {
+  __device__ __forceinline__ void start(const Rows& r, uint32_t m, uint32_t t, uint32_t groups, uint32_t tpr, uint32_t c, uint32_t dim) {
+    bytes = dim * (uint32_t)sizeof(T);
     next = row_of<T>(r, m, t);
     turn = groups * r.tok;
     begin = reinterpret_cast<uintptr_t>(r.p);
     end = reinterpret_cast<uintptr_t>(static_cast<const T*>(r.p) + r.last);
     low = (uint32_t)reinterpret_cast<uintptr_t>(next);
     if (kShared) own = threadIdx.x / tpr * (tpr * kEach * (uint32_t)sizeof(T) + 16);
-    else { own = threadIdx.x * kBytes; next += at.c; }
+    else { own = threadIdx.x * kBytes; next += c; }
   }
   // stage: offset of the tensor's part in the ring
+  template <typename Cols>
   __device__ __forceinline__ void copy(char* ring, uint32_t stage, const Cols& at, uint32_t tpr) const {
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(ring) + stage + own;
     if (kShared) {
-      const uintptr_t from = reinterpret_cast<uintptr_t>(next), past = from + at.dim * sizeof(T), first = from & ~(uintptr_t)15;
-      for (uint32_t i = at.c * 16; first + i < past; i += tpr * 16) {
+      const uintptr_t from = reinterpret_cast<uintptr_t>(next), past = from + bytes, first = from & ~(uintptr_t)15;
+      for (uint32_t i = threadIdx.x % tpr * 16; first + i < past; i += tpr * 16) {
         if (first + i >= begin && first + i + 16 <= end) copy_async<16>(to + i, reinterpret_cast<const void*>(first + i));
         else                                       // at the ends of the tensor: only its own entries
           for (uint32_t e = 0; e < 16; e += sizeof(T))
@@ -184,19 +197,20 @@ struct Ring {
     } else {
 #pragma unroll
       for (int k = 0; k < kChunks; ++k)
-        if (at.has(k)) copy_async<kShared ? 16 : kBytes>(to + k * kRowThreads * kBytes, next + k * at.step);
+        if (at.has(k)) copy_async<kShared ? 16 : kBytes>(to + k * kRowThreads * kBytes, next + k * at.step());
     }
   }
   __device__ __forceinline__ void advance() { next += turn; }
   __device__ __forceinline__ void done() { if (kShared) low += (uint32_t)turn * (uint32_t)sizeof(T); }
   // ahead: 1 for the row after the one that is read next
+  template <typename Cols>
   __device__ __forceinline__ void read(const char* ring, uint32_t stage, const Cols& at, float2* v, int ahead = 0) const {
     float* f = reinterpret_cast<float*>(v);
     uint32_t from = stage + own;
     if (kShared) from += ((low + (ahead ? (uint32_t)turn * (uint32_t)sizeof(T) : 0u)) & 15) + at.c * (uint32_t)sizeof(T);
 #pragma unroll
     for (int k = 0; k < kChunks; ++k) {
-      const T* chunk = reinterpret_cast<const T*>(ring + from + (kShared ? k * at.step * (uint32_t)sizeof(T) : k * kRowThreads * kBytes));
+      const T* chunk = reinterpret_cast<const T*>(ring + from + (kShared ? k * at.step() * (uint32_t)sizeof(T) : k * kRowThreads * kBytes));
       if (at.has(k)) load_floats<T, kVec>(chunk, f + k * kVec);
       else
 #pragma unroll
@@ -206,23 +220,23 @@ struct Ring {
 };
 __host__ __device__ constexpr int stages_of(int bytes, int room) { return room / bytes > 5 ? 5 : room / bytes; }
 
-template <typename T, int kVec, int kFill>
-__device__ __forceinline__ void store_row(T* row, const Columns<kVec, kFill>& at, const float2* v) {
+template <typename T, int kVec, int kForm>
+__device__ __forceinline__ void store_row(T* row, const Columns<kVec, kForm>& at, const float2* v) {
 #pragma unroll
   for (int k = 0; k < kEach / kVec; ++k)
-    if (at.has(k)) store_floats<T, kVec>(row + k * at.step, reinterpret_cast<const float*>(v) + k * kVec);
+    if (at.has(k)) store_floats<T, kVec>(row + k * at.step(), reinterpret_cast<const float*>(v) + k * kVec);
 }
-template <int kVec, int kFill>
-__device__ __forceinline__ void load_param(const void* p, bool bf16, const Columns<kVec, kFill>& at, float otherwise, float2* v) {
+template <int kVec, int kForm>
+__device__ __forceinline__ void load_param(const void* p, bool bf16, const Columns<kVec, kForm>& at, float otherwise, float2* v) {
 #pragma unroll
   for (int k = 0; k < kEach / kVec; ++k)
 #pragma unroll
     for (int e = 0; e < kVec; ++e)
-      reinterpret_cast<float*>(v)[k * kVec + e] = at.has(k) ? param_at(p, bf16, at.c + k * at.step + e, otherwise) : 0.f;
+      reinterpret_cast<float*>(v)[k * kVec + e] = at.has(k) ? param_at(p, bf16, at.c + k * at.step() + e, otherwise) : 0.f;
 }
 // v - mean, zero in columns that the thread does not have
-template <int kVec, int kFill>
-__device__ __forceinline__ void centre(float2* v, float mean, const Columns<kVec, kFill>& at) {
+template <int kVec, int kForm>
+__device__ __forceinline__ void centre(float2* v, float mean, const Columns<kVec, kForm>& at) {
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], both(-mean));
 #pragma unroll
@@ -267,7 +281,7 @@ __device__ __forceinline__ void group_sums(float (&v)[kCount == 0 ? 1 : kCount],
     for (int i = 0; i < kCount; ++i) v[i] = __shfl_sync(kAll, one, i);
     return;
   }
-  const uint32_t w = threadIdx.x / 32, warps = tpr / 32, first = w & ~(warps - 1);
+  const uint32_t w = threadIdx.x / 32, warps = tpr / 32, first = threadIdx.x / tpr * warps;
   if (kCount > 0 && lane < kCount) reinterpret_cast<float*>(room.sums + w)[lane] = one;
   if (kNext && lane == 0) room.next[w] = next;
   group_sync(tpr);
@@ -306,250 +320,264 @@ __device__ __forceinline__ Segment segment(uint32_t begin, uint32_t end, uint32_
 // others, which leaves one exchange a row (65536 x 2048 bf16 with residual: see below); with fewer, waiting for row k + 1 would leave
 // too little on its way.
 constexpr int kNormRoom = 204 * 1024;              // shared memory of the ring
-template <typename X, int kVec, int kFill, bool kAdd>
-constexpr int kNormStage = Ring<X, kVec, kFill>::kStage * (kAdd ? 2 : 1);
+template <typename X, int kVec, bool kAdd>
+constexpr int kNormStage = Ring<X, kVec>::kStage * (kAdd ? 2 : 1);
 
-template <typename X, typename Y, int kVec, int kFill, bool kAdd>
-__global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, uint32_t tpr) {
-  using RingX = Ring<X, kVec, kFill>;
-  constexpr int kStage = kNormStage<X, kVec, kFill, kAdd>, kStages = stages_of(kStage, kNormRoom);
+// Rows begin .. end of worker m.
+template <typename X, typename Y, int kVec, bool kAdd, typename Cols>
+__device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uint32_t end, uint32_t m, uint32_t tpr, const Cols& at, char* ring,
+                                          Room* rooms, const float2* w, const float2* b) {
+  using RingX = Ring<X, kVec>;
+  constexpr int kStage = kNormStage<X, kVec, kAdd>, kStages = stages_of(kStage, kNormRoom);
   constexpr bool kAhead = kStages >= 4;
-  extern __shared__ __align__(16) char ring[];
-  __shared__ Room rooms[2];
   const uint32_t groups = kRowThreads / tpr;
-  const Columns<kVec, kFill> at = {threadIdx.x % tpr * kVec, tpr * kVec, a.dim};
   const float over = 1.f / a.dim;
-  const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
-  float2 w[kPairs], b[kPairs];
-  bool params = false;
-  for (uint32_t begin = r0; begin < r1;) {
-    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T);
-    Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
-    RingX x, add;
-    x.start(a.x, m, s.t, groups, tpr, at);
-    if (kAdd) add.start(a.add, m, s.t, groups, tpr, at);
-    Y* row_y = row_of<Y>(a.y, m, s.t) + at.c;
-    X* row_t = kAdd ? row_of<X>(a.total, m, s.t) + at.c : nullptr;
-    uint32_t to = 0, from = 0;
-    auto after = [](uint32_t stage) { return stage == (kStages - 1) * kStage ? 0u : stage + kStage; };
-    auto issue = [&](bool real) {
-      if (real) {
-        x.copy(ring, to, at, tpr);
-        if (kAdd) add.copy(ring, to + RingX::kStage, at, tpr);
-      }
-      copy_commit();
-      x.advance();
-      if (kAdd) add.advance();
-      to = after(to);
-    };
-    auto read = [&](uint32_t stage, float2* v, int ahead) {
-      x.read(ring, stage, at, v, ahead);
-      if (!kAdd) return;
-      float2 u[kPairs];
-      add.read(ring, stage + RingX::kStage, at, u, ahead);
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) v[i] = rounded<X>(add2(v[i], u[i]));
-    };
-    group_sync(tpr);                                                 // the segment before is read: ring and rooms are free
-    uint32_t flags = 0;                                              // bit k: the row k turns ahead is there
-#pragma unroll
-    for (int k = 0; k + 1 < kStages; ++k) {
-      const bool real = s.there(k);
-      issue(real);
-      flags |= (uint32_t)real << k;
+  Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
+  RingX x, add;
+  x.start(a.x, m, s.t, groups, tpr, at.c, a.dim);
+  if (kAdd) add.start(a.add, m, s.t, groups, tpr, at.c, a.dim);
+  Y* row_y = row_of<Y>(a.y, m, s.t) + at.c;
+  X* row_t = kAdd ? row_of<X>(a.total, m, s.t) + at.c : nullptr;
+  uint32_t to = 0, from = 0;
+  auto after = [](uint32_t stage) { return stage == (kStages - 1) * kStage ? 0u : stage + kStage; };
+  auto issue = [&](bool real) {
+    if (real) {
+      x.copy(ring, to, at, tpr);
+      if (kAdd) add.copy(ring, to + RingX::kStage, at, tpr);
     }
-    bool coming = s.there(kStages - 1);
-    if (!params) {
-      load_param(a.weight, a.param_bf16, at, 1.f, w);
-      load_param(a.bias, a.param_bf16, at, 0.f, b);
-      params = true;
-    }
-    float2 v[kPairs], u[kPairs];                                     // this row, the next one
-    float sum = 0.f, none[1];
+    copy_commit();
+    x.advance();
+    if (kAdd) add.advance();
+    to = after(to);
+  };
+  auto read = [&](uint32_t stage, float2* v, int ahead) {
+    x.read(ring, stage, at, v, ahead);
+    if (!kAdd) return;
+    float2 u[kPairs];
+    add.read(ring, stage + RingX::kStage, at, u, ahead);
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) v[i] = rounded<X>(add2(v[i], u[i]));
+  };
+  group_sync(tpr);                                                   // the segment before is read: ring and rooms are free
+  uint32_t flags = 0;                                                // bit k: the row k turns ahead is there
+#pragma unroll
+  for (int k = 0; k + 1 < kStages; ++k) {
+    const bool real = s.there(k);
+    issue(real);
+    flags |= (uint32_t)real << k;
+  }
+  bool coming = s.there(kStages - 1);
+  float2 v[kPairs], u[kPairs];                                       // this row, the next one
+  float sum = 0.f, none[1];
+  if (kAhead) {
+    copy_wait<kStages - 2>();
+    if (RingX::kShared) group_sync(tpr);
+    if (flags & 1) read(from, u, 0);
+    else clear(u);
+    sum = total_of(u);
+    group_sums<0, true>(none, sum, rooms[1], tpr);
+  }
+  for (uint32_t k = 0; k < s.turns; ++k) {
+    copy_wait<kAhead ? kStages - 3 : kStages - 2>();
+    if (RingX::kShared) group_sync(tpr);
+    issue(coming);
+    flags |= (uint32_t)coming << (kStages - 1);
+    coming = s.there(k + kStages);
+    const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
+    flags >>= 1;
     if (kAhead) {
-      copy_wait<kStages - 2>();
-      if (RingX::kShared) group_sync(tpr);
-      if (flags & 1) read(from, u, 0);
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) v[i] = u[i];
+      if (more) read(after(from), u, 1);
       else clear(u);
-      sum = total_of(u);
+    } else {
+      if (real) read(from, v, 0);
+      else clear(v);
+      sum = total_of(v);
       group_sums<0, true>(none, sum, rooms[1], tpr);
     }
-    for (uint32_t k = 0; k < s.turns; ++k) {
-      copy_wait<kAhead ? kStages - 3 : kStages - 2>();
-      if (RingX::kShared) group_sync(tpr);
-      issue(coming);
-      flags |= (uint32_t)coming << (kStages - 1);
-      coming = s.there(k + kStages);
-      const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
-      flags >>= 1;
-      if (kAhead) {
+    if (kAdd && in) store_row(row_t, at, v);
+    centre(v, sum * over, at);
+    float2 s0 = v[0], s1 = mul2(v[0], v[0]);
 #pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = u[i];
-        if (more) read(after(from), u, 1);
-        else clear(u);
-      } else {
-        if (real) read(from, v, 0);
-        else clear(v);
-        sum = total_of(v);
-        group_sums<0, true>(none, sum, rooms[1], tpr);
-      }
-      if (kAdd && in) store_row(row_t, at, v);
-      centre(v, sum * over, at);
-      float2 s0 = v[0], s1 = mul2(v[0], v[0]);
-#pragma unroll
-      for (int i = 1; i < kPairs; ++i) {
-        s0 = add2(s0, v[i]);
-        s1 = fma2(v[i], v[i], s1);
-      }
-      float sums[2] = {s0.x + s0.y, s1.x + s1.y};
-      if (kAhead) sum = total_of(u);
-      group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-      const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
-      if (in) {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) v[i] = fma2(mul2(add2(v[i], both(-shift)), both(rstd)), w[i], b[i]);
-        if (!real) clear(v);
-        store_row(row_y, at, v);
-      }
-      row_y += groups * a.y.tok;
-      if (kAdd) row_t += groups * a.total.tok;
-      x.done();
-      if (kAdd) add.done();
-      from = after(from);
+    for (int i = 1; i < kPairs; ++i) {
+      s0 = add2(s0, v[i]);
+      s1 = fma2(v[i], v[i], s1);
     }
+    float sums[2] = {s0.x + s0.y, s1.x + s1.y};
+    if (kAhead) sum = total_of(u);
+    group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
+    const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+    if (in) {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) v[i] = fma2(fma2(v[i], both(rstd), both(-shift * rstd)), w[i], b[i]);
+      if (!real) clear(v);
+      store_row(row_y, at, v);
+    }
+    row_y += groups * a.y.tok;
+    if (kAdd) row_t += groups * a.total.tok;
+    x.done();
+    if (kAdd) add.done();
+    from = after(from);
+  }
+}
+
+template <typename X, typename Y, int kVec, int kForm, bool kAdd>
+__global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, uint32_t tpr) {
+  extern __shared__ __align__(16) char ring[];
+  __shared__ Room rooms[2];
+  if (threadIdx.x / tpr >= kRowThreads / tpr) return;                // warps that make no group
+  const Columns<kVec, kForm> at = columns<kVec, kForm>(tpr, a.dim);
+  const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
+  float2 w[kPairs], b[kPairs];
+  load_param(a.weight, a.param_bf16, at, 1.f, w);
+  load_param(a.bias, a.param_bf16, at, 0.f, b);
+  for (uint32_t begin = r0; begin < r1;) {                           // one worker's rows at a time
+    const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T);
+    norm_rows<X, Y, kVec, kAdd>(a, begin, end, m, tpr, at, ring, rooms, w, b);
     begin = end;
   }
 }
 
 constexpr int kGradRoom = 204 * 1024;
-template <typename D, typename X, int kVec, int kFill, bool kMore>
-constexpr int kGradStage = Ring<D, kVec, kFill>::kStage + Ring<X, kVec, kFill>::kStage * (kMore ? 2 : 1);
+template <typename D, typename X, int kVec, bool kMore>
+constexpr int kGradStage = Ring<D, kVec>::kStage + Ring<X, kVec>::kStage * (kMore ? 2 : 1);
 constexpr int kFlushBytes = kRowThreads * 2 * 4 * (int)sizeof(float);
 
-template <typename D, typename X, int kVec, int kFill, bool kMore>
+// Rows begin .. end of worker m; the group's sums of the weight gradients.
+template <typename D, typename X, int kVec, bool kMore, typename Cols>
+__device__ __forceinline__ void grad_rows(const NormGradArgs& a, uint32_t begin, uint32_t end, uint32_t m, uint32_t tpr, const Cols& at, char* ring,
+                                          Room* rooms, const float2* w, float2* dw, float2* db) {
+  using RingD = Ring<D, kVec>; using RingX = Ring<X, kVec>;
+  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kStages = stages_of(kStage, kGradRoom);
+  constexpr bool kAhead = kStages >= 4 && kVec > 1;
+  const uint32_t groups = kRowThreads / tpr;
+  const float over = 1.f / a.dim;
+  Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
+  RingD dy;
+  RingX x, dt;
+  dy.start(a.dy, m, s.t, groups, tpr, at.c, a.dim);
+  x.start(a.x, m, s.t, groups, tpr, at.c, a.dim);
+  if (kMore) dt.start(a.dtotal, m, s.t, groups, tpr, at.c, a.dim);
+  X* row_o = row_of<X>(a.dx, m, s.t) + at.c;
+  uint32_t to = 0, from = 0;
+  auto after = [](uint32_t stage) { return stage == (kStages - 1) * kStage ? 0u : stage + kStage; };
+  auto issue = [&](bool real) {
+    if (real) {
+      x.copy(ring, to, at, tpr);
+      dy.copy(ring, to + RingX::kStage, at, tpr);
+      if (kMore) dt.copy(ring, to + RingX::kStage + RingD::kStage, at, tpr);
+    }
+    copy_commit();
+    dy.advance();
+    x.advance();
+    if (kMore) dt.advance();
+    to = after(to);
+  };
+  group_sync(tpr);                                                   // the segment before is read: ring and rooms are free
+  uint32_t flags = 0;                                                // bit k: the row k turns ahead is there
+#pragma unroll
+  for (int k = 0; k + 1 < kStages; ++k) {
+    const bool real = s.there(k);
+    issue(real);
+    flags |= (uint32_t)real << k;
+  }
+  bool coming = s.there(kStages - 1);
+  float2 v[kPairs], g[kPairs];
+  float sum = 0.f, none[1];
+  if (kAhead) {
+    copy_wait<kStages - 2>();
+    if (RingX::kShared) group_sync(tpr);
+    if (flags & 1) {
+      x.read(ring, from, at, v);
+      sum = total_of(v);
+    }
+    group_sums<0, true>(none, sum, rooms[1], tpr);
+  }
+  for (uint32_t k = 0; k < s.turns; ++k) {
+    copy_wait<kAhead ? kStages - 3 : kStages - 2>();
+    if (RingX::kShared) group_sync(tpr);
+    issue(coming);
+    flags |= (uint32_t)coming << (kStages - 1);
+    coming = s.there(k + kStages);
+    const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
+    flags >>= 1;
+    if (real) {
+      x.read(ring, from, at, v);
+      dy.read(ring, from + RingX::kStage, at, g);
+    } else {
+      clear(v);
+      clear(g);
+    }
+    if (!kAhead) {
+      sum = total_of(v);
+      group_sums<0, true>(none, sum, rooms[1], tpr);
+    }
+    centre(v, sum * over, at);
+    float2 s0 = both(0.f), s1 = s0, s2 = s0, s3 = s0;
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) {
+      const float2 gw = mul2(g[i], w[i]);
+      s0 = add2(s0, v[i]);
+      s1 = fma2(v[i], v[i], s1);
+      s2 = add2(s2, gw);
+      s3 = fma2(gw, v[i], s3);
+    }
+    float sums[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
+    sum = 0.f;
+    if (kAhead && more) {
+      float2 u[kPairs];
+      x.read(ring, after(from), at, u, 1);
+      sum = total_of(u);
+    }
+    group_sums<4, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
+    const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+    const float mg = sums[2] * over, mgx = fmaf(-shift, sums[2], sums[3]) * over * rstd;
+    if (real) {
+#pragma unroll
+      for (int i = 0; i < kPairs; ++i) {
+        const float2 xhat = fma2(v[i], both(rstd), both(-shift * rstd));
+        dw[i] = fma2(g[i], xhat, dw[i]);
+        db[i] = add2(db[i], g[i]);
+        v[i] = mul2(fma2(xhat, both(-mgx), fma2(g[i], w[i], both(-mg))), both(rstd));
+      }
+      if (kMore) {
+        float2 o[kPairs];
+        dt.read(ring, from + RingX::kStage + RingD::kStage, at, o);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], o[i]);
+      }
+    }
+    if (a.dx.p != nullptr && in) {
+      if (!real) clear(v);
+      store_row(row_o, at, v);
+    }
+    row_o += groups * a.dx.tok;
+    dy.done();
+    x.done();
+    if (kMore) dt.done();
+    from = after(from);
+  }
+}
+
+template <typename D, typename X, int kVec, int kForm, bool kMore>
 __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a, uint32_t tpr) {
-  using RingD = Ring<D, kVec, kFill>; using RingX = Ring<X, kVec, kFill>;
-  constexpr int kStage = kGradStage<D, X, kVec, kFill, kMore>, kStages = stages_of(kStage, kGradRoom);
-  constexpr bool kAhead = kStages >= 4;
+  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kStages = stages_of(kStage, kGradRoom);
   extern __shared__ __align__(16) char ring[];
   float* flush = reinterpret_cast<float*>(ring + kStages * kStage);
   __shared__ Room rooms[2];
   const uint32_t groups = kRowThreads / tpr;
-  const Columns<kVec, kFill> at = {threadIdx.x % tpr * kVec, tpr * kVec, a.dim};
-  const float over = 1.f / a.dim;
+  const bool busy = threadIdx.x / tpr < groups;                      // not a warp that makes no group
+  const Columns<kVec, kForm> at = columns<kVec, kForm>(tpr, a.dim);
   grid_dependency_wait();
   const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
   float2 w[kPairs], dw[kPairs], db[kPairs];
   load_param(a.weight, a.weight_bf16, at, 1.f, w);
-  for (uint32_t begin = r0; begin < r1;) {
+  for (uint32_t begin = r0; begin < r1;) {                           // one worker's rows at a time
     const uint32_t m = begin / a.T, end = (uint32_t)min((uint64_t)r1, (uint64_t)(m + 1) * a.T);
-    Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
-    RingD dy;
-    RingX x, dt;
-    dy.start(a.dy, m, s.t, groups, tpr, at);
-    x.start(a.x, m, s.t, groups, tpr, at);
-    if (kMore) dt.start(a.dtotal, m, s.t, groups, tpr, at);
-    X* row_o = row_of<X>(a.dx, m, s.t) + at.c;
-    uint32_t to = 0, from = 0;
-    auto after = [](uint32_t stage) { return stage == (kStages - 1) * kStage ? 0u : stage + kStage; };
-    auto issue = [&](bool real) {
-      if (real) {
-        x.copy(ring, to, at, tpr);
-        dy.copy(ring, to + RingX::kStage, at, tpr);
-        if (kMore) dt.copy(ring, to + RingX::kStage + RingD::kStage, at, tpr);
-      }
-      copy_commit();
-      dy.advance();
-      x.advance();
-      if (kMore) dt.advance();
-      to = after(to);
-    };
-    group_sync(tpr);                                                 // the segment before is read: ring and rooms are free
-    uint32_t flags = 0;                                              // bit k: the row k turns ahead is there
-#pragma unroll
-    for (int k = 0; k + 1 < kStages; ++k) {
-      const bool real = s.there(k);
-      issue(real);
-      flags |= (uint32_t)real << k;
-    }
-    bool coming = s.there(kStages - 1);
     clear(dw);
     clear(db);
-    float2 v[kPairs], g[kPairs];
-    float sum = 0.f, none[1];
-    if (kAhead) {
-      copy_wait<kStages - 2>();
-      if (RingX::kShared) group_sync(tpr);
-      if (flags & 1) {
-        x.read(ring, from, at, v);
-        sum = total_of(v);
-      }
-      group_sums<0, true>(none, sum, rooms[1], tpr);
-    }
-    for (uint32_t k = 0; k < s.turns; ++k) {
-      copy_wait<kAhead ? kStages - 3 : kStages - 2>();
-      if (RingX::kShared) group_sync(tpr);
-      issue(coming);
-      flags |= (uint32_t)coming << (kStages - 1);
-      coming = s.there(k + kStages);
-      const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
-      flags >>= 1;
-      if (real) {
-        x.read(ring, from, at, v);
-        dy.read(ring, from + RingX::kStage, at, g);
-      } else {
-        clear(v);
-        clear(g);
-      }
-      if (!kAhead) {
-        sum = total_of(v);
-        group_sums<0, true>(none, sum, rooms[1], tpr);
-      }
-      centre(v, sum * over, at);
-      float2 s0 = both(0.f), s1 = s0, s2 = s0, s3 = s0;
-#pragma unroll
-      for (int i = 0; i < kPairs; ++i) {
-        const float2 gw = mul2(g[i], w[i]);
-        s0 = add2(s0, v[i]);
-        s1 = fma2(v[i], v[i], s1);
-        s2 = add2(s2, gw);
-        s3 = fma2(gw, v[i], s3);
-      }
-      float sums[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
-      sum = 0.f;
-      if (kAhead && more) {
-        float2 u[kPairs];
-        x.read(ring, after(from), at, u, 1);
-        sum = total_of(u);
-      }
-      group_sums<4, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-      const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
-      const float mg = sums[2] * over, mgx = fmaf(-shift, sums[2], sums[3]) * over * rstd;
-      if (real) {
-#pragma unroll
-        for (int i = 0; i < kPairs; ++i) {
-          const float2 xhat = mul2(add2(v[i], both(-shift)), both(rstd));
-          dw[i] = fma2(g[i], xhat, dw[i]);
-          db[i] = add2(db[i], g[i]);
-          v[i] = mul2(fma2(xhat, both(-mgx), fma2(g[i], w[i], both(-mg))), both(rstd));
-        }
-        if (kMore) {
-          float2 o[kPairs];
-          dt.read(ring, from + RingX::kStage + RingD::kStage, at, o);
-#pragma unroll
-          for (int i = 0; i < kPairs; ++i) v[i] = add2(v[i], o[i]);
-        }
-      }
-      if (a.dx.p != nullptr && in) {
-        if (!real) clear(v);
-        store_row(row_o, at, v);
-      }
-      row_o += groups * a.dx.tok;
-      dy.done();
-      x.done();
-      if (kMore) dt.done();
-      from = after(from);
-    }
+    if (busy) grad_rows<D, X, kVec, kMore>(a, begin, end, m, tpr, at, ring, rooms, w, dw, db);
     if (a.partial != nullptr) {                                      // the groups' sums, four entries a thread at a time
       float* out = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad;
 #pragma unroll
@@ -558,7 +586,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
           dw[i] = add2(dw[i], pair(__shfl_xor_sync(0xffffffffu, bits(dw[i]), o)));
           db[i] = add2(db[i], pair(__shfl_xor_sync(0xffffffffu, bits(db[i]), o)));
         }
-      const uint32_t apart = tpr < 32 ? 32 : tpr;                    // threads from one sum of a column to the next
+      const uint32_t tile = kForm >= kTiles ? tile_columns<kVec>(tpr, a.dim) : a.dim;
+      const uint32_t apart = tpr < 32 ? 32 : tpr, past = tpr < 32 ? kRowThreads : groups * tpr;   // threads from one sum of a column to the next
 #pragma unroll
       for (int part = 0; part < kEach / 4; ++part) {
         __syncthreads();
@@ -569,10 +598,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
         }
         __syncthreads();
         for (uint32_t i = threadIdx.x; i < 8 * tpr; i += kRowThreads) {
-          const uint32_t row = i / tpr, l = i % tpr, e = part * 4 + row % 4, col = l * kVec + e / kVec * at.step + e % kVec;
+          const uint32_t row = i / tpr, l = i % tpr, e = part * 4 + row % 4;
+          const uint32_t in = (kForm >= kTiles ? l % 32 : l) * kVec + e / kVec * at.step() + e % kVec, col = kForm >= kTiles ? l / 32 * tile + in : in;
           float sum = 0.f;
-          for (uint32_t j = l; j < kRowThreads; j += apart) sum += flush[row * kRowThreads + j];
-          if (col < a.dim) out[(row < 4 ? 0 : a.pad) + col] = sum;
+          for (uint32_t j = l; j < past; j += apart) sum += flush[row * kRowThreads + j];
+          if (in < tile && col < a.dim) out[(row < 4 ? 0 : a.pad) + col] = sum;
         }
       }
     }
@@ -792,25 +822,30 @@ bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
   // workers one behind the other, or interleaved (each token's row of all workers side by side)
   return worker >= (T > 1 ? (T - 1) * tok : 0) + dim || (worker >= dim && (T == 1 || tok >= (uint64_t)(M - 1) * worker + dim));
 }
-// threads of a row: the fewest that hold it, but four where groups copy rows together
+// threads of a row: part of a warp (the fewest that hold it, but four where groups copy rows together), or a warp for every 512 entries
 uint32_t threads_per_row(uint64_t dim, int vec) {
+  if (dim > 16 * kEach) return (uint32_t)((dim + 32 * kEach - 1) / (32 * kEach)) * 32;
   uint32_t n = vec == 1 ? 4 : 1;
   while (n * kEach < dim) n *= 2;
   return n;
 }
-// f is called with the width of an access and how a row fills its group, as types.  16-bit rows alone may be read eight entries at a time.
+// f is called with the width of an access and the form of a row, as types.  16-bit rows alone may be read eight entries at a time.
 template <bool kWide, typename F>
 cudaError_t by_row_form(int vec, uint64_t dim, F f) {
-  const uint32_t tpr = threads_per_row(dim, vec);
-  if (vec == 1) return dim <= tpr * kEach / 2 ? f(Width<1>(), Width<kAnyDim>()) : f(Width<1>(), Width<kMoreThanHalf>());
-  if (kWide && vec == 8) return dim == tpr * kEach ? f(Width<kWide ? 8 : 4>(), Width<kFullDim>()) : f(Width<kWide ? 8 : 4>(), Width<kMoreThanHalf>());
-  return dim == tpr * kEach ? f(Width<4>(), Width<kFullDim>()) : f(Width<4>(), Width<kMoreThanHalf>());
+  const bool tiles = dim > 16 * kEach;
+  if (vec == 1) return tiles ? f(Width<1>(), Width<kTiles>()) : dim <= 2 * kEach ? f(Width<1>(), Width<kTiny>()) : f(Width<1>(), Width<kShort>());
+  const bool whole = dim % (32 * kEach) == 0;
+  if (kWide && vec == 8) {
+    constexpr int kVec = kWide ? 8 : 4;
+    return whole ? f(Width<kVec>(), Width<kFullTiles>()) : tiles ? f(Width<kVec>(), Width<kTiles>()) : f(Width<kVec>(), Width<kShort>());
+  }
+  return whole ? f(Width<4>(), Width<kFullTiles>()) : tiles ? f(Width<4>(), Width<kTiles>()) : f(Width<4>(), Width<kShort>());
 }
-template <typename X, typename Y, int kVec, int kFill, bool kAdd>
+template <typename X, typename Y, int kVec, int kForm, bool kAdd>
 cudaError_t enqueue_norm_rows(NormArgs a, cudaStream_t st) {
   static int done[kMaxDevices];
-  constexpr int kStage = kNormStage<X, kVec, kFill, kAdd>, kBytes = stages_of(kStage, kNormRoom) * kStage;
-  auto kernel = norm_row_kernel<X, Y, kVec, kFill, kAdd>;
+  constexpr int kStage = kNormStage<X, kVec, kAdd>, kBytes = stages_of(kStage, kNormRoom) * kStage;
+  auto kernel = norm_row_kernel<X, Y, kVec, kForm, kAdd>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
   const uint32_t runs = sm_count();
@@ -818,11 +853,11 @@ cudaError_t enqueue_norm_rows(NormArgs a, cudaStream_t st) {
   kernel<<<(a.N + a.per - 1) / a.per, kRowThreads, kBytes, st>>>(a, threads_per_row(a.dim, kVec));
   return cudaGetLastError();
 }
-template <typename D, typename X, int kVec, int kFill, bool kMore>
+template <typename D, typename X, int kVec, int kForm, bool kMore>
 cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   static int done[kMaxDevices];
-  constexpr int kStage = kGradStage<D, X, kVec, kFill, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage + kFlushBytes;
-  auto kernel = grad_row_kernel<D, X, kVec, kFill, kMore>;
+  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage + kFlushBytes;
+  auto kernel = grad_row_kernel<D, X, kVec, kForm, kMore>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
   return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, threads_per_row(a.dim, kVec));
@@ -866,8 +901,8 @@ extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_str
     using X = decltype(xt); using Y = decltype(yt);
     if (dim <= kMaxRowDim)
       return by_row_form<sizeof(X) == 2 && sizeof(Y) == 2>(vec, dim, [&](auto v, auto f) {
-        constexpr int kVec = decltype(v)::value, kFill = decltype(f)::value;
-        return opt_add != nullptr ? enqueue_norm_rows<X, Y, kVec, kFill, true>(a, st) : enqueue_norm_rows<X, Y, kVec, kFill, false>(a, st);
+        constexpr int kVec = decltype(v)::value, kForm = decltype(f)::value;
+        return opt_add != nullptr ? enqueue_norm_rows<X, Y, kVec, kForm, true>(a, st) : enqueue_norm_rows<X, Y, kVec, kForm, false>(a, st);
       });
     return by_row_width(vec, [&](auto v) {
       const unsigned most = 8u * sm_count();
@@ -932,8 +967,8 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
       using D = decltype(dt); using X = decltype(xt);
       if (dim <= kMaxRowDim)
         return by_row_form<sizeof(D) == 2 && sizeof(X) == 2>(vec, dim, [&](auto v, auto f) {
-          constexpr int kVec = decltype(v)::value, kFill = decltype(f)::value;
-          return opt_dtotal != nullptr ? enqueue_grad_rows<D, X, kVec, kFill, true>(a, st) : enqueue_grad_rows<D, X, kVec, kFill, false>(a, st);
+          constexpr int kVec = decltype(v)::value, kForm = decltype(f)::value;
+          return opt_dtotal != nullptr ? enqueue_grad_rows<D, X, kVec, kForm, true>(a, st) : enqueue_grad_rows<D, X, kVec, kForm, false>(a, st);
         });
       return by_row_width(vec, [&](auto v) {
         constexpr int kVec = decltype(v)::value;
