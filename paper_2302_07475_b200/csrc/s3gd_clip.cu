@@ -102,29 +102,41 @@ __device__ __forceinline__ double squares(const float* v) {
   for (int e = 0; e < kN; ++e) sum += (double)v[e] * v[e];
   return sum;
 }
+// Entries of a tile that wide accesses miss, at the ends of a tensor: fewer than kVec before the first one and behind the last.
+// f is called with the thread's entry, if it has one.
+template <int kVec, typename F>
+__device__ __forceinline__ void ragged_entries(long long begin, uint64_t n, F f) {
+  const int t = (int)threadIdx.x;
+  if (t >= 2 * kVec) return;
+  if (t < kVec) {
+    const long long at = begin + t;                // the first access begins before the tensor
+    if (begin < 0 && at >= 0 && (uint64_t)at < n) f(at);
+  } else {
+    const long long last = (long long)n - (((long long)n - begin) & (kVec - 1)), at = last + t - kVec;
+    if (last >= 0 && last >= begin && last < begin + (long long)kTile && (uint64_t)at < n) f(at);
+  }
+}
 template <typename T>
 __device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t tile, uint64_t policy) {
-  constexpr int kVec = kWide<T>, kLoads = kTile / (kThreads * kVec);
+  constexpr int kVec = kWide<T>, kLoads = kTile / (kThreads * kVec), kPacks = 8 / kVec;
   const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec;
-  double sum = 0;
-  if (begin >= 0 && (uint64_t)begin + kTile <= n) {
-    Pack<T, kVec> raw[kLoads];
+  const bool whole = begin >= 0 && (uint64_t)begin + kTile <= n;
+  Pack<T, kVec> raw[kLoads];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) raw[i] = load_hint<Pack<T, kVec>>(g + at + i * kThreads * kVec, policy);
-#pragma unroll
-    for (int i = 0; i < kLoads * kVec / 8; ++i) {
-      float v[8];
-#pragma unroll
-      for (int e = 0; e < 8; e += kVec) load_floats<T, kVec>(raw[i * 8 / kVec + e / kVec].v, v + e);
-      sum += squares<8>(v);
-    }
-    return sum;
+  for (int i = 0; i < kLoads; ++i) {
+    const long long c = at + i * kThreads * kVec;
+    raw[i] = {};
+    if (whole || (c >= 0 && (uint64_t)c + kVec <= n)) raw[i] = load_hint<Pack<T, kVec>>(g + c, policy);
   }
-  for (int i = 0; i < kLoads; ++i)
-    for (int e = 0; e < kVec; ++e) {
-      const long long c = at + i * kThreads * kVec + e;
-      if (c >= 0 && (uint64_t)c < n) { const double d = to_f32(g[c]); sum += d * d; }
-    }
+  double sum = 0;
+#pragma unroll
+  for (int i = 0; i < kLoads / kPacks; ++i) {
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < kPacks; ++e) load_floats<T, kVec>(raw[i * kPacks + e].v, v + e * kVec);
+    sum += squares<8>(v);
+  }
+  if (!whole) ragged_entries<kVec>(begin, n, [&](long long c) { const double d = to_f32(g[c]); sum += d * d; });
   return sum;
 }
 
@@ -172,35 +184,42 @@ __global__ void __launch_bounds__(kThreads) norm_kernel(const ClipArgs a) {
   if (blockIdx.x == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
 }
 
+// kBatch accesses of a tile, one behind the other; kWhole: all of them lie in the tensor
+template <typename S, typename D, int kVec, int kBatch, bool kWhole>
+__device__ __forceinline__ void scaled(const S* g, D* out, long long at, long long n, float c, uint64_t policy) {
+  Pack<S, kVec> raw[kBatch];
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) {
+    const long long j = at + i * kThreads * kVec;
+    if (kWhole || (j >= 0 && j + kVec <= n)) raw[i] = load_hint<Pack<S, kVec>>(g + j, policy);
+  }
+#pragma unroll
+  for (int i = 0; i < kBatch; ++i) {
+    const long long j = at + i * kThreads * kVec;
+    if (!kWhole && (j < 0 || j + kVec > n)) continue;
+    float v[kVec];
+    load_floats<S, kVec>(raw[i].v, v);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) v[e] = __fmul_rn(v[e], c);
+    Pack<D, kVec> o;
+    store_floats<D, kVec>(o.v, v);
+    store_hint(out + j, o, policy);
+  }
+}
+// (A call for each kind: put into the kernel, all of them together need 254 registers.)
 template <typename S, typename D, int kVec>
-__device__ __forceinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
-  constexpr int kLoads = kTile / (kThreads * kVec), kBatch = kLoads < 8 ? kLoads : 8;
-  const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec;
-  if (begin >= 0 && (uint64_t)begin + kTile <= n) {
-    const uint64_t policy = drop_policy();
+__device__ __noinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
+  constexpr int kLoads = kTile / (kThreads * kVec), kSpan = kThreads * kVec;
+  const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec, end = (long long)n;
+  const uint64_t policy = drop_policy();
+  if (begin >= 0 && begin + (long long)kTile <= end) {
 #pragma unroll 1
-    for (int b = 0; b < kLoads; b += kBatch) {
-      Pack<S, kVec> raw[kBatch];
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) raw[i] = load_hint<Pack<S, kVec>>(g + at + (b + i) * kThreads * kVec, policy);
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        float v[kVec];
-        load_floats<S, kVec>(raw[i].v, v);
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v[e] = __fmul_rn(v[e], c);
-        Pack<D, kVec> o;
-        store_floats<D, kVec>(o.v, v);
-        store_hint(out + at + (b + i) * kThreads * kVec, o, policy);
-      }
-    }
+    for (int b = 0; b < kLoads; b += 8) scaled<S, D, kVec, 8, true>(g, out, at + b * kSpan, end, c, policy);
     return;
   }
-  for (int i = 0; i < kLoads; ++i)
-    for (int e = 0; e < kVec; ++e) {
-      const long long j = at + i * kThreads * kVec + e;
-      if (j >= 0 && (uint64_t)j < n) out[j] = from_f32<D>(__fmul_rn(to_f32(g[j]), c));
-    }
+#pragma unroll 1
+  for (int b = 0; b < kLoads && begin + b * kSpan < end; b += 4) scaled<S, D, kVec, 4, false>(g, out, at + b * kSpan, end, c, policy);
+  ragged_entries<kVec>(begin, n, [&](long long j) { out[j] = from_f32<D>(__fmul_rn(to_f32(g[j]), c)); });
 }
 template <typename S, typename D>
 __device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t tile, float c) {
@@ -213,7 +232,7 @@ __device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t
 }
 
 template <int kMax>
-__global__ void __launch_bounds__(kThreads) scale_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a, uint32_t runs) {
+__global__ void __launch_bounds__(kThreads, 5) scale_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a, uint32_t runs) {
   grid_dependency_wait();
   const uint32_t m = blockIdx.y, run = runs - 1 - blockIdx.x;      // what was read last is in the L2
   const double norm = norm_of(a, m), held = norm + (double)a.eps;
@@ -259,10 +278,18 @@ bool valid(const s3gd_part* parts, int count, int M, bool clip) {
   return true;
 }
 
+// Runs of a worker's tiles: one for a tile where there are few.  (Several groups of tensors share the partial sums.)
+uint32_t runs_of(const s3gd_part* parts, int count, int M) {
+  const uint32_t most = runs_each(M);
+  uint64_t tiles = 0;
+  for (int i = 0; i < count && tiles < most; ++i) tiles += tiles_of(parts[i].n);
+  return tiles < 1 ? 1 : tiles < most ? (uint32_t)tiles : most;
+}
+
 // Calls f(Parts, ClipArgs of the group) for groups of at most kMax tensors.
 template <int kMax, typename F>
 cudaError_t by_group(const s3gd_part* parts, int count, int M, ClipArgs a, F f) {
-  a.runs = runs_each(M);
+  a.runs = runs_of(parts, count, M);
   for (int i = 0;;) {
     Parts<kMax> group;
     a.count = 0;
@@ -328,7 +355,7 @@ extern "C" s3gd_status s3gd_grad_norm(const s3gd_part* parts, int count, int M, 
   cudaError_t e = count <= kFewParts ? enqueue_squares<kFewParts>(parts, count, M, a, st) : enqueue_squares<kMostParts>(parts, count, M, a, st);
   if (e == cudaSuccess) {
     ClipArgs last = a;
-    last.runs = runs_each(M);
+    last.runs = runs_of(parts, count, M);
     count_launch();
     e = launch_after(norm_kernel, dim3(M), dim3(kThreads), 0, st, last);
   }
