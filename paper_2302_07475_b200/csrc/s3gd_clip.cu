@@ -23,13 +23,13 @@ struct Part {
   uint64_t n;
   long long src_worker, dst_worker;
   uint32_t first_tile;
-  uint32_t src_bf16 : 1, dst_bf16 : 1, in_place : 1;
+  uint32_t in_place;
 };
 struct ClipArgs {
   double* partial;     // [M x runs]
   float* norm;
   uint32_t* hdr;
-  uint32_t count, tiles, per, runs, add, sum_only;
+  uint32_t count, tiles, per, runs, add;
   float max_norm, eps;
 };
 template <int kMax> struct Parts { Part p[kMax]; };
@@ -157,11 +157,14 @@ __device__ __forceinline__ double norm_of(const ClipArgs& a, uint32_t m) {
   return sqrt(cta_sum(sum));
 }
 
-// blockIdx.x: run of tiles, blockIdx.y: worker
-template <int kMax>
-__global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a) {
-  grid_dependency_wait();
-  const uint32_t m = blockIdx.y, begin = blockIdx.x * a.per, end = min(begin + a.per, a.tiles);
+__device__ __forceinline__ float factor_of(const ClipArgs& a, double norm) {
+  const double held = norm + (double)a.eps;
+  return held <= (double)a.max_norm ? 1.f : (float)((double)a.max_norm / held);   // NaN stays NaN
+}
+// the CTA's sum of squares over a run of tiles of worker m, in every thread
+template <typename S, int kMax>
+__device__ __forceinline__ double run_squares(const Parts<kMax>& parts, const ClipArgs& a, uint32_t m, uint32_t run) {
+  const uint32_t begin = run * a.per, end = min(begin + a.per, a.tiles);
   const uint64_t policy = keep_policy();
   double sum = 0;
   uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
@@ -169,11 +172,17 @@ __global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant
     while (k + 1 < a.count && parts.p[k + 1].first_tile <= tile) ++k;
     const Part& p = parts.p[k];
     const uint32_t in = tile - p.first_tile;
-    sum += p.src_bf16 ? tile_squares(static_cast<const __nv_bfloat16*>(p.src) + m * p.src_worker, p.n, in, policy)
-                      : tile_squares(static_cast<const float*>(p.src) + m * p.src_worker, p.n, in, policy);
+    sum += tile_squares(static_cast<const S*>(p.src) + m * p.src_worker, p.n, in, policy);
   }
-  sum = cta_sum(sum);
-  double* to = a.partial + (size_t)m * a.runs + blockIdx.x;
+  return cta_sum(sum);
+}
+
+// blockIdx.x: run of tiles, blockIdx.y: worker
+template <typename S, int kMax>
+__global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a) {
+  grid_dependency_wait();
+  const double sum = run_squares<S>(parts, a, blockIdx.y, blockIdx.x);
+  double* to = a.partial + (size_t)blockIdx.y * a.runs + blockIdx.x;
   if (threadIdx.x == 0) *to = a.add ? *to + sum : sum;
 }
 
@@ -206,9 +215,8 @@ __device__ __forceinline__ void scaled(const S* g, D* out, long long at, long lo
     store_hint(out + j, o, policy);
   }
 }
-// (A call for each kind: put into the kernel, all of them together need 254 registers.)
 template <typename S, typename D, int kVec>
-__device__ __noinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
+__device__ __forceinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
   constexpr int kLoads = kTile / (kThreads * kVec), kSpan = kThreads * kVec;
   const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec, end = (long long)n;
   const uint64_t policy = drop_policy();
@@ -231,14 +239,8 @@ __device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t
   else tile_scaled<S, D, 1>(g, out, p.n, tile, c);
 }
 
-template <int kMax>
-__global__ void __launch_bounds__(kThreads, 5) scale_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a, uint32_t runs) {
-  grid_dependency_wait();
-  const uint32_t m = blockIdx.y, run = runs - 1 - blockIdx.x;      // what was read last is in the L2
-  const double norm = norm_of(a, m), held = norm + (double)a.eps;
-  const float c = held <= (double)a.max_norm ? 1.f : (float)((double)a.max_norm / held);   // NaN stays NaN
-  if (run == 0 && threadIdx.x == 0) a.norm[m] = (float)norm;
-  if (run == 0 && m == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+template <typename S, typename D, int kMax>
+__device__ __forceinline__ void run_scaled(const Parts<kMax>& parts, const ClipArgs& a, uint32_t m, uint32_t run, float c) {
   const uint32_t begin = run * a.per, end = min(begin + a.per, a.tiles);
   uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
   for (uint32_t tile = begin; tile < end; ++tile) {
@@ -246,11 +248,18 @@ __global__ void __launch_bounds__(kThreads, 5) scale_kernel(const __grid_constan
     const Part& p = parts.p[k];
     if (c == 1.f && p.in_place) continue;
     const uint32_t in = tile - p.first_tile;
-    if (p.src_bf16)
-      p.dst_bf16 ? tile_clipped<__nv_bfloat16, __nv_bfloat16>(p, m, in, c) : tile_clipped<__nv_bfloat16, float>(p, m, in, c);
-    else
-      p.dst_bf16 ? tile_clipped<float, __nv_bfloat16>(p, m, in, c) : tile_clipped<float, float>(p, m, in, c);
+    tile_clipped<S, D>(p, m, in, c);
   }
+}
+
+template <typename S, typename D, int kMax>
+__global__ void __launch_bounds__(kThreads, 4) scale_kernel(const __grid_constant__ Parts<kMax> parts, const ClipArgs a, uint32_t runs) {
+  grid_dependency_wait();
+  const uint32_t m = gridDim.y - 1 - blockIdx.y, run = runs - 1 - blockIdx.x;      // what was read last is in the L2
+  const double norm = norm_of(a, m);
+  if (run == 0 && threadIdx.x == 0) a.norm[m] = (float)norm;
+  if (run == 0 && m == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+  run_scaled<S, D>(parts, a, m, run, factor_of(a, norm));
 }
 
 // ------------------------------------------------------------------ host
@@ -278,58 +287,86 @@ bool valid(const s3gd_part* parts, int count, int M, bool clip) {
   return true;
 }
 
-// Runs of a worker's tiles: one for a tile where there are few.  (Several groups of tensors share the partial sums.)
-uint32_t runs_of(const s3gd_part* parts, int count, int M) {
-  const uint32_t most = runs_each(M);
-  uint64_t tiles = 0;
-  for (int i = 0; i < count && tiles < most; ++i) tiles += tiles_of(parts[i].n);
-  return tiles < 1 ? 1 : tiles < most ? (uint32_t)tiles : most;
+cudaError_t launch_norm(const ClipArgs& base, uint32_t runs, int M, cudaStream_t st) {
+  ClipArgs a = base;
+  a.runs = runs;
+  count_launch();
+  return launch_after(norm_kernel, dim3(M), dim3(kThreads), 0, st, a);
 }
 
-// Calls f(Parts, ClipArgs of the group) for groups of at most kMax tensors.
-template <int kMax, typename F>
-cudaError_t by_group(const s3gd_part* parts, int count, int M, ClipArgs a, F f) {
-  a.runs = runs_of(parts, count, M);
-  for (int i = 0;;) {
+// Runs of a worker's tiles: one for a tile where there are few.  (Several groups of tensors share the partial sums.)
+uint64_t tiles_in(const s3gd_part* parts, int count) {
+  uint64_t tiles = 0;
+  for (int i = 0; i < count; ++i) tiles += tiles_of(parts[i].n);
+  return tiles;
+}
+uint32_t runs_of(uint64_t tiles, uint32_t most) { return tiles < 1 ? 1 : tiles < most ? (uint32_t)tiles : most; }
+
+// Calls f(Parts, ClipArgs of the group) for groups of at most kMax of the tensors that `takes` picks; `first`: partial sums are
+// written, not added to.
+template <int kMax, typename P, typename F>
+cudaError_t by_group(const s3gd_part* parts, int count, int M, uint32_t runs, bool* first, ClipArgs a, P takes, F f) {
+  a.runs = runs;
+  for (int i = 0; i < count;) {
     Parts<kMax> group;
     a.count = 0;
     uint64_t tiles = 0;
     for (; i < count && a.count < kMax; ++i) {
       const s3gd_part& p = parts[i];
       const uint64_t more = tiles_of(p.n);
-      if (more == 0) continue;
+      if (more == 0 || !takes(p)) continue;
       if (tiles + more >= (1ull << 31)) break;
       Part& q = group.p[a.count++];
       q.src = p.data; q.dst = p.out; q.n = p.n; q.src_worker = M > 1 ? p.stride : 0; q.dst_worker = M > 1 ? p.out_stride : 0;
-      q.first_tile = (uint32_t)tiles;
-      q.src_bf16 = p.dtype == S3GD_BF16; q.dst_bf16 = p.out_dtype == S3GD_BF16; q.in_place = p.out == p.data;
+      q.first_tile = (uint32_t)tiles; q.in_place = p.out == p.data;
       tiles += more;
     }
+    if (a.count == 0) break;
     a.tiles = (uint32_t)tiles;
     a.per = (uint32_t)((tiles + a.runs - 1) / a.runs);
-    if (a.per == 0) a.per = 1;
+    a.add = !*first;
+    *first = false;
     const cudaError_t e = f(group, a);
-    if (e != cudaSuccess || i >= count) return e;
-    a.add = 1;
+    if (e != cudaSuccess) return e;
   }
+  return cudaSuccess;
+}
+
+// Every tensor's type has launches of its own: a kernel for all of them together would need 254 registers.
+template <int kMax>
+cudaError_t enqueue_squares(const s3gd_part* parts, int count, int M, uint32_t runs, const ClipArgs& base, cudaStream_t st) {
+  bool first = true;
+  for (int dt : {(int)S3GD_F32, (int)S3GD_BF16}) {
+    const cudaError_t e = by_real(dt, [&](auto s) {
+      return by_group<kMax>(parts, count, M, runs, &first, base, [&](const s3gd_part& p) { return p.dtype == dt; }, [&](const Parts<kMax>& group, const ClipArgs& a) {
+        count_launch();
+        return launch_after(squares_kernel<decltype(s), kMax>, dim3(a.runs, M), dim3(kThreads), 0, st, group, a);
+      });
+    });
+    if (e != cudaSuccess) return e;
+  }
+  return first ? cudaMemsetAsync(base.partial, 0, (size_t)M * runs * sizeof(double), st) : cudaSuccess;      // no entries at all
 }
 
 template <int kMax>
-cudaError_t enqueue_squares(const s3gd_part* parts, int count, int M, const ClipArgs& base, cudaStream_t st) {
-  return by_group<kMax>(parts, count, M, base, [&](const Parts<kMax>& group, const ClipArgs& a) {
-    count_launch();
-    return launch_after(squares_kernel<kMax>, dim3(a.runs, M), dim3(kThreads), 0, st, group, a);
-  });
-}
-template <int kMax>
 cudaError_t enqueue_clip(const s3gd_part* parts, int count, int M, const ClipArgs& base, cudaStream_t st) {
-  const cudaError_t e = enqueue_squares<kMax>(parts, count, M, base, st);
+  const uint32_t runs = runs_of(tiles_in(parts, count), runs_each(M));
+  const cudaError_t e = enqueue_squares<kMax>(parts, count, M, runs, base, st);
   if (e != cudaSuccess) return e;
-  return by_group<kMax>(parts, count, M, base, [&](const Parts<kMax>& group, const ClipArgs& a) {
-    const uint32_t busy = (a.tiles + a.per - 1) / a.per, runs = busy < 1 ? 1 : busy;
-    count_launch();
-    return launch_after(scale_kernel<kMax>, dim3(runs, M), dim3(kThreads), 0, st, group, a, runs);
-  });
+  bool first = true;
+  for (int from : {(int)S3GD_F32, (int)S3GD_BF16})
+    for (int to : {(int)S3GD_F32, (int)S3GD_BF16}) {
+      const cudaError_t e = by_real(from, [&](auto s) { return by_real(to, [&](auto d) {
+        return by_group<kMax>(parts, count, M, runs, &first, base, [&](const s3gd_part& p) { return p.dtype == from && p.out_dtype == to; },
+                              [&](const Parts<kMax>& group, const ClipArgs& a) {
+          const uint32_t busy = (a.tiles + a.per - 1) / a.per;
+          count_launch();
+          return launch_after(scale_kernel<decltype(s), decltype(d), kMax>, dim3(busy, M), dim3(kThreads), 0, st, group, a, busy);
+        });
+      }); });
+      if (e != cudaSuccess) return e;
+    }
+  return first ? launch_norm(base, runs, M, st) : cudaSuccess;       // no entries at all: the norms are to be written all the same
 }
 
 ClipArgs clip_args(void* ws, float* norm) {
@@ -352,13 +389,9 @@ extern "C" s3gd_status s3gd_grad_norm(const s3gd_part* parts, int count, int M, 
   if (ws == nullptr || ws_bytes < workspace_bytes(M) || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
   const ClipArgs a = clip_args(ws, out_norm);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = count <= kFewParts ? enqueue_squares<kFewParts>(parts, count, M, a, st) : enqueue_squares<kMostParts>(parts, count, M, a, st);
-  if (e == cudaSuccess) {
-    ClipArgs last = a;
-    last.runs = runs_of(parts, count, M);
-    count_launch();
-    e = launch_after(norm_kernel, dim3(M), dim3(kThreads), 0, st, last);
-  }
+  const uint32_t runs = runs_of(tiles_in(parts, count), runs_each(M));
+  cudaError_t e = count <= kFewParts ? enqueue_squares<kFewParts>(parts, count, M, runs, a, st) : enqueue_squares<kMostParts>(parts, count, M, runs, a, st);
+  if (e == cudaSuccess) e = launch_norm(a, runs, M, st);
   return e == cudaSuccess ? S3GD_OK : S3GD_ERR_CUDA;
 }
 
