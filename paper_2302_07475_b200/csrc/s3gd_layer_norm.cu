@@ -12,6 +12,7 @@
 // in that order either k or m grows).  A last kernel adds a worker's slots in 64 bits, in ascending order: no atomics, and the
 // result depends on the sizes alone.
 #include "s3gd_ops.cuh"
+#include "s3gd_tcgen05.cuh"
 
 namespace s3gd {
 namespace {
@@ -39,6 +40,7 @@ struct NormGradArgs {
   const void *weight, *ids;
   bool weight_bf16, ids64, grads_bf16, accumulate;
   uint32_t M, T, N, dim, pad, per, runs;
+  uint32_t shares;                                 // 0, or the CTAs of a cluster that share a worker's rows and join their sums themselves
   float eps;
   void *dweight, *dbias;
   long long grads_stride;
@@ -75,11 +77,52 @@ __device__ __forceinline__ void cta_sums(double (&v)[kCount], double (&room)[kCo
   }
 }
 
+// ------------------------------------------------------------------ weight gradients from the partial sums
+// [dw | db] of worker m, column `col` of 2 pad
+__device__ __forceinline__ void put_weight_gradient(const NormGradArgs& a, uint32_t m, uint32_t col, double sum) {
+  const uint32_t c = col < a.pad ? col : col - a.pad;
+  void* base = col < a.pad ? a.dweight : a.dbias;
+  if (base == nullptr || c >= a.dim) return;
+  if (a.grads_bf16) {
+    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(base) + m * a.grads_stride + c;
+    *to = __float2bfloat16_rn((float)(a.accumulate ? sum + (double)__bfloat162float(*to) : sum));
+  } else {
+    float* to = static_cast<float*>(base) + m * a.grads_stride + c;
+    *to = (float)(a.accumulate ? sum + (double)*to : sum);
+  }
+}
+// blockIdx.x: 32 columns of [dw | db] (pad entries each), blockIdx.y: worker.  The warps take neighbouring slots in turn.
+constexpr int kJoinWarps = 16;
+__global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(NormGradArgs a) {
+  __shared__ double room[kJoinWarps][32];
+  const uint32_t w = threadIdx.x >> 5, lane = lane_id(), m = blockIdx.y, col = blockIdx.x * 32 + lane;
+  grid_dependency_wait();
+  if (blockIdx.x == 0 && m == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+  if (a.dweight == nullptr && a.dbias == nullptr) return;
+  double sum = 0;
+  if (a.T > 0 && col < 2 * a.pad) {
+    const uint32_t first = (uint32_t)((uint64_t)m * a.T / a.per), last = (uint32_t)(((uint64_t)(m + 1) * a.T - 1) / a.per);
+    const float* from = a.partial + (size_t)m * 2 * a.pad + col;
+#pragma unroll 8
+    for (uint32_t k = first + w; k <= last; k += kJoinWarps) sum += from[(size_t)k * 2 * a.pad];
+  }
+  room[w][lane] = sum;
+  __syncthreads();
+  if (w != 0 || col >= 2 * a.pad) return;
+  for (int k = 1; k < kJoinWarps; ++k) sum += room[k][lane];
+  put_weight_gradient(a, m, col, sum);
+}
+
 // ------------------------------------------------------------------ rows that threads hold in registers
 // A group of `tpr` threads (part of a warp, a power of two, or whole warps) takes a row, kEach entries a thread: chunks of
 // neighbouring kVec entries.  Rows to come are on their way into a ring in shared memory meanwhile (cp.async; empty places are
 // not read).
 constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
+// Few rows: a cluster of eight CTAs takes a worker's rows and joins their sums itself, which saves the second launch.  One row a group
+// at most (64 rows of 768: 7.6 us, with a second launch 8.1; 200 rows 12.1 and 8.8) and eight workers (8 x 64 rows of 768: 6.7 and
+// 7.8 us; 16 workers: 14 and 8 us, more clusters than there is room for at once).
+constexpr int kCluster = 8;
+constexpr int kClusterWorkers = 8;
 constexpr int kEach = 16, kPairs = kEach / 2;
 constexpr uint64_t kMaxRowDim = (uint64_t)kRowThreads * kEach;
 
@@ -570,7 +613,11 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
   const bool busy = threadIdx.x / tpr < groups;                      // not a warp that makes no group
   const Columns<kVec, kForm> at = columns<kVec, kForm>(tpr, a.dim);
   grid_dependency_wait();
-  const uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
+  uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
+  if (a.shares) {                                                    // a cluster for a worker
+    r0 = min(blockIdx.x * a.per, a.T) + blockIdx.y * a.T;
+    r1 = min((blockIdx.x + 1) * a.per, a.T) + blockIdx.y * a.T;
+  }
   float2 w[kPairs], dw[kPairs], db[kPairs];
   load_param(a.weight, a.weight_bf16, at, 1.f, w);
   for (uint32_t begin = r0; begin < r1;) {                           // one worker's rows at a time
@@ -579,7 +626,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
     clear(db);
     if (busy) grad_rows<D, X, kVec, kMore>(a, begin, end, m, tpr, at, ring, rooms, w, dw, db);
     if (a.partial != nullptr) {                                      // the groups' sums, four entries a thread at a time
-      float* out = a.partial + (size_t)(blockIdx.x + m) * 2 * a.pad;
+      float* out = a.partial + (size_t)(blockIdx.x + m * (a.shares ? a.shares : 1u)) * 2 * a.pad;
 #pragma unroll
       for (int i = 0; i < kPairs; ++i)                               // groups of one warp
         for (uint32_t o = tpr; o < 32; o *= 2) {
@@ -607,6 +654,16 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
       }
     }
     begin = end;
+  }
+  if (!a.shares) return;
+  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
+  if (a.partial == nullptr) return;
+  cluster_sync();                                                    // the partial sums of all CTAs are there
+  const float* from = a.partial + (size_t)blockIdx.y * a.shares * 2 * a.pad;
+  for (uint32_t col = blockIdx.x * kRowThreads + threadIdx.x; col < 2 * a.pad; col += kCluster * kRowThreads) {
+    double sum = 0;
+    for (uint32_t k = 0; k < a.shares; ++k) sum += __ldcg(from + (size_t)k * 2 * a.pad + col);
+    put_weight_gradient(a, blockIdx.y, col, sum);
   }
 }
 
@@ -746,38 +803,6 @@ __global__ void __launch_bounds__(kThreads) grad_long_kernel(NormGradArgs a) {
   }
 }
 
-// ------------------------------------------------------------------ weight gradients from the partial sums
-// blockIdx.x: 32 columns of [dw | db] (pad entries each), blockIdx.y: worker.  The warps take neighbouring slots in turn.
-constexpr int kJoinWarps = 16;
-__global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(NormGradArgs a) {
-  __shared__ double room[kJoinWarps][32];
-  const uint32_t w = threadIdx.x >> 5, lane = lane_id(), m = blockIdx.y, col = blockIdx.x * 32 + lane;
-  grid_dependency_wait();
-  if (blockIdx.x == 0 && m == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
-  if (a.dweight == nullptr && a.dbias == nullptr) return;
-  double sum = 0;
-  if (a.T > 0 && col < 2 * a.pad) {
-    const uint32_t first = (uint32_t)((uint64_t)m * a.T / a.per), last = (uint32_t)(((uint64_t)(m + 1) * a.T - 1) / a.per);
-    const float* from = a.partial + (size_t)m * 2 * a.pad + col;
-#pragma unroll 8
-    for (uint32_t k = first + w; k <= last; k += kJoinWarps) sum += from[(size_t)k * 2 * a.pad];
-  }
-  room[w][lane] = sum;
-  __syncthreads();
-  if (w != 0 || col >= 2 * a.pad) return;
-  for (int k = 1; k < kJoinWarps; ++k) sum += room[k][lane];
-  const uint32_t c = col < a.pad ? col : col - a.pad;
-  void* base = col < a.pad ? a.dweight : a.dbias;
-  if (base == nullptr || c >= a.dim) return;
-  if (a.grads_bf16) {
-    __nv_bfloat16* to = static_cast<__nv_bfloat16*>(base) + m * a.grads_stride + c;
-    *to = __float2bfloat16_rn((float)(a.accumulate ? sum + (double)__bfloat162float(*to) : sum));
-  } else {
-    float* to = static_cast<float*>(base) + m * a.grads_stride + c;
-    *to = (float)(a.accumulate ? sum + (double)*to : sum);
-  }
-}
-
 // ------------------------------------------------------------------ host
 struct NormGradLayout {
   uint32_t per, runs, pad;
@@ -860,7 +885,17 @@ cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   auto kernel = grad_row_kernel<D, X, kVec, kForm, kMore>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
-  return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, threads_per_row(a.dim, kVec));
+  const uint32_t tpr = threads_per_row(a.dim, kVec);
+  if (a.shares == 0) return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, tpr);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kCluster, a.M); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = kBytes; cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = kCluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
+  return cudaLaunchKernelEx(&cfg, kernel, a, tpr);
 }
 template <typename F>
 cudaError_t by_row_width(int v, F f) { return v >= 4 ? f(Width<4>()) : f(Width<1>()); }
@@ -963,6 +998,10 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
     const unsigned wide = vec >= 4 ? 4 : 1, tiles = (unsigned)((dim + kThreads * wide - 1) / (kThreads * wide));
     if (tiles > 65535) return S3GD_ERR_INVALID_ARG;
     count_launch(dim > kMaxRowDim ? 2 : 1);
+    if (dim <= kMaxRowDim && M <= kClusterWorkers && T <= (uint64_t)kCluster * (kRowThreads / threads_per_row(dim, vec))) {
+      a.per = (uint32_t)((T + kCluster - 1) / kCluster);
+      a.shares = (uint32_t)((T + a.per - 1) / a.per);
+    }
     e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) {
       using D = decltype(dt); using X = decltype(xt);
       if (dim <= kMaxRowDim)
@@ -979,7 +1018,7 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
       });
     }); });
   }
-  if (e == cudaSuccess) {
+  if (e == cudaSuccess && a.shares == 0) {
     count_launch();
     e = launch_after(norm_join_kernel, dim3(weights ? (2 * a.pad + 31) / 32 : 1, weights ? M : 1), dim3(kJoinWarps * 32), 0, st, a);
   }
