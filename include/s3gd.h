@@ -445,7 +445,7 @@ S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t d
  *                 otherwise overlap nothing.  An input's stride may be 0: the same row repeated
  * An Inf or NaN makes its own row NaN.  Sums, mean and variance are held in 32 bits or more and rows far from zero keep their digits;
  * entries beyond about 1e18 in magnitude, whose squares pass fp32's range, are not provided for.
- * T may be 0.  Limits: M <= 65535, M * T < 2^31, dim < 2^24, 0 <= eps < Inf.
+ * T may be 0.  Limits: M <= 65535, M * T < 2^31, dim <= 2^24 - 256, 0 <= eps < Inf.
  */
 S3GD_API s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_add,
                                      int64_t add_stride, int64_t add_worker_stride, void* opt_total, int64_t total_stride,
@@ -469,7 +469,7 @@ S3GD_API s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_strid
  *             be NULL.  Every entry is written; with accumulate != 0 the sum is added to what is there (one rounding)
  *  ws         >= s3gd_layer_norm_grad_workspace_bytes(M, T, dim), 256-byte aligned, not preserved; one for larger numbers serves
  *             smaller ones
- * Sums over tokens are taken in an order that depends on the sizes alone.  T may be 0.  Limits as for s3gd_layer_norm.
+ * Sums are taken in an order that depends on sizes and alignment alone, not on the run.  T may be 0.  Limits as for s3gd_layer_norm.
  */
 S3GD_API size_t s3gd_layer_norm_grad_workspace_bytes(int M, uint64_t T, uint64_t dim);
 S3GD_API s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_t dy_stride, int64_t dy_worker_stride, const void* x,
@@ -493,7 +493,7 @@ S3GD_API s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_t 
  *  out_norm  dev  [M] fp32        ws  >= s3gd_clip_workspace_bytes(M), 256-byte aligned, not preserved
  * Squares are summed in 64 bits, c is rounded to 32: entries at either end of fp32's range count as they should.  A worker that holds a NaN has norm and
  * outputs NaN; one that holds an Inf has norm Inf and c = 0, so that its infinite entries become NaN and the others 0.  Results depend on
- * the sizes alone, not on the run.  Limits: 1 <= M <= 65535, n < 2^40, 0 <= max_norm < Inf, 0 <= eps < Inf.
+ * sizes and alignment alone, not on the run.  Limits: 1 <= M <= 65535, n < 2^40, 0 <= max_norm < Inf, 0 <= eps < Inf.
  */
 typedef struct s3gd_part {
   const void* data; /* F32 or BF16, aligned to its type */

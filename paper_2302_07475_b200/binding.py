@@ -966,7 +966,14 @@ _T = torch.Tensor
 _dtype_of = operator.attrgetter("dtype")
 
 
-def _plain_parts(grads, outs, index: int, M: int, several: bool):
+def _once(places, entries) -> None:
+    if len(set(places)) != len(places):
+        seen = [p for p, n in zip(places, entries) if n]
+        if len(set(seen)) != len(seen):
+            raise ValueError("an output is named twice: it would be scaled twice, or once, as it happens")
+
+
+def _plain_parts(grads, outs, index: int, M: int, several: bool, writes: bool):
     """As _parts for lists of contiguous gradients of one type (and outputs of one type that lie alike); None for others.
 
     A list has hundreds of tensors and its kernels take some ten microseconds: each question is put to all tensors at once."""
@@ -977,6 +984,8 @@ def _plain_parts(grads, outs, index: int, M: int, several: bool):
     code = _REAL_CODES[dtypes.pop()]
     entries, pointers = [n // M for n in map(_T.numel, grads)] if M > 1 else list(map(_T.numel, grads)), list(map(_T.data_ptr, grads))
     if outs is grads:
+        if writes:
+            _once(pointers, entries)
         return array.array("Q", chain.from_iterable(zip(pointers, pointers, entries, entries, entries, repeat(code | code << 32)))), len(pointers)
     dtypes = set(map(_dtype_of, outs))
     if len(dtypes) != 1 or set(map(_T.get_device, outs)) != devices or sizes != list(map(_T.size, outs)):
@@ -988,10 +997,12 @@ def _plain_parts(grads, outs, index: int, M: int, several: bool):
             return None
         apart = [s[0] for s in strides]
     code |= _REAL_CODES[dtypes.pop()] << 32
-    return array.array("Q", chain.from_iterable(zip(pointers, map(_T.data_ptr, outs), entries, entries, apart, repeat(code)))), len(pointers)
+    places = list(map(_T.data_ptr, outs))
+    _once(places, entries)
+    return array.array("Q", chain.from_iterable(zip(pointers, places, entries, entries, apart, repeat(code)))), len(pointers)
 
 
-def _parts(grads, out, index: int, M: int, several: bool):
+def _parts(grads, out, index: int, M: int, several: bool, writes: bool):
     """The tensors as an array of s3gd_part, and their number."""
     if isinstance(grads, torch.Tensor):
         grads, out = (grads,), (out,) if isinstance(out, torch.Tensor) else out
@@ -1000,7 +1011,7 @@ def _parts(grads, out, index: int, M: int, several: bool):
     if len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
     try:
-        plain = _plain_parts(grads, outs, index, M, several)
+        plain = _plain_parts(grads, outs, index, M, several, writes)
     except (TypeError, AttributeError, KeyError):        # something that is no tensor, or of another type: named below
         plain = None
     if plain is not None:
@@ -1033,6 +1044,8 @@ def _parts(grads, out, index: int, M: int, several: bool):
             if out_strides[first:] != strides[first:] and any(a != b and s != 1 for a, b, s in zip(out_strides[first:], strides[first:], shape[first:])):
                 raise ValueError(f"output {i} does not lie like its gradient: strides {out_strides} and {strides}")
         packed.extend((g.data_ptr(), o.data_ptr(), n, strides[0] if several else 0, out_strides[0] if several else 0, code))
+    if writes:
+        _once(packed[1::6].tolist(), packed[2::6])
     return packed, len(packed) // 6
 
 
@@ -1051,7 +1064,7 @@ def s3gd_grad_norm(grads, norm: torch.Tensor, ws: torch.Tensor) -> None:
     norm is fp32: [] for one norm over everything, or [M] for one per worker, where every tensor's first axis is the M workers.
     Tensors are fp32 or bf16, each in one piece (within a worker)."""
     index, M, several = _norms(norm)
-    packed, count = _parts(grads, None, index, M, several)
+    packed, count = _parts(grads, None, index, M, several, False)
     w = _ptr(ws, torch.uint8, name="ws")
     if ws.get_device() != index:
         raise TypeError(f"ws must be on the device of norm, {norm.device}")
@@ -1067,7 +1080,7 @@ def s3gd_clip(grads, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, out=
     out (None: in place) has a tensor for each of grads, of the same shape and order of axes, fp32 or bf16: e.g. the columns of a
     gradient buffer, out[i] = rows[:, a:b].view_as(grads[i]).  Outputs overlap no other tensor of the call."""
     index, M, several = _norms(norm)
-    packed, count = _parts(grads, out, index, M, several)
+    packed, count = _parts(grads, out, index, M, several, True)
     w = _ptr(ws, torch.uint8, name="ws")
     if ws.get_device() != index:
         raise TypeError(f"ws must be on the device of norm, {norm.device}")

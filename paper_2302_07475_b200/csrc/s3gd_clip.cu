@@ -49,42 +49,24 @@ __device__ __forceinline__ uint32_t part_of(const Parts<kMax>& parts, uint32_t c
 // entries of a 16-byte access, and how many entries the address lies behind such a boundary
 template <typename T> constexpr int kWide = 16 / (int)sizeof(T);
 
-// Accesses of 16, 8, 4 or 2 bytes with a hint to the L2 on what will be read again.
-__device__ __forceinline__ uint64_t keep_policy() {
-  uint64_t p;
-  asm("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(p));
-  return p;
-}
+// What is scaled is read for the last time: wide loads tell the L2 so (67 MB into another buffer and a sum over that: 55 us, without
+// the hint 59; the outputs stay).
 __device__ __forceinline__ uint64_t drop_policy() {
   uint64_t p;
   asm("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
   return p;
 }
 template <typename P>
-__device__ __forceinline__ P load_hint(const void* from, uint64_t policy) {
+__device__ __forceinline__ P load_last(const void* from, uint64_t policy) {
   P v;
-  if constexpr (sizeof(P) == 16) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  if constexpr (sizeof(P) == 16)
     asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(from), "l"(policy) : "memory");
-  } else if constexpr (sizeof(P) == 8) {
-    uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+  else if constexpr (sizeof(P) == 8)
     asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v2.u32 {%0,%1}, [%2], %3;" : "=r"(w[0]), "=r"(w[1]) : "l"(from), "l"(policy) : "memory");
-  } else {
+  else
     v = *static_cast<const P*>(from);
-  }
   return v;
-}
-template <typename P>
-__device__ __forceinline__ void store_hint(void* to, const P& v, uint64_t policy) {
-  if constexpr (sizeof(P) == 16) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
-    asm volatile("st.global.L2::cache_hint.v4.u32 [%0], {%1,%2,%3,%4}, %5;" ::"l"(to), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "l"(policy) : "memory");
-  } else if constexpr (sizeof(P) == 8) {
-    const uint32_t* w = reinterpret_cast<const uint32_t*>(&v);
-    asm volatile("st.global.L2::cache_hint.v2.u32 [%0], {%1,%2}, %3;" ::"l"(to), "r"(w[0]), "r"(w[1]), "l"(policy) : "memory");
-  } else {
-    *static_cast<P*>(to) = v;
-  }
 }
 template <typename T>
 __device__ __forceinline__ uint32_t behind(const T* p, int v) { return (uint32_t)(reinterpret_cast<uintptr_t>(p) / sizeof(T)) % v; }
@@ -119,7 +101,7 @@ __device__ __forceinline__ void ragged_entries(long long begin, uint64_t n, F f)
   }
 }
 template <typename T>
-__device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t tile, uint64_t policy) {
+__device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t tile) {
   constexpr int kVec = kWide<T>, kLoads = kTile / (kThreads * kVec), kPacks = 8 / kVec;
   const long long begin = (long long)tile * kTile - behind(g, kVec), at = begin + threadIdx.x * kVec;
   const bool whole = begin >= 0 && (uint64_t)begin + kTile <= n;
@@ -128,7 +110,7 @@ __device__ __forceinline__ double tile_squares(const T* g, uint64_t n, uint32_t 
   for (int i = 0; i < kLoads; ++i) {
     const long long c = at + i * kThreads * kVec;
     raw[i] = {};
-    if (whole || (c >= 0 && (uint64_t)c + kVec <= n)) raw[i] = load_hint<Pack<T, kVec>>(g + c, policy);
+    if (whole || (c >= 0 && (uint64_t)c + kVec <= n)) raw[i] = *reinterpret_cast<const Pack<T, kVec>*>(g + c);
   }
   double sum = 0;
 #pragma unroll
@@ -167,14 +149,13 @@ __device__ __forceinline__ float factor_of(const ClipArgs& a, double norm) {
 template <typename S, int kMax>
 __device__ __forceinline__ double run_squares(const Parts<kMax>& parts, const ClipArgs& a, uint32_t m, uint32_t run) {
   const uint32_t begin = run * a.per, end = min(begin + a.per, a.tiles);
-  const uint64_t policy = keep_policy();
   double sum = 0;
   uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
   for (uint32_t tile = begin; tile < end; ++tile) {
     while (k + 1 < a.count && parts.p[k + 1].first_tile <= tile) ++k;
     const Part& p = parts.p[k];
     const uint32_t in = tile - p.first_tile;
-    sum += tile_squares(static_cast<const S*>(p.src) + m * p.src_worker, p.n, in, policy);
+    sum += tile_squares(static_cast<const S*>(p.src) + m * p.src_worker, p.n, in);
   }
   return cta_sum(sum);
 }
@@ -202,7 +183,7 @@ __device__ __forceinline__ void scaled(const S* g, D* out, long long at, long lo
 #pragma unroll
   for (int i = 0; i < kBatch; ++i) {
     const long long j = at + i * kThreads * kVec;
-    if (kWhole || (j >= 0 && j + kVec <= n)) raw[i] = load_hint<Pack<S, kVec>>(g + j, policy);
+    if (kWhole || (j >= 0 && j + kVec <= n)) raw[i] = load_last<Pack<S, kVec>>(g + j, policy);
   }
 #pragma unroll
   for (int i = 0; i < kBatch; ++i) {
@@ -214,7 +195,7 @@ __device__ __forceinline__ void scaled(const S* g, D* out, long long at, long lo
     for (int e = 0; e < kVec; ++e) v[e] = __fmul_rn(v[e], c);
     Pack<D, kVec> o;
     store_floats<D, kVec>(o.v, v);
-    store_hint(out + j, o, policy);
+    *reinterpret_cast<Pack<D, kVec>*>(out + j) = o;
   }
 }
 template <typename S, typename D, int kVec>

@@ -18,7 +18,7 @@ namespace s3gd {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr uint64_t kMaxDim = (1ull << 24) - 1;
+constexpr uint64_t kMaxDim = 65535ull * kThreads;   // a grid dimension of tiles with one entry a thread: 2^24 - 256
 constexpr int kRuns = kDefaultSMs;                 // runs of rows at least, where there are as many rows
 constexpr uint64_t kMaxRun = 4096;                 // rows of a run at most: 32-bit sums stay short
 

@@ -215,6 +215,16 @@ def test_binding_refusals_of_combinations():
         S.s3gd_grad_norm([rows], stand((M, 1)), ws)
 
 
+@pytest.mark.parametrize("several", [False, True])
+def test_an_output_that_is_named_twice_is_refused(several):
+    a, b, none = torch.zeros(2, 6), torch.zeros(2, 6), torch.zeros(2, 0)
+    for grads, outs in (([a, a], None), ([a, b], [b, b]), ([a.t(), a.t()], None) if not several else ([a, b, a], None)):
+        with pytest.raises(ValueError, match="twice"):
+            binding._parts(grads, outs, -1, 2 if several else 1, several, True)
+    for grads, outs, writes in (([a, a], None, False), ([a, a], [a, b], True), ([none, a, none], None, True)):     # read twice, or empty: fine
+        assert binding._parts(grads, outs, -1, 2 if several else 1, several, writes)[1] == len(grads)
+
+
 # ------------------------------------------------------------------ the statements themselves
 def test_layer_norm_statement():
     r = np.random.default_rng(3)
