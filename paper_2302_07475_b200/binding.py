@@ -1010,10 +1010,12 @@ def _parts(grads, out, index: int, M: int, several: bool, writes: bool):
     outs = grads if out is None else list(out)
     if len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
-    try:
-        plain = _plain_parts(grads, outs, index, M, several, writes)
-    except (TypeError, AttributeError, KeyError):        # something that is no tensor, or of another type: named below
-        plain = None
+    plain = None
+    if len(grads) > 3:                                   # (a tensor by itself takes 3.6 us below and 5.9 above)
+        try:
+            plain = _plain_parts(grads, outs, index, M, several, writes)
+        except (TypeError, AttributeError, KeyError):    # something that is no tensor, or of another type: named below
+            pass
     if plain is not None:
         return plain
     packed, first = array.array("Q"), 1 if several else 0

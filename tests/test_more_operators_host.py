@@ -216,13 +216,16 @@ def test_binding_refusals_of_combinations():
 
 
 @pytest.mark.parametrize("several", [False, True])
-def test_an_output_that_is_named_twice_is_refused(several):
+@pytest.mark.parametrize("others", [0, 4])                                    # short lists and long ones are looked at in different ways
+def test_an_output_that_is_named_twice_is_refused(several, others):
     a, b, none = torch.zeros(2, 6), torch.zeros(2, 6), torch.zeros(2, 0)
-    for grads, outs in (([a, a], None), ([a, b], [b, b]), ([a.t(), a.t()], None) if not several else ([a, b, a], None)):
+    more, M = [torch.zeros(2, 3) for _ in range(others)], 2 if several else 1
+    for grads, outs in (([a, a], None), ([a, b], [b, b]), ([a, b, a], None)):
         with pytest.raises(ValueError, match="twice"):
-            binding._parts(grads, outs, -1, 2 if several else 1, several, True)
-    for grads, outs, writes in (([a, a], None, False), ([a, a], [a, b], True), ([none, a, none], None, True)):     # read twice, or empty: fine
-        assert binding._parts(grads, outs, -1, 2 if several else 1, several, writes)[1] == len(grads)
+            binding._parts(grads + more, outs and outs + more, -1, M, several, True)
+    for grads, outs, writes, n in (([a, a], None, False, 2), ([a, a], [a, b], True, 2), ([none, a, none], None, True, 1)):   # read twice, or empty: fine
+        packed, count = binding._parts(grads + more, outs and outs + more, -1, M, several, writes)
+        assert sum(1 for k in range(count) if packed[6 * k + 2]) == n + others
 
 
 # ------------------------------------------------------------------ the statements themselves
