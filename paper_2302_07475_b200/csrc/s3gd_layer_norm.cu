@@ -359,9 +359,10 @@ __device__ __forceinline__ Segment segment(uint32_t begin, uint32_t end, uint32_
 }
 
 // The two kernels have the same course.  Turn k: wait until its row has arrived, send for row k + kStages - 1 (into the stage that
-// turn k - 1 read), take the row's sums.  With four stages or more the sum of row k + 1 is taken in turn k and travels with the
-// others, which leaves one exchange a row (65536 x 2048 bf16 with residual: see below); with fewer, waiting for row k + 1 would leave
-// too little on its way.
+// turn k - 1 read), take the row's sums.  With three stages or more the sum of row k + 1 is taken in turn k and travels with the
+// others, which leaves one exchange a row (65536 x 2048 bf16, gradient with residual: 289 -> 223 us; 32768 x 2048 fp32 gradient:
+// 156 -> 147); with two, waiting for row k + 1 would leave nothing on its way.  Backward, rows entry by entry: 128 registers do not
+// hold the next row as well.
 constexpr int kNormRoom = 204 * 1024;              // shared memory of the ring
 template <typename X, int kVec, bool kAdd>
 constexpr int kNormStage = Ring<X, kVec>::kStage * (kAdd ? 2 : 1);
@@ -372,7 +373,7 @@ __device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uin
                                           Room* rooms, const float2* w, const float2* b) {
   using RingX = Ring<X, kVec>;
   constexpr int kStage = kNormStage<X, kVec, kAdd>, kStages = stages_of(kStage, kNormRoom);
-  constexpr bool kAhead = kStages >= 4;
+  constexpr bool kAhead = kStages >= 3;
   const uint32_t groups = kRowThreads / tpr;
   const float over = 1.f / a.dim;
   Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
@@ -493,7 +494,7 @@ __device__ __forceinline__ void grad_rows(const NormGradArgs& a, uint32_t begin,
                                           Room* rooms, const float2* w, float2* dw, float2* db) {
   using RingD = Ring<D, kVec>; using RingX = Ring<X, kVec>;
   constexpr int kStage = kGradStage<D, X, kVec, kMore>, kStages = stages_of(kStage, kGradRoom);
-  constexpr bool kAhead = kStages >= 4 && kVec > 1;
+  constexpr bool kAhead = kStages >= 3 && kVec > 1;
   const uint32_t groups = kRowThreads / tpr;
   const float over = 1.f / a.dim;
   Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
