@@ -7,9 +7,9 @@
 // Sums over a row.  The mean is taken first, then the sums of d = x - mean and d^2 (and of g and g d): the sum of d, which
 // would be zero but for the mean's rounding, corrects both mean and variance, so that rows far from zero keep their digits.
 //
-// Weight gradients.  The rows of all workers, one worker after the other, are dealt to CTAs in runs of `per` rows.  A CTA
-// writes a partial sum for each worker that its run touches; run k and worker m meet in slot k + m (from one slot to the next
-// in that order either k or m grows).  A last kernel adds a worker's slots in 64 bits, in ascending order: no atomics, and the
+// Weight gradients.  The rows of all workers, one worker after the other, are dealt to CTAs in runs of `per` rows, which may end with a
+// worker's rows or go on with the next one's.  A CTA writes a partial sum for each worker that its run touches; where runs go on, run k
+// and worker m meet in slot k + m (from one slot to the next in that order either k or m grows).  A last kernel adds a worker's slots in 64 bits, in ascending order: no atomics, and the
 // result depends on sizes and alignment alone.
 //
 // Bound by memory in 32 bits, by the latency of dependent instructions in 16: 16 warps an SM hold their columns' weights and sums in
@@ -50,7 +50,8 @@ struct NormGradArgs {
   const void *weight, *ids;
   bool weight_bf16, ids64, grads_bf16, accumulate;
   uint32_t M, T, N, dim, pad, per, runs;
-  uint32_t shares;                                 // 0, or the CTAs of a cluster that share a worker's rows and join their sums themselves
+  uint32_t shares;                                 // runs of a worker, where they end with its rows; 0: they may go on with the next worker's
+  bool cluster;                                    // a worker's runs are a cluster's CTAs, which join their sums themselves
   float eps;
   void *dweight, *dbias;
   long long grads_stride;
@@ -111,7 +112,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(NormGradArgs
   if (a.dweight == nullptr && a.dbias == nullptr) return;
   double sum = 0;
   if (a.T > 0 && col < 2 * a.pad) {
-    const uint32_t first = (uint32_t)((uint64_t)m * a.T / a.per), last = (uint32_t)(((uint64_t)(m + 1) * a.T - 1) / a.per);
+    const uint32_t first = a.shares ? m * (a.shares - 1) : (uint32_t)((uint64_t)m * a.T / a.per);      // slot k + m
+    const uint32_t last = a.shares ? first + a.shares - 1 : (uint32_t)(((uint64_t)(m + 1) * a.T - 1) / a.per);
     const float* from = a.partial + (size_t)m * 2 * a.pad + col;
 #pragma unroll 8
     for (uint32_t k = first + w; k <= last; k += kJoinWarps) sum += from[(size_t)k * 2 * a.pad];
@@ -129,8 +131,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32) norm_join_kernel(NormGradArgs
 // not read).
 constexpr int kRowThreads = 512, kRowWarps = kRowThreads / 32;
 // Few rows: a cluster of eight CTAs takes a worker's rows and joins their sums itself, which saves the second launch.  One row a group
-// at most (64 rows of 768: 7.6 us, with a second launch 8.1; 200 rows 12.1 and 8.8) and eight workers (8 x 64 rows of 768: 6.7 and
-// 7.8 us; 16 workers: 14 and 8 us, more clusters than there is room for at once).
+// at most (16 rows of 768: 7.0 us, with a second launch 7.1; 200 rows 12.1 and 8.8; what it saves besides is the host's second launch)
+// and eight workers (8 x 16 rows of 768: 7.0 and 7.7 us; 16 workers: 14 and 8 us, more clusters than there is room for at once).
 constexpr int kCluster = 8;
 constexpr int kClusterWorkers = 8;
 constexpr int kEach = 16, kPairs = kEach / 2;
@@ -496,7 +498,6 @@ __global__ void __launch_bounds__(kRowThreads, 1) norm_row_kernel(NormArgs a, ui
 constexpr int kGradRoom = 204 * 1024;
 template <typename D, typename X, int kVec, bool kMore>
 constexpr int kGradStage = Ring<D, kVec>::kStage + Ring<X, kVec>::kStage * (kMore ? 2 : 1);
-constexpr int kFlushBytes = kRowThreads * 2 * 4 * (int)sizeof(float);
 
 // Rows begin .. end of worker m; the group's sums of the weight gradients.
 template <typename D, typename X, int kVec, bool kMore, typename Cols>
@@ -618,14 +619,15 @@ template <typename D, typename X, int kVec, int kForm, bool kMore>
 __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a, uint32_t tpr) {
   constexpr int kStage = kGradStage<D, X, kVec, kMore>, kStages = stages_of(kStage, kGradRoom);
   extern __shared__ __align__(16) char ring[];
-  float* flush = reinterpret_cast<float*>(ring + kStages * kStage);
+  float* flush = reinterpret_cast<float*>(ring);                     // between two segments, when no row is on its way
+  static_assert(kStages * kStage >= kRowThreads * 2 * kEach * (int)sizeof(float));
   __shared__ Room rooms[2];
   const uint32_t groups = kRowThreads / tpr;
   const bool busy = threadIdx.x / tpr < groups;                      // not a warp that makes no group
   const Columns<kVec, kForm> at = columns<kVec, kForm>(tpr, a.dim);
   grid_dependency_wait();
   uint32_t r0 = blockIdx.x * a.per, r1 = min(r0 + a.per, a.N);
-  if (a.shares) {                                                    // a cluster for a worker
+  if (a.shares) {
     r0 = min(blockIdx.x * a.per, a.T) + blockIdx.y * a.T;
     r1 = min((blockIdx.x + 1) * a.per, a.T) + blockIdx.y * a.T;
   }
@@ -636,7 +638,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
     clear(dw);
     clear(db);
     if (busy) grad_rows<D, X, kVec, kMore>(a, begin, end, m, tpr, at, ring, rooms, w, dw, db);
-    if (a.partial != nullptr) {                                      // the groups' sums, four entries a thread at a time
+    if (a.partial != nullptr) {                                      // the groups' sums
       float* out = a.partial + (size_t)(blockIdx.x + m * (a.shares ? a.shares : 1u)) * 2 * a.pad;
 #pragma unroll
       for (int i = 0; i < kPairs; ++i)                               // groups of one warp
@@ -646,27 +648,25 @@ __global__ void __launch_bounds__(kRowThreads, 1) grad_row_kernel(NormGradArgs a
         }
       const uint32_t tile = kForm >= kTiles ? tile_columns<kVec>(tpr, a.dim) : a.dim;
       const uint32_t apart = tpr < 32 ? 32 : tpr, past = tpr < 32 ? kRowThreads : groups * tpr;   // threads from one sum of a column to the next
+      __syncthreads();
 #pragma unroll
-      for (int part = 0; part < kEach / 4; ++part) {
-        __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          flush[e * kRowThreads + threadIdx.x] = reinterpret_cast<float*>(dw)[part * 4 + e];
-          flush[(4 + e) * kRowThreads + threadIdx.x] = reinterpret_cast<float*>(db)[part * 4 + e];
-        }
-        __syncthreads();
-        for (uint32_t i = threadIdx.x; i < 8 * tpr; i += kRowThreads) {
-          const uint32_t row = i / tpr, l = i % tpr, e = part * 4 + row % 4;
-          const uint32_t in = (kForm >= kTiles ? l % 32 : l) * kVec + e / kVec * at.step() + e % kVec, col = kForm >= kTiles ? l / 32 * tile + in : in;
-          float sum = 0.f;
-          for (uint32_t j = l; j < past; j += apart) sum += flush[row * kRowThreads + j];
-          if (in < tile && col < a.dim) out[(row < 4 ? 0 : a.pad) + col] = sum;
-        }
+      for (int e = 0; e < kEach; ++e) {
+        flush[e * kRowThreads + threadIdx.x] = reinterpret_cast<float*>(dw)[e];
+        flush[(kEach + e) * kRowThreads + threadIdx.x] = reinterpret_cast<float*>(db)[e];
       }
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < 2 * kEach * tpr; i += kRowThreads) {
+        const uint32_t row = i / tpr, l = i % tpr, e = row % kEach;
+        const uint32_t in = (kForm >= kTiles ? l % 32 : l) * kVec + e / kVec * at.step() + e % kVec, col = kForm >= kTiles ? l / 32 * tile + in : in;
+        float sum = 0.f;
+        for (uint32_t j = l; j < past; j += apart) sum += flush[row * kRowThreads + j];
+        if (in < tile && col < a.dim) out[(row < kEach ? 0 : a.pad) + col] = sum;
+      }
+      if (end < r1) __syncthreads();
     }
     begin = end;
   }
-  if (!a.shares) return;
+  if (!a.cluster) return;
   if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x < 8) a.hdr[threadIdx.x] = 0;
   if (a.partial == nullptr) return;
   cluster_sync();                                                    // the partial sums of all CTAs are there
@@ -830,7 +830,7 @@ bool norm_grad_layout(int M, uint64_t T, uint64_t dim, NormGradLayout* L) {
   L->off_stats = align_up(kHdrWords * sizeof(uint32_t), 256);
   L->off_partial = align_up(L->off_stats + (dim > kMaxRowDim ? N * 2 * sizeof(float4) : 0), 256);
   // slots: runs + M, which never shrinks as N grows if runs is counted as follows
-  const uint64_t most = (N < kRuns ? N : (uint64_t)kRuns) + N / kMaxRun + M + 1;
+  const uint64_t most = (N < 2 * kRuns ? N : (uint64_t)2 * kRuns) + N / kMaxRun + M + 1;
   L->total = align_up(L->off_partial + most * 2 * L->pad * sizeof(float), 256);
   return true;
 }
@@ -892,12 +892,12 @@ cudaError_t enqueue_norm_rows(NormArgs a, cudaStream_t st) {
 template <typename D, typename X, int kVec, int kForm, bool kMore>
 cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   static int done[kMaxDevices];
-  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage + kFlushBytes;
+  constexpr int kStage = kGradStage<D, X, kVec, kMore>, kBytes = stages_of(kStage, kGradRoom) * kStage;
   auto kernel = grad_row_kernel<D, X, kVec, kForm, kMore>;
   const cudaError_t e = opt_in_dynamic_smem(reinterpret_cast<const void*>(kernel), kBytes, done);
   if (e != cudaSuccess) return e;
   const uint32_t tpr = threads_per_row(a.dim, kVec);
-  if (a.shares == 0) return launch_after(kernel, dim3(a.runs), dim3(kRowThreads), kBytes, st, a, tpr);
+  if (!a.cluster) return launch_after(kernel, a.shares ? dim3(a.shares, a.M) : dim3(a.runs), dim3(kRowThreads), kBytes, st, a, tpr);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(kCluster, a.M); cfg.blockDim = dim3(kRowThreads); cfg.dynamicSmemBytes = kBytes; cfg.stream = st;
   cudaLaunchAttribute attr[2];
@@ -907,6 +907,39 @@ cudaError_t enqueue_grad_rows(const NormGradArgs& a, cudaStream_t st) {
   attr[1].val.clusterDim.x = kCluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr; cfg.numAttrs = 2;
   return cudaLaunchKernelEx(&cfg, kernel, a, tpr);
+}
+// How rows are dealt to CTAs.  A turn of a CTA takes a row for each of its groups, and what a worker's rows cost a CTA besides
+// (filling the ring, adding the groups' sums) is worth kSegmentTurns turns: runs either go on from one worker to the next, which
+// keeps all CTAs equally busy, or end with the worker, one or two rounds of CTAs, whichever is over sooner (8 x 4096 x 512 fp32: 36.2 us,
+// with runs that go on 39.6; 16 x 200 x 128: 6.8 and 14.2; 40 x 2000 x 1024, where they go on: 179).
+constexpr uint32_t kLeastRun = 8;                  // rows of a run at least, where its CTA has as many groups: fewer sums to join
+constexpr uint64_t kSegmentTurns = 4;
+void plan_runs(NormGradArgs* a, uint32_t groups) {
+  const uint64_t least = groups < kLeastRun ? groups : kLeastRun, M = a->M, T = a->T;
+  auto turns = [&](uint64_t rows) { return (rows + groups - 1) / groups; };
+  if (M <= kClusterWorkers && T <= (uint64_t)kCluster * groups) {
+    a->cluster = true;
+    a->per = (uint32_t)((T + kCluster - 1) / kCluster);
+    a->shares = (uint32_t)((T + a->per - 1) / a->per);
+    return;
+  }
+  if (a->per < least) a->per = (uint32_t)least;
+  a->runs = (uint32_t)((a->N + a->per - 1) / a->per);
+  const uint64_t segments = M == 1 ? 1 : (a->per + T - 1) / T + (T % a->per != 0);
+  uint64_t best = (a->runs + kRuns - 1) / kRuns * (turns(a->per) + (segments - 1) + segments * kSegmentTurns);
+  for (uint64_t rounds = 1; rounds <= 2 && M > 1; ++rounds) {
+    uint64_t shares = rounds * kRuns / M;
+    if (shares == 0) continue;
+    uint64_t per = (T + shares - 1) / shares;
+    per = per < least ? least : per;
+    if (per > kMaxRun) continue;
+    shares = (T + per - 1) / per;
+    const uint64_t cost = (M * shares + kRuns - 1) / kRuns * (turns(per) + kSegmentTurns);
+    if (cost >= best) continue;
+    best = cost;
+    a->per = (uint32_t)per;
+    a->shares = (uint32_t)shares;
+  }
 }
 template <typename F>
 cudaError_t by_row_width(int v, F f) { return v >= 4 ? f(Width<4>()) : f(Width<1>()); }
@@ -1009,10 +1042,7 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
     const unsigned wide = vec >= 4 ? 4 : 1, tiles = (unsigned)((dim + kThreads * wide - 1) / (kThreads * wide));
     if (tiles > 65535) return S3GD_ERR_INVALID_ARG;
     count_launch(dim > kMaxRowDim ? 2 : 1);
-    if (dim <= kMaxRowDim && M <= kClusterWorkers && T <= (uint64_t)kCluster * (kRowThreads / threads_per_row(dim, vec))) {
-      a.per = (uint32_t)((T + kCluster - 1) / kCluster);
-      a.shares = (uint32_t)((T + a.per - 1) / a.per);
-    }
+    if (dim <= kMaxRowDim) plan_runs(&a, kRowThreads / threads_per_row(dim, vec));
     e = by_real(dy_dtype, [&](auto dt) { return by_real(x_dtype, [&](auto xt) {
       using D = decltype(dt); using X = decltype(xt);
       if (dim <= kMaxRowDim)
@@ -1029,7 +1059,7 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
       });
     }); });
   }
-  if (e == cudaSuccess && a.shares == 0) {
+  if (e == cudaSuccess && !a.cluster) {
     count_launch();
     e = launch_after(norm_join_kernel, dim3(weights ? (2 * a.pad + 31) / 32 : 1, weights ? M : 1), dim3(kJoinWarps * 32), 0, st, a);
   }
