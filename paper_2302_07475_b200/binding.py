@@ -1060,6 +1060,14 @@ def _norms(norm: torch.Tensor):
     return norm.get_device(), norm.numel(), several
 
 
+def _clip_room(ws: torch.Tensor, index: int):
+    if not (isinstance(ws, torch.Tensor) and ws.is_cuda and ws.dtype == torch.uint8 and ws.is_contiguous()):
+        raise TypeError("ws must be a contiguous CUDA tensor of dtype torch.uint8")
+    if ws.get_device() != index:
+        raise TypeError(f"ws must be on the device of norm, cuda:{index}, not on {ws.device}")
+    return ws.data_ptr(), ws.numel()
+
+
 def s3gd_grad_norm(grads, norm: torch.Tensor, ws: torch.Tensor) -> None:
     """norm <- the norm over all entries of the tensors in grads (one tensor, or a sequence).
 
@@ -1067,26 +1075,28 @@ def s3gd_grad_norm(grads, norm: torch.Tensor, ws: torch.Tensor) -> None:
     Tensors are fp32 or bf16, each in one piece (within a worker)."""
     index, M, several = _norms(norm)
     packed, count = _parts(grads, None, index, M, several, False)
-    w = _ptr(ws, torch.uint8, name="ws")
-    if ws.get_device() != index:
-        raise TypeError(f"ws must be on the device of norm, {norm.device}")
-    args = (packed.buffer_info()[0] if count else None, count, M, norm.data_ptr(), w, ws.numel())
-    with _on(norm):
+    args = (packed.buffer_info()[0] if count else None, count, M, norm.data_ptr(), *_clip_room(ws, index))
+    if _current_device() == index:
         code = load().s3gd_grad_norm(*args, _stream_of(index))
-    _check("s3gd_grad_norm", code)
+    else:
+        with _on(norm):
+            code = load().s3gd_grad_norm(*args, _stream_of(index))
+    if code:
+        _check("s3gd_grad_norm", code)
 
 
 def s3gd_clip(grads, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, out=None, eps: float = 1e-6) -> None:
     """out <- grads * min(1, max_norm / (norm + eps)), norm as s3gd_grad_norm gives it; per worker where norm is [M].
 
     out (None: in place) has a tensor for each of grads, of the same shape and order of axes, fp32 or bf16: e.g. the columns of a
-    gradient buffer, out[i] = rows[:, a:b].view_as(grads[i]).  Outputs overlap no other tensor of the call."""
+    gradient buffer, out[i] = rows[:, a:b].unflatten(1, shape).  Outputs overlap no other tensor of the call, and none is named twice."""
     index, M, several = _norms(norm)
     packed, count = _parts(grads, out, index, M, several, True)
-    w = _ptr(ws, torch.uint8, name="ws")
-    if ws.get_device() != index:
-        raise TypeError(f"ws must be on the device of norm, {norm.device}")
-    args = (packed.buffer_info()[0] if count else None, count, M, max_norm, eps, norm.data_ptr(), w, ws.numel())
-    with _on(norm):
+    args = (packed.buffer_info()[0] if count else None, count, M, max_norm, eps, norm.data_ptr(), *_clip_room(ws, index))
+    if _current_device() == index:
         code = load().s3gd_clip(*args, _stream_of(index))
-    _check("s3gd_clip", code)
+    else:
+        with _on(norm):
+            code = load().s3gd_clip(*args, _stream_of(index))
+    if code:
+        _check("s3gd_clip", code)

@@ -137,6 +137,34 @@ def test_what_is_not_finite_stays_with_its_worker():
     check([out[::3]], norm[::3], [g[::3]], 1.0)
 
 
+@pytest.mark.parametrize("tiles", [1, 8, 9, 16, 17, 40])
+@pytest.mark.parametrize("M", [1, 8, 9])
+def test_few_and_many_tiles(tiles, M):
+    n = 8192 * tiles - 8                                                  # tiles of 8192 entries, wherever the first one lies
+    g, out = rand((M, n + 3), F32, 1)[:, 1:n + 1], torch.full((M, n + 7), 5.0, dtype=BF16, device=DEV)
+    norm, ws = torch.empty((M,), device=DEV), workspace(M)
+    S.s3gd_clip([g], 3.0, norm, ws, out=[out[:, 4:n + 4]])
+    S.s3gd_device_status(ws)
+    check([out[:, 4:n + 4]], norm, [g], 3.0)
+    assert (out[:, :4] == 5).all() and (out[:, n + 4:] == 5).all()
+    norm.zero_()
+    S.s3gd_grad_norm(g, norm, ws)
+    check(None, norm, [g], 3.0)
+
+
+def test_types_mixed_in_one_list():
+    shapes, kinds = [(3000,), (40, 5), (9000,), (7,), (123,), (20000,)], [(F32, F32), (BF16, F32), (F32, BF16), (BF16, BF16), (BF16, F32), (F32, F32)]
+    grads = [rand((4,) + s, src, i) for i, (s, (src, _)) in enumerate(zip(shapes, kinds))]
+    outs = [torch.empty((4,) + s, dtype=dst, device=DEV) for s, (_, dst) in zip(shapes, kinds)]
+    norm, ws = torch.empty((4,), device=DEV), workspace(4)
+    S.s3gd_clip(grads, 2.0, norm, ws, out=outs)
+    check(outs, norm, grads, 2.0)
+    kept = [g.clone() for g in grads]
+    S.s3gd_clip(grads, 2.0, norm, ws, out=[g if i % 2 else o for i, (g, o) in enumerate(zip(grads, outs))])   # every other one in place
+    check([g if i % 2 else o for i, (g, o) in enumerate(zip(grads, outs))], norm, kept, 2.0)
+    assert all(torch.equal(a, b) for a, b in zip(grads[::2], kept[::2]))
+
+
 def test_values_equal_for_any_place_in_memory():
     base = rand((70000,), F32, 1)
     norms, ws = [], workspace(1)

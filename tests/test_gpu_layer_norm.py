@@ -126,6 +126,17 @@ def test_many_rows_and_workers():
         assert all(torch.equal(a, b) for a, b in zip(got, again))          # no result depends on the run
 
 
+@pytest.mark.parametrize("M,T,dim", [(200, 100, 40), (100, 333, 96), (160, 37, 512), (9, 20, 768), (8, 64, 768), (8, 65, 768), (2, 1025, 33), (37, 150, 264),
+                                     (400, 3, 1030), (1, 9, 4096), (5, 900, 1024)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_dealt_in_all_ways(M, T, dim, dtype):
+    x, dy, w = rand((M, T, dim), dtype, 62, 1.5), rand((M, T, dim), dtype, 63), rand((dim,), F32, 64, 0.3, 1.0)
+    ids, before = places((M, T), 0.1, 65), rand((M, 2 * dim + 3), F32, 66)
+    got = run_grad(dy, x, w, ids, before=before)
+    check_grad(got, dy, x, w, ids, before=before)
+    assert all(torch.equal(a, b) for a, b in zip(got, run_grad(dy, x, w, ids, before=before)))
+
+
 @pytest.mark.parametrize("dim", [64, 100, 1001, 2048, 9000])
 def test_rows_far_from_zero(dim):
     x = rand((1, 6, dim), F32, 16, 1.0, 1e4)
