@@ -10,10 +10,10 @@
 //
 // Bound by memory: squares are read at 5.5 (bf16) to 6.5 TB/s, scaled at 6.2 to 6.6 TB/s of reads and writes together.  Clipping reads
 // everything twice; the second time a part comes from the L2, where workers and tiles are taken last first.
-//     norm of 53 bf16 tensors, 95.6e6 entries     35 us (floor 29), 42 from Python: the host's look at the list
+//     norm of 53 bf16 tensors, 95.6e6 entries     35 us (floor 29), 41 from Python: the host's look at the list
 //     the same clipped into an fp32 row          129 us (floor 87; 116 with the second read)
 //     62 fp32 tensors of 100 workers, 1.12e9     2.06 ms (floor 1.36; 2.04 with the second read)
-//     13 fp32 tensors, 28,000 entries              8 us, 22.5 from Python
+//     13 fp32 tensors, 28,000 entries              8 us, 21.5 from Python
 // Both passes over many workers in one kernel, by tickets, were tried: a worker's entries then come from the L2 the second time, but
 // its CTAs keep less on its way (registers of both passes) and take as long.
 #include "s3gd_ops.cuh"

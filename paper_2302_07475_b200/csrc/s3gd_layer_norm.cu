@@ -15,11 +15,11 @@
 // Bound by memory in 32 bits, by the latency of dependent instructions in 16: 16 warps an SM hold their columns' weights and sums in
 // up to 128 registers, and issue in 45 (forward) to 60 % of the cycles.  One call after the other, in a captured graph where the host
 // would be slower (floor: every row read and written once at 6.57 TB/s):
-//     forward   8 x 4096 x 512 fp32 -> bf16, 5 % empty    22.6 us (15)      backward  8 x 4096 x 512 fp32, 5 % empty       43 us (30)
+//     forward   8 x 4096 x 512 fp32 -> bf16, 5 % empty    22.6 us (15)      backward  8 x 4096 x 512 fp32, 5 % empty       38 us (30)
 //               65536 x 2048 bf16, residual                187 us (163)               65536 x 2048 bf16, residual         216 us (163)
 //               32768 x 2048 bf16 / fp32                  63 / 105 us (41 / 82)       32768 x 2048 bf16 / fp32       102 / 147 us (61 / 123)
 //               67041 x 1001 bf16 / fp32                  79 / 101 us (41 / 82)       67041 x 1001 bf16 / fp32       145 / 165 us (61 / 123)
-//               1 x 1024 bf16                             6 us, 8.5 from Python       200 x 768 fp32, added to       12 us, 17 from Python
+//               1 x 1024 bf16                             4 us, 8.2 from Python       200 x 768 fp32, added to      8.2 us, 17 from Python
 // Rows of more than 8192 entries are read two or three times (4096 x 16384 bf16: 150 us forward, 222 us backward).
 #include "s3gd_ops.cuh"
 #include "s3gd_tcgen05.cuh"
