@@ -443,8 +443,8 @@ S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t d
  *  opt_ids        [M x T] I32 or I64 (ids_dtype; any of the two where opt_ids is NULL)
  *  y              [M x T x dim] F32 or BF16.  y may be x itself, total may be x or add itself (same type and strides); outputs
  *                 otherwise overlap nothing.  An input's stride may be 0: the same row repeated
- * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same.  Sums, mean and variance are held in 32 bits or more and rows far from zero keep their digits;
- * entries beyond about 1e18 in magnitude, whose squares pass fp32's range, are not provided for.
+ * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same.  Sums, mean and variance
+ * are held in 32 bits or more and rows far from zero keep their digits; entries beyond about 1e18 in magnitude, whose squares pass fp32's range, are not provided for.
  * T may be 0.  Limits: M <= 65535, M * T < 2^31, dim <= 2^24 - 256, 0 <= eps < Inf.
  */
 S3GD_API s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_add,
@@ -491,8 +491,8 @@ S3GD_API s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_t 
  * gradient buffer.  s3gd_grad_norm reads neither out nor out_dtype.  Tensors with n = 0 and an empty list are allowed.
  *
  *  out_norm  dev  [M] fp32        ws  >= s3gd_clip_workspace_bytes(M), 256-byte aligned, not preserved
- * Squares are summed in 64 bits, c is rounded to 32: entries at either end of fp32's range count as they should.  A worker that holds a NaN has norm and
- * outputs NaN; one that holds an Inf has norm Inf and c = 0, so that its infinite entries become NaN and the others 0.  Results depend on
+ * Squares are summed in 64 bits (of up to eight neighbours in 32, where those hold them), c is rounded to 32: entries at either
+ * end of fp32's range count as they should.  A worker that holds a NaN has norm and outputs NaN; one that holds an Inf has norm Inf and c = 0, so that its infinite entries become NaN and the others 0.  Results depend on
  * sizes and alignment alone, not on the run.  Limits: 1 <= M <= 65535, n < 2^40, 0 <= max_norm < Inf, 0 <= eps < Inf.
  */
 typedef struct s3gd_part {
