@@ -443,7 +443,8 @@ S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t d
  *  opt_ids        [M x T] I32 or I64 (ids_dtype; any of the two where opt_ids is NULL)
  *  y              [M x T x dim] F32 or BF16.  y may be x itself, total may be x or add itself (same type and strides); outputs
  *                 otherwise overlap nothing.  An input's stride may be 0: the same row repeated
- * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same.  Sums, mean and variance
+ * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same (up to 8192 entries also where
+ * their standard deviation is below 2^-27 of the mean, which takes rows of which few entries differ, by a step).  Sums, mean and variance
  * are held in 32 bits or more and rows far from zero keep their digits; entries beyond about 1e18 in magnitude, whose squares pass fp32's range, are not provided for.
  * T may be 0.  Limits: M <= 65535, M * T < 2^31, dim <= 2^24 - 256, 0 <= eps < Inf.
  */

@@ -356,6 +356,14 @@ __device__ __forceinline__ void group_sums(float (&v)[kCount == 0 ? 1 : kCount],
   if constexpr (kCount > 2) { v[2] = all.z; v[3] = all.w; }
 }
 
+// The variance from the mean of (v - mean)^2 and `shift`, the mean of v - mean.  Where all entries are equal, v - mean is one number d in
+// every column: zero, or what the mean's rounding left.  The sums have at most 31 roundings, with 1 / dim's, so the mean square is at most
+// (1 + 31 u) d^2 and shift^2 at least (1 - 60 u) d^2, u = 2^-24: taking 128 u more than shift^2 leaves nothing, as the formula has it.  In other
+// rows that is no more than the mean square's own rounding where shift is as large as the deviation, and vanishes with shift^2.
+__device__ __forceinline__ float variance(float square, float shift) {
+  return fmaxf(fmaf(-shift * (1.f + 0x1p-17f), shift, square), 0.f);
+}
+
 // One worker's rows begin .. end of a run, of which the group takes every groups-th.
 struct Segment {
   uint32_t m, t, turns, row, groups;
@@ -463,7 +471,7 @@ __device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uin
     float sums[2] = {s0.x + s0.y, s1.x + s1.y};
     if (kAhead) sum = total_of(u);
     group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-    const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+    const float shift = sums[0] * over, rstd = rsqrtf(variance(sums[1] * over, shift) + a.eps);
     if (in) {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) v[i] = fma2(fma2(v[i], both(rstd), both(-shift * rstd)), w[i], b[i]);
@@ -586,7 +594,7 @@ __device__ __forceinline__ void grad_rows(const NormGradArgs& a, uint32_t begin,
       sum = total_of(u);
     }
     group_sums<4, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-    const float shift = sums[0] * over, rstd = rsqrtf(fmaxf(fmaf(-shift, shift, sums[1] * over), 0.f) + a.eps);
+    const float shift = sums[0] * over, rstd = rsqrtf(variance(sums[1] * over, shift) + a.eps);
     const float mg = sums[2] * over, mgx = fmaf(-shift, sums[2], sums[3]) * over * rstd;
     if (real) {
 #pragma unroll
