@@ -443,9 +443,10 @@ S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t d
  *  opt_ids        [M x T] I32 or I64 (ids_dtype; any of the two where opt_ids is NULL)
  *  y              [M x T x dim] F32 or BF16.  y may be x itself, total may be x or add itself (same type and strides); outputs
  *                 otherwise overlap nothing.  An input's stride may be 0: the same row repeated
- * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same (up to 8192 entries also where
- * their standard deviation is below 2^-27 of the mean, which takes rows of which few entries differ, by a step).  Sums, mean and variance
- * are held in 32 bits or more and rows far from zero keep their digits; entries beyond about 1e18 in magnitude, whose squares pass fp32's range, are not provided for.
+ * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same.  Rows far from zero keep their
+ * digits.  Up to 8192 entries a row, sums are held in 32 bits: entries may be as large as 1e18 (a row whose squares pass fp32's range
+ * becomes NaN), and a variance below 2^-116, or below (2^-27 mean)^2, may count as 0, which shows where eps is no larger.  In longer
+ * rows they are held in 64 bits.
  * T may be 0.  Limits: M <= 65535, M * T < 2^31, dim <= 2^24 - 256, 0 <= eps < Inf.
  */
 S3GD_API s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_stride, int64_t x_worker_stride, const void* opt_add,

@@ -360,8 +360,10 @@ __device__ __forceinline__ void group_sums(float (&v)[kCount == 0 ? 1 : kCount],
 // every column: zero, or what the mean's rounding left.  The sums have at most 31 roundings, with 1 / dim's, so the mean square is at most
 // (1 + 31 u) d^2 and shift^2 at least (1 - 60 u) d^2, u = 2^-24: taking 128 u more than shift^2 leaves nothing, as the formula has it.  In other
 // rows that is no more than the mean square's own rounding where shift is as large as the deviation, and vanishes with shift^2.
+// 512 threads' sums below the normal range are off by 2^-150 each: what lies below 2^-116 has lost digits and counts as nothing, too.
 __device__ __forceinline__ float variance(float square, float shift) {
-  return fmaxf(fmaf(-shift * (1.f + 0x1p-17f), shift, square), 0.f);
+  const float rest = fmaf(-shift * (1.f + 0x1p-17f), shift, square);
+  return !(square < INFINITY) ? NAN : rest < 0x1p-116f ? 0.f : rest;           // NaN: squares beyond fp32's range, too
 }
 
 // One worker's rows begin .. end of a run, of which the group takes every groups-th.
@@ -468,10 +470,10 @@ __device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uin
       s0 = add2(s0, v[i]);
       s1 = fma2(v[i], v[i], s1);
     }
-    float sums[2] = {s0.x + s0.y, s1.x + s1.y};
+    float sums[2] = {(s0.x + s0.y) * over, (s1.x + s1.y) * over};     // the row's mean, so that sums of large squares fit
     if (kAhead) sum = total_of(u);
     group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-    const float shift = sums[0] * over, rstd = rsqrtf(variance(sums[1] * over, shift) + a.eps);
+    const float shift = sums[0], rstd = rsqrtf(variance(sums[1], shift) + a.eps);
     if (in) {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) v[i] = fma2(fma2(v[i], both(rstd), both(-shift * rstd)), w[i], b[i]);
@@ -586,7 +588,7 @@ __device__ __forceinline__ void grad_rows(const NormGradArgs& a, uint32_t begin,
       s2 = add2(s2, gw);
       s3 = fma2(gw, v[i], s3);
     }
-    float sums[4] = {s0.x + s0.y, s1.x + s1.y, s2.x + s2.y, s3.x + s3.y};
+    float sums[4] = {(s0.x + s0.y) * over, (s1.x + s1.y) * over, (s2.x + s2.y) * over, (s3.x + s3.y) * over};
     sum = 0.f;
     if (kAhead && more) {
       float2 u[kPairs];
@@ -594,8 +596,8 @@ __device__ __forceinline__ void grad_rows(const NormGradArgs& a, uint32_t begin,
       sum = total_of(u);
     }
     group_sums<4, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
-    const float shift = sums[0] * over, rstd = rsqrtf(variance(sums[1] * over, shift) + a.eps);
-    const float mg = sums[2] * over, mgx = fmaf(-shift, sums[2], sums[3]) * over * rstd;
+    const float shift = sums[0], rstd = rsqrtf(variance(sums[1], shift) + a.eps);
+    const float mg = sums[2], mgx = fmaf(-shift, mg, sums[3]) * rstd;
     if (real) {
 #pragma unroll
       for (int i = 0; i < kPairs; ++i) {

@@ -34,3 +34,30 @@ def test_equal_entries_without_eps_are_nan(dim, dtype):
         check_y(y[:, ~equal], x[:, ~equal], w, b, eps=0.0)
         rest = [t[:, ~equal].contiguous() for t in (dy, x)]
         check_grad(run_grad(*rest, w, eps=0.0), *rest, w, eps=0.0)
+
+
+@pytest.mark.parametrize("dim", [1, 16, 41, 512, 1001, 2047, 4096, 8192, 9000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size,eps", [(1e17, 1e-5), (1e18, 1e-5), (1e18, 0.0), (1e-16, 0.0), (1e-16, 1e-32)])
+def test_large_and_small_entries(dim, dtype, size, eps):
+    x, dy, w = rand((2, 5, dim), dtype, 6, size), rand((2, 5, dim), F32, 7), rand((dim,), F32, 8, 0.1, 1.0)
+    if dim == 1 and eps < 1e-6:
+        pytest.skip("one entry is its own mean")
+    y = torch.empty_like(x, dtype=F32)
+    S.s3gd_layer_norm(x, y, w, None, eps=eps)
+    check_y(y, x, w, None, eps=eps)
+    check_grad(run_grad(dy, x, w, eps=eps), dy, x, w, eps=eps)
+
+
+@pytest.mark.parametrize("dim", [16, 41, 512, 1001, 8192])
+def test_beyond_the_limits(dim):
+    x, dy, y = rand((2, 3, dim), F32, 9), rand((2, 3, dim), F32, 10), torch.empty((2, 3, dim), device=DEV)
+    x[0, 1] *= 1e21                                      # squares pass fp32's range: its row, and its worker's weight gradients
+    S.s3gd_layer_norm(x, y)
+    dx, dw, db = run_grad(dy, x, None)
+    for t in (y, dx):
+        assert t[0, 1].isnan().all() and t[0, ::2].isfinite().all() and t[1].isfinite().all()
+    assert dw[0].isnan().all() and dw[1].isfinite().all() and db.isfinite().all()
+    x[0, 1] *= 1e-41                                     # a variance that counts as zero, with nothing beside it
+    S.s3gd_layer_norm(x, y, eps=0.0)
+    assert not y[0, 1].isfinite().any() and y[0, ::2].isfinite().all() and y[1].isfinite().all()
