@@ -96,7 +96,7 @@ __device__ __forceinline__ void put_weight_gradient(const NormGradArgs& a, uint3
   if (base == nullptr || c >= a.dim) return;
   if (a.grads_bf16) {
     __nv_bfloat16* to = static_cast<__nv_bfloat16*>(base) + m * a.grads_stride + c;
-    *to = __float2bfloat16_rn((float)(a.accumulate ? sum + (double)__bfloat162float(*to) : sum));
+    *to = __double2bfloat16(a.accumulate ? sum + (double)__bfloat162float(*to) : sum);      // to nearest, in one rounding
   } else {
     float* to = static_cast<float*>(base) + m * a.grads_stride + c;
     *to = (float)(a.accumulate ? sum + (double)*to : sum);

@@ -61,3 +61,14 @@ def test_beyond_the_limits(dim):
     x[0, 1] *= 1e-41                                     # a variance that counts as zero, with nothing beside it
     S.s3gd_layer_norm(x, y, eps=0.0)
     assert not y[0, 1].isfinite().any() and y[0, ::2].isfinite().all() and y[1].isfinite().all()
+
+
+@pytest.mark.parametrize("T,dim", [(1, 8), (1, 1001), (1, 9000), (900, 40)])
+def test_weight_gradients_in_16_bits_are_rounded_once(T, dim):
+    # 1 + 2^-8 lies half way between two bf16 numbers: with 2^-31 on top the upper one is nearer, but 32 bits do not hold that
+    dy, x = torch.zeros((2, T, dim), device=DEV), rand((2, T, dim), F32, 11)
+    dy[0, 0], dy[1, T - 1] = 2.0 ** -8 + 2.0 ** -31, -2.0 ** -8 - 2.0 ** -31
+    before = torch.ones((2, 2 * dim + 3), dtype=BF16, device=DEV)
+    before[1] = -1.0
+    db = run_grad(dy, x, None, dst=BF16, before=before)[2]
+    assert (db[0] == 1 + 2.0 ** -7).all() and (db[1] == -1 - 2.0 ** -7).all()
