@@ -151,9 +151,14 @@ __device__ __forceinline__ double norm_of(const ClipArgs& a, uint32_t m) {
   return sqrt(cta_sum(sum));
 }
 
-__device__ __forceinline__ float factor_of(const ClipArgs& a, double norm) {
+// The factor, rounded to 32 bits.  One below their normal range (entries near fp32's end) would lose digits there, although what it makes
+// of such entries may not: it is held times 2^126, and its products are taken back by that, exactly where they are normal.
+struct Factor { float c; bool small; };
+__device__ __forceinline__ Factor factor_of(const ClipArgs& a, double norm) {
   const double held = norm + (double)a.eps;
-  return held <= (double)a.max_norm ? 1.f : (float)((double)a.max_norm / held);   // NaN stays NaN
+  if (held <= (double)a.max_norm) return {1.f, false};
+  const double c = (double)a.max_norm / held;                                     // NaN stays NaN
+  return c > 0 && c < 0x1p-126 ? Factor{(float)(c * 0x1p126), true} : Factor{(float)c, false};
 }
 // the CTA's sum of squares over a run of tiles of worker m, in every thread
 template <typename S, int kMax>
@@ -222,10 +227,19 @@ __device__ __forceinline__ void tile_scaled(const S* g, D* out, uint64_t n, uint
   for (int b = 0; b < kLoads && begin + b * kSpan < end; b += 4) scaled<S, D, kVec, 4, false>(g, out, at + b * kSpan, end, c, policy);
   ragged_entries<kVec>(begin, n, [&](long long j) { out[j] = from_f32<D>(__fmul_rn(to_f32(g[j]), c)); });
 }
+// by a small factor: rare, an entry at a time
 template <typename S, typename D>
-__device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t tile, float c) {
+__device__ __forceinline__ void tile_scaled_small(const S* g, D* out, uint64_t n, uint32_t tile, float c) {
+  const uint64_t begin = (uint64_t)tile * kTile, end = begin + kTile < n ? begin + kTile : n;
+#pragma unroll 1
+  for (uint64_t j = begin + threadIdx.x; j < end; j += kThreads) out[j] = from_f32<D>(__fmul_rn(__fmul_rn(to_f32(g[j]), c), 0x1p-126f));
+}
+template <typename S, typename D>
+__device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t tile, Factor f) {
   const S* g = static_cast<const S*>(p.src) + m * p.src_worker;
   D* out = static_cast<D*>(p.dst) + m * p.dst_worker;
+  const float c = f.c;
+  if (f.small) { tile_scaled_small<S, D>(g, out, p.n, tile, c); return; }
   // four entries at a time where both sides lie alike, two or one where they do not
   if (behind(g, 4) == behind(out, 4)) tile_scaled<S, D, 4>(g, out, p.n, tile, c);
   else if (behind(g, 2) == behind(out, 2)) tile_scaled<S, D, 2>(g, out, p.n, tile, c);
@@ -233,15 +247,15 @@ __device__ __forceinline__ void tile_clipped(const Part& p, uint32_t m, uint32_t
 }
 
 template <typename S, typename D, int kMax>
-__device__ __forceinline__ void run_scaled(const Parts<kMax>& parts, const ClipArgs& a, uint32_t m, uint32_t run, float c) {
+__device__ __forceinline__ void run_scaled(const Parts<kMax>& parts, const ClipArgs& a, uint32_t m, uint32_t run, Factor f) {
   const uint32_t begin = run * a.per, end = min(begin + a.per, a.tiles);
   uint32_t k = begin < end ? part_of(parts, a.count, begin) : 0;
   for (uint32_t tile = begin; tile < end; ++tile) {
     while (k + 1 < a.count && parts.p[k + 1].first_tile <= tile) ++k;
     const Part& p = parts.p[k];
-    if (c == 1.f && p.in_place) continue;
+    if (f.c == 1.f && !f.small && p.in_place) continue;
     const uint32_t in = tile - p.first_tile;
-    tile_clipped<S, D>(p, m, in, c);
+    tile_clipped<S, D>(p, m, in, f);
   }
 }
 
