@@ -381,10 +381,10 @@ __device__ __forceinline__ Segment segment(uint32_t begin, uint32_t end, uint32_
 }
 
 // The two kernels have the same course.  Turn k: wait until its row has arrived, send for row k + kStages - 1 (into the stage that
-// turn k - 1 read), take the row's sums.  With three stages or more the sum of row k + 1 is taken in turn k and travels with the
-// others, which leaves one exchange a row (65536 x 2048 bf16, gradient with residual: 289 -> 223 us; 32768 x 2048 fp32 gradient:
-// 156 -> 147); with two, waiting for row k + 1 would leave nothing on its way.  Backward, rows entry by entry: 128 registers do not
-// hold the next row as well.
+// turn k - 1 read), take the row's sums.  The sum of row k + 1 is taken in turn k and travels with the others, which leaves one exchange
+// a row (65536 x 2048 bf16, gradient with residual: 289 -> 223 us; 32768 x 2048 fp32 gradient: 156 -> 147).  That needs three stages: in
+// fp32 the gradient with dtotal has two, where waiting for row k + 1 would leave nothing on its way.  Backward, rows entry by entry:
+// 128 registers do not hold the next row as well.
 constexpr int kNormRoom = 204 * 1024;              // shared memory of the ring
 template <typename X, int kVec, bool kAdd>
 constexpr int kNormStage = Ring<X, kVec>::kStage * (kAdd ? 2 : 1);
@@ -395,7 +395,7 @@ __device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uin
                                           Room* rooms, const float2* w, const float2* b) {
   using RingX = Ring<X, kVec>;
   constexpr int kStage = kNormStage<X, kVec, kAdd>, kStages = stages_of(kStage, kNormRoom);
-  constexpr bool kAhead = kStages >= 3;
+  static_assert(kStages >= 3, "the next row is read a turn ahead");
   const uint32_t groups = kRowThreads / tpr;
   const float over = 1.f / a.dim;
   Segment s = segment(begin, end, m, a.T, groups, threadIdx.x / tpr, a.ids, a.ids64);
@@ -435,33 +435,24 @@ __device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uin
   bool coming = s.there(kStages - 1);
   float2 v[kPairs], u[kPairs];                                       // this row, the next one
   float sum = 0.f, none[1];
-  if (kAhead) {
-    copy_wait<kStages - 2>();
-    if (RingX::kShared) group_sync(tpr);
-    if (flags & 1) read(from, u, 0);
-    else clear(u);
-    sum = total_of(u);
-    group_sums<0, true>(none, sum, rooms[1], tpr);
-  }
+  copy_wait<kStages - 2>();
+  if (RingX::kShared) group_sync(tpr);
+  if (flags & 1) read(from, u, 0);
+  else clear(u);
+  sum = total_of(u);
+  group_sums<0, true>(none, sum, rooms[1], tpr);
   for (uint32_t k = 0; k < s.turns; ++k) {
-    copy_wait<kAhead ? kStages - 3 : kStages - 2>();
+    copy_wait<kStages - 3>();
     if (RingX::kShared) group_sync(tpr);
     issue(coming);
     flags |= (uint32_t)coming << (kStages - 1);
     coming = s.there(k + kStages);
     const bool real = flags & 1, more = flags & 2, in = (int)(k * groups) < s.left;
     flags >>= 1;
-    if (kAhead) {
 #pragma unroll
-      for (int i = 0; i < kPairs; ++i) v[i] = u[i];
-      if (more) read(after(from), u, 1);
-      else clear(u);
-    } else {
-      if (real) read(from, v, 0);
-      else clear(v);
-      sum = total_of(v);
-      group_sums<0, true>(none, sum, rooms[1], tpr);
-    }
+    for (int i = 0; i < kPairs; ++i) v[i] = u[i];
+    if (more) read(after(from), u, 1);
+    else clear(u);
     if (kAdd && in) store_row(row_t, at, v);
     centre(v, sum * over, at);
     float2 s0 = v[0], s1 = mul2(v[0], v[0]);
@@ -471,8 +462,8 @@ __device__ __forceinline__ void norm_rows(const NormArgs& a, uint32_t begin, uin
       s1 = fma2(v[i], v[i], s1);
     }
     float sums[2] = {(s0.x + s0.y) * over, (s1.x + s1.y) * over};     // the row's mean, so that sums of large squares fit
-    if (kAhead) sum = total_of(u);
-    group_sums<2, kAhead>(sums, sum, rooms[kAhead ? k & 1 : 0], tpr);
+    sum = total_of(u);
+    group_sums<2, true>(sums, sum, rooms[k & 1], tpr);
     const float shift = sums[0], rstd = rsqrtf(variance(sums[1], shift) + a.eps);
     if (in) {
 #pragma unroll
@@ -552,7 +543,6 @@ __device__ __forceinline__ void grad_rows(const NormGradArgs& a, uint32_t begin,
   float sum = 0.f, none[1];
   if (kAhead) {
     copy_wait<kStages - 2>();
-    if (RingX::kShared) group_sync(tpr);
     if (flags & 1) {
       x.read(ring, from, at, v);
       sum = total_of(v);
