@@ -42,3 +42,22 @@ def test_a_small_factor_that_is_held_as_one():
         S.s3gd_clip([t], max_norm, norm, ws, out=[o], eps=0.0)
         S.s3gd_clip([t], max_norm, norm, ws, eps=0.0)
         assert torch.equal(t, o) and abs(float(t[0, 0]) - max_norm) <= 8 * U and not t[0, 1] and float(t[0, 2]) <= 2.0 ** -26
+
+
+def test_long_lists_in_a_captured_graph():
+    M, shapes = 2, [(7,)] * 300 + [(33, 5)] * 300 + [(20001,)] + [(3,)] * 100           # two groups of up to 640 tensors
+    grads = [rand((M,) + s, BF16 if i % 3 else F32, i) for i, s in enumerate(shapes)]
+    sizes = [int(np.prod(s)) for s in shapes]
+    rows, norm, ws = torch.zeros((M, sum(sizes)), device=DEV), torch.zeros((M,), device=DEV), workspace(M)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        S.s3gd_clip(grads, 2.0, norm, ws, out=[p.unflatten(1, s) for p, s in zip(rows.split(sizes, 1), shapes)])
+    for turn in range(2):                                                               # the list is gone; the gradients are others
+        for g in grads:
+            g.mul_(-3)
+        graph.replay()
+        S.s3gd_device_status(ws)
+        flat = np.concatenate([host(g).reshape(M, -1) for g in grads], 1)
+        want = np.sqrt((flat ** 2).sum(1))
+        exact = flat * (2.0 / (want + 1e-6))[:, None]
+        assert (np.abs(host(norm) - want) <= 6 * U * want).all() and (np.abs(host(rows) - exact) <= 8 * U * np.abs(exact)).all()

@@ -72,3 +72,37 @@ def test_weight_gradients_in_16_bits_are_rounded_once(T, dim):
     before[1] = -1.0
     db = run_grad(dy, x, None, dst=BF16, before=before)[2]
     assert (db[0] == 1 + 2.0 ** -7).all() and (db[1] == -1 - 2.0 ** -7).all()
+
+
+def guarded_workspace(M, T, dim):
+    """A workspace of the stated size, and the bytes behind it."""
+    n = S.s3gd_layer_norm_grad_workspace_bytes(M, T, dim)
+    room = torch.full((n + 4096,), 165, dtype=torch.uint8, device=DEV)
+    return room[:n], room[n:]
+
+
+# 148 runs of 4096 rows are not enough: more runs, that go on from worker to worker or end with one
+@pytest.mark.parametrize("M,T", [(1, 700001), (3, 300007), (4, 500003), (300, 2500), (20000, 31)])
+def test_more_rows_than_148_long_runs_hold(M, T):
+    dim = 16
+    x, dy, w = rand((M, T, dim), F32, 12, 2.0, 0.3), rand((M, T, dim), F32, 13), rand((dim,), F32, 14, 0.3, 1.0)
+    grads, dx, (ws, behind) = torch.empty((M, 2 * dim), device=DEV), torch.empty_like(x), guarded_workspace(M, T, dim)
+    S.s3gd_layer_norm_grad(dy, x, dx, w, grads[:, :dim], grads[:, dim:], ws)
+    S.s3gd_device_status(ws)
+    assert (behind == 165).all()
+    check_grad((dx, grads[:, :dim], grads[:, dim:]), dy, x, w)
+    y = torch.empty_like(x)
+    S.s3gd_layer_norm(x, y, w)
+    check_y(y, x, w, None)
+
+
+@pytest.mark.parametrize("dim", [5, 24, 300, 1000, 1001, 8192, 9000])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_what_is_not_finite_takes_its_whole_row(dim, value):
+    x, dy, y = rand((2, 4, dim), F32, 15), rand((2, 4, dim), F32, 16), torch.empty((2, 4, dim), device=DEV)
+    x[0, 1, dim // 2], x[1, 3, dim - 1] = value, value
+    S.s3gd_layer_norm(x, y)
+    dx, dw, db = run_grad(dy, x, None)
+    for t in (y, dx):
+        assert t[0, 1].isnan().all() and t[1, 3].isnan().all() and t[0, [0, 2, 3]].isfinite().all() and t[1, :3].isfinite().all()
+    assert dw.isnan().all() and db.isfinite().all()
