@@ -442,7 +442,7 @@ S3GD_API s3gd_status s3gd_embed_grad(const void* dout, int dout_dtype, int64_t d
  *  opt_weight, opt_bias  [dim], both param_dtype: F32 or BF16
  *  opt_ids        [M x T] I32 or I64 (ids_dtype; any of the two where opt_ids is NULL)
  *  y              [M x T x dim] F32 or BF16.  y may be x itself, total may be x or add itself (same type and strides); outputs
- *                 otherwise overlap nothing.  An input's stride may be 0: the same row repeated
+ *                 otherwise overlap nothing (refused where they begin at one place).  An input's stride may be 0: the same row repeated
  * An Inf or NaN makes its own row NaN, and so does eps = 0 where all entries of a row are the same.  Rows far from zero keep their
  * digits.  Up to 8192 entries a row, sums are held in 32 bits: entries may be as large as 1e18 (a row whose squares pass fp32's range
  * becomes NaN), and a variance below 2^-116, or below (2^-27 mean)^2, may count as 0, which shows where eps is no larger.  In longer
@@ -468,7 +468,7 @@ S3GD_API s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_strid
  *  opt_ids    as above: empty places have zero rows in dx and give nothing to the weights, whatever dy, x and dtotal hold
  *  opt_dx     [M x T x dim] of x's type, or NULL; may be dy, x or dtotal itself (same type and strides)
  *  opt_dweight, opt_dbias  F32 or BF16, dim entries per worker, grads_stride elements from worker to worker (>= dim); either may
- *             be NULL.  Every entry is written; with accumulate != 0 the sum is added to what is there (one rounding)
+ *             be NULL, and they have no entry in common.  Every entry is written; with accumulate != 0 the sum is added to what is there (one rounding)
  *  ws         >= s3gd_layer_norm_grad_workspace_bytes(M, T, dim), 256-byte aligned, not preserved; one for larger numbers serves
  *             smaller ones
  * Sums are taken in an order that depends on sizes and alignment alone, not on the run.  T may be 0.  Limits as for s3gd_layer_norm.

@@ -858,6 +858,19 @@ bool writable(const Rows& r, int dtype, int M, uint64_t T, uint64_t dim) {
   // workers one behind the other, or interleaved (each token's row of all workers side by side)
   return worker >= (T > 1 ? (T - 1) * tok : 0) + dim || (worker >= dim && (T == 1 || tok >= (uint64_t)(M - 1) * worker + dim));
 }
+// an output that begins where an input does: in place, so it must lie the same
+bool lies_alike(const Rows& out, int out_dtype, const Rows& in, int in_dtype, int M, uint64_t T) {
+  return out.p == nullptr || out.p != in.p || (out_dtype == in_dtype && (T == 1 || out.tok == in.tok) && (M == 1 || out.worker == in.worker));
+}
+// do the workers' rows of two gradients have entries in common?  (stride >= dim where there are several)
+bool rows_meet(const void* a, const void* b, size_t size, uint64_t dim, int M, int64_t stride) {
+  if (a == nullptr || b == nullptr) return false;
+  const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
+  const uint64_t apart = (p < q ? q - p : p - q) / size;
+  if (M == 1) return apart < dim;
+  const uint64_t rows = apart / (uint64_t)stride, rest = apart % (uint64_t)stride;
+  return (rows < (uint64_t)M && rest < dim) || (rows + 1 < (uint64_t)M && (uint64_t)stride - rest < dim);
+}
 // threads of a row: part of a warp (the fewest that hold it, but four where groups copy rows together), or a warp for every 512 entries
 uint32_t threads_per_row(uint64_t dim, int vec) {
   if (dim > 16 * kEach) return (uint32_t)((dim + 32 * kEach - 1) / (32 * kEach)) * 32;
@@ -967,7 +980,10 @@ extern "C" s3gd_status s3gd_layer_norm(const void* x, int x_dtype, int64_t x_str
     return S3GD_ERR_INVALID_ARG;
   if (T == 0) return S3GD_OK;
   if (x == nullptr || y == nullptr || !readable(a.x, x_dtype) || !writable(a.y, y_dtype, M, T, dim)) return S3GD_ERR_INVALID_ARG;
-  if (opt_add != nullptr && (!readable(a.add, x_dtype) || !writable(a.total, x_dtype, M, T, dim))) return S3GD_ERR_INVALID_ARG;
+  if (opt_add != nullptr && (!readable(a.add, x_dtype) || !writable(a.total, x_dtype, M, T, dim) || y == opt_total)) return S3GD_ERR_INVALID_ARG;
+  if (!lies_alike(a.y, y_dtype, a.x, x_dtype, M, T) || !lies_alike(a.total, x_dtype, a.x, x_dtype, M, T) ||
+      !lies_alike(a.total, x_dtype, a.add, x_dtype, M, T))
+    return S3GD_ERR_INVALID_ARG;
   a.weight = opt_weight; a.bias = opt_bias; a.param_bf16 = param_dtype == S3GD_BF16;
   a.ids = opt_ids; a.ids64 = ids_dtype == S3GD_I64;
   a.T = (uint32_t)T; a.N = (uint32_t)((uint64_t)M * T); a.dim = (uint32_t)dim; a.eps = eps;
@@ -1023,6 +1039,10 @@ extern "C" s3gd_status s3gd_layer_norm_grad(const void* dy, int dy_dtype, int64_
                 (opt_dtotal != nullptr && !readable(a.dtotal, x_dtype)) || (opt_dx != nullptr && !writable(a.dx, x_dtype, M, T, dim))))
     return S3GD_ERR_INVALID_ARG;
   if (ws == nullptr || ws_bytes < L.total || !is_aligned(ws, 256)) return S3GD_ERR_WORKSPACE;
+  if (rows_meet(opt_dweight, opt_dbias, dtype_bytes(grads_dtype), dim, M, grads_stride)) return S3GD_ERR_INVALID_ARG;
+  if (T > 0 && (!lies_alike(a.dx, x_dtype, a.dy, dy_dtype, M, T) || !lies_alike(a.dx, x_dtype, a.x, x_dtype, M, T) ||
+                !lies_alike(a.dx, x_dtype, a.dtotal, x_dtype, M, T)))
+    return S3GD_ERR_INVALID_ARG;
   a.weight = opt_weight; a.weight_bf16 = weight_dtype == S3GD_BF16;
   a.ids = opt_ids; a.ids64 = ids_dtype == S3GD_I64;
   a.grads_bf16 = grads_dtype == S3GD_BF16; a.accumulate = accumulate != 0;
