@@ -966,14 +966,20 @@ _T = torch.Tensor
 _dtype_of = operator.attrgetter("dtype")
 
 
-def _once(places, entries) -> None:
-    if len(set(places)) != len(places):
+def _once(places, entries, pointers=()) -> None:
+    """Refuses an output that is named twice, or that lies in place of one gradient and is read as another one (pointers) too."""
+    written = set(places)
+    if len(written) != len(places):
         seen = [p for p, n in zip(places, entries) if n]
         if len(set(seen)) != len(seen):
             raise ValueError("an output is named twice: it would be scaled twice, or once, as it happens")
+    if not written.isdisjoint(pointers):
+        read = {p for p, o, n in zip(pointers, places, entries) if n and p != o}
+        if any(n and o in read for o, n in zip(places, entries)):
+            raise ValueError("an output is also read as another gradient: it would be read scaled or not, as it happens")
 
 
-def _plain_parts(grads, outs, index: int, M: int, several: bool, writes: bool):
+def _plain_parts(grads, outs, index: int, M: int, several: bool, writes: bool, apart: bool):
     """As _parts for lists of contiguous gradients of one type (and outputs of one type that lie alike); None for others.
 
     A list has hundreds of tensors and its kernels take some ten microseconds: each question is put to all tensors at once."""
@@ -990,20 +996,20 @@ def _plain_parts(grads, outs, index: int, M: int, several: bool, writes: bool):
     dtypes = set(map(_dtype_of, outs))
     if len(dtypes) != 1 or set(map(_T.get_device, outs)) != devices or sizes != list(map(_T.size, outs)):
         return None
-    apart = entries
+    distances = entries
     if not all(map(_T.is_contiguous, outs)):
         strides = list(map(_T.stride, outs))
         if not several or any(a[1:] != b[1:] for a, b in zip(strides, map(_T.stride, grads))):
             return None
-        apart = [s[0] for s in strides]
+        distances = [s[0] for s in strides]
     code |= _REAL_CODES[dtypes.pop()] << 32
     places = list(map(_T.data_ptr, outs))
-    _once(places, entries)
-    return array.array("Q", chain.from_iterable(zip(pointers, places, entries, entries, apart, repeat(code)))), len(pointers)
+    _once(places, entries, pointers if apart else ())
+    return array.array("Q", chain.from_iterable(zip(pointers, places, entries, entries, distances, repeat(code)))), len(pointers)
 
 
-def _parts(grads, out, index: int, M: int, several: bool, writes: bool):
-    """The tensors as an array of s3gd_part, and their number."""
+def _parts(grads, out, index: int, M: int, several: bool, writes: bool, apart: bool = False):
+    """The tensors as an array of s3gd_part, and their number; apart: an output may be in place, but not read as another gradient."""
     if isinstance(grads, torch.Tensor):
         grads, out = (grads,), (out,) if isinstance(out, torch.Tensor) else out
     grads = list(grads)
@@ -1013,7 +1019,7 @@ def _parts(grads, out, index: int, M: int, several: bool, writes: bool):
     plain = None
     if len(grads) > 3:                                   # (a tensor by itself takes 3.6 us below and 5.9 above)
         try:
-            plain = _plain_parts(grads, outs, index, M, several, writes)
+            plain = _plain_parts(grads, outs, index, M, several, writes, apart)
         except (TypeError, AttributeError, KeyError):    # something that is no tensor, or of another type: named below
             pass
     if plain is not None:
@@ -1047,7 +1053,7 @@ def _parts(grads, out, index: int, M: int, several: bool, writes: bool):
                 raise ValueError(f"output {i} does not lie like its gradient: strides {out_strides} and {strides}")
         packed.extend((g.data_ptr(), o.data_ptr(), n, strides[0] if several else 0, out_strides[0] if several else 0, code))
     if writes:
-        _once(packed[1::6].tolist(), packed[2::6])
+        _once(packed[1::6].tolist(), packed[2::6], packed[::6] if apart else ())
     return packed, len(packed) // 6
 
 
@@ -1089,9 +1095,10 @@ def s3gd_clip(grads, max_norm: float, norm: torch.Tensor, ws: torch.Tensor, out=
     """out <- grads * min(1, max_norm / (norm + eps)), norm as s3gd_grad_norm gives it; per worker where norm is [M].
 
     out (None: in place) has a tensor for each of grads, of the same shape and order of axes, fp32 or bf16: e.g. the columns of a
-    gradient buffer, out[i] = rows[:, a:b].unflatten(1, shape).  Outputs overlap no other tensor of the call, and none is named twice."""
+    gradient buffer, out[i] = rows[:, a:b].unflatten(1, shape).  Outputs overlap no other tensor of the call, and none is named twice
+    (refused where they begin at one place)."""
     index, M, several = _norms(norm)
-    packed, count = _parts(grads, out, index, M, several, True)
+    packed, count = _parts(grads, out, index, M, several, True, True)
     args = (packed.buffer_info()[0] if count else None, count, M, max_norm, eps, norm.data_ptr(), *_clip_room(ws, index))
     if _current_device() == index:
         code = load().s3gd_clip(*args, _stream_of(index))
